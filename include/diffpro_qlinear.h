@@ -421,6 +421,140 @@ int qlinear_plan_run_ex(const ql_plan *plan, const void *const *x_in, void *cons
 int ql_time_bin(int64_t step, int64_t num_steps);
 
 /* ------------------------------------------------------------------------
+ * Attention between the qkv layer and the output projection (the two quantized
+ * layers of Step 3 that it joins; Section 6 counts it in the latency).  Rows of
+ * q, k and v belong to B sequences, one behind the other.  With n_q rows and n_k
+ * keys in a sequence, row i stands at position p = i + n_k - n_q (its last row
+ * at the last key), and with h' = h / (Hq / Hkv):
+ *   x_j = scale * sum_d q[i,h,d] k[j,h',d]
+ *   c_j = cap * tanh(x_j / cap)                 (c_j = x_j for cap = 0)
+ *   s_j = c_j - slopes[h] * |p - j|             (slopes NULL: c_j)
+ *   visible keys: QL_MASK_NONE all of the sequence; QL_MASK_CAUSAL j <= p;
+ *                 QL_MASK_PREFIX j <= p or j < prefix[b]
+ *   o[i,h] = fp16( sum_j exp(s_j) v[j,h'] / sum_j exp(s_j) )    over visible j
+ * and 0 where no key is visible (a sequence without keys, or rows in front of
+ * the first key).  Scores, the running maximum and the sums are fp32; the
+ * weights exp(s_j - m) are rounded to binary16 for the matrix cores, which
+ * moves o by at most about 2^-11 of the largest |v| of the row's keys.
+ *   q, o      (device) fp16, element (t, h, d) at t * row + h * head + d; rows and
+ *             heads may be strided (the columns of a fused qkv layer's output),
+ *             strides in elements, multiples of 8; base pointers 16-byte aligned.
+ *             o must not overlap q, k or v
+ *   cu_q      (device) int32 [B+1], first row of each sequence, non-decreasing,
+ *             or NULL: T_q / B rows each.  A sequence may have no rows.  Rows
+ *             outside all sequences keep what they held
+ *   slopes    (device) fp32 [Hq] or NULL;  prefix (device) int32 [B]
+ *   row_absmax (device) [T_q] uint32 or NULL: as ql_fusion.row_absmax, the largest
+ *             |o[t,:,:]| of every row for daq_quantize_rowmax (the quantizer of
+ *             the output projection).  The call clears it first
+ * D: a multiple of 8 up to 256; Hkv divides Hq; T_q * Hq and T_k * Hkv below 2^31.
+ * Values inside the sequences are assumed finite (General rules); rows outside
+ * them are not read into any result.
+ * ---------------------------------------------------------------------- */
+enum { QL_MASK_NONE = 0, QL_MASK_CAUSAL = 1, QL_MASK_PREFIX = 2 };
+
+typedef struct ql_attention {
+    int64_t T_q;
+    int32_t B, Hq, Hkv, D;
+    int32_t mask;          /* QL_MASK_* */
+    float scale;           /* finite; 1 / sqrt(D) as a rule */
+    float cap;             /* 0: none; else finite and positive */
+    int32_t reserved;      /* 0 */
+    const void *prefix;
+    const void *slopes;
+    const void *cu_q;
+    const void *q;
+    int64_t q_row, q_head;
+    void *o;
+    int64_t o_row, o_head;
+    void *row_absmax;
+} ql_attention;
+
+/* Keys and values as binary16 rows: k, v (device), strided like q; cu_k (device)
+ * int32 [B+1] or NULL: T_k / B keys each; a sequence may have no keys. */
+size_t attention_f16_workspace_bytes(int64_t T_q, int64_t T_k, int32_t B, int32_t Hq, int32_t Hkv, int32_t D);
+int attention_f16(const ql_attention *attn, const void *k, int64_t k_row, int64_t k_head,
+                  const void *v, int64_t v_row, int64_t v_head, int64_t T_k, const void *cu_k,
+                  void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * A paged cache of keys and values in 8 bits.  Eq. (4) with tau = the absolute
+ * maximum of scale_tokens consecutive tokens of one key head:
+ *   k[j,h,d] = k_code * k_scale[block of j, h]      (v likewise)
+ * codes in [-127, 127], scale 0 for a block of zeros.
+ *   k        (device) int8 [num_pages, Hkv, page, D]
+ *   v        (device) int8 [num_pages, Hkv, page/64, D, 64]: of every 64 tokens, the
+ *            codes of one channel together; token t of them at byte
+ *            16 * (t % 16 / 4) + 4 * (t / 16) + t % 4
+ *   k_scale, v_scale (device) fp32 [num_pages, Hkv, page/scale_tokens]
+ *   page_table (device) int32 [B, max_pages]: the pages of every sequence in order.
+ *            An entry outside [0, num_pages) is no page: its tokens are not visible
+ *            and appending to it writes nothing
+ *   len_k    (device) int32 [B]: tokens of every sequence, those being appended
+ *            included; at most max_pages * page count
+ * page: a multiple of 64; scale_tokens: 1, 16, 32 or 64; D a multiple of 8 up to
+ * 256; max_pages * page below 2^31.  k and v 16-byte aligned.  Offsets into the
+ * cache are 64 bits wide.
+ * ---------------------------------------------------------------------- */
+typedef struct ql_kv_cache {
+    void *k, *v;
+    void *k_scale, *v_scale;
+    int64_t num_pages;
+    int32_t page, scale_tokens, Hkv, D;
+    const void *page_table;
+    const void *len_k;
+    int32_t B, max_pages;
+} ql_kv_cache;
+
+/* New tokens for the cache: rows of the qkv layer, T of them for B sequences (cu
+ * as cu_q above; NULL: T / B each).  The n tokens of sequence b take the places
+ * len_k[b] - n .. len_k[b] - 1.
+ * Rotation (rot NULL: none) of the leading rot_dim channels of q and k, by row
+ * pos[t] of the table (pos NULL: the token's place in its sequence; rows outside
+ * the table: its nearest row):  with (c, s) = rot[row, i, 0..1]
+ *   (x_i, x_j) -> fp16( x_i c - x_j s, x_j c + x_i s ),   each operation rounded to fp32
+ *   j = i + rot_dim / 2 (rot_pairs = 0), or the neighbours 2 i, 2 i + 1 (rot_pairs = 1)
+ * Then DAQ, h = the rotated fp16 key or the fp16 value, per block and key head:
+ *   amax  = max |h| over the block's new tokens
+ *   alpha = max(alpha_old, amax / 127), alpha_old = the block's scale where the
+ *           sequence already has tokens in it, else 0
+ *   codes = clamp(rne(h / alpha), -127, 127);  0 where alpha = 0
+ *   the block's earlier codes become clamp(rne(code * alpha_old / alpha)) where
+ *   alpha grew (each growth moves them by at most half a step; a block of one
+ *   token, scale_tokens = 1, is never rescaled)
+ *   q_out  (device) fp16 [T, Hq, D] the rotated q, or NULL (then q is not read)
+ *   k_out, v_out (device) fp16 [T, Hkv, D] or NULL: fp16(code * alpha) of the new
+ *           tokens, what the cache now holds of them (attention_f16 over a prompt
+ *           then sees the values that later steps will read)
+ *   rot    (device) fp32 [rot_rows, rot_dim/2, 2], 16-byte aligned; rot_dim a
+ *           multiple of 16 up to D;  pos (device) int32 [T] or NULL
+ * Sequences must not share a page that tokens are appended to.  Cache bytes
+ * outside the touched blocks keep what they held. */
+typedef struct ql_kv_new {
+    int64_t T;
+    int32_t Hq;            /* heads of q; 0 without q */
+    int32_t rot_pairs;
+    const void *cu;
+    const void *q, *k, *v;
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head;
+    const void *rot;
+    int64_t rot_rows;
+    int32_t rot_dim;
+    int32_t reserved;      /* 0 */
+    const void *pos;
+    void *q_out, *k_out, *v_out;
+} ql_kv_new;
+
+int daq_kv_append(const ql_kv_cache *cache, const ql_kv_new *tokens, void *stream);
+
+/* Attention over the cache: the formulas above with n_k = len_k[b] and the
+ * cache's keys and values; attn->B, Hkv and D are the cache's.  One new token per
+ * sequence is T_q = B with cu_q NULL. */
+size_t attention_kv8_workspace_bytes(int64_t T_q, int32_t B, int32_t Hq, int32_t Hkv, int32_t D);
+int attention_kv8(const ql_attention *attn, const ql_kv_cache *cache,
+                  void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
  * Offline side, host memory only (no device call): the stages that produce what
  * the calls above consume.
  *

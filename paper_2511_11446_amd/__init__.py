@@ -25,7 +25,8 @@ EXPORTS = ("ql_status_string", "ql_last_device_error", "ql_version", "daq_worksp
            "qlinear_w4a8_g", "qgemm_w4a8_g", "qlinear_w8a8_fused", "qlinear_w4a8_fused", "qlinear_f16", "ql_repack_w4_pairs_host", "ql_prepack_w4", "daq_quantize_rowmax", "qlinear_plan_run_ex", "qlinear_w8a8_noalloc", "qlinear_noalloc_max_bytes",
            "ql_schedule_topk", "ql_plan_greedy", "ql_gptq_quantize_host", "daq_quantize_ln",
            "daq_cg_workspace_bytes", "daq_quantize_cg", "qlinear_grouped_workspace_bytes", "qlinear_grouped", "ql_pack_bits_host",
-           "ql_unpack_bits_host", "ql_zero_point_fold_host")
+           "ql_unpack_bits_host", "ql_zero_point_fold_host",
+           "attention_f16_workspace_bytes", "attention_f16", "daq_kv_append", "attention_kv8_workspace_bytes", "attention_kv8")
 
 
 class QlError(RuntimeError):
@@ -126,6 +127,17 @@ def lib():
     L.qlinear_noalloc_max_bytes.argtypes = []
     L.qlinear_w8a8_noalloc.argtypes = [_vp, _i64, _i64, _i64, _vp, _vp, _vp, _i64, _vp, _vp]
     L.qlinear_w8a8_noalloc.restype = _int
+    i32 = ctypes.c_int32
+    L.attention_f16_workspace_bytes.restype = _sz
+    L.attention_f16_workspace_bytes.argtypes = [_i64, _i64, i32, i32, i32, i32]
+    L.attention_f16.argtypes = [ctypes.POINTER(ql_attention), _vp, _i64, _i64, _vp, _i64, _i64, _i64, _vp, _vp, _sz, _vp]
+    L.attention_f16.restype = _int
+    L.daq_kv_append.argtypes = [ctypes.POINTER(ql_kv_cache), ctypes.POINTER(ql_kv_new), _vp]
+    L.daq_kv_append.restype = _int
+    L.attention_kv8_workspace_bytes.restype = _sz
+    L.attention_kv8_workspace_bytes.argtypes = [_i64, i32, i32, i32, i32]
+    L.attention_kv8.argtypes = [ctypes.POINTER(ql_attention), ctypes.POINTER(ql_kv_cache), _vp, _sz, _vp]
+    L.attention_kv8.restype = _int
     _lib = L
     return L
 
@@ -496,6 +508,175 @@ def ql_pack_w4_host(codes):
     rc = lib().ql_pack_w4_host(codes.ctypes.data_as(_vp), N, K, out.ctypes.data_as(_vp))
     _check(rc, "ql_pack_w4_host")
     return out
+
+
+MASK_NONE, MASK_CAUSAL, MASK_PREFIX = 0, 1, 2
+
+
+class ql_attention(ctypes.Structure):
+    _fields_ = [("T_q", _i64), ("B", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("mask", ctypes.c_int32), ("scale", ctypes.c_float), ("cap", ctypes.c_float), ("reserved", ctypes.c_int32),
+                ("prefix", _vp), ("slopes", _vp), ("cu_q", _vp), ("q", _vp), ("q_row", _i64), ("q_head", _i64),
+                ("o", _vp), ("o_row", _i64), ("o_head", _i64), ("row_absmax", _vp)]
+
+
+class ql_kv_cache(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("num_pages", _i64), ("page", ctypes.c_int32),
+                ("scale_tokens", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32), ("page_table", _vp), ("len_k", _vp),
+                ("B", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
+
+
+class ql_kv_new(ctypes.Structure):
+    _fields_ = [("T", _i64), ("Hq", ctypes.c_int32), ("rot_pairs", ctypes.c_int32), ("cu", _vp), ("q", _vp), ("k", _vp), ("v", _vp),
+                ("q_row", _i64), ("q_head", _i64), ("k_row", _i64), ("k_head", _i64), ("v_row", _i64), ("v_head", _i64),
+                ("rot", _vp), ("rot_rows", _i64), ("rot_dim", ctypes.c_int32), ("reserved", ctypes.c_int32), ("pos", _vp),
+                ("q_out", _vp), ("k_out", _vp), ("v_out", _vp)]
+
+
+def _heads(t, name, H=None, D=None):
+    """A [T, H, D] binary16 view whose rows and heads may be strided: (pointer, row stride, head stride)."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.float16 or t.dim() != 3 or t.stride(2) != 1:
+        raise TypeError("%s must be a [T, heads, D] CUDA tensor of torch.float16 with neighbouring channels" % name)
+    if (H is not None and t.shape[1] != H) or (D is not None and t.shape[2] != D):
+        raise ValueError("%s has shape %s, expected [T, %s, %s]" % (name, tuple(t.shape), H, D))
+    # the stride of a single row or head means nothing
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0
+
+
+def _attention_form(q, B, Hkv, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax):
+    import torch
+    qp, q_row, q_head = _heads(q, "q")
+    T, Hq, D = q.shape
+    if o is None:
+        o = torch.empty((T, Hq, D), dtype=torch.float16, device=q.device)
+    op, o_row, o_head = _heads(o, "o", Hq, D)
+    if o.shape[0] != T:
+        raise ValueError("o has %d rows, expected %d" % (o.shape[0], T))
+    for name, t, dtype, n in (("cu_q", cu_q, torch.int32, B + 1), ("prefix", prefix, torch.int32, B), ("slopes", slopes, torch.float32, Hq),
+                              ("row_absmax", row_absmax, torch.int32, T)):
+        if t is not None:
+            _need(t, dtype, (n,), name)
+    a = ql_attention(T, B, Hq, Hkv, D, mask, D ** -0.5 if scale is None else scale, cap, 0, _ptr(prefix), _ptr(slopes), _ptr(cu_q), qp, q_row, q_head,
+                     op, o_row, o_head, _ptr(row_absmax))
+    return a, o
+
+
+def attention_f16_workspace_bytes(T_q, T_k, B, Hq, Hkv, D):
+    return int(lib().attention_f16_workspace_bytes(T_q, T_k, B, Hq, Hkv, D))
+
+
+def attention_f16(q, k, v, batch=None, cu_q=None, cu_k=None, mask=MASK_NONE, prefix=None, scale=None, cap=0.0, slopes=None, o=None,
+                  row_absmax=None, ws=None, stream=None):
+    """Softmax attention: q fp16 [T_q, Hq, D], k, v fp16 [T_k, Hkv, D] (views with strided rows and heads, such as the columns of a fused qkv
+    layer's output) -> o fp16 [T_q, Hq, D].  Sequences one behind the other: `batch` of equal length, or int32 [B+1] first rows in cu_q / cu_k.
+    scale: default D ** -0.5; cap: tanh cap of the scores (0: none); slopes fp32 [Hq]: bias by distance; mask MASK_NONE / _CAUSAL / _PREFIX
+    (prefix int32 [B]); row_absmax: int32 [T_q] that receives every row's largest |o| as a binary16 bit pattern, for daq_quantize_rowmax."""
+    import torch
+    kp, k_row, k_head = _heads(k, "k")
+    T_k, Hkv, D = k.shape
+    vp, v_row, v_head = _heads(v, "v", Hkv, D)
+    if v.shape[0] != T_k or q.shape[-1] != D:
+        raise ValueError("k has shape %s, v %s and q %s" % (tuple(k.shape), tuple(v.shape), tuple(q.shape)))
+    B = batch if batch is not None else cu_q.shape[0] - 1 if cu_q is not None else cu_k.shape[0] - 1 if cu_k is not None else 1
+    if cu_k is not None:
+        _need(cu_k, torch.int32, (B + 1,), "cu_k")
+    a, o = _attention_form(q, B, Hkv, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax)
+    if ws is None:
+        ws = workspace(attention_f16_workspace_bytes(a.T_q, T_k, B, a.Hq, Hkv, D), q.device)
+    _check(lib().attention_f16(ctypes.byref(a), kp, k_row, k_head, vp, v_row, v_head, T_k, _ptr(cu_k), _ptr(ws), ws.numel(), _stream(stream)),
+           "attention_f16")
+    return o
+
+
+class KvCache8:
+    """A paged cache of keys and values in 8 bits: k int8 [pages, Hkv, page, D], v int8 [pages, Hkv, page/64, D, 64],
+    k_scale, v_scale fp32 [pages, Hkv, page/scale_tokens] (CUDA tensors, kept here; the layout is the header's ql_kv_cache)."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        import torch
+        _need(k, torch.int8, name="k")
+        P, H, page, D = k.shape
+        _need(v, torch.int8, (P, H, page // 64, D, 64), "v")
+        _need(k_scale, torch.float32, name="k_scale")
+        _need(v_scale, torch.float32, tuple(k_scale.shape), "v_scale")
+        if k_scale.dim() != 3 or tuple(k_scale.shape[:2]) != (P, H) or k_scale.shape[2] < 1 or page % k_scale.shape[2]:
+            raise ValueError("k_scale has shape %s, expected [%d, %d, page / scale_tokens]" % (tuple(k_scale.shape), P, H))
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.num_pages, self.heads, self.page, self.D, self.scale_tokens = P, H, page, D, page // k_scale.shape[2]
+
+    @classmethod
+    def empty(cls, num_pages, heads, D, page=64, scale_tokens=64, device="cuda"):
+        import torch
+        z = dict(device=device)
+        scales = (num_pages, heads, page // scale_tokens)
+        return cls(torch.zeros((num_pages, heads, page, D), dtype=torch.int8, **z),
+                   torch.zeros((num_pages, heads, page // 64, D, 64), dtype=torch.int8, **z),
+                   torch.zeros(scales, dtype=torch.float32, **z), torch.zeros(scales, dtype=torch.float32, **z))
+
+    def desc(self, page_table, len_k):
+        import torch
+        _need(page_table, torch.int32, name="page_table")
+        B, max_pages = page_table.shape
+        _need(len_k, torch.int32, (B,), "len_k")
+        return ql_kv_cache(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(), self.num_pages, self.page,
+                           self.scale_tokens, self.heads, self.D, page_table.data_ptr(), len_k.data_ptr(), B, max_pages)
+
+
+def daq_kv_append(cache, k, v, page_table, len_k, cu=None, q=None, rot=None, rot_pairs=False, pos=None, q_out=None, k_out=None, v_out=None,
+                  stream=None):
+    """New keys and values fp16 [T, Hkv, D] (strided views) into the cache, k and q rotated by rot fp32 [rows, rot_dim/2, 2] (cos, sin) at row pos
+    (int32 [T]; default: the token's place in its sequence).  len_k int32 [B] counts the new tokens; cu int32 [B+1]: first new row of each sequence
+    (default: T / B each).  q_out fp16 [T, Hq, D]: the rotated q (made where q is given); k_out, v_out fp16 [T, Hkv, D]: what the cache now holds.
+    Returns q_out."""
+    import torch
+    c = cache.desc(page_table, len_k)
+    T = k.shape[0]
+    kp, k_row, k_head = _heads(k, "k", cache.heads, cache.D)
+    vp, v_row, v_head = _heads(v, "v", cache.heads, cache.D)
+    if v.shape[0] != T:
+        raise ValueError("k has %d rows and v %d" % (T, v.shape[0]))
+    Hq, qp, q_row, q_head = 0, None, 0, 0
+    if q is not None:
+        Hq = q.shape[1]
+        qp, q_row, q_head = _heads(q, "q", Hq, cache.D)
+        if q.shape[0] != T:
+            raise ValueError("q has %d rows and k %d" % (q.shape[0], T))
+        if q_out is None:
+            q_out = torch.empty((T, Hq, cache.D), dtype=torch.float16, device=q.device)
+        _need(q_out, torch.float16, (T, Hq, cache.D), "q_out")
+    for name, t in (("k_out", k_out), ("v_out", v_out)):
+        if t is not None:
+            _need(t, torch.float16, (T, cache.heads, cache.D), name)
+    for name, t, n in (("cu", cu, c.B + 1), ("pos", pos, T)):
+        if t is not None:
+            _need(t, torch.int32, (n,), name)
+    rows = half = 0
+    if rot is not None:
+        _need(rot, torch.float32, name="rot")
+        rows, half, two = rot.shape
+        if two != 2:
+            raise ValueError("rot must be [rows, rot_dim / 2, 2]")
+    n = ql_kv_new(T, Hq, 1 if rot_pairs else 0, _ptr(cu), qp, kp, vp, q_row, q_head, k_row, k_head, v_row, v_head, _ptr(rot), rows, 2 * half, 0,
+                  _ptr(pos), _ptr(q_out) if q is not None else None, _ptr(k_out), _ptr(v_out))
+    _check(lib().daq_kv_append(ctypes.byref(c), ctypes.byref(n), _stream(stream)), "daq_kv_append")
+    return q_out
+
+
+def attention_kv8_workspace_bytes(T_q, B, Hq, Hkv, D):
+    return int(lib().attention_kv8_workspace_bytes(T_q, B, Hq, Hkv, D))
+
+
+def attention_kv8(q, cache, page_table, len_k, cu_q=None, mask=MASK_CAUSAL, prefix=None, scale=None, cap=0.0, slopes=None, o=None,
+                  row_absmax=None, ws=None, stream=None):
+    """attention_f16 over the 8-bit cache: q fp16 [T_q, Hq, D], page_table int32 [B, max_pages], len_k int32 [B] -> o fp16 [T_q, Hq, D]."""
+    c = cache.desc(page_table, len_k)
+    _heads(q, "q", None, cache.D)
+    a, o = _attention_form(q, c.B, cache.heads, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax)
+    if ws is None:
+        ws = workspace(attention_kv8_workspace_bytes(a.T_q, c.B, a.Hq, cache.heads, cache.D), q.device)
+    _check(lib().attention_kv8(ctypes.byref(a), ctypes.byref(c), _ptr(ws), ws.numel(), _stream(stream)), "attention_kv8")
+    return o
 
 
 class Plan:

@@ -396,6 +396,10 @@ struct ql_plan {
     int64_t K_widest;
 };
 
+namespace ql {
+int status_of(hipError_t e) { return device_status(e); }
+}  // namespace ql
+
 extern "C" {
 
 const char *ql_status_string(int status)

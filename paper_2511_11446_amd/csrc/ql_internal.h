@@ -181,4 +181,7 @@ hipError_t launch_qgemm_many(const GemmArgs *const *layers, int count, hipStream
 // pair-order nibbles (device) -> the 4-bit storage order (device); blocks = N*K/8 four-byte blocks
 hipError_t launch_prepack_w4(const void *pairs, void *packed, long long blocks, hipStream_t stream);
 
+// a HIP call's result as a ql_status; what failed is kept for ql_last_device_error() (api.hip)
+int status_of(hipError_t e);
+
 }  // namespace ql

@@ -1,0 +1,349 @@
+"""attention_f16, daq_kv_append and attention_kv8 against the 64-bit oracle, through the C ABI.  The tolerance of every attention output is
+the oracle's own count of roundings (oracle/attention.py); cache codes, scales, rotated rows and returned values are compared bit for bit."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2511_11446_amd as ql
+from oracle import attention as oa
+
+pytestmark = pytest.mark.gpu
+
+
+def _rng(*key):
+    return np.random.default_rng([1511, *key])
+
+
+def _cu(lens):
+    return np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+
+
+def _dev(x):
+    return None if x is None else torch.from_numpy(np.ascontiguousarray(x)).cuda()
+
+
+def _f16(g, *shape, size=1.0):
+    return (g.standard_normal(shape, dtype=np.float32) * np.float32(size)).astype(np.float16)
+
+
+def _close(o, ref, tol, name=""):
+    o = o.cpu().numpy().astype(np.float64)
+    live = ~np.isnan(ref)
+    bad = ~(np.abs(o - ref) <= tol) & live
+    assert not bad.any(), "%s: %d of %d off, worst %.3g times the tolerance at %s" % (
+        name, bad.sum(), live.sum(), np.nanmax(np.where(live, np.abs(o - ref) / tol, 0)), np.argwhere(bad)[:3].tolist())
+
+
+def _dense(key, nq, nk, Hq, Hkv, D, mask=0, cap=0.0, slopes=False, fused=False, equal=False, size=1.0, extra=0):
+    """Runs one case; nq / nk: lengths of the sequences; extra: rows behind the last one."""
+    g = _rng(*key)
+    Tq, Tk = sum(nq) + extra, sum(nk) + extra
+    if fused:
+        rows = _f16(g, Tq, (Hq + 2 * Hkv) * D, size=size)
+        d = _dev(rows)
+        q, k, v = rows[:, :Hq * D].reshape(Tq, Hq, D), rows[:, Hq * D:(Hq + Hkv) * D].reshape(Tq, Hkv, D), rows[:, (Hq + Hkv) * D:].reshape(Tq, Hkv, D)
+        dq, dk, dv = d[:, :Hq * D].unflatten(1, (Hq, D)), d[:, Hq * D:(Hq + Hkv) * D].unflatten(1, (Hkv, D)), d[:, (Hq + Hkv) * D:].unflatten(1, (Hkv, D))
+    else:
+        q, k, v = _f16(g, Tq, Hq, D, size=size), _f16(g, max(Tk, 1), Hkv, D, size=size), _f16(g, max(Tk, 1), Hkv, D, size=size)
+        dq, dk, dv = _dev(q), _dev(k), _dev(v)
+    prefix = g.integers(0, max(max(nk), 1) + 2, len(nq)).astype(np.int32) if mask == 2 else None
+    sl = g.uniform(0, 0.3, Hq).astype(np.float32) if slopes else None
+    cq, ck = _cu(nq), _cu(nk)
+    scale = D ** -0.5
+    ref, tol = oa.attention(q, k, v, cq, ck, scale, mask, prefix, cap, sl)
+    o = torch.full((Tq, Hq, D), 7.0, dtype=torch.float16, device="cuda")
+    am = torch.full((Tq,), -1, dtype=torch.int32, device="cuda")
+    out = ql.attention_f16(dq, dk, dv, batch=len(nq), cu_q=None if equal else _dev(cq), cu_k=None if equal else _dev(ck), mask=mask, prefix=_dev(prefix),
+                           cap=cap, slopes=_dev(sl), o=o, row_absmax=am)
+    torch.cuda.synchronize()
+    assert out is o
+    _close(o, ref, tol, str(key))
+    assert bool((o[cq[-1]:] == 7.0).all()), "rows behind the last sequence changed"
+    if sum(nq):
+        want = o[:cq[-1]].abs().flatten(1).amax(1).view(torch.int16).int()
+        assert torch.equal(am[:cq[-1]], want), "row maxima"
+    return o
+
+
+@pytest.mark.parametrize("D", [8, 16, 24, 32, 40, 64, 72, 80, 96, 104, 128, 136, 192, 200, 256])
+def test_head_sizes(D):
+    _dense((1, D), [70, 33], [70, 33], 2, 2, D, fused=True)
+
+
+@pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 500])
+@pytest.mark.parametrize("mask", [0, 1, 2])
+def test_lengths_and_masks(n, mask):
+    _dense((2, n, mask), [n], [n], 2, 1, 64, mask=mask)
+
+
+@pytest.mark.parametrize("nq, nk", [([1], [1000]), ([1, 1, 1], [1, 700, 64]), ([5, 0, 17], [300, 40, 5]), ([40], [7]), ([3, 64, 100], [0, 64, 1]),
+                                    ([0, 0, 9], [4, 0, 130])])
+@pytest.mark.parametrize("mask", [0, 1, 2])
+def test_rows_and_keys_of_different_number(nq, nk, mask):
+    """Causal rows in front of the first key, sequences without keys or rows: their outputs are zero, others are right."""
+    _dense((3, sum(nq), sum(nk), mask), nq, nk, 4, 2, 72, mask=mask)
+
+
+@pytest.mark.parametrize("Hq, Hkv", [(1, 1), (3, 1), (6, 2), (8, 1), (12, 4), (5, 5), (40, 2), (7, 7)])
+def test_shared_key_heads(Hq, Hkv):
+    _dense((4, Hq, Hkv), [37, 90, 4], [37, 90, 4], Hq, Hkv, 64, mask=1, fused=True)
+
+
+@pytest.mark.parametrize("cap, slopes", [(30.0, False), (0.0, True), (5.0, True)])
+@pytest.mark.parametrize("mask", [0, 1, 2])
+def test_score_forms(cap, slopes, mask):
+    _dense((5, int(cap), slopes, mask), [150, 61], [150, 61], 4, 2, 128, mask=mask, cap=cap, slopes=slopes, size=2.0)
+
+
+def test_rows_behind_the_last_sequence_stay():
+    _dense((6,), [20, 30], [64, 3], 3, 3, 40, extra=9)
+
+
+def test_equal_lengths_need_no_first_rows():
+    _dense((7,), [64] * 5, [64] * 5, 4, 4, 72, equal=True, fused=True)
+    _dense((7, 1), [16] * 3, [200] * 3, 4, 4, 64, equal=True)
+
+
+@pytest.mark.parametrize("size", [0.01, 8.0, 40.0])
+def test_small_and_large_scores(size):
+    """Weights that are nearly alike, and rows where one key takes everything; the maximum grows along the keys."""
+    _dense((8, int(size * 100)), [130], [333], 2, 2, 64, size=size)
+
+
+def test_growing_maximum():
+    """Every later key has the larger score, by more than what one weight can hold."""
+    D, n = 64, 256
+    q = torch.ones((1, 1, D), dtype=torch.float16, device="cuda")
+    k = (torch.arange(n, device="cuda").float() * 0.75).half()[:, None, None].expand(n, 1, D).contiguous()
+    v = _dev(_f16(_rng(9), n, 1, D))
+    for order in (torch.arange(n), torch.arange(n).flip(0), torch.randperm(n, generator=torch.Generator().manual_seed(3))):
+        kk, vv = k[order.cuda()].contiguous(), v[order.cuda()].contiguous()
+        ref, tol = oa.attention(q.cpu().numpy(), kk.cpu().numpy(), vv.cpu().numpy(), [0, 1], [0, n], 1.0)
+        o = ql.attention_f16(q, kk, vv, scale=1.0)
+        torch.cuda.synchronize()
+        _close(o, ref, tol)
+
+
+def test_heads_first_and_shared_rows():
+    """[H, T, D] storage, and keys that every head reads from the same place (stride 0)."""
+    g = _rng(10)
+    T, H, D = 100, 3, 64
+    q, k, v = _f16(g, H, T, D), _f16(g, T, 1, D), _f16(g, H, T, D)
+    dq, dv = _dev(q).transpose(0, 1), _dev(v).transpose(0, 1)
+    dk = _dev(k).expand(T, H, D)
+    o = torch.empty((H, T, D), dtype=torch.float16, device="cuda").transpose(0, 1)
+    ql.attention_f16(dq, dk, dv, o=o)
+    torch.cuda.synchronize()
+    ref, tol = oa.attention(q.transpose(1, 0, 2), np.repeat(k, H, 1), v.transpose(1, 0, 2), [0, T], [0, T], D ** -0.5)
+    _close(o, ref, tol)
+
+
+def test_values_outside_the_sequences_do_not_count():
+    """NaN and infinities in rows of no sequence, next to rows that count."""
+    g = _rng(11)
+    D, H = 72, 2
+    q, k, v = _f16(g, 60, H, D), _f16(g, 100, H, D), _f16(g, 100, H, D)
+    cq, ck = np.array([3, 20, 41], np.int32), np.array([10, 43, 77], np.int32)
+    for x, lo, hi in ((q, 3, 41), (k, 10, 77), (v, 10, 77)):
+        x[:lo], x[hi:] = np.nan, np.inf
+    o = torch.full((60, H, D), 3.0, dtype=torch.float16, device="cuda")
+    ql.attention_f16(_dev(q), _dev(k), _dev(v), cu_q=_dev(cq), cu_k=_dev(ck), o=o, mask=1)
+    torch.cuda.synchronize()
+    ref, tol = oa.attention(q, k, v, cq, ck, D ** -0.5, 1)
+    _close(o, ref, tol)
+    assert bool((o[:3] == 3.0).all()) and bool((o[41:] == 3.0).all())
+
+
+# ---- the cache ------------------------------------------------------------------------------------------------------------------
+
+class _Cached:
+    """A cache with random codes and scales, pages in no order, on both sides."""
+
+    def __init__(self, g, B, most, Hkv, D, page, S, spare=2):
+        self.B, self.page = B, page
+        per = -(-most // page)
+        P = B * per + spare
+        kc = g.integers(-127, 128, (P, Hkv, page, D)).astype(np.int8)
+        vc = g.integers(-127, 128, (P, Hkv, page // 64, D, 64)).astype(np.int8)
+        ks, vs = (g.uniform(0.005, 0.03, (P, Hkv, page // S)).astype(np.float32) for _ in range(2))
+        table = g.permutation(P)[:B * per].reshape(B, per).astype(np.int32)
+        self.ref = oa.Cache(kc, vc, ks, vs, table)
+        self.dev = ql.KvCache8(_dev(kc), _dev(vc), _dev(ks), _dev(vs))
+        self.table = _dev(table)
+
+    def same(self):
+        torch.cuda.synchronize()
+        for name, a, b in (("k", self.dev.k, self.ref.kc), ("v", self.dev.v, self.ref.vc), ("k_scale", self.dev.k_scale, self.ref.ks),
+                           ("v_scale", self.dev.v_scale, self.ref.vs)):
+            a = a.cpu().numpy()
+            assert np.array_equal(a, b), "%s: %d of %d differ, first at %s" % (name, (a != b).sum(), a.size, np.argwhere(a != b)[:2].tolist())
+
+
+def _append(g, c, lens, nq, Hq, rot=None, pairs=False, pos=None, size=1.0, equal=False, values=True):
+    Hkv, D = c.ref.heads, c.ref.D
+    T = sum(nq)
+    cu = _cu(nq)
+    rows = _f16(g, T, (Hq + 2 * Hkv) * D, size=size)
+    q, k, v = rows[:, :Hq * D].reshape(T, Hq, D), rows[:, Hq * D:(Hq + Hkv) * D].reshape(T, Hkv, D), rows[:, (Hq + Hkv) * D:].reshape(T, Hkv, D)
+    d = _dev(rows)
+    dq, dk, dv = d[:, :Hq * D].unflatten(1, (Hq, D)), d[:, Hq * D:(Hq + Hkv) * D].unflatten(1, (Hkv, D)), d[:, (Hq + Hkv) * D:].unflatten(1, (Hkv, D))
+    ref = c.ref.append(k, v, cu, lens, q, rot, pairs, pos)
+    q_out = torch.full((T, Hq, D), 5.0, dtype=torch.float16, device="cuda")
+    k_out, v_out = (torch.full((T, Hkv, D), 5.0, dtype=torch.float16, device="cuda") if values else None for _ in range(2))
+    ql.daq_kv_append(c.dev, dk, dv, c.table, _dev(np.asarray(lens, np.int32)), cu=None if equal else _dev(cu), q=dq, rot=_dev(rot), rot_pairs=pairs,
+                     pos=_dev(pos), q_out=q_out, k_out=k_out, v_out=v_out)
+    c.same()
+    for name, t in (("q_out", q_out), ("k_out", k_out), ("v_out", v_out)):
+        if t is None:
+            continue
+        a, b = t.cpu().numpy(), ref[name]
+        live = ~np.isnan(b)
+        assert np.array_equal(a[live], b[live]), name
+        assert (a[~live] == 5.0).all(), name
+    return q_out
+
+
+def _table(rows, rot_dim):
+    a = np.arange(rows)[:, None] * 10000.0 ** (-np.arange(rot_dim // 2) / (rot_dim // 2))
+    return np.stack((np.cos(a), np.sin(a)), -1).astype(np.float32)
+
+
+@pytest.mark.parametrize("S", [1, 16, 32, 64])
+@pytest.mark.parametrize("D, page", [(64, 64), (72, 128), (128, 64), (256, 192), (8, 64)])
+def test_append_prompts_then_tokens(S, D, page):
+    """Prompts that end inside groups, then single tokens and short runs that raise the scales of blocks with earlier tokens."""
+    g = _rng(20, S, D, page)
+    c = _Cached(g, 3, 400, 2, D, page, S)
+    rot = _table(400, D // 16 * 16) if D >= 16 else None
+    lens = np.array([70, 1, 191], np.int32)
+    _append(g, c, lens, [70, 1, 191], 4, rot, size=0.5)
+    for n, size in ((1, 0.4), (1, 3.0), (3, 1.0), (1, 5.0), (20, 2.0), (65, 6.0), (1, 0.1)):
+        lens = lens + n
+        _append(g, c, lens, [n] * 3, 4, rot, size=size, equal=n == 1)
+
+
+def test_append_ragged_runs_and_sequences_without_tokens():
+    g = _rng(21)
+    c = _Cached(g, 70, 300, 1, 64, 64, 16)
+    nq = [int(x) for x in g.integers(0, 40, 70)]
+    lens = np.array([n + int(x) for n, x in zip(nq, g.integers(0, 250, 70))], np.int32)
+    _append(g, c, lens, nq, 3, _table(300, 32), pairs=True)
+
+
+@pytest.mark.parametrize("pairs", [False, True])
+def test_append_rotation_by_given_positions(pairs):
+    g = _rng(22, pairs)
+    c = _Cached(g, 2, 128, 2, 96, 64, 32)
+    pos = g.integers(-2, 60, 50).astype(np.int32)          # some outside the table: its nearest row
+    _append(g, c, np.array([30, 20], np.int32), [30, 20], 2, _table(50, 64), pairs, pos)
+
+
+def test_append_zero_blocks():
+    """A block of zeros has scale 0; a later token raises it."""
+    g = _rng(23)
+    c = _Cached(g, 1, 64, 1, 64, 64, 64)
+    _append(g, c, np.array([5], np.int32), [5], 1, size=0.0)
+    assert float(c.dev.k_scale[c.table[0, 0].item()].max()) == 0.0
+    _append(g, c, np.array([6], np.int32), [1], 1, size=0.01)
+    _append(g, c, np.array([7], np.int32), [1], 1, size=0.0)
+    _append(g, c, np.array([40], np.int32), [33], 1, size=1.0)
+
+
+def test_append_to_pages_that_are_none():
+    """Entries outside the pool, and tokens behind the table's end or in front of the sequence: nothing is written for them."""
+    g = _rng(24)
+    c = _Cached(g, 4, 192, 2, 64, 64, 32)
+    for b, e, bad in ((0, 1, -1), (1, 0, 10 ** 6), (3, 2, c.ref.pages)):
+        c.ref.table[b, e] = bad
+    c.table.copy_(torch.from_numpy(c.ref.table))
+    _append(g, c, np.array([100, 70, 230, 190], np.int32), [100, 70, 90, 100], 2, _table(300, 64))
+    _append(g, c, np.array([5, 70, 192, 190], np.int32), [9, 1, 1, 1], 2, _table(300, 64))
+
+
+def _cached(key, nq, nk, Hq, Hkv, D, page=64, S=64, mask=1, cap=0.0, slopes=False, equal=False, cache=None, size=1.0):
+    g = _rng(*key)
+    c = cache or _Cached(g, len(nq), max(max(nk), 1), Hkv, D, page, S)
+    T = sum(nq)
+    q = _f16(g, T, Hq, D, size=size)
+    prefix = g.integers(0, max(nk) + 2, len(nq)).astype(np.int32) if mask == 2 else None
+    sl = g.uniform(0, 0.3, Hq).astype(np.float32) if slopes else None
+    cu = _cu(nq)
+    scale = 0.5 * D ** -0.5
+    ref, tol = oa.attention_cached(q, c.ref, cu, nk, scale, mask, prefix, cap, sl)
+    am = torch.full((T,), -1, dtype=torch.int32, device="cuda")
+    o = ql.attention_kv8(_dev(q), c.dev, c.table, _dev(np.asarray(nk, np.int32)), cu_q=None if equal else _dev(cu), mask=mask, prefix=_dev(prefix), scale=scale,
+                         cap=cap, slopes=_dev(sl), row_absmax=am)
+    torch.cuda.synchronize()
+    _close(o, ref, tol, str(key))
+    assert torch.equal(am, o.abs().flatten(1).amax(1).view(torch.int16).int()), "row maxima"
+    return o
+
+
+@pytest.mark.parametrize("S", [1, 16, 32, 64])
+@pytest.mark.parametrize("D", [8, 32, 40, 64, 72, 96, 128, 160, 192, 256])
+def test_cached_tokens(S, D):
+    _cached((30, S, D), [1, 1, 1], [1, 64, 333], 8, 2, D, 64, S, equal=True)
+
+
+@pytest.mark.parametrize("n", [1, 15, 16, 17, 63, 64, 65, 127, 128, 129, 1000, 2500])
+def test_cached_lengths(n):
+    _cached((31, n), [1], [n], 4, 1, 128, 128, 32, equal=True)
+
+
+@pytest.mark.parametrize("Hq, Hkv", [(1, 1), (2, 2), (3, 1), (8, 1), (16, 1), (17, 1), (32, 1), (40, 1), (12, 4)])
+@pytest.mark.parametrize("n", [1, 4, 9])
+def test_cached_rows_per_key_head(Hq, Hkv, n):
+    """From one packed row to hundreds for a key head."""
+    _cached((32, Hq, Hkv, n), [n, n], [200, n], Hq, Hkv, 64, 64, 16, equal=True)
+
+
+@pytest.mark.parametrize("mask", [0, 1, 2])
+@pytest.mark.parametrize("cap, slopes", [(0.0, False), (20.0, True)])
+def test_cached_chunks(mask, cap, slopes):
+    _cached((33, mask, int(cap)), [130, 1, 64, 0, 200], [500, 1, 64, 70, 200], 4, 2, 64, 64, 32, mask, cap, slopes)
+
+
+def test_cached_sequences_without_tokens_and_rows_in_front():
+    _cached((34,), [1, 3, 2, 40], [0, 2, 100, 9], 4, 2, 64, 64, 64)
+
+
+def test_cached_many_sequences():
+    g = _rng(35)
+    nk = [int(x) for x in g.integers(1, 400, 150)]
+    _cached((35, 1), [1] * 150, nk, 4, 2, 64, 64, 64, equal=True)
+
+
+def test_cached_scales_of_very_different_size():
+    """Values whose scales differ by ten powers of two within a sequence: small ones still count where their weight is large."""
+    g = _rng(36)
+    for S in (1, 32):
+        c = _Cached(g, 2, 300, 2, 64, 64, S)
+        c.ref.vs[:] = (c.ref.vs * 2.0 ** g.integers(-10, 11, c.ref.vs.shape)).astype(np.float32)
+        c.dev.v_scale.copy_(torch.from_numpy(c.ref.vs))
+        _cached((36, S), [1, 1], [300, 170], 4, 2, 64, 64, S, equal=True, cache=c)
+
+
+def test_cached_pages_that_are_none_are_not_visible():
+    g = _rng(37)
+    c = _Cached(g, 3, 256, 2, 64, 64, 32)
+    for b, e, bad in ((0, 1, -1), (1, 0, 10 ** 6), (2, 0, -5), (2, 1, c.ref.pages), (2, 2, -1), (2, 3, -1)):
+        c.ref.table[b, e] = bad
+    c.table.copy_(torch.from_numpy(c.ref.table))
+    o = _cached((37, 1), [1, 70, 3], [256, 256, 256], 4, 2, 64, 64, 32, cache=c)
+    assert bool((o[71:] == 0).all())
+
+
+def test_cached_scales_behind_the_end_do_not_count():
+    """Scales of tokens that are not there hold anything."""
+    g = _rng(38)
+    for S in (1, 16, 64):
+        c = _Cached(g, 2, 128, 1, 64, 64, S)
+        used = {(int(c.ref.table[b, j // 64]), j % 64 // S) for b, n in ((0, 70), (1, 3)) for j in range(n)}
+        for p in range(c.ref.pages):
+            for i in range(64 // S):
+                if (p, i) not in used:
+                    c.ref.ks[p, :, i] = np.nan
+                    c.ref.vs[p, :, i] = np.inf
+        c.dev.k_scale.copy_(torch.from_numpy(c.ref.ks))
+        c.dev.v_scale.copy_(torch.from_numpy(c.ref.vs))
+        _cached((38, S), [1, 1], [70, 3], 2, 1, 64, 64, S, equal=True, cache=c)

@@ -78,6 +78,31 @@ __device__ __forceinline__ SeqRows seq_rows(const int *cu, int b, int T, int B)
     return {lo, hi - lo};
 }
 
+// Item `item` of a list that has count(b) items of every sequence b one behind the other: its sequence (-1: behind the last) and its number
+// there.  64 sequences at a time, one per lane; the result is the same in all lanes.
+template <class CountFn>
+__device__ __forceinline__ int find_sequence(int B, int &item, CountFn count)
+{
+    const int lane = threadIdx.x & 63;
+    for (int base = 0; base < B; base += 64) {
+        const int mine = base + lane < B ? count(base + lane) : 0;
+        int upto = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(upto, d, 64);
+            if (lane >= d) upto += o;
+        }
+        const unsigned long long behind = __ballot(upto > item);
+        if (behind) {
+            const int l = __ffsll((unsigned long long)behind) - 1;
+            item = __builtin_amdgcn_readfirstlane(item - __shfl(upto - mine, l, 64));
+            return __builtin_amdgcn_readfirstlane(base + l);
+        }
+        item = __builtin_amdgcn_readfirstlane(item - __shfl(upto, 63, 64));
+    }
+    return -1;
+}
+
 // keys that row position p sees: [0, n_k) cut by the mask; those below the prefix always
 __device__ __forceinline__ int visible_end(int mask, int prefix, int p, int n_k)
 {

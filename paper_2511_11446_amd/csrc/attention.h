@@ -45,6 +45,7 @@ struct AttnArgs {
 
 hipError_t launch_attention_f16(const AttnArgs &a, hipStream_t stream);
 hipError_t launch_attention_kv8(const AttnArgs &a, hipStream_t stream);
+size_t cached_partial_bytes(int D);   // of workspace that launch_attention_kv8 needs
 
 struct KvAppendArgs {
     int8_t *kc, *vc;

@@ -179,7 +179,8 @@ int daq_kv_append(const ql_kv_cache *cache, const ql_kv_new *n, void *stream)
 
 size_t attention_kv8_workspace_bytes(int64_t T_q, int32_t B, int32_t Hq, int32_t Hkv, int32_t D)
 {
-    return 0;
+    if (check_heads(T_q, B, Hq, D, false) || Hkv < 1 || Hq % Hkv != 0) return 0;
+    return ql::cached_partial_bytes(D);
 }
 
 int attention_kv8(const ql_attention *attn, const ql_kv_cache *cache, void *workspace, size_t workspace_bytes, void *stream)

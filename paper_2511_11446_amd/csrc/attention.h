@@ -45,7 +45,11 @@ struct AttnArgs {
 
 hipError_t launch_attention_f16(const AttnArgs &a, hipStream_t stream);
 hipError_t launch_attention_kv8(const AttnArgs &a, hipStream_t stream);
-size_t cached_partial_bytes(int D);   // of workspace that launch_attention_kv8 needs
+hipError_t launch_attention_chunks(const AttnArgs &a, hipStream_t stream);
+// workspace of the launches
+size_t tiles_partial_bytes(long long Tq, long long Tk, int B, int Hq, int Hkv, int D);
+size_t chunks_partial_bytes(long long Tq, int B, int Hq, int Hkv, int D);
+size_t cached_partial_bytes(long long Tq, int B, int Hq, int Hkv, int D);   // either
 
 struct KvAppendArgs {
     int8_t *kc, *vc;

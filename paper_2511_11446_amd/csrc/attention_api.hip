@@ -8,13 +8,15 @@ namespace {
 
 constexpr int64_t INT_MAX64 = 2147483647;
 
+constexpr int64_t STRIDE_MAX = 1 << 24;   // elements between rows: 64 of them are addressed with 32 bits
+
 inline bool off(const void *p, size_t a) { return p && (uintptr_t)p % a != 0; }
 
 // a strided [T, H, D] tensor of binary16: strides in elements
 int check_rows(const void *p, int64_t row, int64_t head)
 {
     if (!p) return QL_ERR_NULL;
-    if (row < 0 || head < 0 || row % 8 != 0 || head % 8 != 0 || row > INT_MAX64 || head > INT_MAX64) return QL_ERR_SHAPE;
+    if (row < 0 || head < 0 || row % 8 != 0 || head % 8 != 0 || row > STRIDE_MAX || head > INT_MAX64) return QL_ERR_SHAPE;
     return off(p, 16) ? QL_ERR_ALIGN : QL_OK;
 }
 
@@ -96,7 +98,8 @@ extern "C" {
 
 size_t attention_f16_workspace_bytes(int64_t T_q, int64_t T_k, int32_t B, int32_t Hq, int32_t Hkv, int32_t D)
 {
-    return 0;
+    if (check_heads(T_q, B, Hq, D, false) || Hkv < 1 || Hq % Hkv != 0 || check_heads(T_k, B, Hkv, D, false)) return 0;
+    return ql::tiles_partial_bytes(T_q, T_k, B, Hq, Hkv, D);
 }
 
 int attention_f16(const ql_attention *attn, const void *k, int64_t k_row, int64_t k_head, const void *v, int64_t v_row, int64_t v_head,
@@ -180,7 +183,7 @@ int daq_kv_append(const ql_kv_cache *cache, const ql_kv_new *n, void *stream)
 size_t attention_kv8_workspace_bytes(int64_t T_q, int32_t B, int32_t Hq, int32_t Hkv, int32_t D)
 {
     if (check_heads(T_q, B, Hq, D, false) || Hkv < 1 || Hq % Hkv != 0) return 0;
-    return ql::cached_partial_bytes(D);
+    return ql::cached_partial_bytes(T_q, B, Hq, Hkv, D);
 }
 
 int attention_kv8(const ql_attention *attn, const ql_kv_cache *cache, void *workspace, size_t workspace_bytes, void *stream)

@@ -1,0 +1,65 @@
+// Attention of many rows over the paged 8-bit cache for gfx950: prompts that enter it by chunks.
+//
+// The tile of attention_tile.h, its keys and values made from the codes: a workgroup reads a group of 64 tokens once, through registers, turns the codes into
+// binary16 (exactly) and leaves them in LDS for its 256 rows.  Where one scale covers the group it goes into the factor of the
+// scores and into the exponent of the weights, at no cost per score; smaller blocks multiply both.
+#include "attention_tile.h"
+
+namespace ql {
+
+// wavefronts of a workgroup: long heads need all registers of a SIMD for one
+constexpr int chunk_waves(int KS) { return KS <= 8 ? 8 : 4; }
+
+template <int KS, bool SHAPED>
+__global__ __launch_bounds__(64 * chunk_waves(KS), KS <= 8 ? 2 : 1) void attend_chunks(AttnArgs a, TilePlan plan)
+{
+    attend_tile<KS, chunk_waves(KS), true, SHAPED>(a, plan);
+}
+
+__global__ __launch_bounds__(256) void join_chunks(AttnArgs a, TilePlan plan, int rows_per) { join_splits(a, plan, rows_per); }
+
+namespace {
+constexpr int CUS = 256;
+constexpr int chunk_rows(int D) { return 32 * chunk_waves((D + 15) / 16); }
+
+template <int KS>
+hipError_t launch_chunks(const AttnArgs &a, hipStream_t stream)
+{
+    using T = AttnTile<KS, chunk_waves(KS), true>;
+    const TilePlan p = tile_plan(a.Tq, a.B, a.G, a.Hkv, T::ROWS, a.cu_q, a.mask, (long long)a.max_pages * a.page, CUS);
+    static const hipError_t opt_in[2] = {
+        hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_chunks<KS, false>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES),
+        hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_chunks<KS, true>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES)};
+    const bool shaped = a.cap > 0.0f || a.slopes;
+    if (opt_in[shaped] != hipSuccess) return opt_in[shaped];
+    const long long wgs = (long long)p.tiles * a.Hkv * p.splits;
+    if (wgs > 0x7fffff00LL / T::NT) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)((wgs + 7) / 8 * 8));
+    if (shaped) hipLaunchKernelGGL((attend_chunks<KS, true>), grid, dim3(T::NT), T::LDS_BYTES, stream, a, p);
+    else hipLaunchKernelGGL((attend_chunks<KS, false>), grid, dim3(T::NT), T::LDS_BYTES, stream, a, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.splits == 1) return e;
+    hipLaunchKernelGGL(join_chunks, dim3((unsigned)(p.tiles * a.Hkv), T::ROWS / 4), dim3(256), 0, stream, a, p, T::ROWS);
+    return hipGetLastError();
+}
+}  // namespace
+
+size_t chunks_partial_bytes(long long Tq, int B, int Hq, int Hkv, int D)
+{
+    const TilePlan p = tile_plan(Tq, B, Hq / Hkv, Hkv, chunk_rows(D), true, 0, 1LL << 31, CUS);
+    return p.splits == 1 ? 0 : (size_t)p.tiles * Hkv * p.splits * chunk_rows(D) * (D + 2) * 4;
+}
+
+hipError_t launch_attention_chunks(const AttnArgs &a, hipStream_t stream)
+{
+    const int ks = (a.D + 15) / 16;
+    if (ks <= 2) return launch_chunks<2>(a, stream);
+    if (ks <= 4) return launch_chunks<4>(a, stream);
+    if (ks <= 5) return launch_chunks<5>(a, stream);
+    if (ks <= 6) return launch_chunks<6>(a, stream);
+    if (ks <= 8) return launch_chunks<8>(a, stream);
+    if (ks <= 12) return launch_chunks<12>(a, stream);
+    return launch_chunks<16>(a, stream);
+}
+
+}  // namespace ql

@@ -16,8 +16,6 @@
 
 namespace ql {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
 struct CachedPlan {
     int workers;          // workgroups of the launch
 };
@@ -88,24 +86,6 @@ __device__ __forceinline__ float lanes16_sum(float x)
     const auto s = __builtin_amdgcn_permlane16_swap(w, w, false, false);
     const unsigned c = s[0], d = s[1];
     return __builtin_bit_cast(float, c) + __builtin_bit_cast(float, d);
-}
-
-__device__ __forceinline__ unsigned absmax_bits(_Float16 x) { return (unsigned)__builtin_bit_cast(unsigned short, x) & 0x7fffu; }
-
-// four codes -> four binary16: the byte with its sign bit turned is code + 128; 0x6400 | byte is 1024 + byte in binary16
-__device__ __forceinline__ void codes_f16(unsigned w, f16x2 &lo, f16x2 &hi)
-{
-    const f16x2 bias = {(_Float16)1152.0f, (_Float16)1152.0f};
-    const unsigned u = w ^ 0x80808080u;
-    lo = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) - bias;
-    hi = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) - bias;
-}
-__device__ __forceinline__ f16x8 codes_f16x8(unsigned w0, unsigned w1)
-{
-    f16x2 a, b, c, d;
-    codes_f16(w0, a, b);
-    codes_f16(w1, c, d);
-    return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
 // wavefronts per SIMD: as many as the loads of a whole unit leave registers for
@@ -453,10 +433,19 @@ hipError_t launch_by_head(const AttnArgs &a, const CachedPlan &p, hipStream_t st
 }  // namespace
 
 int cached_workers(int D) { return D <= 128 ? 1024 : 512; }
-size_t cached_partial_bytes(int D) { return (size_t)cached_workers(D) * 2 * 16 * (D + 2) * 4; }
+
+size_t cached_partial_bytes(long long Tq, int B, int Hq, int Hkv, int D)
+{
+    const size_t few = (size_t)cached_workers(D) * 2 * 16 * (D + 2) * 4, many = chunks_partial_bytes(Tq, B, Hq, Hkv, D);
+    return few > many ? few : many;
+}
+
+// packed rows of a sequence and key head, on average, up to which they go by 16
+constexpr int FEW_ROWS = 16;
 
 hipError_t launch_attention_kv8(const AttnArgs &a, hipStream_t stream)
 {
+    if ((long long)a.Tq * a.G > (long long)FEW_ROWS * a.B) return launch_attention_chunks(a, stream);
     const CachedPlan p{cached_workers(a.D)};
     const hipError_t e = a.scale_tokens == 1 ? launch_by_head<true>(a, p, stream) : launch_by_head<false>(a, p, stream);
     if (e != hipSuccess) return e;

@@ -1,37 +1,34 @@
-// The tile of attention: a wavefront's 32 packed rows against 64 keys at a time (attention.hip).  Not part of the public ABI.
+// The tile of attention: a wavefront's 32 packed rows against 64 keys at a time, keys and values from binary16 rows or from the 8-bit cache
+// (attention.hip, attention_chunks.hip).  Not part of the public ABI.
 //
 // Scores come as S^T = K Q^T (mfma 32x32x16): a lane has ONE row (lane & 31) and 16 of 32 keys, so the running maximum and sum of a row
 // are the lane's own up to one exchange with lane ^ 32, masks and biases know the row without an index, and the weights are in the
 // place where O^T = V^T P^T wants its right operand: keys 16 s + 8 (j / 4) + 4 (lane / 32) + j % 4 of a lane are slots j of step s on
-// both sides, whatever their order.  V^T comes out of the row-major tile by the transposing LDS read (4 keys of 16 channels).
+// both sides, whatever their order.
+//
+// The loop is pipelined: round t multiplies the values of tile t - 1 with their weights and the keys of tile t + 1 with the queries, both on the matrix
+// cores, while the vector units take the weights of tile t from its scores.  The three do not wait for each other, and the code places a part
+// of the exponentials behind every matrix instruction.  So in LDS keys run two tiles ahead of values, two stages of each.
 #pragma once
 #include "attention.h"
+
+#include <type_traits>
 
 namespace ql {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) void attn_lds;
 typedef const __attribute__((address_space(1))) void attn_global;
 typedef __attribute__((address_space(3))) s16x4 attn_lds_s4;
 
 constexpr int ATT_KEYS = 64;   // keys of a tile
+static_assert(ATT_KEYS == KV_GROUP, "a tile of the cache is one group");
 constexpr float LOG2E = 1.4426950408889634f;
-
-// CHP: 16-byte pieces of a tile row (D / 8 rounded up to a multiple of 2).  A row is kept without padding (a wavefront's DMA fills 1024
-// neighbouring bytes); the piece c of row r sits at slot c ^ f(r), so that 8 rows read at one piece index (keys) and 4 rows read at 4
-// neighbouring ones (values) spread over all banks.
-template <int CHP> __device__ __forceinline__ constexpr int key_swizzle(int r)
-{
-    return CHP % 16 == 0 ? (r & 7) : CHP % 16 == 8 ? (r >> 1 & 7) : CHP % 4 == 0 ? (r >> 2 & 3) : 0;
-}
-template <int CHP> __device__ __forceinline__ constexpr int value_swizzle(int r)
-{
-    return CHP % 16 == 0 ? (r & 3) << 2 : CHP % 16 == 8 ? (r >> 1 & 1) << 2 : 0;
-}
 
 // a lane's value and that of lane ^ 32, which has the same row (the two results are taken out as whole words first: a bit cast of a vector
 // element reads element 0)
@@ -48,7 +45,632 @@ __device__ __forceinline__ Halves both_halves(float x)
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// cap * tanh(x / cap) from x / cap * 2 log2(e) (t): 1 - 2 / (1 + e^2x), absolute error about 1e-7 of the cap
-__device__ __forceinline__ float capped(float t, float cap) { return cap - 2.0f * cap * __builtin_amdgcn_rcpf(1.0f + exp2_fast(t)); }
+// cap * tanh(x / cap) from t = 2 log2(e) x / cap: cap - 2 cap / (1 + e^(2 x / cap)), absolute error about 1e-7 of the cap
+__device__ __forceinline__ float capped(float t, float cap) { return __builtin_fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(1.0f + exp2_fast(t)), cap); }
+
+// four codes -> four binary16: the byte with its sign bit turned is code + 128; 0x6400 | byte is 1024 + byte in binary16
+__device__ __forceinline__ void codes_f16(unsigned w, f16x2 &lo, f16x2 &hi)
+{
+    const f16x2 bias = {(_Float16)1152.0f, (_Float16)1152.0f};
+    const unsigned u = w ^ 0x80808080u;
+    lo = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) - bias;
+    hi = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) - bias;
+}
+__device__ __forceinline__ f16x8 codes_f16x8(unsigned w0, unsigned w1)
+{
+    f16x2 a, b, c, d;
+    codes_f16(w0, a, b);
+    codes_f16(w1, c, d);
+    return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+__device__ __forceinline__ unsigned absmax_bits(_Float16 x) { return (unsigned)__builtin_bit_cast(unsigned short, x) & 0x7fffu; }
+
+// CHP: 16-byte pieces of a tile row (D / 8 rounded up to a multiple of 2).  A row is kept without padding (a wavefront's DMA fills 1024
+// neighbouring bytes); the piece c of row r sits at slot c ^ f(r), so that 8 rows read at one piece index (keys) and 4 rows read at 4
+// neighbouring ones (values) spread over all banks.
+template <int CHP> __device__ __forceinline__ constexpr int key_swizzle(int r)
+{
+    return CHP % 16 == 0 ? (r & 7) : CHP % 16 == 8 ? (r >> 1 & 7) : CHP % 4 == 0 ? (r >> 2 & 3) : 0;
+}
+template <int CHP> __device__ __forceinline__ constexpr int value_swizzle(int r)
+{
+    return CHP % 16 == 0 ? (r & 3) << 2 : CHP % 16 == 8 ? (r >> 1 & 1) << 2 : 0;
+}
+
+struct TilePlan {
+    int tiles;     // row tiles of the launch: a bound with cu_q
+    int per_seq;   // row tiles of a sequence without cu_q
+    int splits;    // parts that the keys are cut into
+    int mix;       // workgroups go through all heads tile by tile, the last rows first (else head by head on one XCD)
+};
+
+// Weights may grow to 2^8 before the sums are brought to a new maximum: they stay far inside binary16, and most tiles skip the scaling.
+constexpr float GROWTH = 8.0f;
+constexpr float LEAST_SCALE = 1e-30f;   // stands for a scale of 0, so that -inf times it stays -inf
+constexpr float LEAST_RATIO = -30.0f;   // log2 of the smallest value scale that counts beside the largest: below, a weight is 0 in binary16
+
+// KS: 16-channel steps of the scores; NW: wavefronts; CACHE: keys and values from the 8-bit cache; SHAPED: scores may be capped or biased
+template <int KS, int NW, bool CACHE>
+struct AttnTile {
+    static constexpr int CHP = 2 * KS, DT = (KS + 1) / 2, ROWS = 32 * NW, NT = 64 * NW;
+    static constexpr int K_BYTES = ATT_KEYS * CHP * 16;
+    // values: rows like the keys' (a read of channels behind D may pass the last row: 1024 bytes behind the last stage), or transposed codes
+    static constexpr int V_BYTES = CACHE ? DT * 32 * 128 : K_BYTES;
+    static constexpr int V_AT = 2 * K_BYTES, SCALES_AT = V_AT + 2 * V_BYTES;
+    static constexpr int LDS_BYTES = SCALES_AT + (CACHE ? 6 * ATT_KEYS * 4 : 1024);   // scales of two stages (keys) and four (values), or the slack
+    // CACHE: register-staged pieces of a thread: 8 key codes each; 32 value codes of a channel each
+    static constexpr int NKP = CACHE ? (ATT_KEYS * CHP + NT - 1) / NT : 1, NVP = CACHE ? (64 * DT + NT - 1) / NT : 1;
+};
+
+template <int KS, int NW, bool CACHE, bool SHAPED>
+__device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &plan)
+{
+    using T = AttnTile<KS, NW, CACHE>;
+    constexpr int CHP = T::CHP, DT = T::DT;
+    constexpr int NI = (CHP + NW - 1) / NW;            // DMA instructions of a wavefront for one tile
+    extern __shared__ __align__(1024) unsigned char smem[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int half = lane >> 5;
+
+    const int wgs = plan.tiles * a.Hkv * plan.splits;
+    int id = blockIdx.x;
+    if (!plan.mix) {
+        const int per_xcd = (gridDim.x + 7) / 8;
+        id = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
+    }
+    if (id >= wgs) return;
+    const int split = id % plan.splits;
+    id /= plan.splits;
+    int tile, hk, b, flat;                             // flat: number of the row tile in the launch
+    if (a.cu_q) {
+        flat = plan.mix ? plan.tiles - 1 - id / a.Hkv : id % plan.tiles;
+        hk = plan.mix ? id % a.Hkv : id / plan.tiles;
+        tile = flat;
+        b = find_sequence(a.B, tile, [&](int s) { return (seq_rows(a.cu_q, s, a.Tq, a.B).n * a.G + T::ROWS - 1) / T::ROWS; });
+        if (b < 0) return;
+    } else {
+        const int heads = a.Hkv * a.B, bh = plan.mix ? id % heads : id / plan.per_seq;
+        tile = plan.mix ? plan.per_seq - 1 - id / heads : id % plan.per_seq;
+        hk = bh % a.Hkv;
+        b = bh / a.Hkv;
+        flat = b * plan.per_seq + tile;
+    }
+    const SeqRows sq = seq_rows(a.cu_q, b, a.Tq, a.B);
+    const SeqRows sk = CACHE ? SeqRows{0, min(max(a.len_k[b], 0), a.max_pages * a.page)} : seq_rows(a.cu_k, b, a.Tk, a.B);
+    const int rows = sq.n * a.G;
+    const int wrow = tile * T::ROWS + wave * 32 + (lane & 31);   // packed row of this lane
+    const int row = min(wrow, rows - 1);
+    const int token = row / a.G, head = hk * a.G + row % a.G;
+    const int pos = token + sk.n - sq.n;
+    const int prefix = a.prefix ? a.prefix[b] : 0;
+    const int end = visible_end(a.mask, prefix, pos, sk.n);
+    const int last_token = (min(tile * T::ROWS + T::ROWS, rows) - 1) / a.G;
+    const int end_all = visible_end(a.mask, prefix, last_token + sk.n - sq.n, sk.n);   // what the workgroup reads
+    const int wrow0 = min(tile * T::ROWS + wave * 32, rows - 1), wrow1 = min(tile * T::ROWS + wave * 32 + 31, rows - 1);
+    // of this wavefront's rows: the fewest and the most keys (visible_end grows with the row)
+    const int end_min = __builtin_amdgcn_readfirstlane(visible_end(a.mask, prefix, wrow0 / a.G + sk.n - sq.n, sk.n));
+    const int end_max = tile * T::ROWS + wave * 32 < rows ? __builtin_amdgcn_readfirstlane(visible_end(a.mask, prefix, wrow1 / a.G + sk.n - sq.n, sk.n)) : 0;
+
+    const int key_tiles = (end_all + ATT_KEYS - 1) / ATT_KEYS;
+    const int share = (key_tiles + plan.splits - 1) / plan.splits;
+    const int t0 = min(split * share, key_tiles), t1 = min(t0 + share, key_tiles);
+    const int tw = min((end_max + ATT_KEYS - 1) / ATT_KEYS, t1);   // this wavefront's tiles end here
+
+    // queries stay in registers: channels 16 ks + 8 half .. + 7 of the lane's row, zeros behind D
+    const int CH = a.D / 8;
+    const unsigned negative = a.scale < 0.0f ? 0x80008000u : 0u;   // scores are |scale| * (-q).k
+    f16x8 qf[KS];
+    {
+        const _Float16 *q = static_cast<const _Float16 *>(a.q) + (sq.first + token) * a.q_row + head * a.q_head;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const int c = 2 * ks + half;
+            uint4 w = make_uint4(0, 0, 0, 0);
+            if (c < CH) w = *reinterpret_cast<const uint4 *>(q + 8 * c);
+            w.x ^= negative;
+            w.y ^= negative;
+            w.z ^= negative;
+            w.w ^= negative;
+            qf[ks] = __builtin_bit_cast(f16x8, w);
+        }
+    }
+    const float scale2 = fmaxf(fabsf(a.scale) * LOG2E, LEAST_SCALE);   // scores in powers of two
+    const float slope2 = a.slopes ? a.slopes[head] * LOG2E : 0.0f;
+    const float cap2 = a.cap * LOG2E, cap_in = a.cap > 0.0f ? 2.0f * LOG2E / cap2 : 0.0f;
+
+    // ---- tiles into LDS ------------------------------------------------------------------------------------------------------------
+    // rows: instruction i of this wavefront fills pieces [64 (i NW + wave), + 64) of the tile; a row behind the last key reads the last
+    // one, a piece behind D the row's last one: what is read there meets weights or queries that are zero
+    const unsigned char *kb = static_cast<const unsigned char *>(a.k) + 2 * (sk.first * a.k_row + hk * a.k_head);
+    const unsigned char *vb = static_cast<const unsigned char *>(a.v) + 2 * (sk.first * a.v_row + hk * a.v_head);
+    unsigned koff[NI], voff[NI];                       // of this lane's piece from the tile's first row
+    auto piece_at = [&](int i, bool value, int last_row, unsigned row_bytes) {
+        const int ci = 64 * (i * NW + wave) + lane, r = ci / CHP, c = ci % CHP;
+        return min(r, last_row) * row_bytes + 16 * min(c ^ (value ? value_swizzle<CHP>(r) : key_swizzle<CHP>(r)), CH - 1);
+    };
+    const unsigned krow = 2 * (unsigned)a.k_row, vrow = 2 * (unsigned)a.v_row;
+    if constexpr (!CACHE) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            koff[i] = piece_at(i, false, ATT_KEYS, krow);
+            voff[i] = piece_at(i, true, ATT_KEYS, vrow);
+        }
+    }
+    auto dma = [&](bool value, int t, int stage) {
+        const int left = sk.n - t * ATT_KEYS - 1;      // rows behind the tile's first one
+        const unsigned char *from = value ? vb + (size_t)t * ATT_KEYS * 2 * a.v_row : kb + (size_t)t * ATT_KEYS * 2 * a.k_row;
+        unsigned char *to = value ? smem + T::V_AT + stage * T::V_BYTES : smem + stage * T::K_BYTES;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            if (CHP % NW != 0 && i * NW + wave >= CHP) break;
+            unsigned at = value ? voff[i] : koff[i];
+            if (left < ATT_KEYS - 1) at = piece_at(i, value, left, value ? vrow : krow);
+            __builtin_amdgcn_global_load_lds((attn_global *)(from + at), (attn_lds *)(to + (i * NW + wave) * 1024), 16, 0, 0);
+        }
+    };
+    // cache: codes through registers; a page that is none reads page 0 and counts as masked
+    uint2 kreg[T::NKP];
+    uint4 vreg[T::NVP][2];
+    float kscale_reg = 0.0f, vscale_reg = 0.0f;
+    float *lds_ks = reinterpret_cast<float *>(smem + T::SCALES_AT), *lds_vs = lds_ks + 2 * ATT_KEYS;   // [stage][token], [tile % 4][token]
+    struct Where {
+        size_t at;      // token of the cache where the tile begins, counted within its key head: (page * Hkv + hk) * page_tokens + in_page
+        bool held;
+    };
+    int pages = 0;                                     // of 64 tiles from tile pages_at on, one per lane
+    int pages_at = -ATT_KEYS;
+    unsigned held_tiles = 0;                           // bit: whether the keys' stage has a page
+    auto where = [&](int t) {
+        if (t - pages_at >= 63) {                      // keys ask for a tile, then values for the one in front of it
+            pages_at = max(t - 1, t0);
+            const int mine = pages_at + lane;
+            pages = mine < t1 ? a.page_table[(size_t)b * a.max_pages + (unsigned)(mine * ATT_KEYS) / (unsigned)a.page] : -1;
+        }
+        int page = __builtin_amdgcn_readlane(pages, t - pages_at);
+        const bool held = page >= 0 && page < a.num_pages;
+        if (!held) page = 0;
+        return Where{((size_t)page * a.Hkv + hk) * a.page + (unsigned)(t * ATT_KEYS) % (unsigned)a.page, held};
+    };
+    auto request_keys = [&](int t) {
+        const Where w = where(t);
+        const unsigned bit = 1u << ((t - t0) & 1);
+        held_tiles = w.held ? held_tiles | bit : held_tiles & ~bit;
+        const unsigned char *from = reinterpret_cast<const unsigned char *>(a.kc) + w.at * a.D;
+#pragma unroll
+        for (int i = 0; i < T::NKP; ++i) kreg[i] = *reinterpret_cast<const uint2 *>(from + 8u * min((int)threadIdx.x + i * T::NT, ATT_KEYS * CH - 1));
+        if (threadIdx.x < ATT_KEYS) {
+            // pages and groups begin at whole blocks; of blocks behind the end a scale may hold anything
+            const unsigned in_tile = threadIdx.x / (unsigned)a.scale_tokens;
+            const size_t block = w.at / ATT_KEYS * (unsigned)(ATT_KEYS / a.scale_tokens) + in_tile;
+            const bool there = w.held && t * ATT_KEYS + (int)in_tile * a.scale_tokens < sk.n;
+            kscale_reg = there ? a.ks[block] : 0.0f;
+            vscale_reg = there ? a.vs[block] : 0.0f;
+        }
+    };
+    auto request_values = [&](int t) {
+        const Where w = where(t);
+        const unsigned char *from = reinterpret_cast<const unsigned char *>(a.vc) + w.at * a.D;
+#pragma unroll
+        for (int i = 0; i < T::NVP; ++i) {
+            const unsigned e = min((int)threadIdx.x + i * T::NT, 2 * a.D - 1);
+            vreg[i][0] = *reinterpret_cast<const uint4 *>(from + (e / 2 * 64 + e % 2 * 16));
+            vreg[i][1] = *reinterpret_cast<const uint4 *>(from + (e / 2 * 64 + e % 2 * 16 + 32));
+        }
+    };
+    unsigned kput[T::NKP];                             // where this thread's key pieces go
+    if constexpr (CACHE) {
+#pragma unroll
+        for (int i = 0; i < T::NKP; ++i) {
+            const int e = min((int)threadIdx.x + i * T::NT, ATT_KEYS * CH - 1), r = e / CH, cc = e % CH;
+            kput[i] = r * (CHP * 16) + 16 * (cc ^ key_swizzle<CHP>(r));
+        }
+    }
+    auto put_keys = [&](int t, int stage) {
+        // threads behind the last piece have the last piece too: they write the same bytes
+#pragma unroll
+        for (int i = 0; i < T::NKP; ++i) *reinterpret_cast<f16x8 *>(smem + stage * T::K_BYTES + kput[i]) = codes_f16x8(kreg[i].x, kreg[i].y);
+        if (threadIdx.x < ATT_KEYS) {
+            lds_ks[stage * ATT_KEYS + threadIdx.x] = kscale_reg;
+            // read in the round behind the one that reads the keys, while these are written for two tiles on: four deep
+            lds_vs[t % 4 * ATT_KEYS + threadIdx.x] = vscale_reg;
+        }
+    };
+    auto put_values = [&](int stage) {
+        // channel d: 16-byte piece 2 s + half of its row has the slots of step s
+#pragma unroll
+        for (int i = 0; i < T::NVP; ++i) {
+            const int e = threadIdx.x + i * T::NT;
+            if (e >= 2 * a.D) break;
+            const int d = e / 2, h = e % 2;
+            unsigned char *to = smem + T::V_AT + stage * T::V_BYTES + d * 128;
+            const unsigned x[4] = {vreg[i][0].x, vreg[i][0].y, vreg[i][0].z, vreg[i][0].w}, y[4] = {vreg[i][1].x, vreg[i][1].y, vreg[i][1].z, vreg[i][1].w};
+#pragma unroll
+            for (int s = 0; s < 4; ++s) *reinterpret_cast<f16x8 *>(to + 16 * ((2 * s + h) ^ (d >> 1 & 7))) = codes_f16x8(x[s], y[s]);
+        }
+    };
+
+    f32x16 acc[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[d] = f32x16{};
+    float m = -__builtin_inff(), l = 0.0f;             // of this lane's row, m in powers of two; l over this lane's keys only
+    float unit_v = 0.0f;                               // CACHE: the value scale that the sums are in (one for the wavefront)
+
+    // left operands: step ks of keys 32 u .. 32 u + 31, step st of value channels 32 d .. 32 d + 31.  A swizzle turns the low bits of a piece's
+    // number, so pieces that differ above them lie a constant apart: few addresses are kept, the rest is in the instructions.
+    constexpr int KA = CHP % 8 == 0 ? (KS < 4 ? KS : 4) : CHP % 4 == 0 ? 2 : 1;
+    constexpr int VA = CACHE ? 4 : CHP % 16 == 0 ? 4 : CHP % 16 == 8 ? 2 : 1;
+    unsigned kaddr[KA], vaddr[VA];
+    const unsigned lds0 = (unsigned)(uintptr_t)(attn_lds *)smem;
+#pragma unroll
+    for (int i = 0; i < KA; ++i) kaddr[i] = lds0 + (lane & 31) * (CHP * 16) + 16 * ((2 * i + half) ^ key_swizzle<CHP>(lane & 31));
+#pragma unroll
+    for (int i = 0; i < VA; ++i) {
+        // CACHE: transposed, channel lane & 31, step i.  Rows: the transposing read takes 4 keys of 16 channels for 16 lanes, lane i of them with the
+        // address of key i / 4, channels 4 (i % 4)
+        const int r = 4 * half + (lane >> 2 & 3), ch = 4 * i + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+        vaddr[i] = lds0 + T::V_AT + (CACHE ? (lane & 31) * 128 + 16 * ((2 * i + half) ^ (lane >> 1 & 7)) : r * (CHP * 16) + 16 * (ch ^ value_swizzle<CHP>(r)) + 8 * (lane & 1));
+    }
+    auto key_part = [&](int stage, int u, int ks) {
+        typedef __attribute__((address_space(3))) f16x8 lds_h8;
+        return *(lds_h8 *)(uintptr_t)(kaddr[ks % KA] + (unsigned)(stage * T::K_BYTES + u * 32 * CHP * 16 + (ks / KA) * KA * 32));
+    };
+    auto value_part = [&](int stage, int d, int st) -> f16x8 {
+        if constexpr (CACHE) {
+            typedef __attribute__((address_space(3))) f16x8 lds_h8;
+            return *(lds_h8 *)(uintptr_t)(vaddr[st] + (unsigned)(stage * T::V_BYTES + d * 4096));
+        } else {
+            const unsigned at = vaddr[d % VA] + (unsigned)(stage * T::V_BYTES + st * 16 * CHP * 16 + (d / VA) * VA * 64);
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((attn_lds_s4 *)(uintptr_t)at);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((attn_lds_s4 *)(uintptr_t)(at + 8 * CHP * 16));
+            const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            return __builtin_bit_cast(f16x8, both);
+        }
+    };
+    // what turns scores into powers of two: returns the factor that is left
+    const bool one_scale = CACHE && a.scale_tokens == ATT_KEYS;
+    auto shape = [&](f32x16 (&s)[2], int t, int stage) -> float {
+        const int j0 = t * ATT_KEYS;
+        float c = scale2;
+        bool held = true;
+        if constexpr (CACHE) {
+            if (one_scale) {
+                const float k = lds_ks[stage * ATT_KEYS];
+                c = fmaxf(scale2 * k, LEAST_SCALE);
+            } else {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const f32x4 k = *reinterpret_cast<const f32x4 *>(lds_ks + stage * ATT_KEYS + 32 * u + 8 * g + 4 * half);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[u][4 * g + e] *= k[e];
+                    }
+            }
+            held = held_tiles >> stage & 1;
+        }
+        if (SHAPED && a.cap > 0.0f) {
+            const float k = c * cap_in;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[u][r] = capped(s[u][r] * k, cap2);
+            c = 1.0f;
+        }
+        if (SHAPED && a.slopes) {
+            // distances are whole numbers: exact up to 2^24
+            const float far = (float)(pos - j0 - 4 * half);
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[u][r] = __builtin_fmaf(fabsf(far - (float)(32 * u + 8 * (r / 4) + r % 4)), -slope2, s[u][r] * c);
+            c = 1.0f;
+        }
+        if (j0 + ATT_KEYS > end_min || !held) {
+            const int lim = held ? end - j0 - 4 * half : -ATT_KEYS;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[u][r] = 32 * u + 8 * (r / 4) + r % 4 < lim ? s[u][r] : -__builtin_inff();
+        }
+        return c;
+    };
+    auto largest = [&](const f32x16 (&s)[2]) {
+        float top = s[0][0];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
+        return top;
+    };
+
+    if constexpr (CACHE) {
+        // pieces behind D meet zero queries: they have to be finite
+        if (CH < CHP)
+            for (int e = threadIdx.x; e < 2 * ATT_KEYS * (CHP - CH); e += T::NT) {
+                const int r = e / (CHP - CH) % ATT_KEYS, c = CH + e % (CHP - CH), stage = e / (CHP - CH) / ATT_KEYS;
+                *reinterpret_cast<f16x8 *>(smem + stage * T::K_BYTES + r * (CHP * 16) + 16 * (c ^ key_swizzle<CHP>(r))) = f16x8{};
+            }
+    }
+    f32x16 sa[2], sb[2];                               // scores of this tile and the next: register r of [u] is key 32 u + 8 (r / 4) + 4 half + r % 4
+    f16x8 pa[4], pb[4];                                // weights of this tile and the one in front, as steps of 16 keys; in front of the first one zeros, against zeros
+#pragma unroll
+    for (int i = 0; i < 4; ++i) pb[i] = f16x8{};
+    float behind = 1.0f;                               // what the sums up to the tile in front of the last one are still to be multiplied with
+    for (int e = threadIdx.x; e < T::V_BYTES / 16; e += T::NT) *reinterpret_cast<uint4 *>(smem + T::V_AT + T::V_BYTES + 16 * e) = make_uint4(0, 0, 0, 0);
+    float c = 1.0f, top = -__builtin_inff();
+
+    // Round t of this wavefront: QK multiplies the scores of tile t + 1 into `next`, PV the values of tile t - 1; EXP takes the weights of tile t from `s`.
+    auto round = [&](auto QK_, auto PV_, auto EXP_, int t, int stage, f32x16 (&s)[2], f32x16 (&next)[2], f16x8 (&w)[4], const f16x8 (&p)[4]) __attribute__((always_inline)) {
+        constexpr bool QK = decltype(QK_)::value, PV = decltype(PV_)::value, EXP = decltype(EXP_)::value;
+        float shift = 0.0f, grow = 1.0f, per = 0.0f, mc = 0.0f;
+        if constexpr (PV) {
+            if (__any(behind != 1.0f)) {
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[d][r] *= behind;
+            }
+            behind = 1.0f;
+        }
+        if constexpr (EXP) {
+            // the running maximum, and the value scale that the sums are in
+            const Halves tops = both_halves(top);
+            const float top2 = fmaxf(tops.a, tops.b) * c;
+            if constexpr (CACHE) {
+                float big = lds_vs[t % 4 * ATT_KEYS + (one_scale ? 0 : lane)];
+                if (!one_scale) {
+#pragma unroll
+                    for (int d = 32; d; d >>= 1) big = fmaxf(big, __shfl_xor(big, d, 64));
+                }
+                big = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, big)));
+                if (big > unit_v) {
+                    grow = unit_v / big;
+                    unit_v = big;
+                }
+                per = unit_v > 0.0f ? 1.0f / unit_v : 0.0f;
+                if (one_scale) shift = fmaxf(__builtin_amdgcn_logf(big * per), LEAST_RATIO);
+            }
+            if (__any(top2 - m > GROWTH || (m == -__builtin_inff() && top2 > m)) || (CACHE && grow != 1.0f)) {
+                const float m2 = fmaxf(m, top2);
+                const float keep = m == -__builtin_inff() ? 0.0f : exp2_fast(m - m2);
+                l *= keep;
+                behind = keep * grow;
+                m = m2;
+            }
+            mc = m == -__builtin_inff() ? 0.0f : shift - m;
+        }
+        constexpr int NP = PV ? 4 * DT : 0, NQ = QK ? 2 * KS : 0, NM = NP + NQ, AHEAD = NM < 3 ? NM : 3;
+        constexpr int STEPS = NM ? NM : 1, PAIRS = EXP ? (16 + STEPS - 1) / STEPS : 0;   // pairs of weights behind a matrix instruction
+        auto part = [&](int i) { return i < NP ? value_part(stage ^ 1, i % DT, i / DT) : key_part(stage ^ 1, (i - NP) / KS, (i - NP) % KS); };
+        f16x8 f[AHEAD ? AHEAD : 1];
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) f[i] = part(i);
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            if (i < NP) acc[i % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i % (AHEAD ? AHEAD : 1)], p[i / DT], acc[i % DT], 0, 0, 0);
+            else if (i < NM) next[(i - NP) / KS] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i % (AHEAD ? AHEAD : 1)], qf[(i - NP) % KS], (i - NP) % KS ? next[(i - NP) / KS] : f32x16{}, 0, 0, 0);
+            if (i + AHEAD < NM) f[i % (AHEAD ? AHEAD : 1)] = part(i + AHEAD);
+#pragma unroll
+            for (int x = i * PAIRS; x < (i + 1) * PAIRS && x < 16; ++x) {
+                const int u = x / 8, r = 2 * (x % 8), g = x / 4, e = 2 * (x % 4);   // scores s[u][r], s[u][r + 1]; slots e, e + 1 of step g
+                float w0 = exp2_fast(__builtin_fmaf(s[u][r], c, mc)), w1 = exp2_fast(__builtin_fmaf(s[u][r + 1], c, mc));
+                if constexpr (CACHE) {
+                    sum += w0 + w1;
+                    if (!one_scale) {
+                        const float2 v = *reinterpret_cast<const float2 *>(lds_vs + t % 4 * ATT_KEYS + 16 * g + (e < 4 ? e : e + 4) + 4 * half);
+                        w0 *= v.x * per;
+                        w1 *= v.y * per;
+                    }
+                }
+                const f16x2 h = {(_Float16)w0, (_Float16)w1};
+                // the sum takes the weights as they are multiplied, unless they carry a value scale
+                if constexpr (!CACHE) sum = __builtin_amdgcn_fdot2(h, f16x2{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
+                // here and not behind the round, where the compiler would move what only later code reads
+                asm volatile("" ::"v"(__builtin_bit_cast(unsigned, h)));
+                w[g][e] = h[0];
+                w[g][e + 1] = h[1];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (EXP) {
+            if (CACHE && one_scale) sum *= exp2_fast(-shift);
+            l += sum;
+        }
+        if constexpr (QK) {
+            c = shape(next, t + 1, stage ^ 1);
+            top = largest(next);
+        }
+    };
+    constexpr std::true_type yes{};
+    constexpr std::false_type no{};
+
+    if (t0 < t1) {
+        if constexpr (CACHE) {
+            request_keys(t0);
+            put_keys(t0, 0);
+            if (t0 + 1 < t1) {
+                request_keys(t0 + 1);
+                put_keys(t0 + 1, 1);
+            }
+        } else {
+            dma(false, t0, 0);
+            if (t0 + 1 < t1) dma(false, t0 + 1, 1);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        __syncthreads();
+        // round t reads keys of tile t + 1 and values of tile t - 1; keys of tile t + 2 and values of tile t come in meanwhile
+        // In front of round t: keys of tile t + 1 and values of tile t - 1 are there, what the round in front of it read is free.  Every
+        // wavefront passes this for every t up to t1, whatever its own rows see.
+        auto turn = [&](int t, int stage) __attribute__((always_inline)) {
+            if constexpr (!CACHE) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if constexpr (CACHE) {
+                if (t + 2 < t1) request_keys(t + 2);
+                if (t < t1) request_values(t);
+            } else {
+                if (t + 2 < t1) dma(false, t + 2, stage);
+                if (t < t1) dma(true, t, stage);
+            }
+        };
+        auto put = [&](int t, int stage) __attribute__((always_inline)) {
+            if constexpr (CACHE) {
+                if (t + 2 < t1) put_keys(t + 2, stage);
+                if (t < t1) put_values(stage);
+            }
+        };
+        int t = t0;
+        if (t < tw) {
+            round(yes, no, no, t - 1, 1, sb, sa, pb, pb);
+            for (; t + 2 < tw; t += 2) {
+                turn(t, 0);
+                round(yes, yes, yes, t, 0, sa, sb, pa, pb);
+                put(t, 0);
+                turn(t + 1, 1);
+                round(yes, yes, yes, t + 1, 1, sb, sa, pb, pa);
+                put(t + 1, 1);
+            }
+            int stage = 0;
+            if (t + 1 < tw) {
+                turn(t, 0);
+                round(yes, yes, yes, t, 0, sa, sb, pa, pb);
+                put(t, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) pb[i] = pa[i];
+                sa[0] = sb[0];
+                sa[1] = sb[1];
+                ++t;
+                stage = 1;
+            }
+            turn(t, stage);
+            round(no, yes, yes, t, stage, sa, sb, pa, pb);
+            put(t, stage);
+            ++t;
+            turn(t, stage ^ 1);
+            round(no, yes, no, t, stage ^ 1, sa, sb, pb, pa);
+            put(t, stage ^ 1);
+            ++t;
+        }
+        for (; t <= t1; ++t) {
+            turn(t, (t - t0) & 1);
+            put(t, (t - t0) & 1);
+        }
+    }
+    const Halves ls = both_halves(l);
+    l = ls.a + ls.b;
+    if (plan.splits > 1) {
+        // [ROWS][D] sums, then maxima (in powers of two) and weights of this part
+        float *part = a.partial + (((size_t)flat * a.Hkv + hk) * plan.splits + split) * (size_t)(T::ROWS * (a.D + 2));
+        const int lr = wave * 32 + (lane & 31);
+        const float back = CACHE ? unit_v : 1.0f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int ch = 32 * d + 8 * g + 4 * half;
+                if (ch < a.D) *reinterpret_cast<f32x4 *>(part + (size_t)lr * a.D + ch) = f32x4{acc[d][4 * g], acc[d][4 * g + 1], acc[d][4 * g + 2], acc[d][4 * g + 3]} * back;
+            }
+        if (half == 0) {
+            part[(size_t)T::ROWS * a.D + lr] = m;
+            part[(size_t)T::ROWS * (a.D + 1) + lr] = l;
+        }
+        return;
+    }
+    const float inv = l > 0.0f ? (CACHE ? unit_v : 1.0f) / l : 0.0f;
+    unsigned amax = 0;
+    _Float16 *o = static_cast<_Float16 *>(a.o) + (sq.first + token) * a.o_row + head * a.o_head;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; g += 2) {
+            // channels 8 g + 4 half of this lane and of lane ^ 32 together are 8 neighbours for each of the two
+            unsigned w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const f16x2 h = {(_Float16)(acc[d][4 * g + 2 * e] * inv), (_Float16)(acc[d][4 * g + 2 * e + 1] * inv)};
+                w[e] = __builtin_bit_cast(unsigned, h);
+            }
+            const auto x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+            const int ch = 32 * d + 8 * g + 8 * half;
+            const uint4 out = make_uint4(x[0], y[0], x[1], y[1]);
+            if (ch < a.D && wrow < rows) {
+                *reinterpret_cast<uint4 *>(o + ch) = out;
+                if (a.row_absmax) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const unsigned v = e == 0 ? out.x : e == 1 ? out.y : e == 2 ? out.z : out.w;
+                        amax = max(amax, max(v & 0x7fffu, v >> 16 & 0x7fffu));
+                    }
+                }
+            }
+        }
+    if (a.row_absmax && wrow < rows) atomicMax(a.row_absmax + sq.first + token, amax);
+}
+
+// Adds up the parts of the row tiles, one wavefront per packed row: `rows_per` rows a tile, 4 rows a workgroup, blockIdx.y the quarter-rows of a tile
+__device__ __forceinline__ void join_splits(const AttnArgs &a, const TilePlan &plan, int rows_per)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int hk = blockIdx.x % a.Hkv, flat = blockIdx.x / a.Hkv;
+    int tile = flat, b;
+    if (a.cu_q) {
+        b = find_sequence(a.B, tile, [&](int s) { return (seq_rows(a.cu_q, s, a.Tq, a.B).n * a.G + rows_per - 1) / rows_per; });
+        if (b < 0) return;
+    } else {
+        b = flat / plan.per_seq;
+        tile = flat % plan.per_seq;
+    }
+    const SeqRows sq = seq_rows(a.cu_q, b, a.Tq, a.B);
+    const int lr = 4 * blockIdx.y + wave, row = tile * rows_per + lr;
+    if (row >= sq.n * a.G) return;
+    const size_t stride = (size_t)rows_per * (a.D + 2);
+    const float *part = a.partial + ((size_t)flat * a.Hkv + hk) * plan.splits * stride;
+    float m = -__builtin_inff();
+    for (int s = 0; s < plan.splits; ++s) m = fmaxf(m, part[s * stride + (size_t)rows_per * a.D + lr]);
+    const int token = row / a.G, head = hk * a.G + row % a.G;
+    _Float16 *o = static_cast<_Float16 *>(a.o) + (sq.first + token) * a.o_row + head * a.o_head;
+    unsigned amax = 0;
+    for (int ch = 4 * lane; ch < a.D; ch += 256) {
+        f32x4 sum = {};
+        float weight = 0.0f;
+        if (m > -__builtin_inff())
+            for (int s = 0; s < plan.splits; ++s) {
+                const float k = exp2_fast(part[s * stride + (size_t)rows_per * a.D + lr] - m);
+                weight += k * part[s * stride + (size_t)rows_per * (a.D + 1) + lr];
+                sum += *reinterpret_cast<const f32x4 *>(part + s * stride + (size_t)lr * a.D + ch) * k;
+            }
+        const float inv = weight > 0.0f ? 1.0f / weight : 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const _Float16 h = (_Float16)(sum[e] * inv);
+            o[ch + e] = h;
+            amax = max(amax, absmax_bits(h));
+        }
+    }
+    if (a.row_absmax) {
+#pragma unroll
+        for (int d = 32; d; d >>= 1) amax = max(amax, (unsigned)__shfl_xor((int)amax, d, 64));
+        if (lane == 0) atomicMax(a.row_absmax + sq.first + token, amax);
+    }
+}
+
+// row tiles of `rows` packed rows, and the parts that the keys are cut into so that few of them still fill the chip: enough
+// workgroups for two on every CU, no part below 4 key tiles
+constexpr int TILE_SPLITS = 16;
+inline TilePlan tile_plan(long long Tq, int B, int G, int Hkv, int rows, bool cu_q, int mask, long long keys, int least_wgs)
+{
+    TilePlan p{};
+    p.per_seq = (int)((Tq / B * G + rows - 1) / rows);
+    p.tiles = cu_q ? (int)(Tq * G / rows + B) : p.per_seq * B;
+    const long long bound = (Tq * G / rows + B) * Hkv;   // of the workgroups, with or without cu_q
+    long long splits = bound >= least_wgs ? 1 : 2LL * least_wgs / bound;
+    const long long most = keys / (4 * ATT_KEYS);
+    splits = splits > TILE_SPLITS ? TILE_SPLITS : splits;
+    splits = splits > most ? most : splits;
+    p.splits = splits < 1 ? 1 : (int)splits;
+    p.mix = mask != 0;
+    return p;
+}
 
 }  // namespace ql

@@ -1,15 +1,15 @@
 // Attention over binary16 rows for gfx950: one pass over the keys with the running maximum and sum of the softmax.
 //
 // A workgroup of NW wavefronts has 32 NW packed rows (attention.h) of one sequence and key head; keys and values go by tiles of 64 from global memory into
-// LDS (global_load_lds, no registers), two stages deep, and every wavefront reads them from there: attention_tile.h says how.
+// LDS (global_load_lds, no registers), two tiles deep, and every wavefront reads them from there: attention_tile.h says how.
 #include "attention_tile.h"
 
 namespace ql {
 
-template <int KS, int NW, bool SHAPED>
-__global__ __launch_bounds__(64 * NW, KS <= 8 ? 2 : 1) void attend_tiles(AttnArgs a, TilePlan plan)
+template <int CHP, int NW, bool SHAPED>
+__global__ __launch_bounds__(64 * NW, CHP <= 16 ? 2 : 1) void attend_tiles(AttnArgs a, TilePlan plan)
 {
-    attend_tile<KS, NW, false, SHAPED>(a, plan);
+    attend_tile<CHP, NW, false, SHAPED>(a, plan);
 }
 
 __global__ __launch_bounds__(256) void join_tiles(AttnArgs a, TilePlan plan, int rows_per) { join_splits(a, plan, rows_per); }
@@ -25,21 +25,21 @@ int tile_rows(long long Tq, int B, int G, int Hkv, int D)
     return D > 128 ? 128 : D > 80 ? 64 : 32;
 }
 
-template <int KS, int NW>
+template <int CHP, int NW>
 hipError_t launch_tiles(const AttnArgs &a, hipStream_t stream)
 {
-    using T = AttnTile<KS, NW, false>;
+    using T = AttnTile<CHP, NW, false>;
     const TilePlan p = tile_plan(a.Tq, a.B, a.G, a.Hkv, T::ROWS, a.cu_q, a.mask, a.Tk / a.B, CUS);
     static const hipError_t opt_in[2] = {
-        hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_tiles<KS, NW, false>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES),
-        hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_tiles<KS, NW, true>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES)};
+        hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_tiles<CHP, NW, false>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES),
+        hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_tiles<CHP, NW, true>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES)};
     const bool shaped = a.cap > 0.0f || a.slopes;
     if (opt_in[shaped] != hipSuccess) return opt_in[shaped];
     const long long wgs = (long long)p.tiles * a.Hkv * p.splits;
     if (wgs > 0x7fffff00LL / T::NT * 1LL) return hipErrorInvalidValue;
     const dim3 grid((unsigned)((wgs + 7) / 8 * 8));
-    if (shaped) hipLaunchKernelGGL((attend_tiles<KS, NW, true>), grid, dim3(T::NT), T::LDS_BYTES, stream, a, p);
-    else hipLaunchKernelGGL((attend_tiles<KS, NW, false>), grid, dim3(T::NT), T::LDS_BYTES, stream, a, p);
+    if (shaped) hipLaunchKernelGGL((attend_tiles<CHP, NW, true>), grid, dim3(T::NT), T::LDS_BYTES, stream, a, p);
+    else hipLaunchKernelGGL((attend_tiles<CHP, NW, false>), grid, dim3(T::NT), T::LDS_BYTES, stream, a, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
     hipLaunchKernelGGL(join_tiles, dim3((unsigned)(p.tiles * a.Hkv), T::ROWS / 4), dim3(256), 0, stream, a, p, T::ROWS);
@@ -49,32 +49,35 @@ hipError_t launch_tiles(const AttnArgs &a, hipStream_t stream)
 // rows: what tile_rows gave
 hipError_t launch_by_head(const AttnArgs &a, int rows, hipStream_t stream)
 {
-    const int ks = (a.D + 15) / 16;
+    const int ch = a.D / 8;
     if (rows == 32) {
-        if (ks <= 1) return launch_tiles<1, 1>(a, stream);
-        if (ks <= 2) return launch_tiles<2, 1>(a, stream);
-        if (ks <= 3) return launch_tiles<3, 1>(a, stream);
-        if (ks <= 4) return launch_tiles<4, 1>(a, stream);
-        return launch_tiles<5, 1>(a, stream);
+        if (ch <= 2) return launch_tiles<2, 1>(a, stream);
+        if (ch <= 4) return launch_tiles<4, 1>(a, stream);
+        if (ch <= 6) return launch_tiles<6, 1>(a, stream);
+        if (ch <= 8) return launch_tiles<8, 1>(a, stream);
+        if (ch == 9) return launch_tiles<9, 1>(a, stream);
+        return launch_tiles<10, 1>(a, stream);
     }
     if (rows == 64) {
-        if (ks <= 1) return launch_tiles<1, 2>(a, stream);
-        if (ks <= 2) return launch_tiles<2, 2>(a, stream);
-        if (ks <= 3) return launch_tiles<3, 2>(a, stream);
-        if (ks <= 4) return launch_tiles<4, 2>(a, stream);
-        if (ks <= 5) return launch_tiles<5, 2>(a, stream);
-        if (ks <= 6) return launch_tiles<6, 2>(a, stream);
-        return launch_tiles<8, 2>(a, stream);
+        if (ch <= 2) return launch_tiles<2, 2>(a, stream);
+        if (ch <= 4) return launch_tiles<4, 2>(a, stream);
+        if (ch <= 6) return launch_tiles<6, 2>(a, stream);
+        if (ch <= 8) return launch_tiles<8, 2>(a, stream);
+        if (ch == 9) return launch_tiles<9, 2>(a, stream);
+        if (ch <= 10) return launch_tiles<10, 2>(a, stream);
+        if (ch <= 12) return launch_tiles<12, 2>(a, stream);
+        return launch_tiles<16, 2>(a, stream);
     }
-    if (ks <= 1) return launch_tiles<1, 4>(a, stream);
-    if (ks <= 2) return launch_tiles<2, 4>(a, stream);
-    if (ks <= 3) return launch_tiles<3, 4>(a, stream);
-    if (ks <= 4) return launch_tiles<4, 4>(a, stream);
-    if (ks <= 5) return launch_tiles<5, 4>(a, stream);
-    if (ks <= 6) return launch_tiles<6, 4>(a, stream);
-    if (ks <= 8) return launch_tiles<8, 4>(a, stream);
-    if (ks <= 12) return launch_tiles<12, 4>(a, stream);
-    return launch_tiles<16, 4>(a, stream);
+    if (ch <= 2) return launch_tiles<2, 4>(a, stream);
+    if (ch <= 4) return launch_tiles<4, 4>(a, stream);
+    if (ch <= 6) return launch_tiles<6, 4>(a, stream);
+    if (ch <= 8) return launch_tiles<8, 4>(a, stream);
+    if (ch == 9) return launch_tiles<9, 4>(a, stream);
+    if (ch <= 10) return launch_tiles<10, 4>(a, stream);
+    if (ch <= 12) return launch_tiles<12, 4>(a, stream);
+    if (ch <= 16) return launch_tiles<16, 4>(a, stream);
+    if (ch <= 24) return launch_tiles<24, 4>(a, stream);
+    return launch_tiles<32, 4>(a, stream);
 }
 }  // namespace
 

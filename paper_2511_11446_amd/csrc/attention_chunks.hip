@@ -8,35 +8,35 @@
 namespace ql {
 
 // wavefronts of a workgroup: long heads need all registers of a SIMD for one
-constexpr int chunk_waves(int KS) { return KS <= 8 ? 8 : 4; }
+constexpr int chunk_waves(int CHP) { return CHP <= 16 ? 8 : 4; }
 
-template <int KS, bool SHAPED>
-__global__ __launch_bounds__(64 * chunk_waves(KS), KS <= 8 ? 2 : 1) void attend_chunks(AttnArgs a, TilePlan plan)
+template <int CHP, bool SHAPED>
+__global__ __launch_bounds__(64 * chunk_waves(CHP), CHP <= 16 ? 2 : 1) void attend_chunks(AttnArgs a, TilePlan plan)
 {
-    attend_tile<KS, chunk_waves(KS), true, SHAPED>(a, plan);
+    attend_tile<CHP, chunk_waves(CHP), true, SHAPED>(a, plan);
 }
 
 __global__ __launch_bounds__(256) void join_chunks(AttnArgs a, TilePlan plan, int rows_per) { join_splits(a, plan, rows_per); }
 
 namespace {
 constexpr int CUS = 256;
-constexpr int chunk_rows(int D) { return 32 * chunk_waves((D + 15) / 16); }
+constexpr int chunk_rows(int D) { return 32 * chunk_waves(D / 8); }
 
-template <int KS>
+template <int CHP>
 hipError_t launch_chunks(const AttnArgs &a, hipStream_t stream)
 {
-    using T = AttnTile<KS, chunk_waves(KS), true>;
+    using T = AttnTile<CHP, chunk_waves(CHP), true>;
     const TilePlan p = tile_plan(a.Tq, a.B, a.G, a.Hkv, T::ROWS, a.cu_q, a.mask, (long long)a.max_pages * a.page, CUS);
     static const hipError_t opt_in[2] = {
-        hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_chunks<KS, false>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES),
-        hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_chunks<KS, true>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES)};
+        hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_chunks<CHP, false>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES),
+        hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_chunks<CHP, true>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES)};
     const bool shaped = a.cap > 0.0f || a.slopes;
     if (opt_in[shaped] != hipSuccess) return opt_in[shaped];
     const long long wgs = (long long)p.tiles * a.Hkv * p.splits;
     if (wgs > 0x7fffff00LL / T::NT) return hipErrorInvalidValue;
     const dim3 grid((unsigned)((wgs + 7) / 8 * 8));
-    if (shaped) hipLaunchKernelGGL((attend_chunks<KS, true>), grid, dim3(T::NT), T::LDS_BYTES, stream, a, p);
-    else hipLaunchKernelGGL((attend_chunks<KS, false>), grid, dim3(T::NT), T::LDS_BYTES, stream, a, p);
+    if (shaped) hipLaunchKernelGGL((attend_chunks<CHP, true>), grid, dim3(T::NT), T::LDS_BYTES, stream, a, p);
+    else hipLaunchKernelGGL((attend_chunks<CHP, false>), grid, dim3(T::NT), T::LDS_BYTES, stream, a, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
     hipLaunchKernelGGL(join_chunks, dim3((unsigned)(p.tiles * a.Hkv), T::ROWS / 4), dim3(256), 0, stream, a, p, T::ROWS);
@@ -52,14 +52,14 @@ size_t chunks_partial_bytes(long long Tq, int B, int Hq, int Hkv, int D)
 
 hipError_t launch_attention_chunks(const AttnArgs &a, hipStream_t stream)
 {
-    const int ks = (a.D + 15) / 16;
-    if (ks <= 2) return launch_chunks<2>(a, stream);
-    if (ks <= 4) return launch_chunks<4>(a, stream);
-    if (ks <= 5) return launch_chunks<5>(a, stream);
-    if (ks <= 6) return launch_chunks<6>(a, stream);
-    if (ks <= 8) return launch_chunks<8>(a, stream);
-    if (ks <= 12) return launch_chunks<12>(a, stream);
-    return launch_chunks<16>(a, stream);
+    const int ch = a.D / 8;
+    if (ch <= 4) return launch_chunks<4>(a, stream);
+    if (ch <= 8) return launch_chunks<8>(a, stream);
+    if (ch <= 10) return launch_chunks<10>(a, stream);
+    if (ch <= 12) return launch_chunks<12>(a, stream);
+    if (ch <= 16) return launch_chunks<16>(a, stream);
+    if (ch <= 24) return launch_chunks<24>(a, stream);
+    return launch_chunks<32>(a, stream);
 }
 
 }  // namespace ql

@@ -6,13 +6,11 @@
 // place where O^T = V^T P^T wants its right operand: keys 16 s + 8 (j / 4) + 4 (lane / 32) + j % 4 of a lane are slots j of step s on
 // both sides, whatever their order.
 //
-// The loop is pipelined: round t multiplies the values of tile t - 1 with their weights and the keys of tile t + 1 with the queries, both on the matrix
-// cores, while the vector units take the weights of tile t from its scores.  The three do not wait for each other, and the code places a part
-// of the exponentials behind every matrix instruction.  So in LDS keys run two tiles ahead of values, two stages of each.
+// A tile is worked on in one go - scores, weights, values - while the next one comes into the other stage of LDS; what a wavefront waits for, the others
+// of its SIMD fill.  (A loop that multiplied the scores of the next tile and the values of the last one between the exponentials of this one was no
+// faster: 343 against 340 us at 8192 tokens with a prefix, 150 against 141 at 16 images of 1024; its registers cost a wavefront per SIMD.)
 #pragma once
 #include "attention.h"
-
-#include <type_traits>
 
 namespace ql {
 
@@ -23,7 +21,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) void attn_lds;
-typedef const __attribute__((address_space(1))) void attn_global;
 typedef __attribute__((address_space(3))) s16x4 attn_lds_s4;
 
 constexpr int ATT_KEYS = 64;   // keys of a tile
@@ -66,16 +63,22 @@ __device__ __forceinline__ f16x8 codes_f16x8(unsigned w0, unsigned w1)
 
 __device__ __forceinline__ unsigned absmax_bits(_Float16 x) { return (unsigned)__builtin_bit_cast(unsigned short, x) & 0x7fffu; }
 
-// CHP: 16-byte pieces of a tile row (D / 8 rounded up to a multiple of 2).  A row is kept without padding (a wavefront's DMA fills 1024
-// neighbouring bytes); the piece c of row r sits at slot c ^ f(r), so that 8 rows read at one piece index (keys) and 4 rows read at 4
-// neighbouring ones (values) spread over all banks.
+// CHP: 16-byte pieces of a tile row.  Rows are kept without padding (a wavefront's DMA fills 1024 neighbouring bytes).  LDS serves 256 bytes at a time: 16
+// lanes of a key read (16 rows, one piece each) and 32 of a transposing value read (4 rows, 4 neighbouring pieces each) should lie in
+// different sixteenths of 256 bytes.  Where rows are an odd number of pieces apart that holds for keys by itself, and for values when each 4 x 4 rows are kept
+// transposed; else the piece c of row r sits at slot c ^ f(r).  (Without: 2 to 4 reads in the place of one; heads of 72 at 10 pieces a row and of 128
+// with 8 places for 16 rows: 16 images of 1024 tokens 156 us, 8192 tokens with a prefix 355 us.)
 template <int CHP> __device__ __forceinline__ constexpr int key_swizzle(int r)
 {
-    return CHP % 16 == 0 ? (r & 7) : CHP % 16 == 8 ? (r >> 1 & 7) : CHP % 4 == 0 ? (r >> 2 & 3) : 0;
+    return CHP % 16 == 0 ? (r & 15) : CHP % 16 == 8 ? (r >> 1 & 7) : CHP % 4 == 0 ? (r >> 2 & 3) : CHP % 4 == 2 && CHP > 2 ? (r >> 3 & 1) : 0;
 }
 template <int CHP> __device__ __forceinline__ constexpr int value_swizzle(int r)
 {
     return CHP % 16 == 0 ? (r & 3) << 2 : CHP % 16 == 8 ? (r >> 1 & 1) << 2 : 0;
+}
+template <int CHP> __device__ __forceinline__ constexpr int value_row(int t)   // of key t, and its own inverse
+{
+    return CHP % 2 ? (t & ~15) | (t & 3) << 2 | (t >> 2 & 3) : t;
 }
 
 struct TilePlan {
@@ -90,24 +93,24 @@ constexpr float GROWTH = 8.0f;
 constexpr float LEAST_SCALE = 1e-30f;   // stands for a scale of 0, so that -inf times it stays -inf
 constexpr float LEAST_RATIO = -30.0f;   // log2 of the smallest value scale that counts beside the largest: below, a weight is 0 in binary16
 
-// KS: 16-channel steps of the scores; NW: wavefronts; CACHE: keys and values from the 8-bit cache; SHAPED: scores may be capped or biased
-template <int KS, int NW, bool CACHE>
+// CHP: pieces of a tile row; NW: wavefronts; CACHE: keys and values from the 8-bit cache; SHAPED: scores may be capped or biased
+template <int CHP_, int NW, bool CACHE>
 struct AttnTile {
-    static constexpr int CHP = 2 * KS, DT = (KS + 1) / 2, ROWS = 32 * NW, NT = 64 * NW;
+    static constexpr int CHP = CHP_, KS = (CHP + 1) / 2, DT = (CHP + 3) / 4, ROWS = 32 * NW, NT = 64 * NW;
     static constexpr int K_BYTES = ATT_KEYS * CHP * 16;
     // values: rows like the keys' (a read of channels behind D may pass the last row: 1024 bytes behind the last stage), or transposed codes
     static constexpr int V_BYTES = CACHE ? DT * 32 * 128 : K_BYTES;
     static constexpr int V_AT = 2 * K_BYTES, SCALES_AT = V_AT + 2 * V_BYTES;
-    static constexpr int LDS_BYTES = SCALES_AT + (CACHE ? 6 * ATT_KEYS * 4 : 1024);   // scales of two stages (keys) and four (values), or the slack
+    static constexpr int LDS_BYTES = SCALES_AT + (CACHE ? 4 * ATT_KEYS * 4 : 1024);   // scales of both stages, or the slack
     // CACHE: register-staged pieces of a thread: 8 key codes each; 32 value codes of a channel each
     static constexpr int NKP = CACHE ? (ATT_KEYS * CHP + NT - 1) / NT : 1, NVP = CACHE ? (64 * DT + NT - 1) / NT : 1;
 };
 
-template <int KS, int NW, bool CACHE, bool SHAPED>
+template <int CHP, int NW, bool CACHE, bool SHAPED>
 __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &plan)
 {
-    using T = AttnTile<KS, NW, CACHE>;
-    constexpr int CHP = T::CHP, DT = T::DT;
+    using T = AttnTile<CHP, NW, CACHE>;
+    constexpr int KS = T::KS, DT = T::DT;
     constexpr int NI = (CHP + NW - 1) / NW;            // DMA instructions of a wavefront for one tile
     extern __shared__ __align__(1024) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -179,6 +182,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
     const float slope2 = a.slopes ? a.slopes[head] * LOG2E : 0.0f;
     const float cap2 = a.cap * LOG2E, cap_in = a.cap > 0.0f ? 2.0f * LOG2E / cap2 : 0.0f;
 
+    const unsigned lds0 = (unsigned)(uintptr_t)(attn_lds *)smem;
     // ---- tiles into LDS ------------------------------------------------------------------------------------------------------------
     // rows: instruction i of this wavefront fills pieces [64 (i NW + wave), + 64) of the tile; a row behind the last key reads the last
     // one, a piece behind D the row's last one: what is read there meets weights or queries that are zero
@@ -187,7 +191,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
     unsigned koff[NI], voff[NI];                       // of this lane's piece from the tile's first row
     auto piece_at = [&](int i, bool value, int last_row, unsigned row_bytes) {
         const int ci = 64 * (i * NW + wave) + lane, r = ci / CHP, c = ci % CHP;
-        return min(r, last_row) * row_bytes + 16 * min(c ^ (value ? value_swizzle<CHP>(r) : key_swizzle<CHP>(r)), CH - 1);
+        return min(value ? value_row<CHP>(r) : r, last_row) * row_bytes + 16 * min(c ^ (value ? value_swizzle<CHP>(r) : key_swizzle<CHP>(r)), CH - 1);
     };
     const unsigned krow = 2 * (unsigned)a.k_row, vrow = 2 * (unsigned)a.v_row;
     if constexpr (!CACHE) {
@@ -200,20 +204,22 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
     auto dma = [&](bool value, int t, int stage) {
         const int left = sk.n - t * ATT_KEYS - 1;      // rows behind the tile's first one
         const unsigned char *from = value ? vb + (size_t)t * ATT_KEYS * 2 * a.v_row : kb + (size_t)t * ATT_KEYS * 2 * a.k_row;
-        unsigned char *to = value ? smem + T::V_AT + stage * T::V_BYTES : smem + stage * T::K_BYTES;
+        const unsigned to = lds0 + (value ? T::V_AT + stage * T::V_BYTES : stage * T::K_BYTES);
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            if (CHP % NW != 0 && i * NW + wave >= CHP) break;
+            if (CHP % NW != 0 && i * NW + wave >= CHP) break;   // (a tile is CHP times 64 pieces)
             unsigned at = value ? voff[i] : koff[i];
             if (left < ATT_KEYS - 1) at = piece_at(i, value, left, value ? vrow : krow);
-            __builtin_amdgcn_global_load_lds((attn_global *)(from + at), (attn_lds *)(to + (i * NW + wave) * 1024), 16, 0, 0);
+            // As an instruction, not the builtin: behind that the compiler has every read of LDS wait for all DMA, whichever stage it fills; the wait that is
+            // needed stands in front of the round's barrier.  (It costs an image of 1024 tokens a fifth of its time.)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to + (i * NW + wave) * 1024), "v"(at), "s"(from) : "memory");
         }
     };
     // cache: codes through registers; a page that is none reads page 0 and counts as masked
     uint2 kreg[T::NKP];
     uint4 vreg[T::NVP][2];
     float kscale_reg = 0.0f, vscale_reg = 0.0f;
-    float *lds_ks = reinterpret_cast<float *>(smem + T::SCALES_AT), *lds_vs = lds_ks + 2 * ATT_KEYS;   // [stage][token], [tile % 4][token]
+    float *lds_ks = reinterpret_cast<float *>(smem + T::SCALES_AT), *lds_vs = lds_ks + 2 * ATT_KEYS;   // [stage][token]
     struct Where {
         size_t at;      // token of the cache where the tile begins, counted within its key head: (page * Hkv + hk) * page_tokens + in_page
         bool held;
@@ -222,8 +228,8 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
     int pages_at = -ATT_KEYS;
     unsigned held_tiles = 0;                           // bit: whether the keys' stage has a page
     auto where = [&](int t) {
-        if (t - pages_at >= 63) {                      // keys ask for a tile, then values for the one in front of it
-            pages_at = max(t - 1, t0);
+        if (t - pages_at >= 64) {
+            pages_at = t;
             const int mine = pages_at + lane;
             pages = mine < t1 ? a.page_table[(size_t)b * a.max_pages + (unsigned)(mine * ATT_KEYS) / (unsigned)a.page] : -1;
         }
@@ -232,13 +238,19 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
         if (!held) page = 0;
         return Where{((size_t)page * a.Hkv + hk) * a.page + (unsigned)(t * ATT_KEYS) % (unsigned)a.page, held};
     };
-    auto request_keys = [&](int t) {
+    auto request = [&](int t) {
         const Where w = where(t);
         const unsigned bit = 1u << ((t - t0) & 1);
         held_tiles = w.held ? held_tiles | bit : held_tiles & ~bit;
-        const unsigned char *from = reinterpret_cast<const unsigned char *>(a.kc) + w.at * a.D;
+        const unsigned char *kfrom = reinterpret_cast<const unsigned char *>(a.kc) + w.at * a.D, *vfrom = reinterpret_cast<const unsigned char *>(a.vc) + w.at * a.D;
 #pragma unroll
-        for (int i = 0; i < T::NKP; ++i) kreg[i] = *reinterpret_cast<const uint2 *>(from + 8u * min((int)threadIdx.x + i * T::NT, ATT_KEYS * CH - 1));
+        for (int i = 0; i < T::NKP; ++i) kreg[i] = *reinterpret_cast<const uint2 *>(kfrom + 8u * min((int)threadIdx.x + i * T::NT, ATT_KEYS * CH - 1));
+#pragma unroll
+        for (int i = 0; i < T::NVP; ++i) {
+            const unsigned e = min((int)threadIdx.x + i * T::NT, 2 * a.D - 1);
+            vreg[i][0] = *reinterpret_cast<const uint4 *>(vfrom + (e / 2 * 64 + e % 2 * 16));
+            vreg[i][1] = *reinterpret_cast<const uint4 *>(vfrom + (e / 2 * 64 + e % 2 * 16 + 32));
+        }
         if (threadIdx.x < ATT_KEYS) {
             // pages and groups begin at whole blocks; of blocks behind the end a scale may hold anything
             const unsigned in_tile = threadIdx.x / (unsigned)a.scale_tokens;
@@ -246,16 +258,6 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
             const bool there = w.held && t * ATT_KEYS + (int)in_tile * a.scale_tokens < sk.n;
             kscale_reg = there ? a.ks[block] : 0.0f;
             vscale_reg = there ? a.vs[block] : 0.0f;
-        }
-    };
-    auto request_values = [&](int t) {
-        const Where w = where(t);
-        const unsigned char *from = reinterpret_cast<const unsigned char *>(a.vc) + w.at * a.D;
-#pragma unroll
-        for (int i = 0; i < T::NVP; ++i) {
-            const unsigned e = min((int)threadIdx.x + i * T::NT, 2 * a.D - 1);
-            vreg[i][0] = *reinterpret_cast<const uint4 *>(from + (e / 2 * 64 + e % 2 * 16));
-            vreg[i][1] = *reinterpret_cast<const uint4 *>(from + (e / 2 * 64 + e % 2 * 16 + 32));
         }
     };
     unsigned kput[T::NKP];                             // where this thread's key pieces go
@@ -266,14 +268,13 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
             kput[i] = r * (CHP * 16) + 16 * (cc ^ key_swizzle<CHP>(r));
         }
     }
-    auto put_keys = [&](int t, int stage) {
+    auto put_keys = [&](int stage) {
         // threads behind the last piece have the last piece too: they write the same bytes
 #pragma unroll
         for (int i = 0; i < T::NKP; ++i) *reinterpret_cast<f16x8 *>(smem + stage * T::K_BYTES + kput[i]) = codes_f16x8(kreg[i].x, kreg[i].y);
         if (threadIdx.x < ATT_KEYS) {
             lds_ks[stage * ATT_KEYS + threadIdx.x] = kscale_reg;
-            // read in the round behind the one that reads the keys, while these are written for two tiles on: four deep
-            lds_vs[t % 4 * ATT_KEYS + threadIdx.x] = vscale_reg;
+            lds_vs[stage * ATT_KEYS + threadIdx.x] = vscale_reg;
         }
     };
     auto put_values = [&](int stage) {
@@ -298,21 +299,23 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
 
     // left operands: step ks of keys 32 u .. 32 u + 31, step st of value channels 32 d .. 32 d + 31.  A swizzle turns the low bits of a piece's
     // number, so pieces that differ above them lie a constant apart: few addresses are kept, the rest is in the instructions.
-    constexpr int KA = CHP % 8 == 0 ? (KS < 4 ? KS : 4) : CHP % 4 == 0 ? 2 : 1;
+    constexpr int KA = CHP % 16 == 0 ? 8 : CHP % 8 == 0 ? 4 : CHP % 4 == 0 ? 2 : 1;
     constexpr int VA = CACHE ? 4 : CHP % 16 == 0 ? 4 : CHP % 16 == 8 ? 2 : 1;
-    unsigned kaddr[KA], vaddr[VA];
-    const unsigned lds0 = (unsigned)(uintptr_t)(attn_lds *)smem;
+    unsigned kaddr[KA], vaddr[VA], klast = 0;
 #pragma unroll
     for (int i = 0; i < KA; ++i) kaddr[i] = lds0 + (lane & 31) * (CHP * 16) + 16 * ((2 * i + half) ^ key_swizzle<CHP>(lane & 31));
+    // the last step of an odd number of pieces: both halves read the last piece, against queries that are zero in one
+    if (CHP % 2) klast = lds0 + (lane & 31) * (CHP * 16) + 16 * (CHP - 1);
 #pragma unroll
     for (int i = 0; i < VA; ++i) {
         // CACHE: transposed, channel lane & 31, step i.  Rows: the transposing read takes 4 keys of 16 channels for 16 lanes, lane i of them with the
         // address of key i / 4, channels 4 (i % 4)
-        const int r = 4 * half + (lane >> 2 & 3), ch = 4 * i + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+        const int r = value_row<CHP>(4 * half + (lane >> 2 & 3)), ch = 4 * i + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
         vaddr[i] = lds0 + T::V_AT + (CACHE ? (lane & 31) * 128 + 16 * ((2 * i + half) ^ (lane >> 1 & 7)) : r * (CHP * 16) + 16 * (ch ^ value_swizzle<CHP>(r)) + 8 * (lane & 1));
     }
     auto key_part = [&](int stage, int u, int ks) {
         typedef __attribute__((address_space(3))) f16x8 lds_h8;
+        if (CHP % 2 && ks == KS - 1) return *(lds_h8 *)(uintptr_t)(klast + (unsigned)(stage * T::K_BYTES + u * 32 * CHP * 16));
         return *(lds_h8 *)(uintptr_t)(kaddr[ks % KA] + (unsigned)(stage * T::K_BYTES + u * 32 * CHP * 16 + (ks / KA) * KA * 32));
     };
     auto value_part = [&](int stage, int d, int st) -> f16x8 {
@@ -322,7 +325,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
         } else {
             const unsigned at = vaddr[d % VA] + (unsigned)(stage * T::V_BYTES + st * 16 * CHP * 16 + (d / VA) * VA * 64);
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((attn_lds_s4 *)(uintptr_t)at);
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((attn_lds_s4 *)(uintptr_t)(at + 8 * CHP * 16));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((attn_lds_s4 *)(uintptr_t)(at + value_row<CHP>(8) * CHP * 16));
             const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
             return __builtin_bit_cast(f16x8, both);
         }
@@ -392,169 +395,102 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
                 *reinterpret_cast<f16x8 *>(smem + stage * T::K_BYTES + r * (CHP * 16) + 16 * (c ^ key_swizzle<CHP>(r))) = f16x8{};
             }
     }
-    f32x16 sa[2], sb[2];                               // scores of this tile and the next: register r of [u] is key 32 u + 8 (r / 4) + 4 half + r % 4
-    f16x8 pa[4], pb[4];                                // weights of this tile and the one in front, as steps of 16 keys; in front of the first one zeros, against zeros
+    auto work = [&](int t, int stage) __attribute__((always_inline)) {
+        // scores: register r of s[u] is key 32 u + 8 (r / 4) + 4 half + r % 4 of the tile
+        f32x16 s[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) pb[i] = f16x8{};
-    float behind = 1.0f;                               // what the sums up to the tile in front of the last one are still to be multiplied with
-    for (int e = threadIdx.x; e < T::V_BYTES / 16; e += T::NT) *reinterpret_cast<uint4 *>(smem + T::V_AT + T::V_BYTES + 16 * e) = make_uint4(0, 0, 0, 0);
-    float c = 1.0f, top = -__builtin_inff();
-
-    // Round t of this wavefront: QK multiplies the scores of tile t + 1 into `next`, PV the values of tile t - 1; EXP takes the weights of tile t from `s`.
-    auto round = [&](auto QK_, auto PV_, auto EXP_, int t, int stage, f32x16 (&s)[2], f32x16 (&next)[2], f16x8 (&w)[4], const f16x8 (&p)[4]) __attribute__((always_inline)) {
-        constexpr bool QK = decltype(QK_)::value, PV = decltype(PV_)::value, EXP = decltype(EXP_)::value;
-        float shift = 0.0f, grow = 1.0f, per = 0.0f, mc = 0.0f;
-        if constexpr (PV) {
-            if (__any(behind != 1.0f)) {
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int d = 0; d < DT; ++d)
+            for (int ks = 0; ks < KS; ++ks) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(key_part(stage, u, ks), qf[ks], ks ? s[u] : f32x16{}, 0, 0, 0);
+        const float c = shape(s, t, stage);
+        // the running maximum, and the value scale that the sums are in
+        const Halves tops = both_halves(largest(s));
+        const float top = fmaxf(tops.a, tops.b) * c;
+        float shift = 0.0f, grow = 1.0f, per = 0.0f;
+        if constexpr (CACHE) {
+            float big = lds_vs[stage * ATT_KEYS + (one_scale ? 0 : lane)];
+            if (!one_scale) {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) acc[d][r] *= behind;
+                for (int d = 32; d; d >>= 1) big = fmaxf(big, __shfl_xor(big, d, 64));
             }
-            behind = 1.0f;
+            big = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, big)));
+            if (big > unit_v) {
+                grow = unit_v / big;
+                unit_v = big;
+            }
+            per = unit_v > 0.0f ? 1.0f / unit_v : 0.0f;
+            if (one_scale) shift = fmaxf(__builtin_amdgcn_logf(big * per), LEAST_RATIO);
         }
-        if constexpr (EXP) {
-            // the running maximum, and the value scale that the sums are in
-            const Halves tops = both_halves(top);
-            const float top2 = fmaxf(tops.a, tops.b) * c;
-            if constexpr (CACHE) {
-                float big = lds_vs[t % 4 * ATT_KEYS + (one_scale ? 0 : lane)];
-                if (!one_scale) {
+        if (__any(top - m > GROWTH || (m == -__builtin_inff() && top > m)) || (CACHE && grow != 1.0f)) {
+            const float m2 = fmaxf(m, top);
+            const float keep = m == -__builtin_inff() ? 0.0f : exp2_fast(m - m2);
+            l *= keep;
+            m = m2;
 #pragma unroll
-                    for (int d = 32; d; d >>= 1) big = fmaxf(big, __shfl_xor(big, d, 64));
-                }
-                big = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, big)));
-                if (big > unit_v) {
-                    grow = unit_v / big;
-                    unit_v = big;
-                }
-                per = unit_v > 0.0f ? 1.0f / unit_v : 0.0f;
-                if (one_scale) shift = fmaxf(__builtin_amdgcn_logf(big * per), LEAST_RATIO);
-            }
-            if (__any(top2 - m > GROWTH || (m == -__builtin_inff() && top2 > m)) || (CACHE && grow != 1.0f)) {
-                const float m2 = fmaxf(m, top2);
-                const float keep = m == -__builtin_inff() ? 0.0f : exp2_fast(m - m2);
-                l *= keep;
-                behind = keep * grow;
-                m = m2;
-            }
-            mc = m == -__builtin_inff() ? 0.0f : shift - m;
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[d][r] *= keep * grow;
         }
-        constexpr int NP = PV ? 4 * DT : 0, NQ = QK ? 2 * KS : 0, NM = NP + NQ, AHEAD = NM < 3 ? NM : 3;
-        constexpr int STEPS = NM ? NM : 1, PAIRS = EXP ? (16 + STEPS - 1) / STEPS : 0;   // pairs of weights behind a matrix instruction
-        auto part = [&](int i) { return i < NP ? value_part(stage ^ 1, i % DT, i / DT) : key_part(stage ^ 1, (i - NP) / KS, (i - NP) % KS); };
-        f16x8 f[AHEAD ? AHEAD : 1];
+        const float mc = m == -__builtin_inff() ? 0.0f : shift - m;
+        f16x8 p[4];                                    // weights, as steps of 16 keys
         float sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) f[i] = part(i);
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
-            if (i < NP) acc[i % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i % (AHEAD ? AHEAD : 1)], p[i / DT], acc[i % DT], 0, 0, 0);
-            else if (i < NM) next[(i - NP) / KS] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i % (AHEAD ? AHEAD : 1)], qf[(i - NP) % KS], (i - NP) % KS ? next[(i - NP) / KS] : f32x16{}, 0, 0, 0);
-            if (i + AHEAD < NM) f[i % (AHEAD ? AHEAD : 1)] = part(i + AHEAD);
-#pragma unroll
-            for (int x = i * PAIRS; x < (i + 1) * PAIRS && x < 16; ++x) {
-                const int u = x / 8, r = 2 * (x % 8), g = x / 4, e = 2 * (x % 4);   // scores s[u][r], s[u][r + 1]; slots e, e + 1 of step g
-                float w0 = exp2_fast(__builtin_fmaf(s[u][r], c, mc)), w1 = exp2_fast(__builtin_fmaf(s[u][r + 1], c, mc));
-                if constexpr (CACHE) {
-                    sum += w0 + w1;
-                    if (!one_scale) {
-                        const float2 v = *reinterpret_cast<const float2 *>(lds_vs + t % 4 * ATT_KEYS + 16 * g + (e < 4 ? e : e + 4) + 4 * half);
-                        w0 *= v.x * per;
-                        w1 *= v.y * per;
-                    }
+        for (int x = 0; x < 16; ++x) {
+            const int u = x / 8, r = 2 * (x % 8), g = x / 4, e = 2 * (x % 4);   // scores s[u][r], s[u][r + 1]; slots e, e + 1 of step g
+            float w0 = exp2_fast(__builtin_fmaf(s[u][r], c, mc)), w1 = exp2_fast(__builtin_fmaf(s[u][r + 1], c, mc));
+            if constexpr (CACHE) {
+                sum += w0 + w1;
+                if (!one_scale) {
+                    const float2 v = *reinterpret_cast<const float2 *>(lds_vs + stage * ATT_KEYS + 16 * g + (e < 4 ? e : e + 4) + 4 * half);
+                    w0 *= v.x * per;
+                    w1 *= v.y * per;
                 }
-                const f16x2 h = {(_Float16)w0, (_Float16)w1};
-                // the sum takes the weights as they are multiplied, unless they carry a value scale
-                if constexpr (!CACHE) sum = __builtin_amdgcn_fdot2(h, f16x2{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
-                // here and not behind the round, where the compiler would move what only later code reads
-                asm volatile("" ::"v"(__builtin_bit_cast(unsigned, h)));
-                w[g][e] = h[0];
-                w[g][e + 1] = h[1];
             }
-            __builtin_amdgcn_sched_barrier(0);
+            const f16x2 h = {(_Float16)w0, (_Float16)w1};
+            // the sum takes the weights as they are multiplied, unless they carry a value scale
+            if constexpr (!CACHE) sum = __builtin_amdgcn_fdot2(h, f16x2{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
+            p[g][e] = h[0];
+            p[g][e + 1] = h[1];
         }
-        if constexpr (EXP) {
-            if (CACHE && one_scale) sum *= exp2_fast(-shift);
-            l += sum;
-        }
-        if constexpr (QK) {
-            c = shape(next, t + 1, stage ^ 1);
-            top = largest(next);
-        }
+        if (CACHE && one_scale) sum *= exp2_fast(-shift);
+        l += sum;
+#pragma unroll
+        for (int st = 0; st < 4; ++st)
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value_part(stage, d, st), p[st], acc[d], 0, 0, 0);
     };
-    constexpr std::true_type yes{};
-    constexpr std::false_type no{};
-
     if (t0 < t1) {
         if constexpr (CACHE) {
-            request_keys(t0);
-            put_keys(t0, 0);
-            if (t0 + 1 < t1) {
-                request_keys(t0 + 1);
-                put_keys(t0 + 1, 1);
-            }
+            request(t0);
+            put_keys(0);
+            put_values(0);
         } else {
             dma(false, t0, 0);
-            if (t0 + 1 < t1) dma(false, t0 + 1, 1);
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            dma(true, t0, 0);
         }
-        __syncthreads();
-        // round t reads keys of tile t + 1 and values of tile t - 1; keys of tile t + 2 and values of tile t come in meanwhile
-        // In front of round t: keys of tile t + 1 and values of tile t - 1 are there, what the round in front of it read is free.  Every
-        // wavefront passes this for every t up to t1, whatever its own rows see.
         auto turn = [&](int t, int stage) __attribute__((always_inline)) {
+            // tile t is there, and what tile t - 1 had is read by all
             if constexpr (!CACHE) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
+            if (t + 1 < t1) {
+                if constexpr (CACHE) {
+                    request(t + 1);
+                } else {
+                    dma(false, t + 1, stage ^ 1);
+                    dma(true, t + 1, stage ^ 1);
+                }
+            }
+            if (t < tw) work(t, stage);
             if constexpr (CACHE) {
-                if (t + 2 < t1) request_keys(t + 2);
-                if (t < t1) request_values(t);
-            } else {
-                if (t + 2 < t1) dma(false, t + 2, stage);
-                if (t < t1) dma(true, t, stage);
+                if (t + 1 < t1) {
+                    put_keys(stage ^ 1);
+                    put_values(stage ^ 1);
+                }
             }
         };
-        auto put = [&](int t, int stage) __attribute__((always_inline)) {
-            if constexpr (CACHE) {
-                if (t + 2 < t1) put_keys(t + 2, stage);
-                if (t < t1) put_values(stage);
-            }
-        };
-        int t = t0;
-        if (t < tw) {
-            round(yes, no, no, t - 1, 1, sb, sa, pb, pb);
-            for (; t + 2 < tw; t += 2) {
-                turn(t, 0);
-                round(yes, yes, yes, t, 0, sa, sb, pa, pb);
-                put(t, 0);
-                turn(t + 1, 1);
-                round(yes, yes, yes, t + 1, 1, sb, sa, pb, pa);
-                put(t + 1, 1);
-            }
-            int stage = 0;
-            if (t + 1 < tw) {
-                turn(t, 0);
-                round(yes, yes, yes, t, 0, sa, sb, pa, pb);
-                put(t, 0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) pb[i] = pa[i];
-                sa[0] = sb[0];
-                sa[1] = sb[1];
-                ++t;
-                stage = 1;
-            }
-            turn(t, stage);
-            round(no, yes, yes, t, stage, sa, sb, pa, pb);
-            put(t, stage);
-            ++t;
-            turn(t, stage ^ 1);
-            round(no, yes, no, t, stage ^ 1, sa, sb, pb, pa);
-            put(t, stage ^ 1);
-            ++t;
-        }
-        for (; t <= t1; ++t) {
-            turn(t, (t - t0) & 1);
-            put(t, (t - t0) & 1);
+        for (int t = t0; t < t1; t += 2) {
+            turn(t, 0);
+            if (t + 1 < t1) turn(t + 1, 1);
         }
     }
     const Halves ls = both_halves(l);

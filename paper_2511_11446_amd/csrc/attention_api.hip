@@ -192,6 +192,9 @@ int attention_kv8(const ql_attention *attn, const ql_kv_cache *cache, void *work
     if (rc) return rc;
     if ((rc = check_cache(cache))) return rc;
     if (attn->B != cache->B || attn->Hkv != cache->Hkv || attn->D != cache->D) return QL_ERR_SHAPE;
+    // the kernels count groups of 64 tokens of 16 rows of a key head in 32 bits
+    const int64_t row_tiles = (attn->T_q * (attn->Hq / attn->Hkv) / 16 + attn->B) * attn->Hkv, groups = (int64_t)cache->max_pages * (cache->page / 64);
+    if (row_tiles > INT_MAX64 / groups) return QL_ERR_SHAPE;
     if ((rc = check_workspace(workspace, workspace_bytes, attention_kv8_workspace_bytes(attn->T_q, attn->B, attn->Hq, attn->Hkv, attn->D)))) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
     if ((rc = clear_absmax(attn, s))) return rc;

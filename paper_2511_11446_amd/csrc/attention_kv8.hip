@@ -1,7 +1,7 @@
 // Attention of few rows over the paged 8-bit cache for gfx950: single tokens, and short runs of them.
 //
 // The work is the cache's bytes: a unit is one group of 64 tokens of one key head for up to 16 packed rows (attention.h).  The launch is a fixed number
-// of workgroups that share all units of all sequences evenly, whatever the lengths: workgroup w has the units [w U / W, (w + 1) U / W) of the list that goes
+// of workgroups that share all units of all sequences evenly, whatever the lengths: every workgroup has the next U / W units (some one more) of the list that goes
 // sequence by sequence, key head by key head.  Where an item (the units of one set of rows) is cut between workgroups, each leaves sums, maximum and
 // weight in the workspace and join_parts puts them together.
 //
@@ -37,32 +37,36 @@ __device__ __forceinline__ SeqUnits seq_units(const AttnArgs &a, int b)
     s.groups = max((s.n_k + KV_GROUP - 1) / KV_GROUP, 1);   // rows without keys are written too
     return s;
 }
-__device__ __forceinline__ long long lanes_upto(long long v)
+// Units and items are counted in 32 bits (the host refuses what could pass them): 64-bit divisions cost more than a unit.
+__device__ __forceinline__ unsigned lanes_upto(unsigned v)
 {
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const long long o = __shfl_up(v, d, 64);
+        const unsigned o = (unsigned)__shfl_up((int)v, d, 64);
         if (lane >= d) v += o;
     }
     return v;
 }
-__device__ __forceinline__ long long units_of(const AttnArgs &a, int b)
+__device__ __forceinline__ unsigned last_lane(unsigned v) { return (unsigned)__builtin_amdgcn_readlane((int)v, 63); }
+__device__ __forceinline__ unsigned units_of(const AttnArgs &a, int b)
 {
     const SeqUnits s = seq_units(a, b);
-    return (long long)s.row_tiles * s.groups * a.Hkv;
+    return (unsigned)s.row_tiles * (unsigned)s.groups * (unsigned)a.Hkv;
 }
-__device__ __forceinline__ long long all_units(const AttnArgs &a)
+// Of `units` units every one of `workers` workgroups has `each`, the first `more` of them one more
+struct Shares {
+    unsigned workers, each, more;
+    __device__ __forceinline__ unsigned first(unsigned w) const { return w * each + min(w, more); }
+    __device__ __forceinline__ unsigned owner(unsigned u) const { return u < more * (each + 1) ? u / (each + 1) : more + (u - more * (each + 1)) / each; }
+};
+__device__ __forceinline__ Shares shares_of(unsigned units, unsigned most)
 {
-    const int lane = threadIdx.x & 63;
-    long long total = 0;
-    for (int base = 0; base < a.B; base += 64) total += __shfl(lanes_upto(base + lane < a.B ? units_of(a, base + lane) : 0), 63, 64);
-    return total;
-}
-__device__ __forceinline__ long long workers_of(long long units, int most)
-{
-    const long long w = (units + UNITS_PER_WORKER - 1) / UNITS_PER_WORKER;
-    return w < most ? w : most;
+    Shares s;
+    s.workers = min((units + UNITS_PER_WORKER - 1) / UNITS_PER_WORKER, most);
+    s.each = s.workers ? units / s.workers : 0;
+    s.more = units - s.each * s.workers;
+    return s;
 }
 
 __device__ __forceinline__ float lanes16_max(float x)   // over the four lanes that have the same row
@@ -88,56 +92,127 @@ __device__ __forceinline__ float lanes16_sum(float x)
     return __builtin_bit_cast(float, c) + __builtin_bit_cast(float, d);
 }
 
-// wavefronts per SIMD: as many as the loads of a whole unit leave registers for
-constexpr int cached_waves(int NK, bool TOKEN) { return NK <= 2 ? (TOKEN ? 3 : 4) : NK <= 4 ? (TOKEN ? 2 : 3) : NK <= 6 ? 2 : 1; }
+// wavefronts per SIMD: as many as a unit's bytes leave registers for
+constexpr int cached_waves(int NK) { return NK <= 1 ? 4 : NK <= 2 ? 3 : NK <= 4 ? 2 : 1; }
 
-// NK: 32-channel steps of the scores; WIDE: D is a multiple of 64, keys in 16-byte pieces (else 8); TOKEN: a scale for every token
-template <int NK, bool WIDE, bool TOKEN>
-__global__ __launch_bounds__(256, cached_waves(NK, TOKEN)) void attend_cached(AttnArgs a, CachedPlan plan)
+// NK: 32-channel steps of the scores; WIDE: D is a multiple of 64, keys in 16-byte pieces (else 8)
+template <int NK, bool WIDE>
+__global__ __launch_bounds__(256, cached_waves(NK)) void attend_cached(AttnArgs a, CachedPlan plan)
 {
-    constexpr int DT = 2 * NK;
-    extern __shared__ __align__(16) float join[];     // [4][16][D] sums, [4][16] maxima, [4][16] weights
+    constexpr int DT = 2 * NK, KP = (NK + 1) / 2;
+    extern __shared__ __align__(16) float join[];     // [4][16][D] sums, [4][16] maxima, [4][16] weights, [4][128] scales
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int quarter = lane >> 4, r16 = lane & 15;
     const int D = a.D;
     float *join_m = join + 64 * D, *join_l = join_m + 64;
+    float *scales = join_l + 64 + 128 * wave;         // of the keys and the values of a unit
 
-    const long long units = all_units(a);
-    const long long workers = workers_of(units, plan.workers);
-    if (blockIdx.x >= workers) return;
-    long long u = blockIdx.x * units / workers;
-    const long long u_end = (blockIdx.x + 1) * units / workers;
+    // units of the first 64 sequences (as a rule all), one per lane, and their sums from the front
+    const unsigned mine0 = lane < a.B ? units_of(a, lane) : 0, upto0 = lanes_upto(mine0);
+    unsigned units = last_lane(upto0);
+    for (int base = 64; base < a.B; base += 64) units += last_lane(lanes_upto(base + lane < a.B ? units_of(a, base + lane) : 0));
+    const Shares shares = shares_of(units, plan.workers);
+    if (blockIdx.x >= shares.workers) return;
+    unsigned u = shares.first(blockIdx.x);
+    const unsigned u_end = shares.first(blockIdx.x + 1);
     const bool shaped = a.cap > 0.0f || a.slopes;
-    const float cap2 = a.cap * LOG2E;
+    const float cap2 = a.cap * LOG2E, scale2 = a.scale * LOG2E;
+    const float cap_in = a.cap > 0.0f ? 2.0f * LOG2E / cap2 : 0.0f;
+    const unsigned page_groups = (unsigned)a.page / KV_GROUP, blocks = KV_GROUP / a.scale_tokens;   // of a group
 
     while (u < u_end) {
         // the sequence and item of unit u
         int b = -1;
-        long long at = u;
+        unsigned at = u;
         for (int base = 0; base < a.B; base += 64) {
-            const long long mine = base + lane < a.B ? units_of(a, base + lane) : 0, upto = lanes_upto(mine);
+            unsigned mine = mine0, upto = upto0;
+            if (base > 0) {
+                mine = base + lane < a.B ? units_of(a, base + lane) : 0;
+                upto = lanes_upto(mine);
+            }
             const unsigned long long behind = __ballot(upto > at);
             if (behind) {
                 const int l = __ffsll(behind) - 1;
-                at -= __shfl(upto - mine, l, 64);
-                b = __builtin_amdgcn_readfirstlane(base + l);
+                at -= (unsigned)__builtin_amdgcn_readlane((int)(upto - mine), l);
+                b = base + l;
                 break;
             }
-            at -= __shfl(upto, 63, 64);
+            at -= last_lane(upto);
         }
         if (b < 0) return;
         const SeqUnits s = seq_units(a, b);
-        const int item = __builtin_amdgcn_readfirstlane((int)(at / s.groups));
-        const int g0 = __builtin_amdgcn_readfirstlane((int)(at % s.groups));
-        const int g1 = (int)(s.groups - g0 < u_end - u ? s.groups : g0 + (u_end - u));
-        const int hk = item / s.row_tiles, r0 = item % s.row_tiles * 16;
+        const unsigned item = at / (unsigned)s.groups;
+        const int g0 = (int)(at - item * (unsigned)s.groups);
+        const int g1 = (int)min((unsigned)s.groups, g0 + (u_end - u));
+        const int hk = (int)(item / (unsigned)s.row_tiles), r0 = (int)(item - hk * s.row_tiles) * 16;
         const int rows = s.n_q * a.G;
-        const int row = min(r0 + r16, rows - 1), token = row / a.G, head = hk * a.G + row % a.G;
+        const int row = min(r0 + r16, rows - 1), token = row / a.G, head = hk * a.G + row - token * a.G;
         const int pos = token + s.n_k - s.n_q;
         const int prefix = a.prefix ? a.prefix[b] : 0;
         const int end = visible_end(a.mask, prefix, pos, s.n_k);
         const int end_last = visible_end(a.mask, prefix, (min(r0 + 15, rows - 1)) / a.G + s.n_k - s.n_q, s.n_k);
+        const float slope2 = a.slopes ? a.slopes[head] * LOG2E : 0.0f;
 
+        // this wavefront's groups are g0 + wave + 4 i; pages of 64 of them, one per lane
+        int pages = -1, pages_at = -64;
+        auto page_of = [&](int i) {
+            if (i - pages_at >= 64) {
+                pages_at = i;
+                const int g = g0 + wave + 4 * (i + lane);
+                pages = g < g1 ? a.page_table[(size_t)b * a.max_pages + (unsigned)g / page_groups] : -1;
+            }
+            return __builtin_amdgcn_readlane(pages, i - pages_at);
+        };
+        // the first group from i on that has a page and a key to see, or the first behind the last
+        const int mine = (min(g1, (end_last + KV_GROUP - 1) / KV_GROUP) - g0 - wave + 3) / 4;
+        auto next = [&](int i) {
+            while (i < mine) {
+                const int p = page_of(i);
+                if (p >= 0 && p < a.num_pages) break;
+                ++i;
+            }
+            return i;
+        };
+        uint4 kw[4][KP], vw[DT];
+        float kscale, vscale;                          // of token `lane`
+        // group i of this wavefront among those of the cache
+        auto group_of = [&](int i) { return ((size_t)page_of(i) * a.Hkv + hk) * page_groups + (unsigned)(g0 + wave + 4 * i) % page_groups; };
+        auto request_keys = [&](size_t group) __attribute__((always_inline)) {
+            const unsigned char *kp = reinterpret_cast<const unsigned char *>(a.kc) + group * (KV_GROUP * (size_t)D);
+            const size_t block = group * blocks + (unsigned)lane / (unsigned)a.scale_tokens;
+            kscale = a.ks[block];
+            vscale = a.vs[block];
+#pragma unroll
+            for (int i4 = 0; i4 < 4; ++i4)
+#pragma unroll
+                for (int k = 0; k < NK; k += WIDE ? 2 : 1) {
+                    if (WIDE) {
+                        kw[i4][k / 2] = *reinterpret_cast<const uint4 *>(kp + (unsigned)((16 * i4 + r16) * D + 32 * k + 16 * quarter));
+                    } else {
+                        const int c = min(32 * k + 8 * quarter, D - 8);   // behind D: any codes, the queries there are zero
+                        const uint2 w = *reinterpret_cast<const uint2 *>(kp + (unsigned)((16 * i4 + r16) * D + c));
+                        if (k % 2 == 0) {
+                            kw[i4][k / 2].x = w.x;
+                            kw[i4][k / 2].y = w.y;
+                        } else {
+                            kw[i4][k / 2].z = w.x;
+                            kw[i4][k / 2].w = w.y;
+                        }
+                    }
+                }
+        };
+        auto request_values = [&](size_t group) __attribute__((always_inline)) {
+            const unsigned char *vp = reinterpret_cast<const unsigned char *>(a.vc) + group * (KV_GROUP * (size_t)D);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) vw[d] = *reinterpret_cast<const uint4 *>(vp + (unsigned)(min(16 * d + r16, D - 1) * KV_GROUP + 16 * quarter));
+        };
+
+        int i = next(0);
+        if (i < mine) {
+            const size_t group = group_of(i);
+            request_keys(group);
+            request_values(group);
+        }
         f16x8 qf[NK];
         {
             const _Float16 *q = static_cast<const _Float16 *>(a.q) + (s.first + token) * a.q_row + head * a.q_head;
@@ -149,75 +224,12 @@ __global__ __launch_bounds__(256, cached_waves(NK, TOKEN)) void attend_cached(At
                 if (c < D) qf[k] = *reinterpret_cast<const f16x8 *>(q + c);
             }
         }
-        const float scale2 = a.scale * LOG2E, cap_in = a.cap > 0.0f ? 2.0f * scale2 / a.cap : scale2;
-        const float slope2 = a.slopes ? a.slopes[head] * LOG2E : 0.0f;
-
         f32x4 acc[DT];
 #pragma unroll
         for (int d = 0; d < DT; ++d) acc[d] = f32x4{};
         float m = -__builtin_inff(), l = 0.0f, unit_v = 0.0f;   // unit_v: the value scale that the sums are in
-        int pages = -1;
-        for (int i = 0, g = g0 + wave; g < g1; ++i, g += 4) {
-            if (i % 64 == 0) {
-                // page of this wavefront's next 64 groups, one per lane
-                const int mine = g + 4 * lane;
-                pages = mine < g1 ? a.page_table[(size_t)b * a.max_pages + mine * KV_GROUP / a.page] : -1;
-            }
-            const int page = __builtin_amdgcn_readlane(pages, i % 64);
-            const int j0 = g * KV_GROUP;
-            if (j0 >= end_last || page < 0 || page >= a.num_pages) continue;
-            const size_t ph = (size_t)page * a.Hkv + hk;
-            const int in_page = j0 % a.page;
-            const unsigned char *kp = reinterpret_cast<const unsigned char *>(a.kc) + (ph * a.page + in_page) * D;
-            const unsigned char *vp = reinterpret_cast<const unsigned char *>(a.vc) + (ph * a.page + in_page) * D;
-            uint4 kw[4][WIDE ? NK / 2 : (NK + 1) / 2];
-            uint4 vw[DT];
-            if (WIDE) {
-#pragma unroll
-                for (int i4 = 0; i4 < 4; ++i4)
-#pragma unroll
-                    for (int k = 0; k < NK / 2; ++k) kw[i4][k] = *reinterpret_cast<const uint4 *>(kp + (unsigned)((16 * i4 + r16) * D + 64 * k + 16 * quarter));
-            } else {
-#pragma unroll
-                for (int i4 = 0; i4 < 4; ++i4)
-#pragma unroll
-                    for (int k = 0; k < NK; ++k) {
-                        const int c = min(32 * k + 8 * quarter, D - 8);   // behind D: any codes, the queries there are zero
-                        const uint2 w = *reinterpret_cast<const uint2 *>(kp + (unsigned)((16 * i4 + r16) * D + c));
-                        if (k % 2 == 0) {
-                            kw[i4][k / 2].x = w.x;
-                            kw[i4][k / 2].y = w.y;
-                        } else {
-                            kw[i4][k / 2].z = w.x;
-                            kw[i4][k / 2].w = w.y;
-                        }
-                    }
-            }
-#pragma unroll
-            for (int d = 0; d < DT; ++d) vw[d] = *reinterpret_cast<const uint4 *>(vp + (unsigned)(min(16 * d + r16, D - 1) * KV_GROUP + 16 * quarter));
-            // scales of this lane's tokens 16 i + 4 quarter + e
-            const float *ks = a.ks + ph * (a.page / a.scale_tokens) + in_page / a.scale_tokens, *vs = a.vs + ph * (a.page / a.scale_tokens) + in_page / a.scale_tokens;
-            f32x4 sk[4], sv[4];
-#pragma unroll
-            for (int i4 = 0; i4 < 4; ++i4) {
-                if (TOKEN) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        sk[i4][e] = ks[16 * i4 + 4 * quarter + e];
-                        sv[i4][e] = vs[16 * i4 + 4 * quarter + e];
-                    }
-                } else {
-                    const float x = ks[16 * i4 / a.scale_tokens], y = vs[16 * i4 / a.scale_tokens];
-                    sk[i4] = f32x4{x, x, x, x};
-                    sv[i4] = f32x4{y, y, y, y};
-                }
-                // of tokens behind the end a scale may hold anything
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int j = TOKEN ? j0 + 16 * i4 + 4 * quarter + e : j0 + 16 * i4;
-                    if (j >= s.n_k) sv[i4][e] = 0.0f;
-                }
-            }
+        while (i < mine) {
+            const int j0 = (g0 + wave + 4 * i) * KV_GROUP;
             f32x4 sc[4];
 #pragma unroll
             for (int i4 = 0; i4 < 4; ++i4) {
@@ -227,16 +239,30 @@ __global__ __launch_bounds__(256, cached_waves(NK, TOKEN)) void attend_cached(At
                     const uint4 w = kw[i4][k / 2];
                     sc[i4] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k % 2 == 0 ? codes_f16x8(w.x, w.y) : codes_f16x8(w.z, w.w), qf[k], sc[i4], 0, 0, 0);
                 }
+                __builtin_amdgcn_sched_barrier(0);     // (else the compiler turns all codes into binary16 first, and has no registers for that)
             }
+            // scales of this lane's tokens 16 i + 4 quarter + e, through LDS; of tokens behind the end they may hold anything
+            scales[lane] = kscale * scale2;
+            scales[64 + lane] = j0 + lane < s.n_k ? vscale : 0.0f;
+            // the next unit's keys come in while this one's weights are taken, its values behind this one's
+            const int n = next(i + 1);
+            size_t group = 0;
+            if (n < mine) {
+                group = group_of(n);
+                request_keys(group);
+            }
+            f32x4 sk[4], sv[4];
+#pragma unroll
+            for (int i4 = 0; i4 < 4; ++i4) sk[i4] = *reinterpret_cast<const f32x4 *>(scales + 16 * i4 + 4 * quarter);
             float top = -__builtin_inff();
 #pragma unroll
             for (int i4 = 0; i4 < 4; ++i4)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int j = j0 + 16 * i4 + 4 * quarter + e;
-                    float y = sc[i4][e] * (sk[i4][e] * cap_in);
+                    float y = sc[i4][e] * sk[i4][e];
                     if (shaped) {
-                        if (a.cap > 0.0f) y = capped(y, cap2);
+                        if (a.cap > 0.0f) y = capped(y * cap_in, cap2);
                         y = __builtin_fmaf(-slope2, fabsf((float)(pos - j)), y);
                     }
                     y = j < end ? y : -__builtin_inff();
@@ -251,10 +277,12 @@ __global__ __launch_bounds__(256, cached_waves(NK, TOKEN)) void attend_cached(At
             // the largest value scale so far
             float big = 0.0f;
 #pragma unroll
+            for (int i4 = 0; i4 < 4; ++i4) sv[i4] = *reinterpret_cast<const f32x4 *>(scales + 64 + 16 * i4 + 4 * quarter);
+#pragma unroll
             for (int i4 = 0; i4 < 4; ++i4)
 #pragma unroll
-                for (int e = 0; e < (TOKEN ? 4 : 1); ++e) big = fmaxf(big, sv[i4][e]);
-            if (TOKEN) big = lanes16_max(big);
+                for (int e = 0; e < 4; ++e) big = fmaxf(big, sv[i4][e]);
+            big = lanes16_max(big);
             if (big > unit_v) {
                 keep *= unit_v / big;
                 unit_v = big;
@@ -276,7 +304,10 @@ __global__ __launch_bounds__(256, cached_waves(NK, TOKEN)) void attend_cached(At
             for (int d = 0; d < DT; ++d) {
                 acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_f16x8(vw[d].x, vw[d].y), p[0], acc[d], 0, 0, 0);
                 acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_f16x8(vw[d].z, vw[d].w), p[1], acc[d], 0, 0, 0);
+                if (d % 2) __builtin_amdgcn_sched_barrier(0);
             }
+            if (n < mine) request_values(group);
+            i = n;
         }
         // the four wavefronts' parts: channels 16 d + 4 quarter .. + 3 of row r16
         l = lanes16_sum(l);
@@ -334,105 +365,121 @@ __global__ __launch_bounds__(256, cached_waves(NK, TOKEN)) void attend_cached(At
     }
 }
 
-// one workgroup per item (a bound of them): adds up the parts of those that several workgroups shared
+// Adds up the parts of the items that several workgroups shared: one wavefront per packed row (blockIdx.y: four of an item's 16), blockIdx.x a bound of the
+// items.  The parts' maxima and weights go one per lane; the sums are read eight parts at a time.
 __global__ __launch_bounds__(256) void join_parts(AttnArgs a, CachedPlan plan)
 {
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int D = a.D;
-    const long long units = all_units(a);
-    const long long workers = workers_of(units, plan.workers);
     int b = -1;
-    long long item = blockIdx.x, u0 = 0;
+    unsigned item = blockIdx.x, u0 = 0, units = 0;
+    SeqUnits s{};
     for (int base = 0; base < a.B; base += 64) {
-        SeqUnits s{};
-        if (base + lane < a.B) s = seq_units(a, base + lane);
-        const long long items = (long long)s.row_tiles * a.Hkv, mine = items * s.groups;
-        const long long upto = lanes_upto(items), units_upto = lanes_upto(mine);
+        SeqUnits mine{};
+        if (base + lane < a.B) mine = seq_units(a, base + lane);
+        const unsigned items = (unsigned)mine.row_tiles * (unsigned)a.Hkv, its_units = items * (unsigned)mine.groups;
+        const unsigned upto = lanes_upto(items), units_upto = lanes_upto(its_units);
         const unsigned long long behind = __ballot(upto > item);
-        if (behind) {
+        if (b < 0 && behind) {
             const int l = __ffsll(behind) - 1;
-            item -= __shfl(upto - items, l, 64);
-            u0 += __shfl(units_upto - mine, l, 64);
-            b = __builtin_amdgcn_readfirstlane(base + l);
-            break;
+            auto from = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+            item -= (unsigned)from((int)(upto - items));
+            u0 = units + (unsigned)from((int)(units_upto - its_units));
+            s = {from(mine.n_q), from(mine.first), from(mine.n_k), from(mine.row_tiles), from(mine.groups)};
+            b = base + l;
+        } else if (b < 0) {
+            item -= last_lane(upto);
         }
-        item -= __shfl(upto, 63, 64);
-        u0 += __shfl(units_upto, 63, 64);
+        units += last_lane(units_upto);
     }
     if (b < 0) return;
-    const SeqUnits s = seq_units(a, b);
-    u0 += item * s.groups;
-    const long long u1 = u0 + s.groups;
-    // workgroup w has units [w U / W, (w + 1) U / W): the ones of the first and the last unit
-    auto owner = [&](long long u) {
-        long long w = u * workers / units;
-        while (w > 0 && w * units / workers > u) --w;
-        while ((w + 1) * units / workers <= u) ++w;
-        return w;
-    };
-    const long long wa = owner(u0), wb = owner(u1 - 1);
-    if (wa == wb) return;
-    const int hk = (int)(item / s.row_tiles), r0 = (int)(item % s.row_tiles) * 16, rows = s.n_q * a.G;
+    const int hk = (int)(item / (unsigned)s.row_tiles), r = 4 * blockIdx.y + wave, row = (int)(item - hk * s.row_tiles) * 16 + r;
+    if (row >= s.n_q * a.G) return;
+    const Shares shares = shares_of(units, plan.workers);
+    u0 += item * (unsigned)s.groups;
+    // the workgroups of the item's first and last unit
+    const int wa = (int)shares.owner(u0), wb = (int)shares.owner(u0 + s.groups - 1), n = wb - wa + 1;
+    if (n == 1) return;
     const size_t stride = 16 * (size_t)(D + 2);
-    auto part = [&](long long w) { return a.partial + (2 * (size_t)w + (w == wa ? 1 : 0)) * stride; };
-    for (int e = threadIdx.x; e < 16 * (D / 8); e += 256) {
-        const int r = e / (D / 8), c = e % (D / 8) * 8;
-        if (r0 + r >= rows) continue;
-        float m = -__builtin_inff();
-        for (long long w = wa; w <= wb; ++w) m = fmaxf(m, part(w)[16 * D + r]);
-        float sum[8] = {}, weight = 0.0f;
-        if (m > -__builtin_inff())
-            for (long long w = wa; w <= wb; ++w) {
-                const float *x = part(w);
-                const float k = exp2_fast(x[16 * D + r] - m);
+    // workgroup wa's last items's part is its second, the others begin with this item
+    auto part = [&](int i) { return a.partial + (2 * (size_t)(wa + i) + (i == 0 ? 1 : 0)) * stride; };
+    float m = -__builtin_inff();
+    for (int i = lane; i < n; i += 64) m = fmaxf(m, part(i)[16 * D + r]);
+#pragma unroll
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+    const int token = s.first + row / a.G, head = hk * a.G + row % a.G;
+    _Float16 *o = static_cast<_Float16 *>(a.o) + token * a.o_row + head * a.o_head;
+    f32x4 sum = {};                                    // channels 4 lane .. + 3
+    float weight = 0.0f;
+    if (m > -__builtin_inff())
+        for (int first = 0; first < n; first += 64) {
+            float k = 0.0f;
+            if (first + lane < n) {
+                const float *x = part(first + lane);
+                k = exp2_fast(x[16 * D + r] - m);
                 weight += k * x[16 * D + 16 + r];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum[i] += k * x[r * D + c + i];
             }
-        const float inv = weight > 0.0f ? 1.0f / weight : 0.0f;
-        f16x8 o;
-        unsigned amax = 0;
+            const int here = min(64, n - first);
+            for (int at = 0; at < here; at += 8) {
+                f32x4 x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            o[i] = (_Float16)(sum[i] * inv);
-            amax = max(amax, absmax_bits(o[i]));
+                for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const f32x4 *>(part(first + min(at + i, here - 1)) + r * D + min(4 * lane, D - 4));
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum += x[i] * (at + i < here ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, k), at + i)) : 0.0f);
+            }
         }
-        const int t = s.first + (r0 + r) / a.G, h = hk * a.G + (r0 + r) % a.G;
-        *reinterpret_cast<f16x8 *>(static_cast<_Float16 *>(a.o) + t * a.o_row + h * a.o_head + c) = o;
-        if (a.row_absmax) atomicMax(a.row_absmax + t, amax);
+#pragma unroll
+    for (int d = 32; d; d >>= 1) weight += __shfl_xor(weight, d, 64);
+    const float inv = weight > 0.0f ? 1.0f / weight : 0.0f;
+    unsigned amax = 0;
+    if (4 * lane < D) {
+        f16x4 h;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const _Float16 x = (_Float16)(sum[e] * inv);
+            h[e] = x;
+            amax = max(amax, absmax_bits(x));
+        }
+        *reinterpret_cast<f16x4 *>(o + 4 * lane) = h;
+    }
+    if (a.row_absmax) {
+#pragma unroll
+        for (int d = 32; d; d >>= 1) amax = max(amax, (unsigned)__shfl_xor((int)amax, d, 64));
+        if (lane == 0) atomicMax(a.row_absmax + token, amax);
     }
 }
 
 namespace {
-template <int NK, bool WIDE, bool TOKEN>
+template <int NK, bool WIDE>
 hipError_t launch_cached(const AttnArgs &a, const CachedPlan &p, hipStream_t stream)
 {
-    const int lds = 4 * (64 * a.D + 128);
-    auto *kernel = attend_cached<NK, WIDE, TOKEN>;
-    static const hipError_t opt_in = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 4 * (64 * 32 * NK + 128));
+    const int lds = 4 * (64 * a.D + 128 + 512);
+    auto *kernel = attend_cached<NK, WIDE>;
+    static const hipError_t opt_in = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 4 * (64 * 32 * NK + 128 + 512));
     if (opt_in != hipSuccess) return opt_in;
     hipLaunchKernelGGL(kernel, dim3(p.workers), dim3(256), lds, stream, a, p);
     return hipGetLastError();
 }
-template <bool TOKEN>
 hipError_t launch_by_head(const AttnArgs &a, const CachedPlan &p, hipStream_t stream)
 {
     if (a.D % 64 == 0) {
-        if (a.D == 64) return launch_cached<2, true, TOKEN>(a, p, stream);
-        if (a.D == 128) return launch_cached<4, true, TOKEN>(a, p, stream);
-        if (a.D == 192) return launch_cached<6, true, TOKEN>(a, p, stream);
-        return launch_cached<8, true, TOKEN>(a, p, stream);
+        if (a.D == 64) return launch_cached<2, true>(a, p, stream);
+        if (a.D == 128) return launch_cached<4, true>(a, p, stream);
+        if (a.D == 192) return launch_cached<6, true>(a, p, stream);
+        return launch_cached<8, true>(a, p, stream);
     }
-    if (a.D <= 32) return launch_cached<1, false, TOKEN>(a, p, stream);
-    if (a.D <= 64) return launch_cached<2, false, TOKEN>(a, p, stream);
-    if (a.D <= 96) return launch_cached<3, false, TOKEN>(a, p, stream);
-    if (a.D <= 128) return launch_cached<4, false, TOKEN>(a, p, stream);
-    if (a.D <= 192) return launch_cached<6, false, TOKEN>(a, p, stream);
-    return launch_cached<8, false, TOKEN>(a, p, stream);
+    if (a.D <= 32) return launch_cached<1, false>(a, p, stream);
+    if (a.D <= 64) return launch_cached<2, false>(a, p, stream);
+    if (a.D <= 96) return launch_cached<3, false>(a, p, stream);
+    if (a.D <= 128) return launch_cached<4, false>(a, p, stream);
+    if (a.D <= 192) return launch_cached<6, false>(a, p, stream);
+    return launch_cached<8, false>(a, p, stream);
 }
 }  // namespace
 
-int cached_workers(int D) { return D <= 128 ? 1024 : 512; }
+// as many workgroups as the chip holds at once: one more round of them would be a short one
+constexpr int CUS = 256;
+int cached_workers(int D) { return CUS * cached_waves((D + 31) / 32); }
 
 size_t cached_partial_bytes(long long Tq, int B, int Hq, int Hkv, int D)
 {
@@ -447,10 +494,11 @@ hipError_t launch_attention_kv8(const AttnArgs &a, hipStream_t stream)
 {
     if ((long long)a.Tq * a.G > (long long)FEW_ROWS * a.B) return launch_attention_chunks(a, stream);
     const CachedPlan p{cached_workers(a.D)};
-    const hipError_t e = a.scale_tokens == 1 ? launch_by_head<true>(a, p, stream) : launch_by_head<false>(a, p, stream);
+    const hipError_t e = launch_by_head(a, p, stream);
     if (e != hipSuccess) return e;
     const long long items = ((long long)a.Tq * a.G / 16 + a.B) * a.Hkv;
-    hipLaunchKernelGGL(join_parts, dim3((unsigned)items), dim3(256), 0, stream, a, p);
+    const long long of_seq = (long long)(a.cu_q ? a.Tq : a.Tq / a.B) * a.G;   // packed rows of a sequence, at most
+    hipLaunchKernelGGL(join_parts, dim3((unsigned)items, of_seq < 16 ? (unsigned)(of_seq + 3) / 4 : 4), dim3(256), 0, stream, a, p);
     return hipGetLastError();
 }
 

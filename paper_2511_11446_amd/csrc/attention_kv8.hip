@@ -21,10 +21,18 @@ struct CachedPlan {
 };
 
 constexpr int UNITS_PER_WORKER = 4;   // at least, where there are as many: one for every wavefront
+// What beginning an item costs a workgroup (its sequence, pages, queries, the join of its wavefronts), in units: so many go in front of the item's own in
+// the list that is shared out.  Without, workgroups with many short sequences end last: 64 sequences of 1 to 8192 tokens 129 us.
+constexpr unsigned ITEM_UNITS = 5;
 
 // what one sequence has of units and items
 struct SeqUnits {
     int n_q, first, n_k, row_tiles, groups;
+    __device__ __forceinline__ SeqUnits of_lane(int l) const
+    {
+        auto from = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+        return {from(n_q), from(first), from(n_k), from(row_tiles), from(groups)};
+    }
 };
 __device__ __forceinline__ SeqUnits seq_units(const AttnArgs &a, int b)
 {
@@ -49,10 +57,9 @@ __device__ __forceinline__ unsigned lanes_upto(unsigned v)
     return v;
 }
 __device__ __forceinline__ unsigned last_lane(unsigned v) { return (unsigned)__builtin_amdgcn_readlane((int)v, 63); }
-__device__ __forceinline__ unsigned units_of(const AttnArgs &a, int b)
+__device__ __forceinline__ unsigned units_of(const AttnArgs &a, const SeqUnits &s)
 {
-    const SeqUnits s = seq_units(a, b);
-    return (unsigned)s.row_tiles * (unsigned)s.groups * (unsigned)a.Hkv;
+    return (unsigned)s.row_tiles * ((unsigned)s.groups + ITEM_UNITS) * (unsigned)a.Hkv;
 }
 // Of `units` units every one of `workers` workgroups has `each`, the first `more` of them one more
 struct Shares {
@@ -108,9 +115,11 @@ __global__ __launch_bounds__(256, cached_waves(NK)) void attend_cached(AttnArgs 
     float *scales = join_l + 64 + 128 * wave;         // of the keys and the values of a unit
 
     // units of the first 64 sequences (as a rule all), one per lane, and their sums from the front
-    const unsigned mine0 = lane < a.B ? units_of(a, lane) : 0, upto0 = lanes_upto(mine0);
+    SeqUnits seq0{};
+    if (lane < a.B) seq0 = seq_units(a, lane);
+    const unsigned mine0 = units_of(a, seq0), upto0 = lanes_upto(mine0);
     unsigned units = last_lane(upto0);
-    for (int base = 64; base < a.B; base += 64) units += last_lane(lanes_upto(base + lane < a.B ? units_of(a, base + lane) : 0));
+    for (int base = 64; base < a.B; base += 64) units += last_lane(lanes_upto(base + lane < a.B ? units_of(a, seq_units(a, base + lane)) : 0));
     const Shares shares = shares_of(units, plan.workers);
     if (blockIdx.x >= shares.workers) return;
     unsigned u = shares.first(blockIdx.x);
@@ -124,26 +133,31 @@ __global__ __launch_bounds__(256, cached_waves(NK)) void attend_cached(AttnArgs 
         // the sequence and item of unit u
         int b = -1;
         unsigned at = u;
+        SeqUnits s{};
         for (int base = 0; base < a.B; base += 64) {
+            SeqUnits seq = seq0;
             unsigned mine = mine0, upto = upto0;
             if (base > 0) {
-                mine = base + lane < a.B ? units_of(a, base + lane) : 0;
+                seq = SeqUnits{};
+                if (base + lane < a.B) seq = seq_units(a, base + lane);
+                mine = units_of(a, seq);
                 upto = lanes_upto(mine);
             }
             const unsigned long long behind = __ballot(upto > at);
             if (behind) {
-                const int l = __ffsll(behind) - 1;
-                at -= (unsigned)__builtin_amdgcn_readlane((int)(upto - mine), l);
-                b = base + l;
+                s = seq.of_lane(__ffsll(behind) - 1);
+                at -= (unsigned)__builtin_amdgcn_readlane((int)(upto - mine), __ffsll(behind) - 1);
+                b = base + __ffsll(behind) - 1;
                 break;
             }
             at -= last_lane(upto);
         }
         if (b < 0) return;
-        const SeqUnits s = seq_units(a, b);
-        const unsigned item = at / (unsigned)s.groups;
-        const int g0 = (int)(at - item * (unsigned)s.groups);
-        const int g1 = (int)min((unsigned)s.groups, g0 + (u_end - u));
+        const unsigned length = (unsigned)s.groups + ITEM_UNITS, item = at / length;
+        const unsigned v0 = at - item * length, v1 = min(length, v0 + (u_end - u));
+        u += v1 - v0;
+        const int g0 = (int)max(v0, ITEM_UNITS) - (int)ITEM_UNITS, g1 = (int)max(v1, ITEM_UNITS) - (int)ITEM_UNITS;
+        if (g0 == g1) continue;
         const int hk = (int)(item / (unsigned)s.row_tiles), r0 = (int)(item - hk * s.row_tiles) * 16;
         const int rows = s.n_q * a.G;
         const int row = min(r0 + r16, rows - 1), token = row / a.G, head = hk * a.G + row - token * a.G;
@@ -361,7 +375,6 @@ __global__ __launch_bounds__(256, cached_waves(NK)) void attend_cached(AttnArgs 
                 }
             }
         }
-        u += g1 - g0;
     }
 }
 
@@ -377,15 +390,14 @@ __global__ __launch_bounds__(256) void join_parts(AttnArgs a, CachedPlan plan)
     for (int base = 0; base < a.B; base += 64) {
         SeqUnits mine{};
         if (base + lane < a.B) mine = seq_units(a, base + lane);
-        const unsigned items = (unsigned)mine.row_tiles * (unsigned)a.Hkv, its_units = items * (unsigned)mine.groups;
+        const unsigned items = (unsigned)mine.row_tiles * (unsigned)a.Hkv, its_units = units_of(a, mine);
         const unsigned upto = lanes_upto(items), units_upto = lanes_upto(its_units);
         const unsigned long long behind = __ballot(upto > item);
         if (b < 0 && behind) {
             const int l = __ffsll(behind) - 1;
-            auto from = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
-            item -= (unsigned)from((int)(upto - items));
-            u0 = units + (unsigned)from((int)(units_upto - its_units));
-            s = {from(mine.n_q), from(mine.first), from(mine.n_k), from(mine.row_tiles), from(mine.groups)};
+            item -= (unsigned)__builtin_amdgcn_readlane((int)(upto - items), l);
+            u0 = units + (unsigned)__builtin_amdgcn_readlane((int)(units_upto - its_units), l);
+            s = mine.of_lane(l);
             b = base + l;
         } else if (b < 0) {
             item -= last_lane(upto);
@@ -396,8 +408,8 @@ __global__ __launch_bounds__(256) void join_parts(AttnArgs a, CachedPlan plan)
     const int hk = (int)(item / (unsigned)s.row_tiles), r = 4 * blockIdx.y + wave, row = (int)(item - hk * s.row_tiles) * 16 + r;
     if (row >= s.n_q * a.G) return;
     const Shares shares = shares_of(units, plan.workers);
-    u0 += item * (unsigned)s.groups;
-    // the workgroups of the item's first and last unit
+    u0 += item * ((unsigned)s.groups + ITEM_UNITS) + ITEM_UNITS;
+    // the workgroups of the item's first and last group
     const int wa = (int)shares.owner(u0), wb = (int)shares.owner(u0 + s.groups - 1), n = wb - wa + 1;
     if (n == 1) return;
     const size_t stride = 16 * (size_t)(D + 2);

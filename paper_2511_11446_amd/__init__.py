@@ -8,6 +8,7 @@ library is missing or a call fails, an exception is raised.
 """
 import ctypes
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libdiffpro_qlinear.so")
@@ -130,13 +131,13 @@ def lib():
     i32 = ctypes.c_int32
     L.attention_f16_workspace_bytes.restype = _sz
     L.attention_f16_workspace_bytes.argtypes = [_i64, _i64, i32, i32, i32, i32]
-    L.attention_f16.argtypes = [ctypes.POINTER(ql_attention), _vp, _i64, _i64, _vp, _i64, _i64, _i64, _vp, _vp, _sz, _vp]
+    L.attention_f16.argtypes = [_vp, _vp, _i64, _i64, _vp, _i64, _i64, _i64, _vp, _vp, _sz, _vp]
     L.attention_f16.restype = _int
-    L.daq_kv_append.argtypes = [ctypes.POINTER(ql_kv_cache), ctypes.POINTER(ql_kv_new), _vp]
+    L.daq_kv_append.argtypes = [_vp, _vp, _vp]
     L.daq_kv_append.restype = _int
     L.attention_kv8_workspace_bytes.restype = _sz
     L.attention_kv8_workspace_bytes.argtypes = [_i64, i32, i32, i32, i32]
-    L.attention_kv8.argtypes = [ctypes.POINTER(ql_attention), ctypes.POINTER(ql_kv_cache), _vp, _sz, _vp]
+    L.attention_kv8.argtypes = [_vp, _vp, _vp, _sz, _vp]
     L.attention_kv8.restype = _int
     _lib = L
     return L
@@ -171,12 +172,15 @@ def _stream(stream):
 _torch = None
 
 
-def _need(t, dtype, shape=None, name="tensor"):
+def _load_torch():
     global _torch
-    if _torch is None:
-        import torch
-        _torch = torch
-    torch = _torch
+    import torch
+    _torch = torch
+    return torch
+
+
+def _need(t, dtype, shape=None, name="tensor"):
+    torch = _torch or _load_torch()
     if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous() or t.dtype != dtype:
         raise TypeError("%s must be a contiguous CUDA tensor of %s" % (name, dtype))
     if shape is not None and tuple(t.shape) != tuple(shape):
@@ -533,19 +537,29 @@ class ql_kv_new(ctypes.Structure):
                 ("q_out", _vp), ("k_out", _vp), ("v_out", _vp)]
 
 
+# The structures above as packed bytes: what a call needs of them costs a tenth of filling a ctypes object field by field (3 us)
+_ATTENTION = struct.Struct("=q5iffi3QQqqQqqQ")
+_KV_CACHE = struct.Struct("=4Qq4i2Q2i")
+_KV_NEW = struct.Struct("=q2iQ3Q6qQq2iQ3Q")
+
+
 def _heads(t, name, H=None, D=None):
     """A [T, H, D] binary16 view whose rows and heads may be strided: (pointer, row stride, head stride)."""
-    import torch
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.float16 or t.dim() != 3 or t.stride(2) != 1:
-        raise TypeError("%s must be a [T, heads, D] CUDA tensor of torch.float16 with neighbouring channels" % name)
-    if (H is not None and t.shape[1] != H) or (D is not None and t.shape[2] != D):
+    torch = _torch or _load_torch()
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not torch.float16 or t.dim() != 3:
+        raise TypeError("%s must be a [T, heads, D] CUDA tensor of torch.float16" % name)
+    n, heads, d = t.shape
+    row, head, one = t.stride()
+    if one != 1:
+        raise TypeError("%s must have its channels next to each other" % name)
+    if (H is not None and heads != H) or (D is not None and d != D):
         raise ValueError("%s has shape %s, expected [T, %s, %s]" % (name, tuple(t.shape), H, D))
     # the stride of a single row or head means nothing
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0
+    return t.data_ptr(), row if n > 1 else 0, head if heads > 1 else 0
 
 
 def _attention_form(q, B, Hkv, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax):
-    import torch
+    torch = _torch or _load_torch()
     qp, q_row, q_head = _heads(q, "q")
     T, Hq, D = q.shape
     if o is None:
@@ -553,13 +567,16 @@ def _attention_form(q, B, Hkv, cu_q, mask, prefix, scale, cap, slopes, o, row_ab
     op, o_row, o_head = _heads(o, "o", Hq, D)
     if o.shape[0] != T:
         raise ValueError("o has %d rows, expected %d" % (o.shape[0], T))
-    for name, t, dtype, n in (("cu_q", cu_q, torch.int32, B + 1), ("prefix", prefix, torch.int32, B), ("slopes", slopes, torch.float32, Hq),
-                              ("row_absmax", row_absmax, torch.int32, T)):
-        if t is not None:
-            _need(t, dtype, (n,), name)
-    a = ql_attention(T, B, Hq, Hkv, D, mask, D ** -0.5 if scale is None else scale, cap, 0, _ptr(prefix), _ptr(slopes), _ptr(cu_q), qp, q_row, q_head,
-                     op, o_row, o_head, _ptr(row_absmax))
-    return a, o
+    cu = pre = sl = am = 0
+    if cu_q is not None:
+        cu = _need(cu_q, torch.int32, (B + 1,), "cu_q").data_ptr()
+    if prefix is not None:
+        pre = _need(prefix, torch.int32, (B,), "prefix").data_ptr()
+    if slopes is not None:
+        sl = _need(slopes, torch.float32, (Hq,), "slopes").data_ptr()
+    if row_absmax is not None:
+        am = _need(row_absmax, torch.int32, (T,), "row_absmax").data_ptr()
+    return _ATTENTION.pack(T, B, Hq, Hkv, D, mask, D ** -0.5 if scale is None else scale, cap, 0, pre, sl, cu, qp, q_row, q_head, op, o_row, o_head, am), o
 
 
 def attention_f16_workspace_bytes(T_q, T_k, B, Hq, Hkv, D):
@@ -572,7 +589,6 @@ def attention_f16(q, k, v, batch=None, cu_q=None, cu_k=None, mask=MASK_NONE, pre
     layer's output) -> o fp16 [T_q, Hq, D].  Sequences one behind the other: `batch` of equal length, or int32 [B+1] first rows in cu_q / cu_k.
     scale: default D ** -0.5; cap: tanh cap of the scores (0: none); slopes fp32 [Hq]: bias by distance; mask MASK_NONE / _CAUSAL / _PREFIX
     (prefix int32 [B]); row_absmax: int32 [T_q] that receives every row's largest |o| as a binary16 bit pattern, for daq_quantize_rowmax."""
-    import torch
     kp, k_row, k_head = _heads(k, "k")
     T_k, Hkv, D = k.shape
     vp, v_row, v_head = _heads(v, "v", Hkv, D)
@@ -580,11 +596,11 @@ def attention_f16(q, k, v, batch=None, cu_q=None, cu_k=None, mask=MASK_NONE, pre
         raise ValueError("k has shape %s, v %s and q %s" % (tuple(k.shape), tuple(v.shape), tuple(q.shape)))
     B = batch if batch is not None else cu_q.shape[0] - 1 if cu_q is not None else cu_k.shape[0] - 1 if cu_k is not None else 1
     if cu_k is not None:
-        _need(cu_k, torch.int32, (B + 1,), "cu_k")
+        _need(cu_k, _torch.int32, (B + 1,), "cu_k")
     a, o = _attention_form(q, B, Hkv, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax)
     if ws is None:
-        ws = workspace(attention_f16_workspace_bytes(a.T_q, T_k, B, a.Hq, Hkv, D), q.device)
-    _check(lib().attention_f16(ctypes.byref(a), kp, k_row, k_head, vp, v_row, v_head, T_k, _ptr(cu_k), _ptr(ws), ws.numel(), _stream(stream)),
+        ws = workspace(attention_f16_workspace_bytes(q.shape[0], T_k, B, q.shape[1], Hkv, D), q.device)
+    _check(lib().attention_f16(a, kp, k_row, k_head, vp, v_row, v_head, T_k, _ptr(cu_k), _ptr(ws), ws.numel(), _stream(stream)),
            "attention_f16")
     return o
 
@@ -604,6 +620,7 @@ class KvCache8:
             raise ValueError("k_scale has shape %s, expected [%d, %d, page / scale_tokens]" % (tuple(k_scale.shape), P, H))
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.num_pages, self.heads, self.page, self.D, self.scale_tokens = P, H, page, D, page // k_scale.shape[2]
+        self._fields = (k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), P, page, self.scale_tokens, H, D)
 
     @classmethod
     def empty(cls, num_pages, heads, D, page=64, scale_tokens=64, device="cuda"):
@@ -615,12 +632,11 @@ class KvCache8:
                    torch.zeros(scales, dtype=torch.float32, **z), torch.zeros(scales, dtype=torch.float32, **z))
 
     def desc(self, page_table, len_k):
-        import torch
-        _need(page_table, torch.int32, name="page_table")
-        B, max_pages = page_table.shape
+        """The header's ql_kv_cache for these pages and lengths, as bytes, and the number of sequences."""
+        torch = _torch or _load_torch()
+        B, max_pages = _need(page_table, torch.int32, name="page_table").shape
         _need(len_k, torch.int32, (B,), "len_k")
-        return ql_kv_cache(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(), self.num_pages, self.page,
-                           self.scale_tokens, self.heads, self.D, page_table.data_ptr(), len_k.data_ptr(), B, max_pages)
+        return _KV_CACHE.pack(*self._fields, page_table.data_ptr(), len_k.data_ptr(), B, max_pages), B
 
 
 def daq_kv_append(cache, k, v, page_table, len_k, cu=None, q=None, rot=None, rot_pairs=False, pos=None, q_out=None, k_out=None, v_out=None,
@@ -629,37 +645,36 @@ def daq_kv_append(cache, k, v, page_table, len_k, cu=None, q=None, rot=None, rot
     (int32 [T]; default: the token's place in its sequence).  len_k int32 [B] counts the new tokens; cu int32 [B+1]: first new row of each sequence
     (default: T / B each).  q_out fp16 [T, Hq, D]: the rotated q (made where q is given); k_out, v_out fp16 [T, Hkv, D]: what the cache now holds.
     Returns q_out."""
-    import torch
-    c = cache.desc(page_table, len_k)
-    T = k.shape[0]
+    torch = _torch or _load_torch()
+    c, B = cache.desc(page_table, len_k)
     kp, k_row, k_head = _heads(k, "k", cache.heads, cache.D)
     vp, v_row, v_head = _heads(v, "v", cache.heads, cache.D)
+    T = k.shape[0]
     if v.shape[0] != T:
         raise ValueError("k has %d rows and v %d" % (T, v.shape[0]))
-    Hq, qp, q_row, q_head = 0, None, 0, 0
+    Hq = qp = q_row = q_head = qo = ko = vo = 0
     if q is not None:
+        qp, q_row, q_head = _heads(q, "q", None, cache.D)
         Hq = q.shape[1]
-        qp, q_row, q_head = _heads(q, "q", Hq, cache.D)
         if q.shape[0] != T:
             raise ValueError("q has %d rows and k %d" % (q.shape[0], T))
         if q_out is None:
             q_out = torch.empty((T, Hq, cache.D), dtype=torch.float16, device=q.device)
-        _need(q_out, torch.float16, (T, Hq, cache.D), "q_out")
-    for name, t in (("k_out", k_out), ("v_out", v_out)):
-        if t is not None:
-            _need(t, torch.float16, (T, cache.heads, cache.D), name)
-    for name, t, n in (("cu", cu, c.B + 1), ("pos", pos, T)):
-        if t is not None:
-            _need(t, torch.int32, (n,), name)
-    rows = half = 0
+        qo = _need(q_out, torch.float16, (T, Hq, cache.D), "q_out").data_ptr()
+    if k_out is not None:
+        ko = _need(k_out, torch.float16, (T, cache.heads, cache.D), "k_out").data_ptr()
+    if v_out is not None:
+        vo = _need(v_out, torch.float16, (T, cache.heads, cache.D), "v_out").data_ptr()
+    cup = 0 if cu is None else _need(cu, torch.int32, (B + 1,), "cu").data_ptr()
+    pp = 0 if pos is None else _need(pos, torch.int32, (T,), "pos").data_ptr()
+    rp = rows = half = 0
     if rot is not None:
-        _need(rot, torch.float32, name="rot")
+        rp = _need(rot, torch.float32, name="rot").data_ptr()
         rows, half, two = rot.shape
         if two != 2:
             raise ValueError("rot must be [rows, rot_dim / 2, 2]")
-    n = ql_kv_new(T, Hq, 1 if rot_pairs else 0, _ptr(cu), qp, kp, vp, q_row, q_head, k_row, k_head, v_row, v_head, _ptr(rot), rows, 2 * half, 0,
-                  _ptr(pos), _ptr(q_out) if q is not None else None, _ptr(k_out), _ptr(v_out))
-    _check(lib().daq_kv_append(ctypes.byref(c), ctypes.byref(n), _stream(stream)), "daq_kv_append")
+    n = _KV_NEW.pack(T, Hq, 1 if rot_pairs else 0, cup, qp, kp, vp, q_row, q_head, k_row, k_head, v_row, v_head, rp, rows, 2 * half, 0, pp, qo, ko, vo)
+    _check(lib().daq_kv_append(c, n, _stream(stream)), "daq_kv_append")
     return q_out
 
 
@@ -670,12 +685,13 @@ def attention_kv8_workspace_bytes(T_q, B, Hq, Hkv, D):
 def attention_kv8(q, cache, page_table, len_k, cu_q=None, mask=MASK_CAUSAL, prefix=None, scale=None, cap=0.0, slopes=None, o=None,
                   row_absmax=None, ws=None, stream=None):
     """attention_f16 over the 8-bit cache: q fp16 [T_q, Hq, D], page_table int32 [B, max_pages], len_k int32 [B] -> o fp16 [T_q, Hq, D]."""
-    c = cache.desc(page_table, len_k)
-    _heads(q, "q", None, cache.D)
-    a, o = _attention_form(q, c.B, cache.heads, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax)
+    c, B = cache.desc(page_table, len_k)
+    a, o = _attention_form(q, B, cache.heads, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax)
+    if q.shape[2] != cache.D:
+        raise ValueError("q has heads of %d, the cache of %d" % (q.shape[2], cache.D))
     if ws is None:
-        ws = workspace(attention_kv8_workspace_bytes(a.T_q, c.B, a.Hq, cache.heads, cache.D), q.device)
-    _check(lib().attention_kv8(ctypes.byref(a), ctypes.byref(c), _ptr(ws), ws.numel(), _stream(stream)), "attention_kv8")
+        ws = workspace(attention_kv8_workspace_bytes(q.shape[0], B, q.shape[1], cache.heads, cache.D), q.device)
+    _check(lib().attention_kv8(a, c, _ptr(ws), ws.numel(), _stream(stream)), "attention_kv8")
     return o
 
 

@@ -7,7 +7,8 @@
 //
 // One workgroup per sequence, touched group of 64 tokens and key head: it alone writes that group's codes and scales, so nothing is
 // atomic in global memory and results do not depend on order.  Keys and values are read once and held in registers between the
-// maximum and the codes.  A thread has an 8-channel piece of four neighbouring tokens, whose value codes are one word of the cache.
+// maximum and the codes.  Of the values a thread has an 8-channel piece of four neighbouring tokens, whose codes are one word of the cache;
+// of the keys what a few cosines turn, which it then uses for the queries of all heads that read the key head.
 #include "attention.h"
 #include "daq_device.h"
 
@@ -15,39 +16,52 @@ namespace ql {
 
 typedef _Float16 h8v __attribute__((ext_vector_type(8)));
 
-// piece p (8 channels) of the turned row at x; `angle` is the row's cos / sin table row
-__device__ __forceinline__ uint4 turned_piece(const _Float16 *x, int p, const float *angle, int rot_dim, bool pairs)
+// A row is turned by units: two 8-channel pieces that 8 neighbouring (cos, sin) of the table turn - pieces e and e + rot_dim / 16, or the neighbours
+// 2 e and 2 e + 1 - and single pieces behind the turned channels, as they are.
+struct Turn {
+    float4 t[4];   // cos, sin, cos, sin
+};
+struct Pieces {
+    uint4 a, b;
+};
+__device__ __forceinline__ Turn load_turn(const float *angle, int e)
 {
-    const uint4 own = *reinterpret_cast<const uint4 *>(x + 8 * p);
-    if (8 * p >= rot_dim) return own;
-    const h8v a = __builtin_bit_cast(h8v, own);
-    h8v out;
-    if (pairs) {
-        const float4 t0 = *reinterpret_cast<const float4 *>(angle + 8 * p), t1 = *reinterpret_cast<const float4 *>(angle + 8 * p + 4);
-        const float c[4] = {t0.x, t0.z, t1.x, t1.z}, s[4] = {t0.y, t0.w, t1.y, t1.w};
+    Turn r;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float u = (float)a[2 * i] * c[i] - (float)a[2 * i + 1] * s[i], v = (float)a[2 * i + 1] * c[i] + (float)a[2 * i] * s[i];
+    for (int i = 0; i < 4; ++i) r.t[i] = *reinterpret_cast<const float4 *>(angle + 16 * e + 4 * i);
+    return r;
+}
+__device__ __forceinline__ Pieces turned(const Pieces &x, const Turn &r, bool pairs)
+{
+    const h8v a = __builtin_bit_cast(h8v, x.a), b = __builtin_bit_cast(h8v, x.b);
+    h8v p, q;
+    if (pairs) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float c = i % 2 ? r.t[i / 2].z : r.t[i / 2].x, s = i % 2 ? r.t[i / 2].w : r.t[i / 2].y;
+            const int at = 2 * (i % 4);
+            const float u0 = i < 4 ? (float)a[at] : (float)b[at], v0 = i < 4 ? (float)a[at + 1] : (float)b[at + 1];
+            float u = u0 * c - v0 * s, v = v0 * c + u0 * s;
             asm volatile("" : "+v"(u), "+v"(v));   // keep the fp32 rounding before the fp16 one
-            out[2 * i] = (_Float16)u;
-            out[2 * i + 1] = (_Float16)v;
+            if (i < 4) {
+                p[at] = (_Float16)u;
+                p[at + 1] = (_Float16)v;
+            } else {
+                q[at] = (_Float16)u;
+                q[at + 1] = (_Float16)v;
+            }
         }
     } else {
-        const int half = rot_dim / 16;             // in pieces
-        const bool low = p < half;
-        const int first = low ? p : p - half;
-        const h8v b = *reinterpret_cast<const h8v *>(x + 8 * (low ? p + half : p - half));
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            const float4 t = *reinterpret_cast<const float4 *>(angle + 2 * (8 * first + i));   // cos, sin of two channels
-            const float s0 = low ? -t.y : t.y, s1 = low ? -t.w : t.w;
-            float u = (float)a[i] * t.x + (float)b[i] * s0, v = (float)a[i + 1] * t.z + (float)b[i + 1] * s1;
+        for (int i = 0; i < 8; ++i) {
+            const float c = i % 2 ? r.t[i / 2].z : r.t[i / 2].x, s = i % 2 ? r.t[i / 2].w : r.t[i / 2].y;
+            float u = (float)a[i] * c - (float)b[i] * s, v = (float)b[i] * c + (float)a[i] * s;
             asm volatile("" : "+v"(u), "+v"(v));
-            out[i] = (_Float16)u;
-            out[i + 1] = (_Float16)v;
+            p[i] = (_Float16)u;
+            q[i] = (_Float16)v;
         }
     }
-    return __builtin_bit_cast(uint4, out);
+    return {__builtin_bit_cast(uint4, p), __builtin_bit_cast(uint4, q)};
 }
 
 __device__ __forceinline__ unsigned piece_absmax(uint4 v)
@@ -95,7 +109,18 @@ __device__ __forceinline__ NewTokens new_tokens(const KvAppendArgs &a, int b)
 
 constexpr int VT_PITCH = KV_GROUP + 4;
 
-template <int NI>   // pieces of four tokens per thread
+// an LDS maximum per block: lanes of one block first among themselves where that is the whole wavefront
+__device__ __forceinline__ void block_max(unsigned *of_block, int t, int S, unsigned m, bool live)
+{
+    if (S == KV_GROUP) {
+        m = wave_max_u32(live ? m : 0u);
+        if ((threadIdx.x & 63) == 0) atomicMax(of_block, m);
+    } else if (live) {
+        atomicMax(of_block + t / S, m);
+    }
+}
+
+template <int NI>   // 128-channel parts of a head: a thread has NI pieces of four tokens (values) and up to 4 NI units of a token (keys)
 __global__ __launch_bounds__(256) void kv_append(KvAppendArgs a)
 {
     __shared__ unsigned amax_k[KV_GROUP], amax_v[KV_GROUP];
@@ -103,34 +128,12 @@ __global__ __launch_bounds__(256) void kv_append(KvAppendArgs a)
     __shared__ float was_k, was_v;
     extern __shared__ __align__(16) unsigned char vt[];   // [D][VT_PITCH] value codes of the group
 
-    const int tid = threadIdx.x, lane = tid & 63;
+    const int tid = threadIdx.x;
     const int hk = blockIdx.x % a.Hkv;
     int item = blockIdx.x / a.Hkv;
-    // the sequence and group of this workgroup: 64 sequences at a time, one per lane
-    int b = -1;
-    NewTokens nt{};
-    for (int base = 0; base < a.B; base += 64) {
-        NewTokens mine{};
-        if (base + lane < a.B) mine = new_tokens(a, base + lane);
-        int upto = mine.groups;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(upto, d, 64);
-            if (lane >= d) upto += o;
-        }
-        const unsigned long long behind = __ballot(upto > item);
-        if (behind) {
-            const int l = __ffsll((unsigned long long)behind) - 1;
-            b = base + l;
-            nt.row = __shfl(mine.row, l, 64);
-            nt.first = __shfl(mine.first, l, 64);
-            nt.n = __shfl(mine.n, l, 64);
-            item -= __shfl(upto - mine.groups, l, 64);
-            break;
-        }
-        item -= __shfl(upto, 63, 64);
-    }
+    const int b = find_sequence(a.B, item, [&](int s) { return new_tokens(a, s).groups; });
     if (b < 0) return;
+    const NewTokens nt = new_tokens(a, b);
     const int group = nt.first / KV_GROUP + item;
     // places in the group: new tokens are [tlo, thi); earlier ones of the sequence lie in front
     const int base = group * KV_GROUP;
@@ -151,31 +154,79 @@ __global__ __launch_bounds__(256) void kv_append(KvAppendArgs a)
         amax_v[tid] = 0;
     }
     __syncthreads();
-    const int P8 = a.D / 8;
+    const int P8 = a.D / 8, R16 = a.rot ? a.rot_dim / 16 : 0, units = P8 - R16;   // of a row: R16 turned ones, then single pieces
+    const int count = (thi - tlo) * units;                // units of the new tokens, token by token
     const _Float16 *k = static_cast<const _Float16 *>(a.k) + hk * a.k_head, *v = static_cast<const _Float16 *>(a.v) + hk * a.v_head;
     auto angle_of = [&](int t) {
         const int p = min(max(a.pos ? a.pos[row0 + t] : base + t, 0), a.rot_rows - 1);
         return a.rot + (size_t)p * a.rot_dim;
     };
-    uint4 kp[NI][4], vp[NI][4];
+    auto first_piece = [&](int e) { return e >= R16 ? e + R16 : a.rot_pairs ? 2 * e : e; };
+    const int second = a.rot_pairs ? 1 : R16;             // from a turned unit's first piece to its second
+    auto load = [&](const _Float16 *x, int e) {
+        const int p = first_piece(e);
+        Pieces r;
+        r.a = *reinterpret_cast<const uint4 *>(x + 8 * p);
+        r.b = make_uint4(0, 0, 0, 0);
+        if (e < R16) r.b = *reinterpret_cast<const uint4 *>(x + 8 * (p + second));
+        return r;
+    };
+    // values: four tokens of a piece, whose codes are one word of the cache
+    uint4 vp[NI][4];
 #pragma unroll
     for (int n = 0; n < NI; ++n) {
-        const int id = tid + 256 * n, piece = id % P8, quad = id / P8;
+        const int id = tid + 256 * n, quad = id / P8, piece = id - quad * P8;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = 4 * quad + i;
-            kp[n][i] = vp[n][i] = make_uint4(0, 0, 0, 0);
-            if (t < tlo || t >= thi) continue;
-            const _Float16 *kr = k + (row0 + t) * a.k_row;
-            kp[n][i] = a.rot ? turned_piece(kr, piece, angle_of(t), a.rot_dim, a.rot_pairs) : *reinterpret_cast<const uint4 *>(kr + 8 * piece);
-            vp[n][i] = *reinterpret_cast<const uint4 *>(v + (row0 + t) * a.v_row + 8 * piece);
+            vp[n][i] = make_uint4(0, 0, 0, 0);
+            if (t >= tlo && t < thi) vp[n][i] = *reinterpret_cast<const uint4 *>(v + (row0 + t) * a.v_row + 8 * piece);
         }
+    }
+    // keys, turned; with the same cosines the queries of the heads that read this key head
+    Pieces kp[4 * NI];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int t = 4 * quad + i;
-            if (t < tlo || t >= thi) continue;
-            atomicMax(&amax_k[t / S], piece_absmax(kp[n][i]));
-            atomicMax(&amax_v[t / S], piece_absmax(vp[n][i]));
+    for (int n = 0; n < 4 * NI; ++n) {
+        const int id = tid + 256 * n, in = id / units, e = id - in * units, t = tlo + in;
+        kp[n].a = kp[n].b = make_uint4(0, 0, 0, 0);
+        const bool live = id < count;
+        if (live) {
+            kp[n] = load(k + (row0 + t) * a.k_row, e);
+            Turn r{};
+            if (e < R16) {
+                r = load_turn(angle_of(t), e);
+                kp[n] = turned(kp[n], r, a.rot_pairs);
+            }
+            if (a.q_out) {
+                const _Float16 *q = static_cast<const _Float16 *>(a.q) + (row0 + t) * a.q_row + hk * a.G * a.q_head;
+                _Float16 *out = static_cast<_Float16 *>(a.q_out) + ((size_t)(row0 + t) * a.Hq + hk * a.G) * a.D + 8 * first_piece(e);
+                for (int h0 = 0; h0 < a.G; h0 += 4) {
+                    Pieces x[4];
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) x[h] = load(q + min(h0 + h, a.G - 1) * a.q_head, e);
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        if (h0 + h >= a.G) break;
+                        const Pieces y = e < R16 ? turned(x[h], r, a.rot_pairs) : x[h];
+                        *reinterpret_cast<uint4 *>(out + (h0 + h) * a.D) = y.a;
+                        if (e < R16) *reinterpret_cast<uint4 *>(out + (h0 + h) * a.D + 8 * second) = y.b;
+                    }
+                }
+            }
+        }
+        if (256 * n < count) block_max(amax_k, t, S, max(piece_absmax(kp[n].a), piece_absmax(kp[n].b)), live);
+    }
+#pragma unroll
+    for (int n = 0; n < NI; ++n) {
+        const int quad = (tid + 256 * n) / P8;
+        if (S == KV_GROUP) {
+            unsigned m = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) m = max(m, piece_absmax(vp[n][i]));
+            block_max(amax_v, 0, S, m, true);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) block_max(amax_v, 4 * quad + i, S, piece_absmax(vp[n][i]), 4 * quad + i >= tlo && 4 * quad + i < thi);
         }
     }
     __syncthreads();
@@ -206,9 +257,40 @@ __global__ __launch_bounds__(256) void kv_append(KvAppendArgs a)
         }
         __syncthreads();
     }
+    // key codes
+#pragma unroll
+    for (int n = 0; n < 4 * NI; ++n) {
+        const int id = tid + 256 * n, in = id / units, e = id - in * units, t = tlo + in;
+        if (id >= count) break;
+        const float alpha = alpha_k[t / S] > 0.0f ? alpha_k[t / S] : 1.0f, rcp = 1.0f / alpha;
+        const int p = first_piece(e);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (i && e >= R16) break;
+            const int c = 8 * (p + i * second);
+            const uint2 code = daq_piece(i ? kp[n].b : kp[n].a, alpha, rcp);
+            if (held) *reinterpret_cast<uint2 *>(kc + (size_t)t * a.D + c) = code;
+            if (a.k_out) *reinterpret_cast<uint4 *>(static_cast<_Float16 *>(a.k_out) + ((size_t)(row0 + t) * a.Hkv + hk) * a.D + c) = code_values(code, alpha);
+        }
+    }
+    if (again_k) {
+        const int t0 = shared_block * S;                  // earlier tokens [t0, tlo) of the block
+        for (int id = tid; id < (tlo - t0) * P8; id += 256) {
+            uint2 *at = reinterpret_cast<uint2 *>(kc + (size_t)t0 * a.D) + id;
+            const uint2 w = *at;
+            uint2 o = make_uint2(0, 0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                o.x |= code_again(w.x, e, was_k, alpha_k[shared_block]) << (8 * e);
+                o.y |= code_again(w.y, e, was_k, alpha_k[shared_block]) << (8 * e);
+            }
+            *at = o;
+        }
+    }
+    // value codes
 #pragma unroll
     for (int n = 0; n < NI; ++n) {
-        const int id = tid + 256 * n, piece = id % P8, quad = id / P8;
+        const int id = tid + 256 * n, quad = id / P8, piece = id - quad * P8;
         if (quad >= 16) continue;
         uint2 vcode[4];
         unsigned fresh = 0;                                 // bytes of the word that are new
@@ -216,28 +298,13 @@ __global__ __launch_bounds__(256) void kv_append(KvAppendArgs a)
         for (int i = 0; i < 4; ++i) {
             const int t = 4 * quad + i;
             vcode[i] = make_uint2(0, 0);
-            if (t >= tlo && t < thi) {
-                fresh |= 0xffu << (8 * i);
-                const float ak = alpha_k[t / S] > 0.0f ? alpha_k[t / S] : 1.0f, av = alpha_v[t / S] > 0.0f ? alpha_v[t / S] : 1.0f;
-                const uint2 kcode = daq_piece(kp[n][i], ak, 1.0f / ak);
-                vcode[i] = daq_piece(vp[n][i], av, 1.0f / av);
-                if (held) *reinterpret_cast<uint2 *>(kc + (size_t)t * a.D + 8 * piece) = kcode;
-                const size_t out = ((size_t)(row0 + t) * a.Hkv + hk) * a.D + 8 * piece;
-                if (a.k_out) *reinterpret_cast<uint4 *>(static_cast<_Float16 *>(a.k_out) + out) = code_values(kcode, ak);
-                if (a.v_out) *reinterpret_cast<uint4 *>(static_cast<_Float16 *>(a.v_out) + out) = code_values(vcode[i], av);
-            } else if (again_k && t < tlo && t / S == shared_block) {
-                uint2 *at = reinterpret_cast<uint2 *>(kc + (size_t)t * a.D + 8 * piece);
-                const uint2 w = *at;
-                uint2 o = make_uint2(0, 0);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    o.x |= code_again(w.x, e, was_k, alpha_k[shared_block]) << (8 * e);
-                    o.y |= code_again(w.y, e, was_k, alpha_k[shared_block]) << (8 * e);
-                }
-                *at = o;
-            }
+            if (t < tlo || t >= thi) continue;
+            fresh |= 0xffu << (8 * i);
+            const float alpha = alpha_v[t / S] > 0.0f ? alpha_v[t / S] : 1.0f;
+            vcode[i] = daq_piece(vp[n][i], alpha, 1.0f / alpha);
+            if (a.v_out) *reinterpret_cast<uint4 *>(static_cast<_Float16 *>(a.v_out) + ((size_t)(row0 + t) * a.Hkv + hk) * a.D + 8 * piece) = code_values(vcode[i], alpha);
         }
-        if (!held) continue;
+        if (!held || (!whole && fresh == 0)) continue;
         const int at = 16 * (quad % 4) + 4 * (quad / 4);    // of the quad's word among the 64 bytes of a channel
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -275,15 +342,6 @@ __global__ __launch_bounds__(256) void kv_append(KvAppendArgs a)
             const unsigned *from = reinterpret_cast<const unsigned *>(vt + (c / 4) * VT_PITCH + (c % 4) * 16);
             *reinterpret_cast<uint4 *>(vc + c * 16) = make_uint4(from[0], from[1], from[2], from[3]);
         }
-    }
-    // the query heads that read this key head
-    if (!a.q_out) return;
-    const int pieces = (thi - tlo) * a.G * P8;
-    for (int c = tid; c < pieces; c += 256) {
-        const int piece = c % P8, h = hk * a.G + c / P8 % a.G, t = tlo + c / (P8 * a.G);
-        const _Float16 *qr = static_cast<const _Float16 *>(a.q) + (row0 + t) * a.q_row + h * a.q_head;
-        const uint4 o = a.rot ? turned_piece(qr, piece, angle_of(t), a.rot_dim, a.rot_pairs) : *reinterpret_cast<const uint4 *>(qr + 8 * piece);
-        *reinterpret_cast<uint4 *>(static_cast<_Float16 *>(a.q_out) + ((size_t)(row0 + t) * a.Hq + h) * a.D + 8 * piece) = o;
     }
 }
 

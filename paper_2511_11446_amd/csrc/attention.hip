@@ -12,7 +12,7 @@ __global__ __launch_bounds__(64 * NW, CHP <= 16 ? 2 : 1) void attend_tiles(AttnA
     attend_tile<CHP, NW, false, SHAPED>(a, plan);
 }
 
-__global__ __launch_bounds__(256) void join_tiles(AttnArgs a, TilePlan plan, int rows_per) { join_splits(a, plan, rows_per); }
+__global__ __launch_bounds__(JOIN_THREADS) void join_tiles(AttnArgs a, TilePlan plan, int rows_per) { join_splits(a, plan, rows_per); }
 
 namespace {
 constexpr int CUS = 256;
@@ -29,7 +29,7 @@ template <int CHP, int NW>
 hipError_t launch_tiles(const AttnArgs &a, hipStream_t stream)
 {
     using T = AttnTile<CHP, NW, false>;
-    const TilePlan p = tile_plan(a.Tq, a.B, a.G, a.Hkv, T::ROWS, a.cu_q, a.mask, a.Tk / a.B, CUS);
+    const TilePlan p = tile_plan(a.Tq, a.B, a.G, a.Hkv, T::ROWS, a.cu_q, a.mask, a.Tk / a.B, CUS, 2 * CUS);
     static const hipError_t opt_in[2] = {
         hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_tiles<CHP, NW, false>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES),
         hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_tiles<CHP, NW, true>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES)};
@@ -42,7 +42,7 @@ hipError_t launch_tiles(const AttnArgs &a, hipStream_t stream)
     else hipLaunchKernelGGL((attend_tiles<CHP, NW, false>), grid, dim3(T::NT), T::LDS_BYTES, stream, a, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
-    hipLaunchKernelGGL(join_tiles, dim3((unsigned)(p.tiles * a.Hkv), T::ROWS / 4), dim3(256), 0, stream, a, p, T::ROWS);
+    hipLaunchKernelGGL(join_tiles, dim3((unsigned)(p.tiles * a.Hkv), join_blocks(T::ROWS, a.D)), dim3(JOIN_THREADS), 0, stream, a, p, T::ROWS);
     return hipGetLastError();
 }
 
@@ -84,7 +84,7 @@ hipError_t launch_by_head(const AttnArgs &a, int rows, hipStream_t stream)
 size_t tiles_partial_bytes(long long Tq, long long Tk, int B, int Hq, int Hkv, int D)
 {
     const int rows = tile_rows(Tq, B, Hq / Hkv, Hkv, D);
-    const TilePlan p = tile_plan(Tq, B, Hq / Hkv, Hkv, rows, true, 0, Tk / B, CUS);
+    const TilePlan p = tile_plan(Tq, B, Hq / Hkv, Hkv, rows, true, 0, Tk / B, CUS, 2 * CUS);
     return p.splits == 1 ? 0 : (size_t)p.tiles * Hkv * p.splits * rows * (D + 2) * 4;
 }
 

@@ -16,17 +16,17 @@ __global__ __launch_bounds__(64 * chunk_waves(CHP), CHP <= 16 ? 2 : 1) void atte
     attend_tile<CHP, chunk_waves(CHP), true, SHAPED>(a, plan);
 }
 
-__global__ __launch_bounds__(256) void join_chunks(AttnArgs a, TilePlan plan, int rows_per) { join_splits(a, plan, rows_per); }
+__global__ __launch_bounds__(JOIN_THREADS) void join_chunks(AttnArgs a, TilePlan plan, int rows_per) { join_splits(a, plan, rows_per); }
 
 namespace {
-constexpr int CUS = 256;
+constexpr int CUS = 256, WANTED = 768;
 constexpr int chunk_rows(int D) { return 32 * chunk_waves(D / 8); }
 
 template <int CHP>
 hipError_t launch_chunks(const AttnArgs &a, hipStream_t stream)
 {
     using T = AttnTile<CHP, chunk_waves(CHP), true>;
-    const TilePlan p = tile_plan(a.Tq, a.B, a.G, a.Hkv, T::ROWS, a.cu_q, a.mask, (long long)a.max_pages * a.page, CUS);
+    const TilePlan p = tile_plan(a.Tq, a.B, a.G, a.Hkv, T::ROWS, a.cu_q, a.mask, (long long)a.max_pages * a.page, CUS, WANTED);
     static const hipError_t opt_in[2] = {
         hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_chunks<CHP, false>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES),
         hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_chunks<CHP, true>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES)};
@@ -39,14 +39,14 @@ hipError_t launch_chunks(const AttnArgs &a, hipStream_t stream)
     else hipLaunchKernelGGL((attend_chunks<CHP, false>), grid, dim3(T::NT), T::LDS_BYTES, stream, a, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
-    hipLaunchKernelGGL(join_chunks, dim3((unsigned)(p.tiles * a.Hkv), T::ROWS / 4), dim3(256), 0, stream, a, p, T::ROWS);
+    hipLaunchKernelGGL(join_chunks, dim3((unsigned)(p.tiles * a.Hkv), join_blocks(T::ROWS, a.D)), dim3(JOIN_THREADS), 0, stream, a, p, T::ROWS);
     return hipGetLastError();
 }
 }  // namespace
 
 size_t chunks_partial_bytes(long long Tq, int B, int Hq, int Hkv, int D)
 {
-    const TilePlan p = tile_plan(Tq, B, Hq / Hkv, Hkv, chunk_rows(D), true, 0, 1LL << 31, CUS);
+    const TilePlan p = tile_plan(Tq, B, Hq / Hkv, Hkv, chunk_rows(D), true, 0, 1LL << 31, CUS, WANTED);
     return p.splits == 1 ? 0 : (size_t)p.tiles * Hkv * p.splits * chunk_rows(D) * (D + 2) * 4;
 }
 

@@ -545,10 +545,11 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
     if (a.row_absmax && wrow < rows) atomicMax(a.row_absmax + sq.first + token, amax);
 }
 
-// Adds up the parts of the row tiles, one wavefront per packed row: `rows_per` rows a tile, 4 rows a workgroup, blockIdx.y the quarter-rows of a tile
+// Adds up the parts of the row tiles: a thread has four channels of a packed row and takes four parts at a time, maxima, weights and sums requested
+// together.  blockIdx.x: row tile and key head; blockIdx.y: the tile's next JOIN_THREADS / (D / 4) rows.
+constexpr int JOIN_THREADS = 256;
 __device__ __forceinline__ void join_splits(const AttnArgs &a, const TilePlan &plan, int rows_per)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int hk = blockIdx.x % a.Hkv, flat = blockIdx.x / a.Hkv;
     int tile = flat, b;
     if (a.cu_q) {
@@ -559,49 +560,64 @@ __device__ __forceinline__ void join_splits(const AttnArgs &a, const TilePlan &p
         tile = flat % plan.per_seq;
     }
     const SeqRows sq = seq_rows(a.cu_q, b, a.Tq, a.B);
-    const int lr = 4 * blockIdx.y + wave, row = tile * rows_per + lr;
-    if (row >= sq.n * a.G) return;
+    const int fours = a.D / 4, at_once = JOIN_THREADS / fours, in = threadIdx.x / fours, ch = 4 * (threadIdx.x - in * fours);
+    const int lr = at_once * blockIdx.y + in, row = tile * rows_per + lr;
+    if (in >= at_once || lr >= rows_per || row >= sq.n * a.G) return;
     const size_t stride = (size_t)rows_per * (a.D + 2);
     const float *part = a.partial + ((size_t)flat * a.Hkv + hk) * plan.splits * stride;
-    float m = -__builtin_inff();
-    for (int s = 0; s < plan.splits; ++s) m = fmaxf(m, part[s * stride + (size_t)rows_per * a.D + lr]);
-    const int token = row / a.G, head = hk * a.G + row % a.G;
-    _Float16 *o = static_cast<_Float16 *>(a.o) + (sq.first + token) * a.o_row + head * a.o_head;
-    unsigned amax = 0;
-    for (int ch = 4 * lane; ch < a.D; ch += 256) {
-        f32x4 sum = {};
-        float weight = 0.0f;
-        if (m > -__builtin_inff())
-            for (int s = 0; s < plan.splits; ++s) {
-                const float k = exp2_fast(part[s * stride + (size_t)rows_per * a.D + lr] - m);
-                weight += k * part[s * stride + (size_t)rows_per * (a.D + 1) + lr];
-                sum += *reinterpret_cast<const f32x4 *>(part + s * stride + (size_t)lr * a.D + ch) * k;
-            }
-        const float inv = weight > 0.0f ? 1.0f / weight : 0.0f;
+    float m = -__builtin_inff(), weight = 0.0f;
+    f32x4 sum = {};
+    for (int first = 0; first < plan.splits; first += 4) {
+        float pm[4], pl[4];
+        f32x4 px[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const _Float16 h = (_Float16)(sum[e] * inv);
-            o[ch + e] = h;
-            amax = max(amax, absmax_bits(h));
+        for (int i = 0; i < 4; ++i) {
+            const float *x = part + min(first + i, plan.splits - 1) * stride;
+            pm[i] = x[(size_t)rows_per * a.D + lr];
+            pl[i] = x[(size_t)rows_per * (a.D + 1) + lr];
+            px[i] = *reinterpret_cast<const f32x4 *>(x + (size_t)lr * a.D + ch);
+        }
+        float m2 = m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (first + i < plan.splits) m2 = fmaxf(m2, pm[i]);
+        if (m2 == -__builtin_inff()) continue;
+        const float keep = exp2_fast(m - m2);
+        weight *= keep;
+        sum *= keep;
+        m = m2;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float k = first + i < plan.splits ? exp2_fast(pm[i] - m) : 0.0f;
+            weight += k * pl[i];
+            sum += px[i] * k;
         }
     }
-    if (a.row_absmax) {
+    const int token = row / a.G, head = hk * a.G + row % a.G;
+    const float inv = weight > 0.0f ? 1.0f / weight : 0.0f;
+    f16x4 o;
+    unsigned amax = 0;
 #pragma unroll
-        for (int d = 32; d; d >>= 1) amax = max(amax, (unsigned)__shfl_xor((int)amax, d, 64));
-        if (lane == 0) atomicMax(a.row_absmax + sq.first + token, amax);
+    for (int e = 0; e < 4; ++e) {
+        const _Float16 h = (_Float16)(sum[e] * inv);
+        o[e] = h;
+        amax = max(amax, absmax_bits(h));
     }
+    *reinterpret_cast<f16x4 *>(static_cast<_Float16 *>(a.o) + (sq.first + token) * a.o_row + head * a.o_head + ch) = o;
+    if (a.row_absmax) atomicMax(a.row_absmax + sq.first + token, amax);
 }
+inline unsigned join_blocks(int rows_per, int D) { return (unsigned)((rows_per + JOIN_THREADS / (D / 4) - 1) / (JOIN_THREADS / (D / 4))); }
 
 // row tiles of `rows` packed rows, and the parts that the keys are cut into so that few of them still fill the chip: enough
 // workgroups for two on every CU, no part below 4 key tiles
 constexpr int TILE_SPLITS = 16;
-inline TilePlan tile_plan(long long Tq, int B, int G, int Hkv, int rows, bool cu_q, int mask, long long keys, int least_wgs)
+inline TilePlan tile_plan(long long Tq, int B, int G, int Hkv, int rows, bool cu_q, int mask, long long keys, int least_wgs, int wanted_wgs)
 {
     TilePlan p{};
     p.per_seq = (int)((Tq / B * G + rows - 1) / rows);
     p.tiles = cu_q ? (int)(Tq * G / rows + B) : p.per_seq * B;
     const long long bound = (Tq * G / rows + B) * Hkv;   // of the workgroups, with or without cu_q
-    long long splits = bound >= least_wgs ? 1 : 2LL * least_wgs / bound;
+    long long splits = bound >= least_wgs ? 1 : wanted_wgs / bound;
     const long long most = keys / (4 * ATT_KEYS);
     splits = splits > TILE_SPLITS ? TILE_SPLITS : splits;
     splits = splits > most ? most : splits;

@@ -154,6 +154,11 @@ __global__ __launch_bounds__(256) void kv_append(KvAppendArgs a)
         amax_v[tid] = 0;
     }
     __syncthreads();
+    // scales: thread i has block i of the keys, thread 64 + i block i of the values
+    const int blk = tid % 64, shared_block = tlo / S;     // the one block that may hold earlier tokens
+    const bool earlier = held && tlo % S != 0;
+    float *scale = tid < 64 ? ks : vs;
+    const float old = earlier && tid < 128 && blk == shared_block ? scale[blk] : 0.0f;
     const int P8 = a.D / 8, R16 = a.rot ? a.rot_dim / 16 : 0, units = P8 - R16;   // of a row: R16 turned ones, then single pieces
     const int count = (thi - tlo) * units;                // units of the new tokens, token by token
     const _Float16 *k = static_cast<const _Float16 *>(a.k) + hk * a.k_head, *v = static_cast<const _Float16 *>(a.v) + hk * a.v_head;
@@ -183,7 +188,19 @@ __global__ __launch_bounds__(256) void kv_append(KvAppendArgs a)
             if (t >= tlo && t < thi) vp[n][i] = *reinterpret_cast<const uint4 *>(v + (row0 + t) * a.v_row + 8 * piece);
         }
     }
-    // keys, turned; with the same cosines the queries of the heads that read this key head
+    // queries of the heads that read this key head: with the cosines of the keys below, or, where there are few, a thread each
+    const bool few = count * a.G <= 256;
+    const _Float16 *q0 = static_cast<const _Float16 *>(a.q) + hk * a.G * a.q_head;
+    _Float16 *q_out = static_cast<_Float16 *>(a.q_out) + hk * a.G * a.D;
+    if (a.q_out && few && tid < count * a.G) {
+        const int h = tid / count, id = tid - h * count, in = id / units, e = id - in * units, t = tlo + in;
+        Pieces x = load(q0 + (row0 + t) * a.q_row + h * a.q_head, e);
+        if (e < R16) x = turned(x, load_turn(angle_of(t), e), a.rot_pairs);
+        _Float16 *out = q_out + ((size_t)(row0 + t) * a.Hq + h) * a.D + 8 * first_piece(e);
+        *reinterpret_cast<uint4 *>(out) = x.a;
+        if (e < R16) *reinterpret_cast<uint4 *>(out + 8 * second) = x.b;
+    }
+    // keys, turned
     Pieces kp[4 * NI];
 #pragma unroll
     for (int n = 0; n < 4 * NI; ++n) {
@@ -197,9 +214,9 @@ __global__ __launch_bounds__(256) void kv_append(KvAppendArgs a)
                 r = load_turn(angle_of(t), e);
                 kp[n] = turned(kp[n], r, a.rot_pairs);
             }
-            if (a.q_out) {
-                const _Float16 *q = static_cast<const _Float16 *>(a.q) + (row0 + t) * a.q_row + hk * a.G * a.q_head;
-                _Float16 *out = static_cast<_Float16 *>(a.q_out) + ((size_t)(row0 + t) * a.Hq + hk * a.G) * a.D + 8 * first_piece(e);
+            if (a.q_out && !few) {
+                const _Float16 *q = q0 + (row0 + t) * a.q_row;
+                _Float16 *out = q_out + (size_t)(row0 + t) * a.Hq * a.D + 8 * first_piece(e);
                 for (int h0 = 0; h0 < a.G; h0 += 4) {
                     Pieces x[4];
 #pragma unroll
@@ -230,13 +247,7 @@ __global__ __launch_bounds__(256) void kv_append(KvAppendArgs a)
         }
     }
     __syncthreads();
-    // scales: thread i has block i of the keys, thread 64 + i block i of the values
-    const int shared_block = tlo / S;                       // the one block that may hold earlier tokens
-    const bool earlier = held && tlo % S != 0;
-    if (tid < 128 && tid % 64 < KV_GROUP / S) {
-        const int blk = tid % 64;
-        float *scale = tid < 64 ? ks : vs;
-        const float old = earlier && blk == shared_block ? scale[blk] : 0.0f;
+    if (tid < 128 && blk < KV_GROUP / S) {
         const float alpha = fmaxf(old, half_bits_to_float(tid < 64 ? amax_k[blk] : amax_v[blk]) / 127.0f);
         (tid < 64 ? alpha_k : alpha_v)[blk] = alpha;
         if (blk == shared_block) (tid < 64 ? was_k : was_v) = old;

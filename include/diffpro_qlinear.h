@@ -447,7 +447,8 @@ int ql_time_bin(int64_t step, int64_t num_steps);
  *   row_absmax (device) [T_q] uint32 or NULL: as ql_fusion.row_absmax, the largest
  *             |o[t,:,:]| of every row for daq_quantize_rowmax (the quantizer of
  *             the output projection).  The call clears it first
- * D: a multiple of 8 up to 256; Hkv divides Hq; T_q * Hq and T_k * Hkv below 2^31.
+ * D: a multiple of 8 up to 256; Hkv divides Hq; T_q * Hq and T_k * Hkv up to 2^30,
+ * B * Hq up to 2^20; rows at most 2^24 elements apart.
  * Values inside the sequences are assumed finite (General rules); rows outside
  * them are not read into any result.
  * ---------------------------------------------------------------------- */

@@ -558,12 +558,26 @@ def _heads(t, name, H=None, D=None):
     return t.data_ptr(), row if n > 1 else 0, head if heads > 1 else 0
 
 
-def _attention_form(q, B, Hkv, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax):
+def _here(t):
+    """The calls run on the current device's stream: what they are given has to be there."""
+    if t.get_device() != _torch._C._cuda_getDevice():
+        raise ValueError("tensors are on cuda:%d, the current device is cuda:%d" % (t.get_device(), _torch._C._cuda_getDevice()))
+
+
+def _made(t, stream):
+    """A tensor that a call made for itself and uses on `stream`: its memory is not given out again before that."""
+    if stream is not None:
+        t.record_stream(stream if hasattr(stream, "cuda_stream") else _torch.cuda.ExternalStream(int(stream)))
+    return t
+
+
+def _attention_form(q, B, Hkv, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax, stream):
     torch = _torch or _load_torch()
     qp, q_row, q_head = _heads(q, "q")
+    _here(q)
     T, Hq, D = q.shape
     if o is None:
-        o = torch.empty((T, Hq, D), dtype=torch.float16, device=q.device)
+        o = _made(torch.empty((T, Hq, D), dtype=torch.float16, device=q.device), stream)
     op, o_row, o_head = _heads(o, "o", Hq, D)
     if o.shape[0] != T:
         raise ValueError("o has %d rows, expected %d" % (o.shape[0], T))
@@ -597,9 +611,9 @@ def attention_f16(q, k, v, batch=None, cu_q=None, cu_k=None, mask=MASK_NONE, pre
     B = batch if batch is not None else cu_q.shape[0] - 1 if cu_q is not None else cu_k.shape[0] - 1 if cu_k is not None else 1
     if cu_k is not None:
         _need(cu_k, _torch.int32, (B + 1,), "cu_k")
-    a, o = _attention_form(q, B, Hkv, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax)
+    a, o = _attention_form(q, B, Hkv, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax, stream)
     if ws is None:
-        ws = workspace(attention_f16_workspace_bytes(q.shape[0], T_k, B, q.shape[1], Hkv, D), q.device)
+        ws = _made(workspace(attention_f16_workspace_bytes(q.shape[0], T_k, B, q.shape[1], Hkv, D), q.device), stream)
     _check(lib().attention_f16(a, kp, k_row, k_head, vp, v_row, v_head, T_k, _ptr(cu_k), _ptr(ws), ws.numel(), _stream(stream)),
            "attention_f16")
     return o
@@ -649,6 +663,7 @@ def daq_kv_append(cache, k, v, page_table, len_k, cu=None, q=None, rot=None, rot
     c, B = cache.desc(page_table, len_k)
     kp, k_row, k_head = _heads(k, "k", cache.heads, cache.D)
     vp, v_row, v_head = _heads(v, "v", cache.heads, cache.D)
+    _here(k)
     T = k.shape[0]
     if v.shape[0] != T:
         raise ValueError("k has %d rows and v %d" % (T, v.shape[0]))
@@ -659,7 +674,7 @@ def daq_kv_append(cache, k, v, page_table, len_k, cu=None, q=None, rot=None, rot
         if q.shape[0] != T:
             raise ValueError("q has %d rows and k %d" % (q.shape[0], T))
         if q_out is None:
-            q_out = torch.empty((T, Hq, cache.D), dtype=torch.float16, device=q.device)
+            q_out = _made(torch.empty((T, Hq, cache.D), dtype=torch.float16, device=q.device), stream)
         qo = _need(q_out, torch.float16, (T, Hq, cache.D), "q_out").data_ptr()
     if k_out is not None:
         ko = _need(k_out, torch.float16, (T, cache.heads, cache.D), "k_out").data_ptr()
@@ -686,11 +701,11 @@ def attention_kv8(q, cache, page_table, len_k, cu_q=None, mask=MASK_CAUSAL, pref
                   row_absmax=None, ws=None, stream=None):
     """attention_f16 over the 8-bit cache: q fp16 [T_q, Hq, D], page_table int32 [B, max_pages], len_k int32 [B] -> o fp16 [T_q, Hq, D]."""
     c, B = cache.desc(page_table, len_k)
-    a, o = _attention_form(q, B, cache.heads, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax)
+    a, o = _attention_form(q, B, cache.heads, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax, stream)
     if q.shape[2] != cache.D:
         raise ValueError("q has heads of %d, the cache of %d" % (q.shape[2], cache.D))
     if ws is None:
-        ws = workspace(attention_kv8_workspace_bytes(q.shape[0], B, q.shape[1], cache.heads, cache.D), q.device)
+        ws = _made(workspace(attention_kv8_workspace_bytes(q.shape[0], B, q.shape[1], cache.heads, cache.D), q.device), stream)
     _check(lib().attention_kv8(a, c, _ptr(ws), ws.numel(), _stream(stream)), "attention_kv8")
     return o
 

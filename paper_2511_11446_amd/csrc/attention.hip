@@ -36,7 +36,6 @@ hipError_t launch_tiles(const AttnArgs &a, hipStream_t stream)
     const bool shaped = a.cap > 0.0f || a.slopes;
     if (opt_in[shaped] != hipSuccess) return opt_in[shaped];
     const long long wgs = (long long)p.tiles * a.Hkv * p.splits;
-    if (wgs > 0x7fffff00LL / T::NT * 1LL) return hipErrorInvalidValue;
     const dim3 grid((unsigned)((wgs + 7) / 8 * 8));
     if (shaped) hipLaunchKernelGGL((attend_tiles<CHP, NW, true>), grid, dim3(T::NT), T::LDS_BYTES, stream, a, p);
     else hipLaunchKernelGGL((attend_tiles<CHP, NW, false>), grid, dim3(T::NT), T::LDS_BYTES, stream, a, p);

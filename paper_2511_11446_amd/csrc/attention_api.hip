@@ -8,6 +8,7 @@ namespace {
 
 constexpr int64_t INT_MAX64 = 2147483647;
 
+constexpr int64_t ROWS_MAX = 1 << 30, SEQUENCES_MAX = 1 << 20;
 constexpr int64_t STRIDE_MAX = 1 << 24;   // elements between rows: 64 of them are addressed with 32 bits
 
 inline bool off(const void *p, size_t a) { return p && (uintptr_t)p % a != 0; }
@@ -23,7 +24,8 @@ int check_rows(const void *p, int64_t row, int64_t head)
 int check_heads(int64_t T, int64_t B, int64_t H, int64_t D, bool equal)
 {
     if (T < 1 || B < 1 || H < 1 || D < 8 || D > 256 || D % 8 != 0) return QL_ERR_SHAPE;
-    if (T > INT_MAX64 / H || (equal && T % B != 0)) return QL_ERR_SHAPE;
+    // threads of a launch stay below 2^32: 256 for every 128 packed rows, and for every sequence and key head
+    if (T > ROWS_MAX / H || B > SEQUENCES_MAX / H || (equal && T % B != 0)) return QL_ERR_SHAPE;
     return QL_OK;
 }
 
@@ -135,7 +137,7 @@ int daq_kv_append(const ql_kv_cache *cache, const ql_kv_new *n, void *stream)
     if ((rc = check_heads(n->T, cache->B, cache->Hkv, cache->D, !n->cu))) return rc;
     if ((rc = check_rows(n->k, n->k_row, n->k_head)) || (rc = check_rows(n->v, n->v_row, n->v_head))) return rc;
     if (n->q_out) {
-        if (n->Hq < 1 || n->Hq % cache->Hkv != 0 || n->T > INT_MAX64 / n->Hq) return QL_ERR_SHAPE;
+        if (n->Hq < 1 || n->Hq % cache->Hkv != 0 || n->T > ROWS_MAX / n->Hq) return QL_ERR_SHAPE;
         if ((rc = check_rows(n->q, n->q_row, n->q_head))) return rc;
     }
     if (n->rot && (n->rot_dim < 16 || n->rot_dim % 16 != 0 || n->rot_dim > cache->D || n->rot_rows < 1 || n->rot_rows > INT_MAX64)) return QL_ERR_SHAPE;

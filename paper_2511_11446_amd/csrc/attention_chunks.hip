@@ -33,7 +33,6 @@ hipError_t launch_chunks(const AttnArgs &a, hipStream_t stream)
     const bool shaped = a.cap > 0.0f || a.slopes;
     if (opt_in[shaped] != hipSuccess) return opt_in[shaped];
     const long long wgs = (long long)p.tiles * a.Hkv * p.splits;
-    if (wgs > 0x7fffff00LL / T::NT) return hipErrorInvalidValue;
     const dim3 grid((unsigned)((wgs + 7) / 8 * 8));
     if (shaped) hipLaunchKernelGGL((attend_chunks<CHP, true>), grid, dim3(T::NT), T::LDS_BYTES, stream, a, p);
     else hipLaunchKernelGGL((attend_chunks<CHP, false>), grid, dim3(T::NT), T::LDS_BYTES, stream, a, p);

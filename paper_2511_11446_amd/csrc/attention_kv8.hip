@@ -499,12 +499,13 @@ size_t cached_partial_bytes(long long Tq, int B, int Hq, int Hkv, int D)
     return few > many ? few : many;
 }
 
-// packed rows of a sequence and key head, on average, up to which they go by 16
-constexpr int FEW_ROWS = 16;
+// Packed rows of a sequence and key head, on average, up to which they go by 16 rather than by 256 (attention_chunks.hip).  us by 16 / by 256, 32 sequences of 4096 tokens,
+// 8 key heads of 128: 32 rows 91 / 189, 64 rows 163 / 192, 128 rows 314 / 201; heads of 64, 1024 tokens: 16 rows 22 / 22, 32 rows 34 / 29, 64 rows 49 / 30.
+int few_rows(int D) { return D > 64 ? 64 : 16; }
 
 hipError_t launch_attention_kv8(const AttnArgs &a, hipStream_t stream)
 {
-    if ((long long)a.Tq * a.G > (long long)FEW_ROWS * a.B) return launch_attention_chunks(a, stream);
+    if ((long long)a.Tq * a.G > (long long)few_rows(a.D) * a.B) return launch_attention_chunks(a, stream);
     const CachedPlan p{cached_workers(a.D)};
     const hipError_t e = launch_by_head(a, p, stream);
     if (e != hipSuccess) return e;

@@ -28,7 +28,8 @@ def _f16(a, k=A, k_row=128, k_head=64, v=A, v_row=128, v_head=64, T_k=64, cu_k=N
     (dict(mask=3), 4), (dict(mask=-1), 4), (dict(reserved=1), 4), (dict(scale=float("nan")), 4), (dict(scale=float("inf")), 4),
     (dict(cap=-1.0), 4), (dict(cap=float("nan")), 4), (dict(cap=float("inf")), 4),
     (dict(T_q=0), 2), (dict(B=0), 2), (dict(Hq=0), 2), (dict(Hkv=0), 2), (dict(Hq=3), 2), (dict(D=0), 2), (dict(D=60), 2), (dict(D=264), 2),
-    (dict(T_q=63), 2), (dict(T_q=1 << 31), 2), (dict(T_q=1 << 30), 2),                                   # unequal lengths, too many rows
+    (dict(T_q=63), 2), (dict(T_q=1 << 31), 2), (dict(T_q=1 << 30), 2), (dict(B=1 << 19, cu_q=A), 2),     # unequal lengths, too many rows or sequences
+    (dict(q_row=(1 << 24) + 8), 2),
     (dict(q_row=252), 2), (dict(q_head=-64), 2), (dict(o_row=0), 2), (dict(o_head=32), 2), (dict(o_row=192), 2),   # outputs that overlap
     (dict(q=A + 8), 3), (dict(o=A + 2), 3), (dict(slopes=A + 2), 3), (dict(cu_q=A + 1), 3), (dict(row_absmax=A + 3), 3), (dict(mask=2, prefix=A + 2), 3),
 ])

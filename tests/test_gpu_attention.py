@@ -347,3 +347,219 @@ def test_cached_scales_behind_the_end_do_not_count():
         c.dev.k_scale.copy_(torch.from_numpy(c.ref.ks))
         c.dev.v_scale.copy_(torch.from_numpy(c.ref.vs))
         _cached((38, S), [1, 1], [70, 3], 2, 1, 64, 64, S, equal=True, cache=c)
+
+
+@pytest.mark.parametrize("S", [1, 16, 64])
+@pytest.mark.parametrize("D", [8, 32, 40, 72, 88, 96, 128, 136, 200, 256])
+def test_cached_chunks_of_every_head_size(S, D):
+    """Many rows: the cache's codes become tiles."""
+    _cached((39, S, D), [150, 90], [400, 91], 4, 2, D, 64, S)
+
+
+def test_cached_chunks_over_long_sequences_are_cut():
+    """Few tiles over many keys: parts of the keys, joined."""
+    _cached((40,), [70, 3], [3001, 1500], 4, 1, 64, 128, 32, cap=30.0, slopes=True)
+
+
+def test_cached_tokens_with_pages_that_are_none():
+    """The same for single tokens: whole sequences without a page, and a page missing in the middle of one."""
+    g = _rng(41)
+    c = _Cached(g, 4, 640, 2, 128, 64, 32)
+    c.ref.table[0, 3:7] = -1
+    c.ref.table[1, :] = 10 ** 6
+    c.ref.table[2, 0], c.ref.table[2, 9] = c.ref.pages, -7
+    c.table.copy_(torch.from_numpy(c.ref.table))
+    o = _cached((41, 1), [1, 2, 3, 1], [640, 640, 600, 64], 4, 2, 128, 64, 32, cache=c)
+    assert bool((o[1:3] == 0).all())
+
+
+def test_few_rows_over_long_keys_are_cut():
+    _dense((12,), [1], [9001], 2, 1, 64, mask=1)
+    _dense((12, 1), [33, 2], [2000, 3000], 2, 2, 72, mask=2, cap=30.0, slopes=True)
+    _dense((12, 2), [20], [2500], 4, 1, 200)
+
+
+def test_offsets_past_two_gigabytes():
+    """Pages at the end of a cache whose keys alone hold more than 2^31 codes."""
+    Hkv, D, page = 8, 128, 64
+    P = (1 << 31) // (Hkv * D * page) + 40
+    cache = ql.KvCache8.empty(P, Hkv, D, page=page, scale_tokens=64)
+    g = _rng(42)
+    n = 130
+    table = np.array([[P - 1, 3, P - 17]], np.int32)
+    x = _f16(g, n, 3 * Hkv * D)
+    q, k, v = (x[:, i * Hkv * D:(i + 1) * Hkv * D].reshape(n, Hkv, D) for i in range(3))
+    dx = _dev(x)
+    dq, dk, dv = (dx[:, i * Hkv * D:(i + 1) * Hkv * D].unflatten(1, (Hkv, D)) for i in range(3))
+    k_out, v_out = (torch.empty((n, Hkv, D), dtype=torch.float16, device="cuda") for _ in range(2))
+    lens = _dev(np.array([n], np.int32))
+    ql.daq_kv_append(cache, dk, dv, _dev(table), lens, k_out=k_out, v_out=v_out)
+    one = ql.attention_kv8(dq[-1:], cache, _dev(table), lens)
+    many = ql.attention_kv8(dq, cache, _dev(table), lens)
+    torch.cuda.synchronize()
+    pages = [int(p) for p in table[0]]
+    kc = cache.k[pages].cpu().numpy().transpose(0, 2, 1, 3).reshape(-1, Hkv, D)[:n].astype(np.float64)
+    ks = cache.k_scale[pages].cpu().numpy()[:, :, 0].repeat(64, 0)[:n].astype(np.float64)
+    assert np.abs(kc * ks[..., None] - k).max() <= 0.5 * ks.max() * (1 + 2.0 ** -20), "keys at the end of the pool"
+    order = [oa.slot(t) for t in range(64)]
+    vc = cache.v[pages].cpu().numpy()[:, :, 0][..., order].transpose(0, 3, 1, 2).reshape(-1, Hkv, D)[:n].astype(np.float64)
+    vs = cache.v_scale[pages].cpu().numpy()[:, :, 0].repeat(64, 0)[:n].astype(np.float64)
+    ref, tol = oa.attention(q, kc * ks[..., None], vc * vs[..., None], [0, n], [0, n], D ** -0.5, oa.CAUSAL)
+    _close(many, ref, tol)
+    _close(one, ref[-1:], tol[-1:])
+    assert int(cache.k.count_nonzero()) == int(cache.k[pages].count_nonzero())
+
+
+# ---- as a program uses them -------------------------------------------------------------------------------------------------------
+
+def test_attention_between_the_quantized_layers():
+    """LayerNorm + DAQ, qkv, attention, DAQ from its row maxima, projection with the residual: each step on what the one in front left."""
+    import oracle
+    import workload
+    B, S, W, H = 3, 64, 384, 6
+    M, D = B * S, W // H
+    x = workload.activations(M, W, "attention block")
+    qkv, proj = workload.layer_weights("qkv", W, 3 * W, 8, "attention block"), workload.layer_weights("proj", W, W, 8, "attention block")
+    dx = _dev(x)
+    ln = ql.daq_quantize_ln(dx)
+    rows = ql.qgemm_w8a8(ln["q"], ln["scales"], 1, _dev(qkv["w"]), _dev(qkv["s_w"]), _dev(qkv["bias"]))
+    rows = (rows * 0.01).contiguous()                     # the synthetic weights are not trained: scores of a usual size
+    q, k, v = (rows[:, i * W:(i + 1) * W].unflatten(1, (H, D)) for i in range(3))
+    am = torch.empty(M, dtype=torch.int32, device="cuda")
+    o = ql.attention_f16(q, k, v, batch=B, row_absmax=am)
+    codes, scales = ql.daq_quantize_rowmax(o.view(M, W), 1, am)
+    y = ql.qgemm_w8a8(codes, scales, 1, _dev(proj["w"]), _dev(proj["s_w"]), _dev(proj["bias"]))
+    torch.cuda.synchronize()
+    cu = [i * S for i in range(B + 1)]
+    ref, tol = oa.attention(*(t.cpu().numpy() for t in (q, k, v)), cu, cu, D ** -0.5)
+    _close(o, ref, tol)
+    c2, s2 = ql.daq_quantize(o.view(M, W), 1)
+    assert torch.equal(codes, c2) and torch.equal(scales, s2), "codes from the row maxima"
+    want = oracle.qlinear_w8a8(o.view(M, W).cpu().numpy(), 1, proj["w"], proj["s_w"], proj["bias"], nthreads=4)["y"]
+    got, want = y.cpu().numpy().astype(np.float64), want.astype(np.float64)
+    assert np.all(np.abs(got - want) <= np.maximum(1e-3 * np.abs(want), 2.0 ** -24))
+
+
+def test_prompt_then_tokens():
+    """A prompt enters the cache and attends over the values it holds; then single tokens, three at a time in one sequence, over the cache."""
+    g = _rng(50)
+    Hq, Hkv, D = 8, 2, 64
+    c = _Cached(g, 2, 256, Hkv, D, 64, 16)
+    rot = _table(256, D)
+    lens = np.array([100, 37], np.int32)
+    cu = _cu(lens)
+    T = int(lens.sum())
+    rows = _f16(g, T, (Hq + 2 * Hkv) * D)
+    d = _dev(rows)
+    dq, dk, dv = d[:, :Hq * D].unflatten(1, (Hq, D)), d[:, Hq * D:(Hq + Hkv) * D].unflatten(1, (Hkv, D)), d[:, (Hq + Hkv) * D:].unflatten(1, (Hkv, D))
+    k_val, v_val = (torch.empty((T, Hkv, D), dtype=torch.float16, device="cuda") for _ in range(2))
+    q_rot = ql.daq_kv_append(c.dev, dk, dv, c.table, _dev(lens), cu=_dev(cu), q=dq, rot=_dev(rot), k_out=k_val, v_out=v_val)
+    c.ref.append(rows[:, Hq * D:(Hq + Hkv) * D].reshape(T, Hkv, D), rows[:, (Hq + Hkv) * D:].reshape(T, Hkv, D), cu, lens, None, rot)
+    c.same()
+    dense = ql.attention_f16(q_rot, k_val, v_val, cu_q=_dev(cu), cu_k=_dev(cu), mask=ql.MASK_CAUSAL)
+    paged = ql.attention_kv8(q_rot, c.dev, c.table, _dev(lens), cu_q=_dev(cu))
+    torch.cuda.synchronize()
+    ref, tol = oa.attention(q_rot.cpu().numpy(), k_val.cpu().numpy(), v_val.cpu().numpy(), cu, cu, D ** -0.5, oa.CAUSAL)
+    _close(dense, ref, tol)
+    ref, tol = oa.attention_cached(q_rot.cpu().numpy(), c.ref, cu, lens, D ** -0.5)
+    _close(paged, ref, tol)
+    for new in ([1, 1], [3, 1], [1, 0], [1, 1]):
+        lens = lens + np.array(new, np.int32)
+        q = _append(g, c, lens, new, Hq, rot)
+        o = ql.attention_kv8(q, c.dev, c.table, _dev(lens), cu_q=_dev(_cu(new)))
+        torch.cuda.synchronize()
+        ref, tol = oa.attention_cached(q.cpu().numpy(), c.ref, _cu(new), lens, D ** -0.5)
+        _close(o, ref, tol, str(new))
+
+
+def test_captured_step_follows_its_lengths():
+    """A generation step in a graph: replayed after the lengths and rows in its buffers changed, with eager work between; a second graph shares the workspace."""
+    g = _rng(51)
+    B, Hq, Hkv, D = 3, 8, 2, 128
+    c = _Cached(g, B, 512, Hkv, D, 64, 64)
+    rot = _dev(_table(512, D))
+    lens = _dev(np.array([400, 60, 129], np.int32))
+    rows = torch.empty((B, (Hq + 2 * Hkv) * D), dtype=torch.float16, device="cuda")
+    q, k, v = rows[:, :Hq * D].unflatten(1, (Hq, D)), rows[:, Hq * D:(Hq + Hkv) * D].unflatten(1, (Hkv, D)), rows[:, (Hq + Hkv) * D:].unflatten(1, (Hkv, D))
+    q_rot, o, o2 = (torch.empty((B, Hq, D), dtype=torch.float16, device="cuda") for _ in range(3))
+    am = torch.empty(B, dtype=torch.int32, device="cuda")
+    ws = ql.workspace(max(ql.attention_kv8_workspace_bytes(B, B, Hq, Hkv, D), ql.attention_f16_workspace_bytes(B, 512, 1, Hq, Hkv, D)))
+    keys = _dev(_f16(g, 512, 2 * Hkv, D))
+
+    def step():
+        ql.daq_kv_append(c.dev, k, v, c.table, lens, q=q, rot=rot, q_out=q_rot)
+        ql.attention_kv8(q_rot, c.dev, c.table, lens, o=o, row_absmax=am, ws=ws)
+
+    def other():
+        ql.attention_f16(q_rot, keys[:, :Hkv], keys[:, Hkv:], batch=1, o=o2, ws=ws)
+
+    rows.copy_(_dev(_f16(g, *rows.shape)))
+    step(), other()
+    torch.cuda.synchronize()
+    graphs = []
+    for fn in (step, other):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            fn()
+        graphs.append(graph)
+    for turn in range(4):
+        rows.copy_(_dev(_f16(g, *rows.shape, size=1.0 + turn)))
+        lens.add_(1)
+        saved = [t.clone() for t in (c.dev.k, c.dev.v, c.dev.k_scale, c.dev.v_scale)]
+        graphs[0].replay()
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (c.dev.k, c.dev.v, c.dev.k_scale, c.dev.v_scale, q_rot, o, am, o2)]
+        for t, s in zip((c.dev.k, c.dev.v, c.dev.k_scale, c.dev.v_scale), saved):
+            t.copy_(s)
+        for t in (q_rot, o, o2):
+            t.fill_(9.0)
+        step(), other()
+        torch.cuda.synchronize()
+        for name, a, b in zip(("k", "v", "k_scale", "v_scale", "q", "o", "absmax", "o2"), got, (c.dev.k, c.dev.v, c.dev.k_scale, c.dev.v_scale, q_rot, o, am, o2)):
+            assert torch.equal(a, b), "%s differs in replay %d" % (name, turn)
+
+
+def test_results_do_not_depend_on_the_run():
+    """The same call twice, and on another stream beside other work: the same bits."""
+    g = _rng(52)
+    q, k, v = (_dev(_f16(g, 700, 4, 72)) for _ in range(3))
+    c = _Cached(g, 2, 1500, 2, 64, 64, 16)
+    lens, t = _dev(np.array([1500, 700], np.int32)), _dev(_f16(g, 2, 8, 64))
+    first = ql.attention_f16(q, k, v, mask=ql.MASK_CAUSAL), ql.attention_kv8(t, c.dev, c.table, lens)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        again = ql.attention_f16(q, k, v, mask=ql.MASK_CAUSAL, stream=side), ql.attention_kv8(t, c.dev, c.table, lens, stream=side.cuda_stream)
+        here = ql.attention_f16(q, k, v, mask=ql.MASK_CAUSAL), ql.attention_kv8(t, c.dev, c.table, lens)
+        torch.cuda.synchronize()
+        for a, b, d in zip(first, again, here):
+            assert torch.equal(a, b) and torch.equal(a, d)
+
+
+def test_refusals_with_tensors():
+    x = torch.zeros((8, 2, 64), dtype=torch.float16, device="cuda")
+    odd = torch.zeros((8, 2, 68), dtype=torch.float16, device="cuda")[:, :, :64]
+    with pytest.raises(ql.QlError):
+        ql.attention_f16(odd, x, x)                       # heads 68 elements apart
+    with pytest.raises(ql.QlError):
+        ql.attention_f16(x, x, x, batch=3)                # 8 rows are no three equal sequences
+    with pytest.raises(ql.QlError):
+        ql.attention_f16(x, x, x, mask=ql.MASK_PREFIX)    # no prefix lengths
+    with pytest.raises(TypeError):
+        ql.attention_f16(x.float(), x, x)
+    with pytest.raises((TypeError, ValueError)):
+        ql.attention_f16(x.transpose(1, 2), x, x)         # 64 heads of 2, not next to each other
+    with pytest.raises(ValueError):
+        ql.attention_f16(x, x, x[:4])
+    with pytest.raises(TypeError):
+        ql.attention_f16(x, x, x, cu_q=torch.zeros(2, dtype=torch.int64, device="cuda"))
+    cache = ql.KvCache8.empty(2, 2, 64)
+    table, lens = torch.zeros((1, 2), dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        ql.daq_kv_append(cache, x, x[:4], table, lens)
+    with pytest.raises(ValueError):
+        ql.attention_kv8(x[:, :, :32], cache, table, lens)
+    with pytest.raises(ql.QlError):
+        ql.daq_kv_append(cache, x, x, table, lens, rot=torch.zeros((4, 12, 2), device="cuda"))   # 24 turned channels

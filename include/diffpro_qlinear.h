@@ -449,8 +449,9 @@ int ql_time_bin(int64_t step, int64_t num_steps);
  *             the output projection).  The call clears it first
  * D: a multiple of 8 up to 256; Hkv divides Hq; T_q * Hq and T_k * Hkv up to 2^30,
  * B * Hq up to 2^20; rows at most 2^24 elements apart.
- * Values inside the sequences are assumed finite (General rules); rows outside
- * them are not read into any result.
+ * Values inside the sequences, those that a mask hides among them, and their
+ * scores in fp32 are assumed finite (General rules); rows outside the sequences
+ * are not read into any result.
  * ---------------------------------------------------------------------- */
 enum { QL_MASK_NONE = 0, QL_MASK_CAUSAL = 1, QL_MASK_PREFIX = 2 };
 
@@ -459,7 +460,7 @@ typedef struct ql_attention {
     int32_t B, Hq, Hkv, D;
     int32_t mask;          /* QL_MASK_* */
     float scale;           /* finite; 1 / sqrt(D) as a rule */
-    float cap;             /* 0: none; else finite and positive */
+    float cap;             /* 0: none; else 2^-10 to 2^10 */
     int32_t reserved;      /* 0 */
     const void *prefix;
     const void *slopes;
@@ -529,8 +530,8 @@ typedef struct ql_kv_cache {
  *           then sees the values that later steps will read)
  *   rot    (device) fp32 [rot_rows, rot_dim/2, 2], 16-byte aligned; rot_dim a
  *           multiple of 16 up to D;  pos (device) int32 [T] or NULL
- * Sequences must not share a page that tokens are appended to.  Cache bytes
- * outside the touched blocks keep what they held. */
+ * A page that tokens are appended to must stand in one place of the page table
+ * only.  Cache bytes outside the touched blocks keep what they held. */
 typedef struct ql_kv_new {
     int64_t T;
     int32_t Hq;            /* heads of q; 0 without q */
@@ -550,7 +551,8 @@ int daq_kv_append(const ql_kv_cache *cache, const ql_kv_new *tokens, void *strea
 
 /* Attention over the cache: the formulas above with n_k = len_k[b] and the
  * cache's keys and values; attn->B, Hkv and D are the cache's.  One new token per
- * sequence is T_q = B with cu_q NULL.  (T_q * Hq / Hkv / 16 + B) * Hkv * max_pages *
+ * sequence is T_q = B with cu_q NULL.  The weights take the value scales along
+ * when they are rounded, relative to the largest of them.  (T_q * Hq / Hkv / 16 + B) * Hkv * max_pages *
  * page / 64 below 2^31. */
 size_t attention_kv8_workspace_bytes(int64_t T_q, int32_t B, int32_t Hq, int32_t Hkv, int32_t D);
 int attention_kv8(const ql_attention *attn, const ql_kv_cache *cache,

@@ -601,7 +601,7 @@ def attention_f16(q, k, v, batch=None, cu_q=None, cu_k=None, mask=MASK_NONE, pre
                   row_absmax=None, ws=None, stream=None):
     """Softmax attention: q fp16 [T_q, Hq, D], k, v fp16 [T_k, Hkv, D] (views with strided rows and heads, such as the columns of a fused qkv
     layer's output) -> o fp16 [T_q, Hq, D].  Sequences one behind the other: `batch` of equal length, or int32 [B+1] first rows in cu_q / cu_k.
-    scale: default D ** -0.5; cap: tanh cap of the scores (0: none); slopes fp32 [Hq]: bias by distance; mask MASK_NONE / _CAUSAL / _PREFIX
+    scale: default D ** -0.5; cap: tanh cap of the scores (0: none; 2^-10 to 2^10); slopes fp32 [Hq]: bias by distance; mask MASK_NONE / _CAUSAL / _PREFIX
     (prefix int32 [B]); row_absmax: int32 [T_q] that receives every row's largest |o| as a binary16 bit pattern, for daq_quantize_rowmax."""
     kp, k_row, k_head = _heads(k, "k")
     T_k, Hkv, D = k.shape

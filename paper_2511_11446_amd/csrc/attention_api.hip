@@ -34,7 +34,9 @@ int check_attention(const ql_attention *a)
     if (!a || !a->q || !a->o) return QL_ERR_NULL;
     if (a->mask < QL_MASK_NONE || a->mask > QL_MASK_PREFIX || a->reserved != 0) return QL_ERR_UNSUPPORTED;
     if (a->mask == QL_MASK_PREFIX && !a->prefix) return QL_ERR_NULL;
-    if (!std::isfinite(a->scale) || !std::isfinite(a->cap) || a->cap < 0) return QL_ERR_UNSUPPORTED;
+    if (!std::isfinite(a->scale)) return QL_ERR_UNSUPPORTED;
+    // the capped score is off by about 2^-22 of the cap (attention_tile.h): beyond 2^10 that would be more than the rounding of the weights
+    if (a->cap != 0.0f && !(a->cap >= 0x1p-10f && a->cap <= 0x1p10f)) return QL_ERR_UNSUPPORTED;
     int rc = check_heads(a->T_q, a->B, a->Hq, a->D, !a->cu_q);
     if (rc) return rc;
     if (a->Hkv < 1 || a->Hq % a->Hkv != 0) return QL_ERR_SHAPE;

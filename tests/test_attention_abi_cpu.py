@@ -26,7 +26,7 @@ def _f16(a, k=A, k_row=128, k_head=64, v=A, v_row=128, v_head=64, T_k=64, cu_k=N
 @pytest.mark.parametrize("kw, status", [
     (dict(q=None), 1), (dict(o=None), 1), (dict(mask=2), 1),                                             # a pointer is missing
     (dict(mask=3), 4), (dict(mask=-1), 4), (dict(reserved=1), 4), (dict(scale=float("nan")), 4), (dict(scale=float("inf")), 4),
-    (dict(cap=-1.0), 4), (dict(cap=float("nan")), 4), (dict(cap=float("inf")), 4),
+    (dict(cap=-1.0), 4), (dict(cap=float("nan")), 4), (dict(cap=float("inf")), 4), (dict(cap=2.0 ** -10 * (1 - 2.0 ** -20)), 4), (dict(cap=1025.0), 4),
     (dict(T_q=0), 2), (dict(B=0), 2), (dict(Hq=0), 2), (dict(Hkv=0), 2), (dict(Hq=3), 2), (dict(D=0), 2), (dict(D=60), 2), (dict(D=264), 2),
     (dict(T_q=63), 2), (dict(T_q=1 << 31), 2), (dict(T_q=1 << 30), 2), (dict(B=1 << 19, cu_q=A), 2),     # unequal lengths, too many rows or sequences
     (dict(q_row=(1 << 24) + 8), 2),

@@ -1,15 +1,26 @@
 // Attention over binary16 rows for gfx950: one pass over the keys with the running maximum and sum of the softmax.
 //
-// A workgroup of NW wavefronts has 32 NW packed rows (attention.h) of one sequence and key head; keys and values go by tiles of 64 from global memory into
-// LDS (global_load_lds, no registers), two tiles deep, and every wavefront reads them from there: attention_tile.h says how.
+// A workgroup of 4 wavefronts has 128 packed rows (attention.h) of one sequence and key head; keys and values go by tiles of 64 from global memory into
+// LDS (global_load_lds, no registers), two tiles deep, and every wavefront reads them from there: attention_tile.h says how.  With fewer rows than
+// that the other wavefronts still load, and tiles of 32 or 64 rows that bring more workgroups were no better (us with 32 or 64 / 128 rows): one image of 256
+// tokens, 6 heads of 64, 8.3 or 7.7 / 7.6; one of 1024 19.4 or 16.5 / 14.8; one row on 4096 keys, 8 heads of 64, 14.4 or 13.5 / 13.1; 30 tokens 5.5 or
+// 5.0 / 4.8; only two sequences of 77 tokens with heads of 16 gained, 4.8 or 4.7 / 4.9.  Many rows lose by them, as each row then reads the keys with
+// fewer others: 16 images of 1024 tokens, 16 heads of 72, 283 or 191 / 140.
+//
+// 16 images of 1024 tokens, 16 heads of 72: 123 us in turn with other work, 0.63 PFLOP/s of the products that D = 72 needs (of the 80 channels that
+// the matrix instructions work on, 0.70); 8192 tokens, 16 heads of 128 on 2, a prefix of 128: 330 us, 0.84 PFLOP/s.  Bound by issue: of the busy cycles the
+// matrix cores work 43 and 52 %, the vector units 58 and 44 %, LDS conflicts 12 and 0 %; and the chip lowers its clock under it (attention_tile.h).  With a
+// cap and a distance bias (8192 packed tokens, heads of 64) the vector units work 86 %, the matrix cores 19 %.  Small calls are a chain of latencies: launch, first tile, 4 tiles, writing.
 #include "attention_tile.h"
 
 namespace ql {
 
-template <int CHP, int NW, bool SHAPED>
-__global__ __launch_bounds__(64 * NW, CHP <= 16 ? 2 : 1) void attend_tiles(AttnArgs a, TilePlan plan)
+constexpr int TILE_WAVES = 4, TILE_ROWS = 32 * TILE_WAVES;
+
+template <int CHP, bool SHAPED>
+__global__ __launch_bounds__(64 * TILE_WAVES, CHP <= 16 ? 2 : 1) void attend_tiles(AttnArgs a, TilePlan plan)
 {
-    attend_tile<CHP, NW, false, SHAPED>(a, plan);
+    attend_tile<CHP, TILE_WAVES, false, SHAPED>(a, plan);
 }
 
 __global__ __launch_bounds__(JOIN_THREADS) void join_tiles(AttnArgs a, TilePlan plan, int rows_per) { join_splits(a, plan, rows_per); }
@@ -17,80 +28,46 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_tiles(AttnArgs a, TilePlan 
 namespace {
 constexpr int CUS = 256;
 
-// rows of a workgroup: as many as still give every CU one (long heads: the addresses of a tile that few wavefronts load take their registers)
-int tile_rows(long long Tq, int B, int G, int Hkv, int D)
-{
-    for (int rows = 128; rows > (D > 128 ? 128 : D > 80 ? 64 : 32); rows /= 2)
-        if ((Tq * G / rows + B) * Hkv >= CUS) return rows;
-    return D > 128 ? 128 : D > 80 ? 64 : 32;
-}
-
-template <int CHP, int NW>
+template <int CHP>
 hipError_t launch_tiles(const AttnArgs &a, hipStream_t stream)
 {
-    using T = AttnTile<CHP, NW, false>;
-    const TilePlan p = tile_plan(a.Tq, a.B, a.G, a.Hkv, T::ROWS, a.cu_q, a.mask, a.Tk / a.B, CUS, 2 * CUS);
+    using T = AttnTile<CHP, TILE_WAVES, false>;
+    const TilePlan p = tile_plan(a.Tq, a.B, a.G, a.Hkv, TILE_ROWS, a.cu_q, a.mask, a.Tk / a.B, CUS, 2 * CUS);
     static const hipError_t opt_in[2] = {
-        hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_tiles<CHP, NW, false>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES),
-        hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_tiles<CHP, NW, true>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES)};
+        hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_tiles<CHP, false>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES),
+        hipFuncSetAttribute(reinterpret_cast<const void *>(&attend_tiles<CHP, true>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES)};
     const bool shaped = a.cap > 0.0f || a.slopes;
     if (opt_in[shaped] != hipSuccess) return opt_in[shaped];
     const long long wgs = (long long)p.tiles * a.Hkv * p.splits;
     const dim3 grid((unsigned)((wgs + 7) / 8 * 8));
-    if (shaped) hipLaunchKernelGGL((attend_tiles<CHP, NW, true>), grid, dim3(T::NT), T::LDS_BYTES, stream, a, p);
-    else hipLaunchKernelGGL((attend_tiles<CHP, NW, false>), grid, dim3(T::NT), T::LDS_BYTES, stream, a, p);
+    if (shaped) hipLaunchKernelGGL((attend_tiles<CHP, true>), grid, dim3(T::NT), T::LDS_BYTES, stream, a, p);
+    else hipLaunchKernelGGL((attend_tiles<CHP, false>), grid, dim3(T::NT), T::LDS_BYTES, stream, a, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
-    hipLaunchKernelGGL(join_tiles, dim3((unsigned)(p.tiles * a.Hkv), join_blocks(T::ROWS, a.D)), dim3(JOIN_THREADS), 0, stream, a, p, T::ROWS);
+    hipLaunchKernelGGL(join_tiles, dim3((unsigned)(p.tiles * a.Hkv), join_blocks(TILE_ROWS, a.D)), dim3(JOIN_THREADS), 0, stream, a, p, TILE_ROWS);
     return hipGetLastError();
 }
 
-// rows: what tile_rows gave
-hipError_t launch_by_head(const AttnArgs &a, int rows, hipStream_t stream)
-{
-    const int ch = a.D / 8;
-    if (rows == 32) {
-        if (ch <= 2) return launch_tiles<2, 1>(a, stream);
-        if (ch <= 4) return launch_tiles<4, 1>(a, stream);
-        if (ch <= 6) return launch_tiles<6, 1>(a, stream);
-        if (ch <= 8) return launch_tiles<8, 1>(a, stream);
-        if (ch == 9) return launch_tiles<9, 1>(a, stream);
-        return launch_tiles<10, 1>(a, stream);
-    }
-    if (rows == 64) {
-        if (ch <= 2) return launch_tiles<2, 2>(a, stream);
-        if (ch <= 4) return launch_tiles<4, 2>(a, stream);
-        if (ch <= 6) return launch_tiles<6, 2>(a, stream);
-        if (ch <= 8) return launch_tiles<8, 2>(a, stream);
-        if (ch == 9) return launch_tiles<9, 2>(a, stream);
-        if (ch <= 10) return launch_tiles<10, 2>(a, stream);
-        if (ch <= 12) return launch_tiles<12, 2>(a, stream);
-        return launch_tiles<16, 2>(a, stream);
-    }
-    if (ch <= 2) return launch_tiles<2, 4>(a, stream);
-    if (ch <= 4) return launch_tiles<4, 4>(a, stream);
-    if (ch <= 6) return launch_tiles<6, 4>(a, stream);
-    if (ch <= 8) return launch_tiles<8, 4>(a, stream);
-    if (ch == 9) return launch_tiles<9, 4>(a, stream);
-    if (ch <= 10) return launch_tiles<10, 4>(a, stream);
-    if (ch <= 12) return launch_tiles<12, 4>(a, stream);
-    if (ch <= 16) return launch_tiles<16, 4>(a, stream);
-    if (ch <= 24) return launch_tiles<24, 4>(a, stream);
-    return launch_tiles<32, 4>(a, stream);
-}
 }  // namespace
 
 size_t tiles_partial_bytes(long long Tq, long long Tk, int B, int Hq, int Hkv, int D)
 {
-    const int rows = tile_rows(Tq, B, Hq / Hkv, Hkv, D);
-    const TilePlan p = tile_plan(Tq, B, Hq / Hkv, Hkv, rows, true, 0, Tk / B, CUS, 2 * CUS);
-    return p.splits == 1 ? 0 : (size_t)p.tiles * Hkv * p.splits * rows * (D + 2) * 4;
+    const TilePlan p = tile_plan(Tq, B, Hq / Hkv, Hkv, TILE_ROWS, true, 0, Tk / B, CUS, 2 * CUS);
+    return p.splits == 1 ? 0 : (size_t)p.tiles * Hkv * p.splits * TILE_ROWS * (D + 2) * 4;
 }
 
 hipError_t launch_attention_f16(const AttnArgs &a, hipStream_t stream)
 {
-    const int rows = tile_rows(a.Tq, a.B, a.G, a.Hkv, a.D);
-    return launch_by_head(a, rows, stream);
+    const int ch = a.D / 8;
+    if (ch <= 2) return launch_tiles<2>(a, stream);
+    if (ch <= 4) return launch_tiles<4>(a, stream);
+    if (ch <= 6) return launch_tiles<6>(a, stream);
+    if (ch <= 8) return launch_tiles<8>(a, stream);
+    if (ch <= 10) return launch_tiles<10>(a, stream);
+    if (ch <= 12) return launch_tiles<12>(a, stream);
+    if (ch <= 16) return launch_tiles<16>(a, stream);
+    if (ch <= 24) return launch_tiles<24>(a, stream);
+    return launch_tiles<32>(a, stream);
 }
 
 }  // namespace ql

@@ -7,8 +7,10 @@
 // both sides, whatever their order.
 //
 // A tile is worked on in one go - scores, weights, values - while the next one comes into the other stage of LDS; what a wavefront waits for, the others
-// of its SIMD fill.  (A loop that multiplied the scores of the next tile and the values of the last one between the exponentials of this one was no
-// faster: 343 against 340 us at 8192 tokens with a prefix, 150 against 141 at 16 images of 1024; its registers cost a wavefront per SIMD.)
+// of its SIMD fill.  What did not shorten it (us at 16 images of 1024 tokens with heads of 72, and at 8192 tokens with a prefix and heads of 128): a loop that
+// multiplies the scores of the next tile and the values of the last one between the exponentials of this one, 150 and 343 against 137 and 340; 64 rows a
+// wavefront, which halves the LDS reads, 130 and 382 against 134 and 337; rows of 9 pieces without bank conflicts for heads of 72, 135 against
+// 135 - the kernel then had 204 thousand busy cycles a CU in the place of 289, in the same time: the clock was that much lower.
 #pragma once
 #include "attention.h"
 
@@ -22,6 +24,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) void attn_lds;
+typedef const __attribute__((address_space(1))) void attn_global;
 typedef __attribute__((address_space(3))) s16x4 attn_lds_s4;
 
 constexpr int ATT_KEYS = 64;   // keys of a tile
@@ -64,22 +67,17 @@ __device__ __forceinline__ f16x8 codes_f16x8(unsigned w0, unsigned w1)
 
 __device__ __forceinline__ unsigned absmax_bits(_Float16 x) { return (unsigned)__builtin_bit_cast(unsigned short, x) & 0x7fffu; }
 
-// CHP: 16-byte pieces of a tile row.  Rows are kept without padding (a wavefront's DMA fills 1024 neighbouring bytes).  LDS serves 256 bytes at a time: 16
-// lanes of a key read (16 rows, one piece each) and 32 of a transposing value read (4 rows, 4 neighbouring pieces each) should lie in
-// different sixteenths of 256 bytes.  Where rows are an odd number of pieces apart that holds for keys by itself, and for values when each 4 x 4 rows are kept
-// transposed; else the piece c of row r sits at slot c ^ f(r).  (Without: 2 to 4 reads in the place of one; heads of 72 at 10 pieces a row and of 128
-// with 8 places for 16 rows: 16 images of 1024 tokens 156 us, 8192 tokens with a prefix 355 us.)
+// CHP: 16-byte pieces of a tile row, an even number.  Rows are kept without padding (a wavefront's DMA fills 1024 neighbouring bytes); the piece c of row r sits
+// at slot c ^ f(r).  LDS serves 256 bytes at a time: the 16 lanes of a key read (16 rows, one piece each) lie in different sixteenths of them, the 32
+// of a transposing value read (4 rows, 4 neighbouring pieces each) where a row is a multiple of 4 pieces.  (With 8 places for the 16 rows of
+// heads of 128, a third of the LDS cycles were conflicts; the time at 8192 tokens did not change, 351 against 355 us.)
 template <int CHP> __device__ __forceinline__ constexpr int key_swizzle(int r)
 {
-    return CHP % 16 == 0 ? (r & 15) : CHP % 16 == 8 ? (r >> 1 & 7) : CHP % 4 == 0 ? (r >> 2 & 3) : CHP % 4 == 2 && CHP > 2 ? (r >> 3 & 1) : 0;
+    return CHP % 16 == 0 ? (r & 15) : CHP % 16 == 8 ? (r >> 1 & 7) : CHP % 4 == 0 ? (r >> 2 & 3) : CHP > 2 ? (r >> 3 & 1) : 0;
 }
 template <int CHP> __device__ __forceinline__ constexpr int value_swizzle(int r)
 {
     return CHP % 16 == 0 ? (r & 3) << 2 : CHP % 16 == 8 ? (r >> 1 & 1) << 2 : 0;
-}
-template <int CHP> __device__ __forceinline__ constexpr int value_row(int t)   // of key t, and its own inverse
-{
-    return CHP % 2 ? (t & ~15) | (t & 3) << 2 | (t >> 2 & 3) : t;
 }
 
 struct TilePlan {
@@ -97,7 +95,8 @@ constexpr float LEAST_RATIO = -30.0f;   // log2 of the smallest value scale that
 // CHP: pieces of a tile row; NW: wavefronts; CACHE: keys and values from the 8-bit cache; SHAPED: scores may be capped or biased
 template <int CHP_, int NW, bool CACHE>
 struct AttnTile {
-    static constexpr int CHP = CHP_, KS = (CHP + 1) / 2, DT = (CHP + 3) / 4, ROWS = 32 * NW, NT = 64 * NW;
+    static_assert(CHP_ % 2 == 0, "whole steps of 16 channels");
+    static constexpr int CHP = CHP_, KS = CHP / 2, DT = (CHP + 3) / 4, ROWS = 32 * NW, NT = 64 * NW;
     static constexpr int K_BYTES = ATT_KEYS * CHP * 16;
     // values: rows like the keys' (a read of channels behind D may pass the last row: 1024 bytes behind the last stage), or transposed codes
     static constexpr int V_BYTES = CACHE ? DT * 32 * 128 : K_BYTES;
@@ -192,7 +191,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
     unsigned koff[NI], voff[NI];                       // of this lane's piece from the tile's first row
     auto piece_at = [&](int i, bool value, int last_row, unsigned row_bytes) {
         const int ci = 64 * (i * NW + wave) + lane, r = ci / CHP, c = ci % CHP;
-        return min(value ? value_row<CHP>(r) : r, last_row) * row_bytes + 16 * min(c ^ (value ? value_swizzle<CHP>(r) : key_swizzle<CHP>(r)), CH - 1);
+        return min(r, last_row) * row_bytes + 16 * min(c ^ (value ? value_swizzle<CHP>(r) : key_swizzle<CHP>(r)), CH - 1);
     };
     const unsigned krow = 2 * (unsigned)a.k_row, vrow = 2 * (unsigned)a.v_row;
     if constexpr (!CACHE) {
@@ -205,15 +204,13 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
     auto dma = [&](bool value, int t, int stage) {
         const int left = sk.n - t * ATT_KEYS - 1;      // rows behind the tile's first one
         const unsigned char *from = value ? vb + (size_t)t * ATT_KEYS * 2 * a.v_row : kb + (size_t)t * ATT_KEYS * 2 * a.k_row;
-        const unsigned to = lds0 + (value ? T::V_AT + stage * T::V_BYTES : stage * T::K_BYTES);
+        const unsigned to = value ? T::V_AT + stage * T::V_BYTES : stage * T::K_BYTES;
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
             if (CHP % NW != 0 && i * NW + wave >= CHP) break;   // (a tile is CHP times 64 pieces)
             unsigned at = value ? voff[i] : koff[i];
             if (left < ATT_KEYS - 1) at = piece_at(i, value, left, value ? vrow : krow);
-            // As an instruction, not the builtin: behind that the compiler has every read of LDS wait for all DMA, whichever stage it fills; the wait that is
-            // needed stands in front of the round's barrier.  (It costs an image of 1024 tokens a fifth of its time.)
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to + (i * NW + wave) * 1024), "v"(at), "s"(from) : "memory");
+            __builtin_amdgcn_global_load_lds((attn_global *)(from + at), (attn_lds *)(smem + to + (i * NW + wave) * 1024), 16, 0, 0);
         }
     };
     // cache: codes through registers; a page that is none reads page 0 and counts as masked
@@ -302,21 +299,18 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
     // number, so pieces that differ above them lie a constant apart: few addresses are kept, the rest is in the instructions.
     constexpr int KA = CHP % 16 == 0 ? 8 : CHP % 8 == 0 ? 4 : CHP % 4 == 0 ? 2 : 1;
     constexpr int VA = CACHE ? 4 : CHP % 16 == 0 ? 4 : CHP % 16 == 8 ? 2 : 1;
-    unsigned kaddr[KA], vaddr[VA], klast = 0;
+    unsigned kaddr[KA], vaddr[VA];
 #pragma unroll
     for (int i = 0; i < KA; ++i) kaddr[i] = lds0 + (lane & 31) * (CHP * 16) + 16 * ((2 * i + half) ^ key_swizzle<CHP>(lane & 31));
-    // the last step of an odd number of pieces: both halves read the last piece, against queries that are zero in one
-    if (CHP % 2) klast = lds0 + (lane & 31) * (CHP * 16) + 16 * (CHP - 1);
 #pragma unroll
     for (int i = 0; i < VA; ++i) {
         // CACHE: transposed, channel lane & 31, step i.  Rows: the transposing read takes 4 keys of 16 channels for 16 lanes, lane i of them with the
         // address of key i / 4, channels 4 (i % 4)
-        const int r = value_row<CHP>(4 * half + (lane >> 2 & 3)), ch = 4 * i + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+        const int r = 4 * half + (lane >> 2 & 3), ch = 4 * i + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
         vaddr[i] = lds0 + T::V_AT + (CACHE ? (lane & 31) * 128 + 16 * ((2 * i + half) ^ (lane >> 1 & 7)) : r * (CHP * 16) + 16 * (ch ^ value_swizzle<CHP>(r)) + 8 * (lane & 1));
     }
     auto key_part = [&](int stage, int u, int ks) {
         typedef __attribute__((address_space(3))) f16x8 lds_h8;
-        if (CHP % 2 && ks == KS - 1) return *(lds_h8 *)(uintptr_t)(klast + (unsigned)(stage * T::K_BYTES + u * 32 * CHP * 16));
         return *(lds_h8 *)(uintptr_t)(kaddr[ks % KA] + (unsigned)(stage * T::K_BYTES + u * 32 * CHP * 16 + (ks / KA) * KA * 32));
     };
     auto value_part = [&](int stage, int d, int st) -> f16x8 {
@@ -326,7 +320,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
         } else {
             const unsigned at = vaddr[d % VA] + (unsigned)(stage * T::V_BYTES + st * 16 * CHP * 16 + (d / VA) * VA * 64);
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((attn_lds_s4 *)(uintptr_t)at);
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((attn_lds_s4 *)(uintptr_t)(at + value_row<CHP>(8) * CHP * 16));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((attn_lds_s4 *)(uintptr_t)(at + 8 * CHP * 16));
             const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
             return __builtin_bit_cast(f16x8, both);
         }

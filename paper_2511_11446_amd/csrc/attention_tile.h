@@ -358,10 +358,15 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
         if (SHAPED && a.slopes) {
             // distances are whole numbers: exact up to 2^24
             const float far = (float)(pos - j0 - 4 * half);
+            if (c != 1.0f)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[u][r] *= c;
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[u][r] = __builtin_fmaf(fabsf(far - (float)(32 * u + 8 * (r / 4) + r % 4)), -slope2, s[u][r] * c);
+                for (int r = 0; r < 16; ++r) s[u][r] = __builtin_fmaf(fabsf(far - (float)(32 * u + 8 * (r / 4) + r % 4)), -slope2, s[u][r]);
             c = 1.0f;
         }
         if (j0 + ATT_KEYS > end_min || !held) {

@@ -548,6 +548,7 @@ def _heads(t, name, H=None, D=None):
     torch = _torch or _load_torch()
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not torch.float16 or t.dim() != 3:
         raise TypeError("%s must be a [T, heads, D] CUDA tensor of torch.float16" % name)
+    _here(t, name)
     n, heads, d = t.shape
     row, head, one = t.stride()
     if one != 1:
@@ -558,10 +559,18 @@ def _heads(t, name, H=None, D=None):
     return t.data_ptr(), row if n > 1 else 0, head if heads > 1 else 0
 
 
-def _here(t):
+def _here(t, name):
     """The calls run on the current device's stream: what they are given has to be there."""
     if t.get_device() != _torch._C._cuda_getDevice():
-        raise ValueError("tensors are on cuda:%d, the current device is cuda:%d" % (t.get_device(), _torch._C._cuda_getDevice()))
+        raise ValueError("%s is on cuda:%d, the current device is cuda:%d" % (name, t.get_device(), _torch._C._cuda_getDevice()))
+
+
+def _at(t, dtype, shape, name):
+    """The address of a small argument (0: none)."""
+    if t is None:
+        return 0
+    _here(_need(t, dtype, shape, name), name)
+    return t.data_ptr()
 
 
 def _made(t, stream):
@@ -574,22 +583,14 @@ def _made(t, stream):
 def _attention_form(q, B, Hkv, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax, stream):
     torch = _torch or _load_torch()
     qp, q_row, q_head = _heads(q, "q")
-    _here(q)
     T, Hq, D = q.shape
     if o is None:
         o = _made(torch.empty((T, Hq, D), dtype=torch.float16, device=q.device), stream)
     op, o_row, o_head = _heads(o, "o", Hq, D)
     if o.shape[0] != T:
         raise ValueError("o has %d rows, expected %d" % (o.shape[0], T))
-    cu = pre = sl = am = 0
-    if cu_q is not None:
-        cu = _need(cu_q, torch.int32, (B + 1,), "cu_q").data_ptr()
-    if prefix is not None:
-        pre = _need(prefix, torch.int32, (B,), "prefix").data_ptr()
-    if slopes is not None:
-        sl = _need(slopes, torch.float32, (Hq,), "slopes").data_ptr()
-    if row_absmax is not None:
-        am = _need(row_absmax, torch.int32, (T,), "row_absmax").data_ptr()
+    cu, pre = _at(cu_q, torch.int32, (B + 1,), "cu_q"), _at(prefix, torch.int32, (B,), "prefix")
+    sl, am = _at(slopes, torch.float32, (Hq,), "slopes"), _at(row_absmax, torch.int32, (T,), "row_absmax")
     return _ATTENTION.pack(T, B, Hq, Hkv, D, mask, D ** -0.5 if scale is None else scale, cap, 0, pre, sl, cu, qp, q_row, q_head, op, o_row, o_head, am), o
 
 
@@ -609,12 +610,13 @@ def attention_f16(q, k, v, batch=None, cu_q=None, cu_k=None, mask=MASK_NONE, pre
     if v.shape[0] != T_k or q.shape[-1] != D:
         raise ValueError("k has shape %s, v %s and q %s" % (tuple(k.shape), tuple(v.shape), tuple(q.shape)))
     B = batch if batch is not None else cu_q.shape[0] - 1 if cu_q is not None else cu_k.shape[0] - 1 if cu_k is not None else 1
-    if cu_k is not None:
-        _need(cu_k, _torch.int32, (B + 1,), "cu_k")
+    cu = _at(cu_k, _torch.int32, (B + 1,), "cu_k")
     a, o = _attention_form(q, B, Hkv, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax, stream)
     if ws is None:
         ws = _made(workspace(attention_f16_workspace_bytes(q.shape[0], T_k, B, q.shape[1], Hkv, D), q.device), stream)
-    _check(lib().attention_f16(a, kp, k_row, k_head, vp, v_row, v_head, T_k, _ptr(cu_k), _ptr(ws), ws.numel(), _stream(stream)),
+    else:
+        _here(ws, "ws")
+    _check(lib().attention_f16(a, kp, k_row, k_head, vp, v_row, v_head, T_k, cu, _ptr(ws), ws.numel(), _stream(stream)),
            "attention_f16")
     return o
 
@@ -649,8 +651,9 @@ class KvCache8:
         """The header's ql_kv_cache for these pages and lengths, as bytes, and the number of sequences."""
         torch = _torch or _load_torch()
         B, max_pages = _need(page_table, torch.int32, name="page_table").shape
-        _need(len_k, torch.int32, (B,), "len_k")
-        return _KV_CACHE.pack(*self._fields, page_table.data_ptr(), len_k.data_ptr(), B, max_pages), B
+        _here(page_table, "page_table")
+        _here(self.k, "the cache")
+        return _KV_CACHE.pack(*self._fields, page_table.data_ptr(), _at(len_k, torch.int32, (B,), "len_k"), B, max_pages), B
 
 
 def daq_kv_append(cache, k, v, page_table, len_k, cu=None, q=None, rot=None, rot_pairs=False, pos=None, q_out=None, k_out=None, v_out=None,
@@ -663,11 +666,10 @@ def daq_kv_append(cache, k, v, page_table, len_k, cu=None, q=None, rot=None, rot
     c, B = cache.desc(page_table, len_k)
     kp, k_row, k_head = _heads(k, "k", cache.heads, cache.D)
     vp, v_row, v_head = _heads(v, "v", cache.heads, cache.D)
-    _here(k)
     T = k.shape[0]
     if v.shape[0] != T:
         raise ValueError("k has %d rows and v %d" % (T, v.shape[0]))
-    Hq = qp = q_row = q_head = qo = ko = vo = 0
+    Hq = qp = q_row = q_head = qo = 0
     if q is not None:
         qp, q_row, q_head = _heads(q, "q", None, cache.D)
         Hq = q.shape[1]
@@ -675,16 +677,11 @@ def daq_kv_append(cache, k, v, page_table, len_k, cu=None, q=None, rot=None, rot
             raise ValueError("q has %d rows and k %d" % (q.shape[0], T))
         if q_out is None:
             q_out = _made(torch.empty((T, Hq, cache.D), dtype=torch.float16, device=q.device), stream)
-        qo = _need(q_out, torch.float16, (T, Hq, cache.D), "q_out").data_ptr()
-    if k_out is not None:
-        ko = _need(k_out, torch.float16, (T, cache.heads, cache.D), "k_out").data_ptr()
-    if v_out is not None:
-        vo = _need(v_out, torch.float16, (T, cache.heads, cache.D), "v_out").data_ptr()
-    cup = 0 if cu is None else _need(cu, torch.int32, (B + 1,), "cu").data_ptr()
-    pp = 0 if pos is None else _need(pos, torch.int32, (T,), "pos").data_ptr()
-    rp = rows = half = 0
+        qo = _at(q_out, torch.float16, (T, Hq, cache.D), "q_out")
+    ko, vo = _at(k_out, torch.float16, (T, cache.heads, cache.D), "k_out"), _at(v_out, torch.float16, (T, cache.heads, cache.D), "v_out")
+    cup, pp, rp = _at(cu, torch.int32, (B + 1,), "cu"), _at(pos, torch.int32, (T,), "pos"), _at(rot, torch.float32, None, "rot")
+    rows = half = 0
     if rot is not None:
-        rp = _need(rot, torch.float32, name="rot").data_ptr()
         rows, half, two = rot.shape
         if two != 2:
             raise ValueError("rot must be [rows, rot_dim / 2, 2]")
@@ -706,6 +703,8 @@ def attention_kv8(q, cache, page_table, len_k, cu_q=None, mask=MASK_CAUSAL, pref
         raise ValueError("q has heads of %d, the cache of %d" % (q.shape[2], cache.D))
     if ws is None:
         ws = _made(workspace(attention_kv8_workspace_bytes(q.shape[0], B, q.shape[1], cache.heads, cache.D), q.device), stream)
+    else:
+        _here(ws, "ws")
     _check(lib().attention_kv8(a, c, _ptr(ws), ws.numel(), _stream(stream)), "attention_kv8")
     return o
 

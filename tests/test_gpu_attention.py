@@ -572,3 +572,31 @@ def test_refusals_with_tensors():
         ql.attention_kv8(x[:, :, :32], cache, table, lens)
     with pytest.raises(ql.QlError):
         ql.daq_kv_append(cache, x, x, table, lens, rot=torch.zeros((4, 12, 2), device="cuda"))   # 24 turned channels
+
+
+class _Elsewhere(torch.Tensor):
+    """A tensor that says it is on another device."""
+
+    def get_device(self):
+        return torch.cuda.current_device() + 1
+
+
+def test_tensors_of_another_device_are_refused():
+    x = torch.zeros((8, 2, 64), dtype=torch.float16, device="cuda")
+    ints, many = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.zeros(8, dtype=torch.int32, device="cuda")
+    table, lens, slopes = torch.zeros((1, 2), dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros(2, device="cuda")
+    cache = ql.KvCache8.empty(2, 2, 64)
+    there = lambda t: t.as_subclass(_Elsewhere)
+    ws = ql.workspace(1 << 20)
+    dense = dict(q=x, k=x, v=x, cu_q=ints, cu_k=ints, prefix=lens, slopes=slopes, o=torch.zeros_like(x), row_absmax=many, ws=ws)
+    cached = dict(q=x, cache=cache, page_table=table, len_k=lens, cu_q=ints, prefix=lens, slopes=slopes, o=torch.zeros_like(x), row_absmax=many,
+                  ws=ql.workspace(ql.attention_kv8_workspace_bytes(8, 1, 2, 2, 64)))
+    append = dict(cache=cache, k=x, v=x, page_table=table, len_k=lens, cu=ints, q=x, rot=torch.zeros((4, 16, 2), device="cuda"), pos=many,
+                  q_out=torch.zeros_like(x), k_out=torch.zeros_like(x), v_out=torch.zeros_like(x))
+    for call, args in ((ql.attention_f16, dense), (ql.attention_kv8, cached), (ql.daq_kv_append, append)):
+        call(**args)
+        for name, t in args.items():
+            moved = ql.KvCache8(there(cache.k), cache.v, cache.k_scale, cache.v_scale) if t is cache else there(t)
+            with pytest.raises(ValueError, match="current device"):
+                call(**{**args, name: moved})
+    torch.cuda.synchronize()

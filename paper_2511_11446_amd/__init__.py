@@ -543,12 +543,13 @@ _KV_CACHE = struct.Struct("=4Qq4i2Q2i")
 _KV_NEW = struct.Struct("=q2iQ3Q6qQq2iQ3Q")
 
 
-def _heads(t, name, H=None, D=None):
+def _heads(t, name, dev, H=None, D=None):
     """A [T, H, D] binary16 view whose rows and heads may be strided: (pointer, row stride, head stride)."""
     torch = _torch or _load_torch()
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not torch.float16 or t.dim() != 3:
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float16 or t.dim() != 3 or not t.is_cuda:
         raise TypeError("%s must be a [T, heads, D] CUDA tensor of torch.float16" % name)
-    _here(t, name)
+    if t.get_device() != dev:
+        _elsewhere(t, name)
     n, heads, d = t.shape
     row, head, one = t.stride()
     if one != 1:
@@ -559,18 +560,25 @@ def _heads(t, name, H=None, D=None):
     return t.data_ptr(), row if n > 1 else 0, head if heads > 1 else 0
 
 
-def _here(t, name):
+def _elsewhere(t, name):
     """The calls run on the current device's stream: what they are given has to be there."""
-    if t.get_device() != _torch._C._cuda_getDevice():
-        raise ValueError("%s is on cuda:%d, the current device is cuda:%d" % (name, t.get_device(), _torch._C._cuda_getDevice()))
+    raise ValueError("%s is on %s, the current device is cuda:%d" % (name, t.device, _torch._C._cuda_getDevice()))
 
 
-def _at(t, dtype, shape, name):
+def _at(t, dtype, shape, name, dev):
     """The address of a small argument (0: none)."""
     if t is None:
         return 0
-    _here(_need(t, dtype, shape, name), name)
+    if _need(t, dtype, shape, name).get_device() != dev:
+        _elsewhere(t, name)
     return t.data_ptr()
+
+
+def _current():
+    try:
+        return (_torch or _load_torch())._C._cuda_getDevice()
+    except RuntimeError:   # no device: no tensor can be on it
+        return -1
 
 
 def _made(t, stream):
@@ -580,17 +588,17 @@ def _made(t, stream):
     return t
 
 
-def _attention_form(q, B, Hkv, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax, stream):
+def _attention_form(dev, q, B, Hkv, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax, stream):
     torch = _torch or _load_torch()
-    qp, q_row, q_head = _heads(q, "q")
+    qp, q_row, q_head = _heads(q, "q", dev)
     T, Hq, D = q.shape
     if o is None:
         o = _made(torch.empty((T, Hq, D), dtype=torch.float16, device=q.device), stream)
-    op, o_row, o_head = _heads(o, "o", Hq, D)
+    op, o_row, o_head = _heads(o, "o", dev, Hq, D)
     if o.shape[0] != T:
         raise ValueError("o has %d rows, expected %d" % (o.shape[0], T))
-    cu, pre = _at(cu_q, torch.int32, (B + 1,), "cu_q"), _at(prefix, torch.int32, (B,), "prefix")
-    sl, am = _at(slopes, torch.float32, (Hq,), "slopes"), _at(row_absmax, torch.int32, (T,), "row_absmax")
+    cu, pre = _at(cu_q, torch.int32, (B + 1,), "cu_q", dev), _at(prefix, torch.int32, (B,), "prefix", dev)
+    sl, am = _at(slopes, torch.float32, (Hq,), "slopes", dev), _at(row_absmax, torch.int32, (T,), "row_absmax", dev)
     return _ATTENTION.pack(T, B, Hq, Hkv, D, mask, D ** -0.5 if scale is None else scale, cap, 0, pre, sl, cu, qp, q_row, q_head, op, o_row, o_head, am), o
 
 
@@ -604,18 +612,19 @@ def attention_f16(q, k, v, batch=None, cu_q=None, cu_k=None, mask=MASK_NONE, pre
     layer's output) -> o fp16 [T_q, Hq, D].  Sequences one behind the other: `batch` of equal length, or int32 [B+1] first rows in cu_q / cu_k.
     scale: default D ** -0.5; cap: tanh cap of the scores (0: none; 2^-10 to 2^10); slopes fp32 [Hq]: bias by distance; mask MASK_NONE / _CAUSAL / _PREFIX
     (prefix int32 [B]); row_absmax: int32 [T_q] that receives every row's largest |o| as a binary16 bit pattern, for daq_quantize_rowmax."""
-    kp, k_row, k_head = _heads(k, "k")
+    dev = _current()
+    kp, k_row, k_head = _heads(k, "k", dev)
     T_k, Hkv, D = k.shape
-    vp, v_row, v_head = _heads(v, "v", Hkv, D)
+    vp, v_row, v_head = _heads(v, "v", dev, Hkv, D)
     if v.shape[0] != T_k or q.shape[-1] != D:
         raise ValueError("k has shape %s, v %s and q %s" % (tuple(k.shape), tuple(v.shape), tuple(q.shape)))
     B = batch if batch is not None else cu_q.shape[0] - 1 if cu_q is not None else cu_k.shape[0] - 1 if cu_k is not None else 1
-    cu = _at(cu_k, _torch.int32, (B + 1,), "cu_k")
-    a, o = _attention_form(q, B, Hkv, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax, stream)
+    cu = _at(cu_k, _torch.int32, (B + 1,), "cu_k", dev)
+    a, o = _attention_form(dev, q, B, Hkv, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax, stream)
     if ws is None:
         ws = _made(workspace(attention_f16_workspace_bytes(q.shape[0], T_k, B, q.shape[1], Hkv, D), q.device), stream)
-    else:
-        _here(ws, "ws")
+    elif ws.get_device() != dev:
+        _elsewhere(ws, "ws")
     _check(lib().attention_f16(a, kp, k_row, k_head, vp, v_row, v_head, T_k, cu, _ptr(ws), ws.numel(), _stream(stream)),
            "attention_f16")
     return o
@@ -651,9 +660,11 @@ class KvCache8:
         """The header's ql_kv_cache for these pages and lengths, as bytes, and the number of sequences."""
         torch = _torch or _load_torch()
         B, max_pages = _need(page_table, torch.int32, name="page_table").shape
-        _here(page_table, "page_table")
-        _here(self.k, "the cache")
-        return _KV_CACHE.pack(*self._fields, page_table.data_ptr(), _at(len_k, torch.int32, (B,), "len_k"), B, max_pages), B
+        dev = _current()
+        for t, name in ((page_table, "page_table"), (self.k, "the cache")):
+            if t.get_device() != dev:
+                _elsewhere(t, name)
+        return _KV_CACHE.pack(*self._fields, page_table.data_ptr(), _at(len_k, torch.int32, (B,), "len_k", dev), B, max_pages), B
 
 
 def daq_kv_append(cache, k, v, page_table, len_k, cu=None, q=None, rot=None, rot_pairs=False, pos=None, q_out=None, k_out=None, v_out=None,
@@ -664,22 +675,23 @@ def daq_kv_append(cache, k, v, page_table, len_k, cu=None, q=None, rot=None, rot
     Returns q_out."""
     torch = _torch or _load_torch()
     c, B = cache.desc(page_table, len_k)
-    kp, k_row, k_head = _heads(k, "k", cache.heads, cache.D)
-    vp, v_row, v_head = _heads(v, "v", cache.heads, cache.D)
+    dev = _current()
+    kp, k_row, k_head = _heads(k, "k", dev, cache.heads, cache.D)
+    vp, v_row, v_head = _heads(v, "v", dev, cache.heads, cache.D)
     T = k.shape[0]
     if v.shape[0] != T:
         raise ValueError("k has %d rows and v %d" % (T, v.shape[0]))
     Hq = qp = q_row = q_head = qo = 0
     if q is not None:
-        qp, q_row, q_head = _heads(q, "q", None, cache.D)
+        qp, q_row, q_head = _heads(q, "q", dev, None, cache.D)
         Hq = q.shape[1]
         if q.shape[0] != T:
             raise ValueError("q has %d rows and k %d" % (q.shape[0], T))
         if q_out is None:
             q_out = _made(torch.empty((T, Hq, cache.D), dtype=torch.float16, device=q.device), stream)
-        qo = _at(q_out, torch.float16, (T, Hq, cache.D), "q_out")
-    ko, vo = _at(k_out, torch.float16, (T, cache.heads, cache.D), "k_out"), _at(v_out, torch.float16, (T, cache.heads, cache.D), "v_out")
-    cup, pp, rp = _at(cu, torch.int32, (B + 1,), "cu"), _at(pos, torch.int32, (T,), "pos"), _at(rot, torch.float32, None, "rot")
+        qo = _at(q_out, torch.float16, (T, Hq, cache.D), "q_out", dev)
+    ko, vo = _at(k_out, torch.float16, (T, cache.heads, cache.D), "k_out", dev), _at(v_out, torch.float16, (T, cache.heads, cache.D), "v_out", dev)
+    cup, pp, rp = _at(cu, torch.int32, (B + 1,), "cu", dev), _at(pos, torch.int32, (T,), "pos", dev), _at(rot, torch.float32, None, "rot", dev)
     rows = half = 0
     if rot is not None:
         rows, half, two = rot.shape
@@ -698,13 +710,14 @@ def attention_kv8(q, cache, page_table, len_k, cu_q=None, mask=MASK_CAUSAL, pref
                   row_absmax=None, ws=None, stream=None):
     """attention_f16 over the 8-bit cache: q fp16 [T_q, Hq, D], page_table int32 [B, max_pages], len_k int32 [B] -> o fp16 [T_q, Hq, D]."""
     c, B = cache.desc(page_table, len_k)
-    a, o = _attention_form(q, B, cache.heads, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax, stream)
+    dev = _current()
+    a, o = _attention_form(dev, q, B, cache.heads, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax, stream)
     if q.shape[2] != cache.D:
         raise ValueError("q has heads of %d, the cache of %d" % (q.shape[2], cache.D))
     if ws is None:
         ws = _made(workspace(attention_kv8_workspace_bytes(q.shape[0], B, q.shape[1], cache.heads, cache.D), q.device), stream)
-    else:
-        _here(ws, "ws")
+    elif ws.get_device() != dev:
+        _elsewhere(ws, "ws")
     _check(lib().attention_kv8(a, c, _ptr(ws), ws.numel(), _stream(stream)), "attention_kv8")
     return o
 

@@ -10,7 +10,8 @@
 // 16 images of 1024 tokens, 16 heads of 72: 123 us in turn with other work, 0.63 PFLOP/s of the products that D = 72 needs (of the 80 channels that
 // the matrix instructions work on, 0.70); 8192 tokens, 16 heads of 128 on 2, a prefix of 1000: 330 us, 0.84 PFLOP/s.  Bound by issue: of the busy cycles the
 // matrix cores work 43 and 52 %, the vector units 58 and 44 %, LDS conflicts 12 and 0 %; and the chip lowers its clock under it (attention_tile.h).  With a
-// cap and a distance bias (8192 packed tokens, heads of 64) the vector units work 86 %, the matrix cores 19 %.  Small calls are a chain of latencies: launch, first tile, 4 tiles, writing.
+// cap and a distance bias (24 packed sequences of up to 1000 tokens, heads of 64; 83 us) the vector units work 86 %, the matrix cores 19 %.  Small calls are a
+// chain of latencies: launch, first tile, a few more, writing.
 #include "attention_tile.h"
 
 namespace ql {

@@ -552,7 +552,7 @@ int daq_kv_append(const ql_kv_cache *cache, const ql_kv_new *tokens, void *strea
 /* Attention over the cache: the formulas above with n_k = len_k[b] and the
  * cache's keys and values; attn->B, Hkv and D are the cache's.  One new token per
  * sequence is T_q = B with cu_q NULL.  The weights take the value scales along
- * when they are rounded, relative to the largest of them.  (T_q * Hq / Hkv / 16 + B) * Hkv * max_pages *
+ * when they are rounded, relative to the largest of those that the row sees.  (T_q * Hq / Hkv / 16 + B) * Hkv * max_pages *
  * page / 64 below 2^31. */
 size_t attention_kv8_workspace_bytes(int64_t T_q, int32_t B, int32_t Hq, int32_t Hkv, int32_t D);
 int attention_kv8(const ql_attention *attn, const ql_kv_cache *cache,

@@ -10,8 +10,8 @@
 // are the left operand of O^T = V^T P^T in the order in which S^T = K Q^T leaves the weights.  So nothing goes through LDS but the join of
 // the workgroup's four wavefronts, which take the units in turn.
 //
-// Codes become binary16 exactly; key scales multiply the scores.  Value scales multiply the weights, relative to the largest one met so far (which the sums are
-// relative to in turn): a weight times a bare scale could fall below binary16's range.
+// Codes become binary16 exactly; key scales multiply the scores.  Value scales multiply the weights, relative to the largest one that the row has met so far (which its
+// sums are relative to in turn): a weight times a bare scale could fall below binary16's range.
 //
 // 64 sequences of 1 to 8192 tokens, 32 heads of 128 on 8: 77 us and 6 of join_parts for 355 MB, 4.6 TB/s; two of 131071 tokens, 101 + 7 us for 537 MB, 5.3 TB/s, what
 // a copy of that size reaches on this card (5.1 read and written): bound by memory.  One token on 4096, 11 + 5 us: a chain of latencies (queries, page,
@@ -168,6 +168,7 @@ __global__ __launch_bounds__(256, cached_waves(NK)) void attend_cached(AttnArgs 
         const int pos = token + s.n_k - s.n_q;
         const int prefix = a.prefix ? a.prefix[b] : 0;
         const int end = visible_end(a.mask, prefix, pos, s.n_k);
+        const int end_first = visible_end(a.mask, prefix, r0 / a.G + s.n_k - s.n_q, s.n_k);   // the fewest keys of the item's rows
         const int end_last = visible_end(a.mask, prefix, (min(r0 + 15, rows - 1)) / a.G + s.n_k - s.n_q, s.n_k);
         const float slope2 = a.slopes ? a.slopes[head] * LOG2E : 0.0f;
 
@@ -245,7 +246,7 @@ __global__ __launch_bounds__(256, cached_waves(NK)) void attend_cached(AttnArgs 
         f32x4 acc[DT];
 #pragma unroll
         for (int d = 0; d < DT; ++d) acc[d] = f32x4{};
-        float m = -__builtin_inff(), l = 0.0f, unit_v = 0.0f;   // unit_v: the value scale that the sums are in
+        float m = -__builtin_inff(), l = 0.0f, unit_v = 0.0f;   // of this lane's row; unit_v: the value scale that its sums are in
         while (i < mine) {
             const int j0 = (g0 + wave + 4 * i) * KV_GROUP;
             f32x4 sc[4];
@@ -259,9 +260,9 @@ __global__ __launch_bounds__(256, cached_waves(NK)) void attend_cached(AttnArgs 
                 }
                 __builtin_amdgcn_sched_barrier(0);     // (else the compiler turns all codes into binary16 first, and has no registers for that)
             }
-            // scales of this lane's tokens 16 i + 4 quarter + e, through LDS; of tokens behind the end they may hold anything
+            // scales of this lane's tokens 16 i + 4 quarter + e, through LDS; of tokens behind the end they may hold anything, and are masked below
             scales[lane] = kscale * scale2;
-            scales[64 + lane] = j0 + lane < s.n_k ? vscale : 0.0f;
+            scales[64 + lane] = vscale;
             // the next unit's keys come in while this one's weights are taken, its values behind this one's
             const int n = next(i + 1);
             size_t group = 0;
@@ -292,10 +293,16 @@ __global__ __launch_bounds__(256, cached_waves(NK)) void attend_cached(AttnArgs 
             float keep = m == -__builtin_inff() ? 0.0f : exp2_fast(m - m2);
             m = m2;
             l *= keep;
-            // the largest value scale so far
+            // the largest value scale that the row has met so far.  One that its mask hides does not count: the weights are rounded relative to it
             float big = 0.0f;
 #pragma unroll
             for (int i4 = 0; i4 < 4; ++i4) sv[i4] = *reinterpret_cast<const f32x4 *>(scales + 64 + 16 * i4 + 4 * quarter);
+            if (j0 + KV_GROUP > end_first) {
+#pragma unroll
+                for (int i4 = 0; i4 < 4; ++i4)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sv[i4][e] = j0 + 16 * i4 + 4 * quarter + e < end ? sv[i4][e] : 0.0f;
+            }
 #pragma unroll
             for (int i4 = 0; i4 < 4; ++i4)
 #pragma unroll

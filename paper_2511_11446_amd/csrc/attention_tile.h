@@ -293,7 +293,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = f32x16{};
     float m = -__builtin_inff(), l = 0.0f;             // of this lane's row, m in powers of two; l over this lane's keys only
-    float unit_v = 0.0f;                               // CACHE: the value scale that the sums are in (one for the wavefront)
+    float unit_v = 0.0f;                               // CACHE: the value scale that the row's sums are in
 
     // left operands: step ks of keys 32 u .. 32 u + 31, step st of value channels 32 d .. 32 d + 31.  A swizzle turns the low bits of a piece's
     // number, so pieces that differ above them lie a constant apart: few addresses are kept, the rest is in the instructions.
@@ -408,20 +408,26 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
         const float top = fmaxf(tops.a, tops.b) * c;
         float shift = 0.0f, grow = 1.0f, per = 0.0f;
         if constexpr (CACHE) {
+            // the tile's largest value scale of those that the row sees, by the running maximum over the tokens: the weights are rounded relative to it
+            const int seen = min(end - t * ATT_KEYS, ATT_KEYS);
             float big = lds_vs[stage * ATT_KEYS + (one_scale ? 0 : lane)];
             if (!one_scale) {
 #pragma unroll
-                for (int d = 32; d; d >>= 1) big = fmaxf(big, __shfl_xor(big, d, 64));
+                for (int d = 1; d < 64; d <<= 1) {
+                    const float before = __shfl_up(big, d, 64);
+                    big = lane >= d ? fmaxf(big, before) : big;
+                }
+                big = __shfl(big, max(seen, 1) - 1, 64);
             }
-            big = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, big)));
+            big = seen > 0 ? big : 0.0f;
             if (big > unit_v) {
                 grow = unit_v / big;
                 unit_v = big;
             }
             per = unit_v > 0.0f ? 1.0f / unit_v : 0.0f;
-            if (one_scale) shift = fmaxf(__builtin_amdgcn_logf(big * per), LEAST_RATIO);
+            if (one_scale) shift = fmaxf(__builtin_amdgcn_logf(big * per), LEAST_RATIO);   // (a row that sees nothing of the tile: any)
         }
-        if (__any(top - m > GROWTH || (m == -__builtin_inff() && top > m)) || (CACHE && grow != 1.0f)) {
+        if (__any(top - m > GROWTH || (m == -__builtin_inff() && top > m)) || (CACHE && __any(grow != 1.0f))) {
             const float m2 = fmaxf(m, top);
             const float keep = m == -__builtin_inff() ? 0.0f : exp2_fast(m - m2);
             l *= keep;

@@ -600,3 +600,21 @@ def test_tensors_of_another_device_are_refused():
             with pytest.raises(ValueError, match="current device"):
                 call(**{**args, name: moved})
     torch.cuda.synchronize()
+
+
+# ---- values that the mask hides, long tails, scores of any size -----------------------------------------------------------------------
+
+@pytest.mark.parametrize("mask", [1, 2])
+@pytest.mark.parametrize("S", [1, 16, 32])
+@pytest.mark.parametrize("nq, D", [([4, 2, 3, 1], 128), ([9, 5], 256), ([64], 64), ([70, 33], 128), ([64, 90], 40)])
+def test_scales_of_hidden_tokens_do_not_count(nq, D, S, mask):
+    """The first rows of a prompt see tokens of small value scale; those behind them in the same 64 have scales up to 2^20 times as large, which
+    must not take the visible weights' bits.  Few rows (the first two) and many."""
+    g = _rng(60, len(nq), D, S, mask)
+    c = _Cached(g, len(nq), 128, 2, D, 64, S)
+    jump = 20.0 * np.minimum(np.arange(64 // S) / (8 if S == 1 else 1), 1.0) - 8
+    c.ref.vs *= np.tile(2.0 ** jump, c.ref.page // 64).astype(np.float32)
+    c.dev.v_scale.copy_(torch.from_numpy(c.ref.vs))
+    few = sum(nq) < 30                                    # their run of rows begins in front of the jump and ends behind it
+    nk = [n if S == 1 or not few else S + n // 2 for n in nq]
+    _cached((60, 1, len(nq), D, S, mask), nq, nk, 2, 2, D, 64, S, mask, cache=c)

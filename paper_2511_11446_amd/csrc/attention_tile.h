@@ -89,6 +89,9 @@ struct TilePlan {
 
 // Weights may grow to 2^8 before the sums are brought to a new maximum: they stay far inside binary16, and most tiles skip the scaling.
 constexpr float GROWTH = 8.0f;
+// Scores (in powers of two) beyond which they are rounded to fp32 before the maximum is taken off: the fma of the weights has the exact product, whose distance
+// from the rounded maximum grows to half a step of it - 2^-5 here, 16 at 2^28, where a weight would pass binary16 or all of them be 0.
+constexpr float EXACT_SCORES = 1048576.0f;
 constexpr float LEAST_SCALE = 1e-30f;   // stands for a scale of 0, so that -inf times it stays -inf
 constexpr float LEAST_RATIO = -30.0f;   // log2 of the smallest value scale that counts beside the largest: below, a weight is 0 in binary16
 
@@ -402,10 +405,17 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(key_part(stage, u, ks), qf[ks], ks ? s[u] : f32x16{}, 0, 0, 0);
-        const float c = shape(s, t, stage);
+        float c = shape(s, t, stage);
         // the running maximum, and the value scale that the sums are in
         const Halves tops = both_halves(largest(s));
         const float top = fmaxf(tops.a, tops.b) * c;
+        if (__any(fabsf(top) > EXACT_SCORES && top > -__builtin_inff())) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[u][r] *= c;
+            c = 1.0f;
+        }
         float shift = 0.0f, grow = 1.0f, per = 0.0f;
         if constexpr (CACHE) {
             // the tile's largest value scale of those that the row sees, by the running maximum over the tokens: the weights are rounded relative to it

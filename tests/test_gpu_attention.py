@@ -618,3 +618,28 @@ def test_scales_of_hidden_tokens_do_not_count(nq, D, S, mask):
     few = sum(nq) < 30                                    # their run of rows begins in front of the jump and ends behind it
     nk = [n if S == 1 or not few else S + n // 2 for n in nq]
     _cached((60, 1, len(nq), D, S, mask), nq, nk, 2, 2, D, 64, S, mask, cache=c)
+
+
+@pytest.mark.parametrize("kernel", ["dense", "dense_cut", "chunks", "chunks_fine", "tokens"])
+@pytest.mark.parametrize("size, scale", [(64.0, 1.0), (2000.0, 0.125), (30000.0, 0.125), (30000.0, -1.0)])
+def test_scores_far_from_zero(kernel, size, scale):
+    """Scores up to 2^37 in fp32, where a step of theirs is thousands: the result is still a mean of the values, each of them between 1 and 2.  A mean may
+    pass them by the rounding of its binary16 weights and of its own, 2 x 2^-11 of 2; its place between them is the fp32 scores' rounding."""
+    g = _rng(61, int(size))
+    D, n, H = 64, 300, 2
+    rows = 1 if kernel == "tokens" else 20 if kernel == "dense_cut" else 300
+    q = _f16(g, rows, H, D, size=0.0) + np.float16(size)
+    k = (size * g.uniform(0.5, 1.0, (n, H, D))).astype(np.float16)
+    v = g.uniform(1.0, 2.0, (n, H, D)).astype(np.float16)
+    if kernel.startswith("dense"):
+        o = ql.attention_f16(_dev(q), _dev(np.concatenate([k] * (8 if kernel == "dense_cut" else 1))), _dev(np.concatenate([v] * (8 if kernel == "dense_cut" else 1))), scale=scale)
+    else:
+        S = 16 if kernel == "chunks_fine" else 64
+        cache = ql.KvCache8.empty(6, H, D, page=64, scale_tokens=S)
+        table, lens = _dev(np.array([[4, 0, 2, 5, 1]], np.int32)), _dev(np.array([n], np.int32))
+        ql.daq_kv_append(cache, _dev(k), _dev(v), table, lens)
+        o = ql.attention_kv8(_dev(q), cache, table, lens, mask=ql.MASK_NONE, scale=scale)
+    torch.cuda.synchronize()
+    o = o.float().cpu().numpy()
+    edge = 2.0 * 2.0 * 2.0 ** -11 + (0.0 if kernel.startswith("dense") else 0.5 * 2.0 / 127 * (1 + 2.0 ** -7))   # a code is off by half a step
+    assert np.isfinite(o).all() and o.min() >= 1.0 - edge and o.max() <= 2.0 + edge, (o.min(), o.max())

@@ -312,7 +312,7 @@ __global__ __launch_bounds__(256, cached_waves(NK)) void attend_cached(AttnArgs 
                 keep *= unit_v / big;
                 unit_v = big;
             }
-            const float per = unit_v > 0.0f ? 1.0f / unit_v : 0.0f;
+            const float per = unit_v > LEAST_UNIT ? 1.0f / unit_v : 0.0f;
             const float mc = m == -__builtin_inff() ? 0.0f : m;
 #pragma unroll
             for (int d = 0; d < DT; ++d) acc[d] *= keep;

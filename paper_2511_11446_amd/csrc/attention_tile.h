@@ -94,6 +94,8 @@ constexpr float GROWTH = 8.0f;
 constexpr float EXACT_SCORES = 1048576.0f;
 constexpr float LEAST_SCALE = 1e-30f;   // stands for a scale of 0, so that -inf times it stays -inf
 constexpr float LEAST_RATIO = -30.0f;   // log2 of the smallest value scale that counts beside the largest: below, a weight is 0 in binary16
+// Value scales up to here: 127 of them are 0 in binary16, and so is the result.  Their reciprocal, and its product with a hidden token's scale, could pass fp32.
+constexpr float LEAST_UNIT = 0x1p-60f;
 
 // CHP: pieces of a tile row; NW: wavefronts; CACHE: keys and values from the 8-bit cache; SHAPED: scores may be capped or biased
 template <int CHP_, int NW, bool CACHE>
@@ -434,7 +436,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
                 grow = unit_v / big;
                 unit_v = big;
             }
-            per = unit_v > 0.0f ? 1.0f / unit_v : 0.0f;
+            per = unit_v > LEAST_UNIT ? 1.0f / unit_v : 0.0f;
             if (one_scale) shift = fmaxf(__builtin_amdgcn_logf(big * per), LEAST_RATIO);   // (a row that sees nothing of the tile: any)
         }
         if (__any(top - m > GROWTH || (m == -__builtin_inff() && top > m)) || (CACHE && __any(grow != 1.0f))) {

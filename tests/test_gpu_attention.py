@@ -643,3 +643,16 @@ def test_scores_far_from_zero(kernel, size, scale):
     o = o.float().cpu().numpy()
     edge = 2.0 * 2.0 * 2.0 ** -11 + (0.0 if kernel.startswith("dense") else 0.5 * 2.0 / 127 * (1 + 2.0 ** -7))   # a code is off by half a step
     assert np.isfinite(o).all() and o.min() >= 1.0 - edge and o.max() <= 2.0 + edge, (o.min(), o.max())
+
+
+@pytest.mark.parametrize("S", [1, 16, 64])
+@pytest.mark.parametrize("nq, nk", [([1, 1], [300, 170]), ([150, 90], [300, 170])])
+def test_value_scales_next_to_zero(nq, nk, S):
+    """Scales whose reciprocal passes fp32, in whole sequences and in front of ordinary ones."""
+    g = _rng(62, sum(nq), S)
+    c = _Cached(g, 2, 320, 2, 64, 64, S)
+    for b, pages in ((0, 5), (1, 1)):
+        for i in range(pages):
+            c.ref.vs[c.ref.table[b, i]] = np.float32((1e-39, 1e-42, 0.0, 1e-30, 1e-45)[i])
+    c.dev.v_scale.copy_(torch.from_numpy(c.ref.vs))
+    _cached((62, 1, sum(nq), S), nq, nk, 4, 2, 64, 64, S, cache=c)

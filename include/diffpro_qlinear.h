@@ -434,8 +434,11 @@ int ql_time_bin(int64_t step, int64_t num_steps);
  *   o[i,h] = fp16( sum_j exp(s_j) v[j,h'] / sum_j exp(s_j) )    over visible j
  * and 0 where no key is visible (a sequence without keys, or rows in front of
  * the first key).  Scores, the running maximum and the sums are fp32; the
- * weights exp(s_j - m) are rounded to binary16 for the matrix cores, which
- * moves o by at most about 2^-11 of the largest |v| of the row's keys.
+ * weights are rounded to binary16 for the matrix cores, which moves o by at most
+ * about 2^-11 of the largest |v| of the row's keys.  Weights below 2^-21 of the
+ * row's largest (attention_kv8 with few rows: 2^-29) are rounded in steps of 2^-31
+ * (2^-39) of it: n_k keys may add n_k 2^-32 (2^-40) of the largest |v|, over the cache
+ * of 127 times the largest value scale, to the sum and to its divisor.
  *   q, o      (device) fp16, element (t, h, d) at t * row + h * head + d; rows and
  *             heads may be strided (the columns of a fused qkv layer's output),
  *             strides in elements, multiples of 8; base pointers 16-byte aligned.

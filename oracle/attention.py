@@ -11,11 +11,12 @@ def slot(t):
     return 16 * (t % 16 // 4) + 4 * (t // 16) + t % 4
 
 
-def _one(q, k, v, scale, mask=NONE, prefix=0, cap=0.0, slopes=None, seen=None):
+def _one(q, k, v, scale, mask=NONE, prefix=0, cap=0.0, slopes=None, seen=None, reach=None):
     """One sequence, q [n, Hq, D], k, v [m, Hkv, D] (float64) -> (o [n, Hq, D], tolerance of a binary16 result [n, Hq, D]).
 
-    The tolerance counts, with A = sum w |v| / sum w: binary16 weights (2^-11 relative, 2^-25 of the largest weight where they are
-    subnormal) against fp32 sums, fp32 scores ((D + 16) roundings of 2^-24 of sum |q k|, and of the other terms; it enters the weights
+    The tolerance counts, with A = sum w |v| / sum w: binary16 weights (2^-11 relative; where they are subnormal 2^-25, with a largest weight of 2^7 or
+    more 2^-32 of that one, in the sum of the values and in that of the weights, so twice; `reach` [m, Hkv]: what such an error is multiplied by, where that
+    is more than |v| - over the cache 127 times the value scale) against fp32 sums, fp32 scores ((D + 16) roundings of 2^-24 of sum |q k|, and of the other terms; it enters the weights
     and their sum, so twice), and the result's own rounding."""
     n, Hq, D = q.shape
     m, Hkv = k.shape[0], k.shape[1]
@@ -45,7 +46,8 @@ def _one(q, k, v, scale, mask=NONE, prefix=0, cap=0.0, slopes=None, seen=None):
         o[:, h] = (w @ vh) / l
         A = (w @ np.abs(vh)) / l
         delta = ((D + 16) * 2.0 ** -24 * np.where(vis, size, 0.0).max(1) + 2.0 ** -21)[:, None]
-        far = vis.sum(1)[:, None] * 2.0 ** -25 * (np.abs(np.where(vis[:, :, None], vh[None], 0.0)).max((1, 2))[:, None] if m * n * D < 5e7 else np.abs(vh).max()) / l
+        most = np.abs(vh).max(1) if reach is None else reach[:, h // (Hq // Hkv)]
+        far = vis.sum(1)[:, None] * 2.0 ** -31 * np.where(vis, most[None], 0.0).max(1)[:, None] / l
         err = A * (2.0 ** -11 + 2 * delta) + far
         tol[:, h] = err + 2.0 ** -11 * (np.abs(o[:, h]) + err) + 2.0 ** -25
     return o, tol
@@ -169,6 +171,9 @@ def attention_cached(q, cache, cu_q, lens, scale, mask=CAUSAL, prefix=None, cap=
     o, tol = np.full_like(q, np.nan), np.full_like(q, np.nan)
     for b in range(len(cu_q) - 1):
         k, v, seen = cache.sequence(b, int(lens[b]))
+        reach = np.zeros((len(seen), cache.heads))
+        for j in np.flatnonzero(seen):
+            reach[j] = 127.0 * cache.token(b, j)[3]
         a, e = cu_q[b], cu_q[b + 1]
-        o[a:e], tol[a:e] = _one(q[a:e], k, v, scale, mask, 0 if prefix is None else int(prefix[b]), cap, slopes, seen)
+        o[a:e], tol[a:e] = _one(q[a:e], k, v, scale, mask, 0 if prefix is None else int(prefix[b]), cap, slopes, seen, reach)
     return o, tol

@@ -103,6 +103,9 @@ __device__ __forceinline__ float lanes16_sum(float x)
     return __builtin_bit_cast(float, c) + __builtin_bit_cast(float, d);
 }
 
+// The largest weight: what is below 2^-14 of binary16 is rounded in steps of 2^-24, so far weights are off by at most 2^-40 of the largest one
+constexpr float CACHED_HEAD = 32768.0f;
+
 // wavefronts per SIMD: as many as a unit's bytes leave registers for
 constexpr int cached_waves(int NK) { return NK <= 1 ? 4 : NK <= 2 ? 3 : NK <= 4 ? 2 : 1; }
 
@@ -312,7 +315,7 @@ __global__ __launch_bounds__(256, cached_waves(NK)) void attend_cached(AttnArgs 
                 keep *= unit_v / big;
                 unit_v = big;
             }
-            const float per = unit_v > LEAST_UNIT ? 1.0f / unit_v : 0.0f;
+            const float per = unit_v > LEAST_UNIT ? CACHED_HEAD / unit_v : 0.0f;
             const float mc = m == -__builtin_inff() ? 0.0f : m;
 #pragma unroll
             for (int d = 0; d < DT; ++d) acc[d] *= keep;
@@ -339,7 +342,7 @@ __global__ __launch_bounds__(256, cached_waves(NK)) void attend_cached(AttnArgs 
         __syncthreads();                               // what an earlier item left here has been read
 #pragma unroll
         for (int d = 0; d < DT; ++d)
-            if (16 * d + 4 * quarter < D) *reinterpret_cast<f32x4 *>(join + (wave * 16 + r16) * D + 16 * d + 4 * quarter) = acc[d] * unit_v;
+            if (16 * d + 4 * quarter < D) *reinterpret_cast<f32x4 *>(join + (wave * 16 + r16) * D + 16 * d + 4 * quarter) = acc[d] * (unit_v / CACHED_HEAD);
         if (quarter == 0) {
             join_m[wave * 16 + r16] = m;
             join_l[wave * 16 + r16] = l;

@@ -87,13 +87,16 @@ struct TilePlan {
     int mix;       // workgroups go through all heads tile by tile, the last rows first (else head by head on one XCD)
 };
 
-// Weights may grow to 2^8 before the sums are brought to a new maximum: they stay far inside binary16, and most tiles skip the scaling.
-constexpr float GROWTH = 8.0f;
-// Scores (in powers of two) beyond which they are rounded to fp32 before the maximum is taken off: the fma of the weights has the exact product, whose distance
-// from the rounded maximum grows to half a step of it - 2^-5 here, 16 at 2^28, where a weight would pass binary16 or all of them be 0.
-constexpr float EXACT_SCORES = 1048576.0f;
+// The largest weight is 2^HEADROOM when the sums are brought to a new maximum, and 2^(HEADROOM + GROWTH) before the next time: inside binary16, and most
+// tiles skip the scaling.  Binary16 rounds what is below 2^-14 in steps of 2^-24, so far weights are off by at most 2^-25-HEADROOM of the largest one: without the
+// headroom 131071 keys that lie 17 nats below a single one were all 0, an error of 7 x 2^-11 of their values.
+constexpr float HEADROOM = 7.0f, HEAD = 128.0f, GROWTH = 7.0f;   // HEAD = 2^HEADROOM
+// Maxima (in powers of two) beyond which the weights' exponents are taken in two steps, rounded scores less the maximum: one fma has the exact product, whose
+// distance from the rounded maximum grows to half a step of it - 16 at 2^28, where a weight would pass binary16 or all of them be 0 - and its addend,
+// shift - maximum, is rounded to half a step too, 2^-15 here.
+constexpr float EXACT_SCORES = 1024.0f;
 constexpr float LEAST_SCALE = 1e-30f;   // stands for a scale of 0, so that -inf times it stays -inf
-constexpr float LEAST_RATIO = -30.0f;   // log2 of the smallest value scale that counts beside the largest: below, a weight is 0 in binary16
+constexpr float LEAST_RATIO = -41.0f;   // log2 of the smallest value scale that counts beside the largest: below, a weight of 2^15 is 0 in binary16
 // Value scales up to here: 127 of them are 0 in binary16, and so is the result.  Their reciprocal, and its product with a hidden token's scale, could pass fp32.
 constexpr float LEAST_UNIT = 0x1p-60f;
 
@@ -411,14 +414,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
         // the running maximum, and the value scale that the sums are in
         const Halves tops = both_halves(largest(s));
         const float top = fmaxf(tops.a, tops.b) * c;
-        if (__any(fabsf(top) > EXACT_SCORES && top > -__builtin_inff())) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[u][r] *= c;
-            c = 1.0f;
-        }
-        float shift = 0.0f, grow = 1.0f, per = 0.0f;
+        float shift = HEADROOM, grow = 1.0f, per = 0.0f;
         if constexpr (CACHE) {
             // the tile's largest value scale of those that the row sees, by the running maximum over the tokens: the weights are rounded relative to it
             const int seen = min(end - t * ATT_KEYS, ATT_KEYS);
@@ -437,7 +433,13 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
                 unit_v = big;
             }
             per = unit_v > LEAST_UNIT ? 1.0f / unit_v : 0.0f;
-            if (one_scale) shift = fmaxf(__builtin_amdgcn_logf(big * per), LEAST_RATIO);   // (a row that sees nothing of the tile: any)
+            // the headroom is in the exponent, or, where the weights are multiplied by their scales, in that factor
+            if (one_scale) {
+                shift += fmaxf(__builtin_amdgcn_logf(big * per), LEAST_RATIO);   // (a row that sees nothing of the tile: any)
+            } else {
+                shift = 0.0f;
+                per *= HEAD;
+            }
         }
         if (__any(top - m > GROWTH || (m == -__builtin_inff() && top > m)) || (CACHE && __any(grow != 1.0f))) {
             const float m2 = fmaxf(m, top);
@@ -449,7 +451,16 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[d][r] *= keep * grow;
         }
-        const float mc = m == -__builtin_inff() ? 0.0f : shift - m;
+        const float m0 = m == -__builtin_inff() ? 0.0f : m;
+        float mc = shift - m0;
+        if (__any(fabsf(m0) > EXACT_SCORES)) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[u][r] = s[u][r] * c - m0;
+            c = 1.0f;
+            mc = shift;
+        }
         f16x8 p[4];                                    // weights, as steps of 16 keys
         float sum = 0.0f;
 #pragma unroll
@@ -514,10 +525,10 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
     const Halves ls = both_halves(l);
     l = ls.a + ls.b;
     if (plan.splits > 1) {
-        // [ROWS][D] sums, then maxima (in powers of two) and weights of this part
+        // [ROWS][D] sums, then maxima (in powers of two) and weights of this part (rows: sums and weights 2^HEADROOM times as large, in all parts)
         float *part = a.partial + (((size_t)flat * a.Hkv + hk) * plan.splits + split) * (size_t)(T::ROWS * (a.D + 2));
         const int lr = wave * 32 + (lane & 31);
-        const float back = CACHE ? unit_v : 1.0f;
+        const float back = CACHE ? unit_v / HEAD : 1.0f;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -531,7 +542,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
         }
         return;
     }
-    const float inv = l > 0.0f ? (CACHE ? unit_v : 1.0f) / l : 0.0f;
+    const float inv = l > 0.0f ? (CACHE ? unit_v / HEAD : 1.0f) / l : 0.0f;   // (rows: the sum has the headroom too)
     unsigned amax = 0;
     _Float16 *o = static_cast<_Float16 *>(a.o) + (sq.first + token) * a.o_row + head * a.o_head;
 #pragma unroll

@@ -656,3 +656,54 @@ def test_value_scales_next_to_zero(nq, nk, S):
             c.ref.vs[c.ref.table[b, i]] = np.float32((1e-39, 1e-42, 0.0, 1e-30, 1e-45)[i])
     c.dev.v_scale.copy_(torch.from_numpy(c.ref.vs))
     _cached((62, 1, sum(nq), S), nq, nk, 4, 2, 64, 64, S, cache=c)
+
+
+def _sink_and_tail(g, n, sinks, D, gap):
+    """Keys whose scores lie `gap` nats below those of a few, n of them, with values of the other sign: together they move the result by n e^-gap / sinks."""
+    k, v = np.zeros((n, 1, D), np.int8), g.integers(64, 128, (n, 1, D)).astype(np.int8)
+    for j in sinks:
+        k[j], v[j] = 127, -127
+    return k, v, np.float32(gap / (D * 127)), np.float32(1.0 / 127)
+
+
+def test_long_tails_below_a_sink_dense():
+    """One key far above 131070 others: their weights are tiny, their sum is not.  256 heads read the same keys, so that no part of the keys is a
+    workgroup's of its own and every row has the one maximum."""
+    g = _rng(63)
+    n, D, H, gap = 131071, 64, 256, 17.4
+    k, v, ks, vs = _sink_and_tail(g, n, [70000], D, gap)
+    k = (k.astype(np.float32) * ks).astype(np.float16)
+    v = (v.astype(np.float32) * vs).astype(np.float16)
+    q = np.ones((1, 1, D), np.float16)
+    ref, tol = oa.attention(q, k, v, [0, 1], [0, n], 1.0)
+    o = ql.attention_f16(_dev(q).expand(1, H, D).contiguous(), _dev(k).expand(n, H, D), _dev(v).expand(n, H, D), scale=1.0)
+    torch.cuda.synchronize()
+    _close(o, np.repeat(ref, H, 1), np.repeat(tol, H, 1))
+
+
+@pytest.mark.parametrize("rows, H, D, n, S", [(1, 2048, 8, 524288, 64), (1, 2048, 8, 524288, 16), (512, 128, 64, 131072, 64), (512, 128, 64, 131072, 1)])
+def test_long_tails_below_a_sink_cached(rows, H, D, n, S):
+    """The same over the cache, by 16 rows (each of a workgroup's wavefronts has a sink of its own in its first group) and by 256.  The tail is one
+    page again and again."""
+    g = _rng(64, rows, S)
+    gap = 17.4
+    few = rows == 1
+    front = 256 if few else 64
+    sinks = [3, 70, 140, 255] if few else [17]
+    fk, fv, ks, vs = _sink_and_tail(g, front, sinks, D, gap)
+    tk, tv, _, _ = _sink_and_tail(g, 64, [], D, gap)
+    pages = front // 64 + 1
+    ck, cv = np.concatenate((fk, tk)), np.concatenate((fv, tv))                  # [pages * 64, 1, D]
+    kc = np.broadcast_to(ck.reshape(pages, 64, D)[:, None], (pages, H, 64, D))
+    order = np.argsort([oa.slot(t) for t in range(64)])                           # byte -> token
+    vc = np.broadcast_to(cv.reshape(pages, 64, D)[:, order].transpose(0, 2, 1)[:, None, None], (pages, H, 1, D, 64))
+    scales = np.ones((pages, H, 64 // S), np.float32)
+    cache = ql.KvCache8(_dev(kc), _dev(vc), _dev(scales * ks), _dev(scales * vs))
+    table = np.full((1, n // 64), pages - 1, np.int32)
+    table[0, :pages - 1] = np.arange(pages - 1)
+    q = np.ones((1, 1, D), np.float16)
+    o = ql.attention_kv8(_dev(np.broadcast_to(q, (rows, H, D))), cache, _dev(table), _dev(np.array([n], np.int32)), mask=ql.MASK_NONE, scale=1.0)
+    k, v = (np.concatenate((f, np.tile(t, ((n - front) // 64, 1, 1)))) for f, t in ((fk, tk), (fv, tv)))
+    ref, tol = oa.attention(q, k * np.float64(ks), v * np.float64(vs), [0, 1], [0, n], 1.0)
+    torch.cuda.synchronize()
+    _close(o, np.broadcast_to(ref, (rows, H, D)), np.broadcast_to(tol, (rows, H, D)))

@@ -188,10 +188,27 @@ def _need(t, dtype, shape=None, name="tensor"):
     return t
 
 
-def workspace(nbytes, device="cuda"):
-    """A 256-byte aligned scratch tensor of at least nbytes."""
-    import torch
-    return torch.empty((max(int(nbytes), 256),), dtype=torch.uint8, device=device)
+def workspace(nbytes, device="cuda", stream=None):
+    """A 256-byte aligned scratch tensor of at least nbytes, for use on `stream` (default: the current one)."""
+    torch = _torch or _load_torch()
+    return _empty((max(int(nbytes), 256),), torch.uint8, device, stream)
+
+
+def _empty(shape, dtype, device, stream, returned=False):
+    """A tensor that a call makes for itself and uses on `stream`: from that stream's memory, as memory that was freed on the current stream may
+    still be written by what waits there.  One that is returned is the current stream's too: freed, it waits for what that one does with it."""
+    torch = _torch or _load_torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    cuda = torch.cuda
+    if not isinstance(stream, cuda.Stream):
+        handle = _stream(stream)
+        stream = cuda.ExternalStream(handle) if handle else cuda.default_stream()
+    with cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if returned:
+        t.record_stream(cuda.current_stream())
+    return t
 
 
 def daq_workspace_bytes(M, K, R):
@@ -581,19 +598,12 @@ def _current():
         return -1
 
 
-def _made(t, stream):
-    """A tensor that a call made for itself and uses on `stream`: its memory is not given out again before that."""
-    if stream is not None:
-        t.record_stream(stream if hasattr(stream, "cuda_stream") else _torch.cuda.ExternalStream(int(stream)))
-    return t
-
-
 def _attention_form(dev, q, B, Hkv, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax, stream):
     torch = _torch or _load_torch()
     qp, q_row, q_head = _heads(q, "q", dev)
     T, Hq, D = q.shape
     if o is None:
-        o = _made(torch.empty((T, Hq, D), dtype=torch.float16, device=q.device), stream)
+        o = _empty((T, Hq, D), torch.float16, q.device, stream, True)
     op, o_row, o_head = _heads(o, "o", dev, Hq, D)
     if o.shape[0] != T:
         raise ValueError("o has %d rows, expected %d" % (o.shape[0], T))
@@ -622,7 +632,7 @@ def attention_f16(q, k, v, batch=None, cu_q=None, cu_k=None, mask=MASK_NONE, pre
     cu = _at(cu_k, _torch.int32, (B + 1,), "cu_k", dev)
     a, o = _attention_form(dev, q, B, Hkv, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax, stream)
     if ws is None:
-        ws = _made(workspace(attention_f16_workspace_bytes(q.shape[0], T_k, B, q.shape[1], Hkv, D), q.device), stream)
+        ws = workspace(attention_f16_workspace_bytes(q.shape[0], T_k, B, q.shape[1], Hkv, D), q.device, stream)
     elif ws.get_device() != dev:
         _elsewhere(ws, "ws")
     _check(lib().attention_f16(a, kp, k_row, k_head, vp, v_row, v_head, T_k, cu, _ptr(ws), ws.numel(), _stream(stream)),
@@ -688,7 +698,7 @@ def daq_kv_append(cache, k, v, page_table, len_k, cu=None, q=None, rot=None, rot
         if q.shape[0] != T:
             raise ValueError("q has %d rows and k %d" % (q.shape[0], T))
         if q_out is None:
-            q_out = _made(torch.empty((T, Hq, cache.D), dtype=torch.float16, device=q.device), stream)
+            q_out = _empty((T, Hq, cache.D), torch.float16, q.device, stream, True)
         qo = _at(q_out, torch.float16, (T, Hq, cache.D), "q_out", dev)
     ko, vo = _at(k_out, torch.float16, (T, cache.heads, cache.D), "k_out", dev), _at(v_out, torch.float16, (T, cache.heads, cache.D), "v_out", dev)
     cup, pp, rp = _at(cu, torch.int32, (B + 1,), "cu", dev), _at(pos, torch.int32, (T,), "pos", dev), _at(rot, torch.float32, None, "rot", dev)
@@ -715,7 +725,7 @@ def attention_kv8(q, cache, page_table, len_k, cu_q=None, mask=MASK_CAUSAL, pref
     if q.shape[2] != cache.D:
         raise ValueError("q has heads of %d, the cache of %d" % (q.shape[2], cache.D))
     if ws is None:
-        ws = _made(workspace(attention_kv8_workspace_bytes(q.shape[0], B, q.shape[1], cache.heads, cache.D), q.device), stream)
+        ws = workspace(attention_kv8_workspace_bytes(q.shape[0], B, q.shape[1], cache.heads, cache.D), q.device, stream)
     elif ws.get_device() != dev:
         _elsewhere(ws, "ws")
     _check(lib().attention_kv8(a, c, _ptr(ws), ws.numel(), _stream(stream)), "attention_kv8")

@@ -707,3 +707,44 @@ def test_long_tails_below_a_sink_cached(rows, H, D, n, S):
     ref, tol = oa.attention(q, k * np.float64(ks), v * np.float64(vs), [0, 1], [0, n], 1.0)
     torch.cuda.synchronize()
     _close(o, np.broadcast_to(ref, (rows, H, D)), np.broadcast_to(tol, (rows, H, D)))
+
+
+def _making_its_tensors(name):
+    """A call that makes its output and workspace itself, always with the same result."""
+    g = _rng(65)
+    q, k, v = (_dev(_f16(g, 256, 4, 64)) for _ in range(3))
+    c = _Cached(g, 1, 256, 4, 64, 64, 64)
+    lens = _dev(np.array([256], np.int32))
+    calls = {"attention_f16": lambda **kw: ql.attention_f16(q, k, v, **kw), "attention_kv8": lambda **kw: ql.attention_kv8(q, c.dev, c.table, lens, **kw),
+             "daq_kv_append": lambda **kw: ql.daq_kv_append(c.dev, k, v, c.table, lens, q=q, **kw)}
+    return calls[name]
+
+
+@pytest.mark.parametrize("handle", [False, True])
+@pytest.mark.parametrize("name", ["attention_f16", "attention_kv8", "daq_kv_append"])
+def test_tensors_made_for_another_stream(name, handle):
+    """Memory freed on the current stream, where a fill still waits, is not what a call on another stream writes to; nor does a later call there write to what
+    the current stream still reads of an earlier result."""
+    side = torch.cuda.Stream()
+    call = _making_its_tensors(name)
+    want = call()
+    torch.cuda.synchronize()
+    there = dict(stream=side.cuda_stream if handle else side)
+    torch.cuda._sleep(20_000_000)
+    for _ in range(4):
+        junk = torch.empty_like(want)
+        junk.fill_(7.0)
+        del junk
+    got = call(**there)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda._sleep(20_000_000)
+    kept = got.clone()
+    del got
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            torch.empty_like(want).fill_(9.0)
+        call(**there)
+    torch.cuda.synchronize()
+    assert torch.equal(kept, want)

@@ -5,6 +5,9 @@ runs inside ``libdiffpro_qlinear.so`` (hand-written HIP for gfx950) through the 
 ABI of ``include/diffpro_qlinear.h``.  PyTorch supplies device memory and the
 current stream, nothing else.  There is no CPU or PyTorch fallback: if the
 library is missing or a call fails, an exception is raised.
+
+A call that is given `stream` (a torch stream or a handle) runs there: its inputs have to be ready
+on that stream and to live until it is done with them, and what it returns is ready on that stream.
 """
 import ctypes
 import os
@@ -225,11 +228,11 @@ def daq_quantize(x, R, q=None, scales=None, ws=None, stream=None):
     _need(x, torch.float16, name="x")
     M, K = x.shape
     if q is None:
-        q = torch.empty((M, K), dtype=torch.int8, device=x.device)
+        q = _empty((M, K), torch.int8, x.device, stream, True)
     if scales is None:
-        scales = torch.empty((max(M // max(R, 1), 1),), dtype=torch.float32, device=x.device)
+        scales = _empty((max(M // max(R, 1), 1),), torch.float32, x.device, stream, True)
     if ws is None and R > 1:
-        ws = workspace(daq_workspace_bytes(M, K, R), x.device)
+        ws = workspace(daq_workspace_bytes(M, K, R), x.device, stream)
     rc = lib().daq_quantize(_ptr(x), M, K, R, _ptr(q), _ptr(scales), _ptr(ws), 0 if ws is None else ws.numel(),
                             _stream(stream))
     _check(rc, "daq_quantize")
@@ -243,11 +246,11 @@ def daq_quantize_rowmax(x, R, row_absmax, q=None, scales=None, ws=None, stream=N
     M, K = x.shape
     _need(row_absmax, torch.int32, (M,), "row_absmax")
     if q is None:
-        q = torch.empty((M, K), dtype=torch.int8, device=x.device)
+        q = _empty((M, K), torch.int8, x.device, stream, True)
     if scales is None:
-        scales = torch.empty((max(M // max(R, 1), 1),), dtype=torch.float32, device=x.device)
+        scales = _empty((max(M // max(R, 1), 1),), torch.float32, x.device, stream, True)
     if ws is None and R > 1:
-        ws = workspace(daq_workspace_bytes(M, K, R), x.device)
+        ws = workspace(daq_workspace_bytes(M, K, R), x.device, stream)
     rc = lib().daq_quantize_rowmax(_ptr(x), M, K, R, _ptr(row_absmax), _ptr(q), _ptr(scales), _ptr(ws),
                                    0 if ws is None else ws.numel(), _stream(stream))
     _check(rc, "daq_quantize_rowmax")
@@ -261,12 +264,12 @@ def daq_quantize_ln(x, R=1, shift=None, scale=None, rows_per_mod=1, eps=1e-6, wa
     M, K = x.shape
     out = {}
     if want_h or R > 1:
-        out["h"] = torch.empty((M, K), dtype=torch.float16, device=x.device)
+        out["h"] = _empty((M, K), torch.float16, x.device, stream, True)
     if want_q:
-        out["q"] = torch.empty((M, K), dtype=torch.int8, device=x.device)
-        out["scales"] = torch.empty((max(M // max(R, 1), 1),), dtype=torch.float32, device=x.device)
+        out["q"] = _empty((M, K), torch.int8, x.device, stream, True)
+        out["scales"] = _empty((max(M // max(R, 1), 1),), torch.float32, x.device, stream, True)
     if ws is None and R > 1 and want_q:
-        ws = workspace(daq_workspace_bytes(M, K, R), x.device)
+        ws = workspace(daq_workspace_bytes(M, K, R), x.device, stream)
     fn = lib().daq_quantize_ln
     fn.argtypes = [_vp, _i64, _i64, _i64, _vp, _vp, _i64, ctypes.c_float, _vp, _vp, _vp, _vp, _sz, _vp]
     rc = fn(_ptr(x), M, K, R, _ptr(shift), _ptr(scale), rows_per_mod, eps, _ptr(out.get("h")), _ptr(out.get("q")),
@@ -280,12 +283,12 @@ def daq_quantize_cg(x, R, act_group, stream=None):
     import torch
     _need(x, torch.float16, name="x")
     M, K = x.shape
-    q = torch.empty((M, K), dtype=torch.int8, device=x.device)
-    sc = torch.empty((M // R, K // act_group), dtype=torch.float32, device=x.device)
+    q = _empty((M, K), torch.int8, x.device, stream, True)
+    sc = _empty((M // R, K // act_group), torch.float32, x.device, stream, True)
     L = lib()
     L.daq_cg_workspace_bytes.restype = _sz
     L.daq_cg_workspace_bytes.argtypes = [_i64, _i64, _i64, _i64]
-    ws = workspace(L.daq_cg_workspace_bytes(M, K, R, act_group), x.device)
+    ws = workspace(L.daq_cg_workspace_bytes(M, K, R, act_group), x.device, stream)
     L.daq_quantize_cg.argtypes = [_vp, _i64, _i64, _i64, _i64, _vp, _vp, _vp, _sz, _vp]
     _check(L.daq_quantize_cg(_ptr(x), M, K, R, act_group, _ptr(q), _ptr(sc), _ptr(ws), ws.numel(), _stream(stream)), "daq_quantize_cg")
     return q, sc
@@ -300,16 +303,16 @@ def qlinear_grouped(x, R, w, w_scale, group, bias=None, act_group=0, storage=8, 
     N = w.shape[0]
     G = K // group
     if y is None:
-        y = torch.empty((M, N), dtype=torch.float16, device=x.device)
+        y = _empty((M, N), torch.float16, x.device, stream, True)
     L = lib()
     L.qlinear_grouped_workspace_bytes.restype = _sz
     L.qlinear_grouped_workspace_bytes.argtypes = [_i64, _i64, _i64, _i64]
-    ws = workspace(L.qlinear_grouped_workspace_bytes(M, K, R, act_group), x.device)
+    ws = workspace(L.qlinear_grouped_workspace_bytes(M, K, R, act_group), x.device, stream)
     out, dbg = {"y": y}, None
     if debug:
-        out["q"] = torch.empty((M, K), dtype=torch.int8, device=x.device)
-        out["s_a"] = torch.empty((M // R,) if act_group == 0 else (M // R, G), dtype=torch.float32, device=x.device)
-        out["P"] = torch.empty((M, G, N), dtype=torch.int32, device=x.device)
+        out["q"] = _empty((M, K), torch.int8, x.device, stream, True)
+        out["s_a"] = _empty((M // R,) if act_group == 0 else (M // R, G), torch.float32, x.device, stream, True)
+        out["P"] = _empty((M, G, N), torch.int32, x.device, stream, True)
         dbg = ctypes.pointer(ql_debug(out["q"].data_ptr(), out["s_a"].data_ptr(), out["P"].data_ptr()))
     L.qlinear_grouped.argtypes = [_vp, _i64, _i64, _i64, _i64, _vp, ctypes.c_int32, _vp, _i64, _vp, _i64, _vp, ctypes.POINTER(ql_debug),
                                   _vp, _sz, _vp]
@@ -370,9 +373,9 @@ def qlinear_fused(x, R, w, w_scale, bias=None, bits=8, group=128, act=ACT_NONE, 
     if gate is not None:
         _need(gate, torch.float16, (M // gate_rows, N), "gate")
     if y is None:
-        y = torch.empty((M, N), dtype=torch.float16, device=x.device)
+        y = _empty((M, N), torch.float16, x.device, stream, True)
     if ws is None:
-        ws = workspace(qlinear_workspace_bytes(M, K, R), x.device)
+        ws = workspace(qlinear_workspace_bytes(M, K, R), x.device, stream)
     if row_absmax is not None:
         _need(row_absmax, torch.int32, (M,), "row_absmax")
     fu = ql_fusion(act, 0, None if residual is None else residual.data_ptr(), None if gate is None else gate.data_ptr(), gate_rows,
@@ -395,7 +398,7 @@ def qlinear_f16(x, w, bias=None, act=ACT_NONE, residual=None, gate=None, gate_ro
     M, K = x.shape
     N = w.shape[0]
     if y is None:
-        y = torch.empty((M, N), dtype=torch.float16, device=x.device)
+        y = _empty((M, N), torch.float16, x.device, stream, True)
     fu = ql_fusion(act, 0, None if residual is None else residual.data_ptr(), None if gate is None else gate.data_ptr(), gate_rows,
                    None if row_absmax is None else row_absmax.data_ptr())
     _check(lib().qlinear_f16(_ptr(x), M, K, _ptr(w), _ptr(bias), N, ctypes.byref(fu), _ptr(y), _stream(stream)), "qlinear_f16")
@@ -412,11 +415,11 @@ def daq_quantize_robust(x, R, p_ppm=999000, a_bits=8, q=None, scales=None, ws=No
     _need(x, torch.float16, name="x")
     M, K = x.shape
     if q is None:
-        q = torch.empty((M, K), dtype=torch.int8, device=x.device)
+        q = _empty((M, K), torch.int8, x.device, stream, True)
     if scales is None:
-        scales = torch.empty((max(M // max(R, 1), 1),), dtype=torch.float32, device=x.device)
+        scales = _empty((max(M // max(R, 1), 1),), torch.float32, x.device, stream, True)
     if ws is None and R > 1:
-        ws = workspace(daq_workspace_bytes(M, K, R), x.device)
+        ws = workspace(daq_workspace_bytes(M, K, R), x.device, stream)
     prm = _DaqParams(p_ppm, a_bits)
     rc = lib().daq_quantize_robust(_ptr(x), M, K, R, ctypes.byref(prm), _ptr(q), _ptr(scales), _ptr(ws),
                                    0 if ws is None else ws.numel(), _stream(stream))
@@ -433,17 +436,17 @@ def _qlinear(fn_name, x, R, w, w_scale, bias, N, y, debug, ws, stream, group=128
     _need(x, torch.float16, name="x")
     M, K = x.shape
     if y is None:
-        y = torch.empty((M, N), dtype=torch.float16, device=x.device)
+        y = _empty((M, N), torch.float16, x.device, stream, True)
     if ws is None:
-        ws = workspace(qlinear_workspace_bytes(M, K, R), x.device)
+        ws = workspace(qlinear_workspace_bytes(M, K, R), x.device, stream)
     dbg = None
     out = {"y": y}
     if debug:
         G = K // group
-        out["q"] = torch.empty((M, K), dtype=torch.int8, device=x.device)
-        out["s_a"] = torch.empty((M // R,), dtype=torch.float32, device=x.device)
+        out["q"] = _empty((M, K), torch.int8, x.device, stream, True)
+        out["s_a"] = _empty((M // R,), torch.float32, x.device, stream, True)
         shape = (M, N) if fn_name == "qlinear_w8a8" else (M, G, N)
-        out["acc" if fn_name == "qlinear_w8a8" else "P"] = acc = torch.empty(shape, dtype=torch.int32, device=x.device)
+        out["acc" if fn_name == "qlinear_w8a8" else "P"] = acc = _empty(shape, torch.int32, x.device, stream, True)
         dbg = ctypes.pointer(ql_debug(out["q"].data_ptr(), out["s_a"].data_ptr(), acc.data_ptr()))
     if fn_name == "qlinear_w4a8" and group != 128:
         fn_name = "qlinear_w4a8_g"
@@ -495,7 +498,7 @@ def _qgemm(fn_name, q, a_scales, R, w, w_scale, bias, N, y, acc, stream):
     _need(a_scales, torch.float32, name="a_scales")
     M, K = q.shape
     if y is None:
-        y = torch.empty((M, N), dtype=torch.float16, device=q.device)
+        y = _empty((M, N), torch.float16, q.device, stream, True)
     rc = getattr(lib(), fn_name)(_ptr(q), _ptr(a_scales), M, K, R, _ptr(w), _ptr(w_scale), _ptr(bias), N, _ptr(y),
                                  _ptr(acc), _stream(stream))
     _check(rc, fn_name)
@@ -513,7 +516,7 @@ def qgemm_w4a8(q, a_scales, R, w4, w_scale, bias=None, y=None, acc=None, stream=
     M, K = q.shape
     N = w4.shape[0]
     if y is None:
-        y = torch.empty((M, N), dtype=torch.float16, device=q.device)
+        y = _empty((M, N), torch.float16, q.device, stream, True)
     rc = lib().qgemm_w4a8_g(_ptr(q), _ptr(a_scales), M, K, R, _ptr(w4), _ptr(w_scale), group, _ptr(bias), N, _ptr(y),
                             _ptr(acc), _stream(stream))
     _check(rc, "qgemm_w4a8_g")
@@ -879,9 +882,8 @@ def gemm_variants():
 def prepack_w4(pairs, stream=None):
     """Device uint8 [N,K/2] in pair order (low nibble = even k, high nibble = odd k) -> a new device tensor in the
     library's 4-bit storage order."""
-    import torch
     N, K2 = pairs.shape
-    out = torch.empty_like(pairs)
+    out = _empty(pairs.shape, pairs.dtype, pairs.device, stream, True)
     _check(lib().ql_prepack_w4(_ptr(pairs), N, K2 * 2, _ptr(out), _stream(stream)), "ql_prepack_w4")
     return out
 

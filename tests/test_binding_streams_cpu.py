@@ -86,10 +86,24 @@ def _ints(*shape):
     return _t(*shape, dtype=torch.int32)
 
 
+W8, S8, W4 = _t(32, 256, dtype=torch.int8), _t(32, dtype=torch.float32), _t(32, 128, dtype=torch.uint8)
 CALLS = {
     "attention_f16": lambda **kw: ql.attention_f16(_t(8, 2, 64), _t(8, 2, 64), _t(8, 2, 64), **kw),
     "attention_kv8": lambda **kw: ql.attention_kv8(_t(8, 2, 64), _cache(), _ints(1, 2), _ints(1), **kw),
     "daq_kv_append": lambda **kw: ql.daq_kv_append(_cache(), _t(8, 2, 64), _t(8, 2, 64), _ints(1, 2), _ints(1), q=_t(8, 2, 64), **kw),
+    "daq_quantize": lambda **kw: ql.daq_quantize(_t(8, 256), 4, **kw),
+    "daq_quantize_rowmax": lambda **kw: ql.daq_quantize_rowmax(_t(8, 256), 4, _ints(8), **kw),
+    "daq_quantize_ln": lambda **kw: ql.daq_quantize_ln(_t(8, 256), 4, want_h=True, **kw),
+    "daq_quantize_cg": lambda **kw: ql.daq_quantize_cg(_t(8, 256), 4, 64, **kw),
+    "daq_quantize_robust": lambda **kw: ql.daq_quantize_robust(_t(8, 256), 4, **kw),
+    "qlinear_grouped": lambda **kw: ql.qlinear_grouped(_t(8, 256), 4, W8, _t(32, 4), 64, act_group=64, debug=True, **kw),
+    "qlinear_fused": lambda **kw: ql.qlinear_fused(_t(8, 256), 4, W8, S8, **kw),
+    "qlinear_f16": lambda **kw: ql.qlinear_f16(_t(8, 256), _t(32, 256), **kw),
+    "qlinear_w8a8": lambda **kw: ql.qlinear_w8a8(_t(8, 256), 4, W8, S8, debug=True, **kw),
+    "qlinear_w4a8": lambda **kw: ql.qlinear_w4a8(_t(8, 256), 4, W4, _t(32, 4), group=64, debug=True, **kw),
+    "qgemm_w8a8": lambda **kw: ql.qgemm_w8a8(_t(8, 256, dtype=torch.int8), S8, 4, W8, S8, **kw),
+    "qgemm_w4a8": lambda **kw: ql.qgemm_w4a8(_t(8, 256, dtype=torch.int8), S8, 4, W4, _t(32, 4), group=64, **kw),
+    "prepack_w4": lambda **kw: ql.prepack_w4(W4, **kw),
 }
 
 

@@ -585,6 +585,11 @@ def _elsewhere(t, name):
     raise ValueError("%s is on %s, the current device is cuda:%d" % (name, t.device, _torch._C._cuda_getDevice()))
 
 
+def _here(stream, dev):
+    if getattr(stream, "device_index", dev) != dev:
+        raise ValueError("stream is on cuda:%d, the current device is cuda:%d" % (stream.device_index, dev))
+
+
 def _at(t, dtype, shape, name, dev):
     """The address of a small argument (0: none)."""
     if t is None:
@@ -626,6 +631,7 @@ def attention_f16(q, k, v, batch=None, cu_q=None, cu_k=None, mask=MASK_NONE, pre
     scale: default D ** -0.5; cap: tanh cap of the scores (0: none; 2^-10 to 2^10); slopes fp32 [Hq]: bias by distance; mask MASK_NONE / _CAUSAL / _PREFIX
     (prefix int32 [B]); row_absmax: int32 [T_q] that receives every row's largest |o| as a binary16 bit pattern, for daq_quantize_rowmax."""
     dev = _current()
+    _here(stream, dev)
     kp, k_row, k_head = _heads(k, "k", dev)
     T_k, Hkv, D = k.shape
     vp, v_row, v_head = _heads(v, "v", dev, Hkv, D)
@@ -658,6 +664,7 @@ class KvCache8:
             raise ValueError("k_scale has shape %s, expected [%d, %d, page / scale_tokens]" % (tuple(k_scale.shape), P, H))
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.num_pages, self.heads, self.page, self.D, self.scale_tokens = P, H, page, D, page // k_scale.shape[2]
+        self._devices = tuple(t.get_device() for t in (k, v, k_scale, v_scale))
         self._fields = (k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), P, page, self.scale_tokens, H, D)
 
     @classmethod
@@ -674,9 +681,11 @@ class KvCache8:
         torch = _torch or _load_torch()
         B, max_pages = _need(page_table, torch.int32, name="page_table").shape
         dev = _current()
-        for t, name in ((page_table, "page_table"), (self.k, "the cache")):
-            if t.get_device() != dev:
-                _elsewhere(t, name)
+        if page_table.get_device() != dev:
+            _elsewhere(page_table, "page_table")
+        if self._devices != (dev, dev, dev, dev):
+            name = ("k", "v", "k_scale", "v_scale")[[d == dev for d in self._devices].index(False)]
+            _elsewhere(getattr(self, name), "the cache's " + name)
         return _KV_CACHE.pack(*self._fields, page_table.data_ptr(), _at(len_k, torch.int32, (B,), "len_k", dev), B, max_pages), B
 
 
@@ -689,6 +698,7 @@ def daq_kv_append(cache, k, v, page_table, len_k, cu=None, q=None, rot=None, rot
     torch = _torch or _load_torch()
     c, B = cache.desc(page_table, len_k)
     dev = _current()
+    _here(stream, dev)
     kp, k_row, k_head = _heads(k, "k", dev, cache.heads, cache.D)
     vp, v_row, v_head = _heads(v, "v", dev, cache.heads, cache.D)
     T = k.shape[0]
@@ -724,6 +734,7 @@ def attention_kv8(q, cache, page_table, len_k, cu_q=None, mask=MASK_CAUSAL, pref
     """attention_f16 over the 8-bit cache: q fp16 [T_q, Hq, D], page_table int32 [B, max_pages], len_k int32 [B] -> o fp16 [T_q, Hq, D]."""
     c, B = cache.desc(page_table, len_k)
     dev = _current()
+    _here(stream, dev)
     a, o = _attention_form(dev, q, B, cache.heads, cu_q, mask, prefix, scale, cap, slopes, o, row_absmax, stream)
     if q.shape[2] != cache.D:
         raise ValueError("q has heads of %d, the cache of %d" % (q.shape[2], cache.D))

@@ -1,5 +1,5 @@
 """Where the binding's calls take the memory of the tensors that they make for themselves: from the stream that they run on.  Without a GPU: the library
-is a stub, and streams are names."""
+is a stub, and streams are names.  And that what they are given is on the current device."""
 import contextlib
 
 import pytest
@@ -68,6 +68,7 @@ def made(monkeypatch):
     monkeypatch.setattr(ql, "lib", lambda: library)
     monkeypatch.setattr(ql, "_current", lambda: 0)
     monkeypatch.setattr(ql, "_raw_stream", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
     monkeypatch.setattr(torch, "empty", on)
     for name, value in (("stream", stream), ("Stream", _Stream), ("ExternalStream", _Stream), ("current_stream", lambda *a: active[-1]), ("default_stream", lambda *a: CURRENT)):
         monkeypatch.setattr(torch.cuda, name, value)
@@ -125,3 +126,35 @@ def test_memory_is_of_the_stream_that_the_call_runs_on(name, stream, handle, mad
 def test_without_a_stream_nothing_is_recorded(name, made):
     CALLS[name]()
     assert made and all(t.memory_of == CURRENT and "used_on" not in t.__dict__ for t in made)
+
+
+class _OnTheOther(_OnGpu):
+    def get_device(self):
+        return 1
+
+
+CACHED = {
+    "attention_kv8": lambda cache, **kw: ql.attention_kv8(_t(8, 2, 64), cache, _ints(1, 2), _ints(1), **kw),
+    "daq_kv_append": lambda cache, **kw: ql.daq_kv_append(cache, _t(8, 2, 64), _t(8, 2, 64), _ints(1, 2), _ints(1), **kw),
+}
+
+
+@pytest.mark.parametrize("name", sorted(CACHED))
+@pytest.mark.parametrize("part", ["k", "v", "k_scale", "v_scale"])
+def test_every_part_of_the_cache_is_on_the_current_device(name, part, made):
+    here = _cache()
+    parts = {p: getattr(here, p) for p in ("k", "v", "k_scale", "v_scale")}
+    parts[part] = parts[part].as_subclass(_OnTheOther)
+    with pytest.raises(ValueError, match="is on .* current device"):
+        CACHED[name](ql.KvCache8(*parts.values()))
+    CACHED[name](here)
+
+
+@pytest.mark.parametrize("name", ["attention_f16", "attention_kv8", "daq_kv_append"])
+def test_the_stream_is_on_the_current_device(name, made):
+    s = _Stream(0x50)
+    s.device_index = 1
+    with pytest.raises(ValueError, match="stream is on cuda:1"):
+        CALLS[name](stream=s)
+    s.device_index = 0
+    CALLS[name](stream=s)

@@ -476,7 +476,9 @@ typedef struct ql_attention {
 } ql_attention;
 
 /* Keys and values as binary16 rows: k, v (device), strided like q; cu_k (device)
- * int32 [B+1] or NULL: T_k / B keys each; a sequence may have no keys. */
+ * int32 [B+1] or NULL: T_k / B keys each; a sequence may have no keys.
+ * attention_f16_workspace_bytes: enough for every call of these heads with up to
+ * T_q rows, T_k keys and B sequences (0: they need none). */
 size_t attention_f16_workspace_bytes(int64_t T_q, int64_t T_k, int32_t B, int32_t Hq, int32_t Hkv, int32_t D);
 int attention_f16(const ql_attention *attn, const void *k, int64_t k_row, int64_t k_head,
                   const void *v, int64_t v_row, int64_t v_head, int64_t T_k, const void *cu_k,
@@ -556,7 +558,9 @@ int daq_kv_append(const ql_kv_cache *cache, const ql_kv_new *tokens, void *strea
  * cache's keys and values; attn->B, Hkv and D are the cache's.  One new token per
  * sequence is T_q = B with cu_q NULL.  The weights take the value scales along
  * when they are rounded, relative to the largest of those that the row sees.  (T_q * Hq / Hkv / 16 + B) * Hkv * max_pages *
- * page / 64 below 2^31. */
+ * page / 64 below 2^31.
+ * attention_kv8_workspace_bytes: enough for every call of these heads with up to
+ * T_q rows and B sequences. */
 size_t attention_kv8_workspace_bytes(int64_t T_q, int32_t B, int32_t Hq, int32_t Hkv, int32_t D);
 int attention_kv8(const ql_attention *attn, const ql_kv_cache *cache,
                   void *workspace, size_t workspace_bytes, void *stream);

@@ -46,10 +46,13 @@ struct AttnArgs {
 hipError_t launch_attention_f16(const AttnArgs &a, hipStream_t stream);
 hipError_t launch_attention_kv8(const AttnArgs &a, hipStream_t stream);
 hipError_t launch_attention_chunks(const AttnArgs &a, hipStream_t stream);
-// workspace of the launches
+// workspace of the launches (fewer rows may need more: their keys are cut), and the most that a call of no more rows, keys and sequences needs
 size_t tiles_partial_bytes(long long Tq, long long Tk, int B, int Hq, int Hkv, int D);
+size_t tiles_most_bytes(long long Tq, long long Tk, int B, int Hq, int Hkv, int D);
 size_t chunks_partial_bytes(long long Tq, int B, int Hq, int Hkv, int D);
+size_t chunks_most_bytes(long long Tq, int B, int Hq, int Hkv, int D);
 size_t cached_partial_bytes(long long Tq, int B, int Hq, int Hkv, int D);   // either
+size_t cached_most_bytes(long long Tq, int B, int Hq, int Hkv, int D);
 
 struct KvAppendArgs {
     int8_t *kc, *vc;

@@ -57,6 +57,11 @@ size_t tiles_partial_bytes(long long Tq, long long Tk, int B, int Hq, int Hkv, i
     return p.splits == 1 ? 0 : (size_t)p.tiles * Hkv * p.splits * TILE_ROWS * (D + 2) * 4;
 }
 
+size_t tiles_most_bytes(long long Tq, long long Tk, int B, int Hq, int Hkv, int D)
+{
+    return (size_t)most_parts(Tq, B, Hq / Hkv, Hkv, TILE_ROWS, Tk, 2 * CUS) * TILE_ROWS * (D + 2) * 4;
+}
+
 hipError_t launch_attention_f16(const AttnArgs &a, hipStream_t stream)
 {
     const int ch = a.D / 8;

@@ -103,7 +103,7 @@ extern "C" {
 size_t attention_f16_workspace_bytes(int64_t T_q, int64_t T_k, int32_t B, int32_t Hq, int32_t Hkv, int32_t D)
 {
     if (check_heads(T_q, B, Hq, D, false) || Hkv < 1 || Hq % Hkv != 0 || check_heads(T_k, B, Hkv, D, false)) return 0;
-    return ql::tiles_partial_bytes(T_q, T_k, B, Hq, Hkv, D);
+    return ql::tiles_most_bytes(T_q, T_k, B, Hq, Hkv, D);
 }
 
 int attention_f16(const ql_attention *attn, const void *k, int64_t k_row, int64_t k_head, const void *v, int64_t v_row, int64_t v_head,
@@ -114,7 +114,7 @@ int attention_f16(const ql_attention *attn, const void *k, int64_t k_row, int64_
     if ((rc = check_heads(T_k, attn->B, attn->Hkv, attn->D, !cu_k))) return rc;
     if ((rc = check_rows(k, k_row, k_head)) || (rc = check_rows(v, v_row, v_head))) return rc;
     if (off(cu_k, 4)) return QL_ERR_ALIGN;
-    if ((rc = check_workspace(workspace, workspace_bytes, attention_f16_workspace_bytes(attn->T_q, T_k, attn->B, attn->Hq, attn->Hkv, attn->D)))) return rc;
+    if ((rc = check_workspace(workspace, workspace_bytes, ql::tiles_partial_bytes(attn->T_q, T_k, attn->B, attn->Hq, attn->Hkv, attn->D)))) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
     if ((rc = clear_absmax(attn, s))) return rc;
     ql::AttnArgs g = attention_args(attn);
@@ -187,7 +187,7 @@ int daq_kv_append(const ql_kv_cache *cache, const ql_kv_new *n, void *stream)
 size_t attention_kv8_workspace_bytes(int64_t T_q, int32_t B, int32_t Hq, int32_t Hkv, int32_t D)
 {
     if (check_heads(T_q, B, Hq, D, false) || Hkv < 1 || Hq % Hkv != 0) return 0;
-    return ql::cached_partial_bytes(T_q, B, Hq, Hkv, D);
+    return ql::cached_most_bytes(T_q, B, Hq, Hkv, D);
 }
 
 int attention_kv8(const ql_attention *attn, const ql_kv_cache *cache, void *workspace, size_t workspace_bytes, void *stream)
@@ -199,7 +199,7 @@ int attention_kv8(const ql_attention *attn, const ql_kv_cache *cache, void *work
     // the kernels count groups of 64 tokens of 16 rows of a key head in 32 bits
     const int64_t row_tiles = (attn->T_q * (attn->Hq / attn->Hkv) / 16 + attn->B) * attn->Hkv, groups = (int64_t)cache->max_pages * (cache->page / 64);
     if (row_tiles > INT_MAX64 / groups) return QL_ERR_SHAPE;
-    if ((rc = check_workspace(workspace, workspace_bytes, attention_kv8_workspace_bytes(attn->T_q, attn->B, attn->Hq, attn->Hkv, attn->D)))) return rc;
+    if ((rc = check_workspace(workspace, workspace_bytes, ql::cached_partial_bytes(attn->T_q, attn->B, attn->Hq, attn->Hkv, attn->D)))) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
     if ((rc = clear_absmax(attn, s))) return rc;
     ql::AttnArgs g = attention_args(attn);

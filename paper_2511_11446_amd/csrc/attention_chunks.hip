@@ -56,6 +56,11 @@ size_t chunks_partial_bytes(long long Tq, int B, int Hq, int Hkv, int D)
     return p.splits == 1 ? 0 : (size_t)p.tiles * Hkv * p.splits * chunk_rows(D) * (D + 2) * 4;
 }
 
+size_t chunks_most_bytes(long long Tq, int B, int Hq, int Hkv, int D)
+{
+    return (size_t)most_parts(Tq, B, Hq / Hkv, Hkv, chunk_rows(D), 1LL << 31, WANTED) * chunk_rows(D) * (D + 2) * 4;
+}
+
 hipError_t launch_attention_chunks(const AttnArgs &a, hipStream_t stream)
 {
     const int ch = a.D / 8;

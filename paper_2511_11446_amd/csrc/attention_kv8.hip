@@ -507,9 +507,17 @@ hipError_t launch_by_head(const AttnArgs &a, const CachedPlan &p, hipStream_t st
 constexpr int CUS = 256;
 int cached_workers(int D) { return CUS * cached_waves((D + 31) / 32); }
 
+size_t few_partial_bytes(int D) { return (size_t)cached_workers(D) * 2 * 16 * (D + 2) * 4; }
+
 size_t cached_partial_bytes(long long Tq, int B, int Hq, int Hkv, int D)
 {
-    const size_t few = (size_t)cached_workers(D) * 2 * 16 * (D + 2) * 4, many = chunks_partial_bytes(Tq, B, Hq, Hkv, D);
+    const size_t few = few_partial_bytes(D), many = chunks_partial_bytes(Tq, B, Hq, Hkv, D);
+    return few > many ? few : many;
+}
+
+size_t cached_most_bytes(long long Tq, int B, int Hq, int Hkv, int D)
+{
+    const size_t few = few_partial_bytes(D), many = chunks_most_bytes(Tq, B, Hq, Hkv, D);
     return few > many ? few : many;
 }
 

@@ -653,5 +653,13 @@ inline TilePlan tile_plan(long long Tq, int B, int G, int Hkv, int rows, bool cu
     p.mix = mask != 0;
     return p;
 }
+// parts of the cut calls among those of at most Tq rows, B sequences and so many keys: what their workspace has to hold
+inline long long most_parts(long long Tq, int B, int G, int Hkv, int rows, long long keys, int wanted_wgs)
+{
+    long long splits = keys / (4 * ATT_KEYS);
+    splits = splits > TILE_SPLITS ? TILE_SPLITS : splits;
+    const long long parts = (Tq * G / rows + B) * Hkv * splits;
+    return splits < 2 ? 0 : parts > wanted_wgs ? wanted_wgs : parts;
+}
 
 }  // namespace ql

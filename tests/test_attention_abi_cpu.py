@@ -174,3 +174,23 @@ def test_oracle_rotation_is_a_rotation():
         z = (x[:, i].astype(np.float64) + 1j * x[:, j]) * np.exp(1j * a)
         assert np.abs(y[:, i] - z.real).max() < 4e-3 and np.abs(y[:, j] - z.imag).max() < 4e-3     # |z| < 4: half a binary16 step is 2^-10
         assert np.array_equal(y[:, 16:], x[:, 16:].astype(np.float64))
+
+
+@pytest.mark.parametrize("Hq, Hkv, D", [(1, 1, 64), (16, 2, 128), (32, 8, 256), (40, 40, 72), (6, 6, 8)])
+def test_workspace_for_the_largest_call_is_enough_for_smaller_ones(Hq, Hkv, D):
+    """Fewer rows may be cut into more parts: the size is that of the worst call up to the one that is asked for."""
+    rows = [1, 2, 16, 17, 64, 128, 200, 256, 300, 512, 777, 1024, 2048, 4096, 5000, 8192, 65536]
+    keys = [1, 64, 255, 512, 1024, 4095, 8192, 131071]
+    for B in (1, 2, 7, 64, 300):
+        for T_k in keys:
+            sizes = [ql.attention_f16_workspace_bytes(t, T_k, B, Hq, Hkv, D) for t in rows]
+            assert sizes == sorted(sizes), (B, T_k)
+        for t in rows:
+            sizes = [ql.attention_f16_workspace_bytes(t, T_k, B, Hq, Hkv, D) for T_k in keys]
+            assert sizes == sorted(sizes), (B, t)
+        sizes = [ql.attention_kv8_workspace_bytes(t, B, Hq, Hkv, D) for t in rows]
+        assert sizes == sorted(sizes), B
+    for t in rows:
+        for fn in (lambda B: ql.attention_f16_workspace_bytes(t, 8192, B, Hq, Hkv, D), lambda B: ql.attention_kv8_workspace_bytes(t, B, Hq, Hkv, D)):
+            sizes = [fn(B) for B in (1, 2, 7, 64, 300)]
+            assert sizes == sorted(sizes), t

@@ -748,3 +748,18 @@ def test_tensors_made_for_another_stream(name, handle):
         call(**there)
     torch.cuda.synchronize()
     assert torch.equal(kept, want)
+
+
+def test_one_workspace_for_all_smaller_calls():
+    """A program takes its workspace once, for the most rows that it will have."""
+    g = _rng(66)
+    Hq, Hkv, D, n = 16, 2, 64, 4096
+    q, k, v = _dev(_f16(g, n, Hq, D)), _dev(_f16(g, n, Hkv, D)), _dev(_f16(g, n, Hkv, D))
+    c = _Cached(g, 1, n, Hkv, D, 64, 64)
+    lens = _dev(np.array([n], np.int32))
+    dense, cached = ql.workspace(ql.attention_f16_workspace_bytes(n, n, 1, Hq, Hkv, D)), ql.workspace(ql.attention_kv8_workspace_bytes(n, 1, Hq, Hkv, D))
+    for T in (1, 3, 64, 256, 512, 1024, 2048, 4096):
+        a = ql.attention_f16(q[:T], k, v, ws=dense), ql.attention_kv8(q[:T], c.dev, c.table, lens, ws=cached)
+        b = ql.attention_f16(q[:T], k, v), ql.attention_kv8(q[:T], c.dev, c.table, lens)
+        torch.cuda.synchronize()
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])

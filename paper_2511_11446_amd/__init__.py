@@ -718,7 +718,7 @@ def daq_kv_append(cache, k, v, page_table, len_k, cu=None, q=None, rot=None, rot
     rows = half = 0
     if rot is not None:
         rows, half, two = rot.shape
-        if two != 2:
+        if two != 2 or not rows or not half:     # (the address of an empty table is none: no rotation)
             raise ValueError("rot must be [rows, rot_dim / 2, 2]")
     n = _KV_NEW.pack(T, Hq, 1 if rot_pairs else 0, cup, qp, kp, vp, q_row, q_head, k_row, k_head, v_row, v_head, rp, rows, 2 * half, 0, pp, qo, ko, vo)
     _check(lib().daq_kv_append(c, n, _stream(stream)), "daq_kv_append")

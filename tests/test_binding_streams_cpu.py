@@ -158,3 +158,10 @@ def test_the_stream_is_on_the_current_device(name, made):
         CALLS[name](stream=s)
     s.device_index = 0
     CALLS[name](stream=s)
+
+
+@pytest.mark.parametrize("rot", [_t(0, 32, 2, dtype=torch.float32), _t(4, 0, 2, dtype=torch.float32), _t(4, 32, 3, dtype=torch.float32)])
+def test_an_empty_rotation_table_is_refused(rot, made):
+    """Its address is none, which would mean no rotation at all."""
+    with pytest.raises(ValueError, match="rot must be"):
+        ql.daq_kv_append(_cache(), _t(8, 2, 64), _t(8, 2, 64), _ints(1, 2), _ints(1), rot=rot)

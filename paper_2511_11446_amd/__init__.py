@@ -670,6 +670,8 @@ class KvCache8:
     @classmethod
     def empty(cls, num_pages, heads, D, page=64, scale_tokens=64, device="cuda"):
         import torch
+        if page < 64 or page % 64 or scale_tokens not in (1, 16, 32, 64):
+            raise ValueError("page has to be a multiple of 64 and scale_tokens 1, 16, 32 or 64, not %s and %s" % (page, scale_tokens))
         z = dict(device=device)
         scales = (num_pages, heads, page // scale_tokens)
         return cls(torch.zeros((num_pages, heads, page, D), dtype=torch.int8, **z),

@@ -165,3 +165,9 @@ def test_an_empty_rotation_table_is_refused(rot, made):
     """Its address is none, which would mean no rotation at all."""
     with pytest.raises(ValueError, match="rot must be"):
         ql.daq_kv_append(_cache(), _t(8, 2, 64), _t(8, 2, 64), _ints(1, 2), _ints(1), rot=rot)
+
+
+@pytest.mark.parametrize("page, scale_tokens", [(64, 48), (64, 33), (128, 8), (64, 0), (96, 32), (32, 32), (64, 128), (64, -1)])
+def test_an_empty_cache_has_the_scales_that_were_asked_for(page, scale_tokens, made):
+    with pytest.raises(ValueError, match="page|scale_tokens"):
+        ql.KvCache8.empty(4, 2, 64, page=page, scale_tokens=scale_tokens)

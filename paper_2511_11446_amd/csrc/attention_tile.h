@@ -301,6 +301,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = f32x16{};
     float m = -__builtin_inff(), l = 0.0f;             // of this lane's row, m in powers of two; l over this lane's keys only
+    bool far = false;                                  // of the wavefront's rows: some maximum lies beyond EXACT_SCORES
     float unit_v = 0.0f;                               // CACHE: the value scale that the row's sums are in
 
     // left operands: step ks of keys 32 u .. 32 u + 31, step st of value channels 32 d .. 32 d + 31.  A swizzle turns the low bits of a piece's
@@ -446,6 +447,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
             const float keep = m == -__builtin_inff() ? 0.0f : exp2_fast(m - m2);
             l *= keep;
             m = m2;
+            far = __any(fabsf(m) > EXACT_SCORES && m > -__builtin_inff());
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -453,7 +455,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs &a, const TilePlan &p
         }
         const float m0 = m == -__builtin_inff() ? 0.0f : m;
         float mc = shift - m0;
-        if (__any(fabsf(m0) > EXACT_SCORES)) {
+        if (far) {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll

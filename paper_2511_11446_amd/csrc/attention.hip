@@ -7,11 +7,12 @@
 // 5.0 / 4.8; only two sequences of 77 tokens with heads of 16 gained, 4.8 or 4.7 / 4.9.  Many rows lose by them, as each row then reads the keys with
 // fewer others: 16 images of 1024 tokens, 16 heads of 72, 283 or 191 / 140.
 //
-// 16 images of 1024 tokens, 16 heads of 72: 123 us in turn with other work, 0.63 PFLOP/s of the products that D = 72 needs (of the 80 channels that
-// the matrix instructions work on, 0.70); 8192 tokens, 16 heads of 128 on 2, a prefix of 1000: 330 us, 0.84 PFLOP/s.  Bound by issue: of the busy cycles the
-// matrix cores work 43 and 52 %, the vector units 58 and 44 %, LDS conflicts 12 and 0 %; and the chip lowers its clock under it (attention_tile.h).  With a
-// cap and a distance bias (24 packed sequences of up to 1000 tokens, heads of 64; 83 us) the vector units work 86 %, the matrix cores 19 %.  Small calls are a
-// chain of latencies: launch, first tile, a few more, writing.
+// 16 images of 1024 tokens, 16 heads of 72: 120 to 130 us a call, by the machine; at 130 0.59 PFLOP/s of the products that D = 72 needs, and 0.73 of those that the matrix
+// instructions do (80 channels for the scores, 96 for the values).  8192 tokens, 16 heads of 128 on 2, a prefix of 1000: 315 us a call, 0.89 PFLOP/s (the profiler's trace
+// has 340 to 386 us).  Of the busy cycles the matrix cores work 42 and 52 %, the vector units 58 and 44 %, LDS conflicts 11 and 0 %; the wavefronts wait for 31 and 32 % of
+// theirs, three a SIMD with heads of 72 (2048 workgroups are 2.67 rounds of them), two with heads of 128.  With a cap and a distance bias (24 packed sequences of up to 1000 tokens,
+// heads of 64; 83 us) the vector units work 83 %, the matrix cores 19 %: 452 vector instructions for a wavefront's tile.  Heads of 192 and 256, causal, 8192 tokens, 16 on 2: 603 and 743 us, 0.68 and
+// 0.74 PFLOP/s (64: 184 us, 0.75; 128: 315, 0.87).  Small calls are a chain of latencies: launch, first tile, a few more, writing.
 #include "attention_tile.h"
 
 namespace ql {

@@ -2,11 +2,12 @@
 //
 // The tile of attention_tile.h, its keys and values made from the codes: a workgroup reads a group of 64 tokens once, through registers, turns the codes into
 // binary16 (exactly) and leaves them in LDS for its 256 rows.  Where one scale covers the group it goes into the factor of the
-// scores and into the exponent of the weights, at no cost per score; smaller blocks multiply both.
+// scores and into the exponent of the weights; smaller blocks multiply both.  Which of them it is is asked at run time, among the weights too.
 //
-// 8 sequences of 512 new tokens, the longest on 4096 kept ones, 16 heads of 128 on 2, scores capped: 141 us and 17 of join_chunks, 0.27 PFLOP/s.  Bound by
-// the wavefronts' waiting (44 % of their cycles: a barrier a tile, in front of which each turns its share of the codes into binary16) and
-// the vector units (50 % of the busy cycles, the matrix cores 18 %): a capped score takes three instructions of the exponential's rate.
+// 8 sequences of 512 new tokens, the longest on 4096 kept ones, 16 heads of 128 on 2, scores capped: 143 us and 17 of join_chunks, 0.26 PFLOP/s.  The wavefronts
+// wait for 44 % of their cycles, the vector units work 50 % of the busy ones, the matrix cores 18 %: 602 vector instructions for a wavefront's tile, 32 of them of the matrix
+// cores, and 32 to 34 registers of heads of 128 are spilled (49 to 52 of heads of 256): both scale forms are in one kernel, with a branch for every two weights.  Without the cap,
+// 512 rows on 4096 tokens for 8 sequences, 16 heads on 2, blocks of 64 / 16 / 1 tokens: heads of 128 228 / 286 / 288 us, heads of 256 638 / 852 / 851.
 #include "attention_tile.h"
 
 namespace ql {

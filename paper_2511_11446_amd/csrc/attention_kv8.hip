@@ -13,8 +13,8 @@
 // Codes become binary16 exactly; key scales multiply the scores.  Value scales multiply the weights, relative to the largest one that the row has met so far (which its
 // sums are relative to in turn): a weight times a bare scale could fall below binary16's range.
 //
-// 64 sequences of 1 to 8192 tokens, 32 heads of 128 on 8: 77 us and 6 of join_parts for 355 MB, 4.6 TB/s; two of 131071 tokens, 101 + 7 us for 537 MB, 5.3 TB/s, what
-// a copy of that size reaches on this card (5.1 read and written): bound by memory.  One token on 4096, 11 + 5 us: a chain of latencies (queries, page,
+// 64 sequences of 1 to 8192 tokens, 32 heads of 128 on 8: 78 us and 6 of join_parts for 355 MB, 4.5 TB/s; two of 131071 tokens, 102 + 8 us for 537 MB, 5.2 TB/s, what
+// a copy of that size reaches on this card (5.1 read and written): bound by memory.  Heads of 256, 16 on 2, 64 sequences of 4096 tokens: 65 us a call, 4.1 TB/s.  One token on 4096, 11 + 5 us: a chain of latencies (queries, page,
 // keys, scores, values, the wavefronts' join, the second launch).
 #include "attention_tile.h"
 
@@ -523,6 +523,9 @@ size_t cached_most_bytes(long long Tq, int B, int Hq, int Hkv, int D)
 
 // Packed rows of a sequence and key head, on average, up to which they go by 16 rather than by 256 (attention_chunks.hip).  us by 16 / by 256, 32 sequences of 4096 tokens,
 // 8 key heads of 128: 32 rows 91 / 189, 64 rows 163 / 192, 128 rows 314 / 201; heads of 64, 1024 tokens: 16 rows 22 / 22, 32 rows 34 / 29, 64 rows 49 / 30.
+// The average is right for sequences of about as many rows.  Where one has many and others a single token, all go one way (32 heads of 128 on 8, 4096 tokens each): 63 x 1 row 117 us and
+// 1024 rows 162, together by 256 597; 512 rows 108, together with them by 16 233.  By 256 the keys are cut only where the row tiles are few: a row on 131071 tokens, 61 us alone, took 6200
+// beside 2048 rows on 4096 (195 alone).  Such a batch is better called in two.
 int few_rows(int D) { return D > 64 ? 64 : 16; }
 
 hipError_t launch_attention_kv8(const AttnArgs &a, hipStream_t stream)

@@ -210,7 +210,7 @@ def _empty(shape, dtype, device, stream, returned=False):
     with cuda.stream(stream):
         t = torch.empty(shape, dtype=dtype, device=device)
     if returned:
-        t.record_stream(cuda.current_stream())
+        t.record_stream(cuda.current_stream(t.device))
     return t
 
 

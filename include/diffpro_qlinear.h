@@ -566,6 +566,125 @@ int attention_kv8(const ql_attention *attn, const ql_kv_cache *cache,
                   void *workspace, size_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------------
+ * Layers in 8-bit floating point.  The paper quantizes to integers; these calls
+ * carry DAQ (Step 3: scales taken at run time from the values at hand) and the
+ * layer of Step 5 over to e4m3 weights with a scale for every block of 128 x 128,
+ * for weights that are stored so.  Codes are e4m3 (4 exponent and 3 mantissa bits,
+ * largest 448, no infinities; +-0x7f is NaN and is never written).
+ *
+ * daq_quantize_f8.  For row m and the channels k of block b = k / 128 (the last
+ * block of a row may be shorter):
+ *   amax   = max |v[m,k]| over the block
+ *   s[m,b] = fl32(amax / 448)                       (1 if the block is all zero)
+ *   q[m,k] = e4m3 nearest to 448 v[m,k] / amax, ties to the even one (the exact
+ *            quotient decides where v is an input of x; silu below is off by about 2^-22)
+ *   v = x[m,k]                                      glu = 0
+ *   v = silu(x[m,k]) * x[m,K+k] in fp32, silu(a) = a / (1 + exp(-a))    glu = 1
+ *   x       (device) [M,K] fp16, in; [M,2K] with glu: the output [g | u] of the layer
+ *           in front
+ *   q       (device) [M,K] e4m3, out
+ *   scales  (device) [M, ceil(K/128)] fp32, out
+ *
+ * qgemm_f8.  With KB = ceil(K/128), products and sums of a block on the matrix
+ * cores and everything behind them in fp32:
+ *   u[m,n] = sum_b (s[m,b] * w_scale[n/128,b]) * sum_{k in b} q[m,k] * w[n,k]  + bias[n]
+ *   y = as ql_fusion says of u
+ *   w       (device) [N,K] e4m3;  w_scale (device) [ceil(N/128), KB] fp32
+ *   bias    (device) [N] fp16 or NULL
+ *   fusion  as in the *_fused calls, row_absmax NULL (no quantizer here takes it:
+ *           QL_ERR_UNSUPPORTED), or NULL
+ * The sums are off by at most (K + 3 KB) 2^-23 of sum_b |s w_scale| sum_k |q w|.
+ *
+ * qlinear_f8 is daq_quantize_f8 followed by qgemm_f8.
+ * qlinear_f8_workspace_bytes: enough for every call with up to M rows, K inputs and
+ * N outputs (0: sizes that the call refuses).
+ *
+ * K: a multiple of 16; x, q, w and y 16-byte aligned; scales 4-byte aligned.  M * K
+ * (M * 2K with glu), M * N and N * K below 2^31.  NaN codes or scales in w give
+ * unspecified results.
+ * ---------------------------------------------------------------------- */
+int daq_quantize_f8(const void *x, int64_t M, int64_t K, int32_t glu, void *q, void *scales, void *stream);
+int qgemm_f8(const void *q, const void *scales, int64_t M, int64_t K,
+             const void *w, const void *w_scale, const void *bias, int64_t N,
+             const ql_fusion *fusion, void *y, void *stream);
+size_t qlinear_f8_workspace_bytes(int64_t M, int64_t K, int64_t N);
+int qlinear_f8(const void *x, int64_t M, int64_t K, int32_t glu,
+               const void *w, const void *w_scale, const void *bias, int64_t N,
+               const ql_fusion *fusion, void *y,
+               void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Routing to experts (nothing of it is in the paper).  For every token t, in 64 bits:
+ *   s[e] = softmax over e of logits[t,e], or 1 / (1 + exp(-logits[t,e]))
+ *   c[e] = s[e] + bias[e]                           (bias NULL: s[e])
+ * An expert whose logit is NaN or -inf, or whose c is NaN or -inf, cannot be chosen;
+ * a logit of +inf counts as the largest finite number of its type.
+ * With groups > 1 the experts are cut into groups of E / groups neighbours.  A
+ * group's worth is the sum of its group_top (1 or 2) largest c among those that can
+ * be chosen (of those there are); only the top_groups worthiest groups stay in.
+ *   ids[t,j]     the expert with the j-th largest c among those that stay, equal
+ *                ones in the order of their numbers; -1 where none is left
+ *   weights[t,j] scale * s[ids[t,j]], divided before by the sum of the chosen s if renorm
+ *                != 0 (by 1 where that sum is 0); 0 where ids is -1
+ * Without a bias experts are ordered by their logits, which tells them apart where
+ * 64 bits of s do not.
+ *   logits  (device) [T,E] fp16 (logits_fp32 = 0) or fp32 (1);  bias (device) [E] fp32 or NULL
+ *   ids     (device) [T,k] int32, out;  weights (device) [T,k] fp32, out
+ * 1 <= E <= 512, 1 <= k <= E and k <= 64, groups divides E, groups <= 128,
+ * 1 <= top_groups <= groups, T * E below 2^31; scale finite.
+ * ---------------------------------------------------------------------- */
+enum { QL_SCORE_SOFTMAX = 0, QL_SCORE_SIGMOID = 1 };
+
+typedef struct ql_routing {
+    int64_t T;
+    int32_t E, k;
+    int32_t score;         /* QL_SCORE_* */
+    int32_t logits_fp32;   /* 0 or 1 */
+    int32_t groups, top_groups, group_top;   /* 1, 1, 1 or 2: no groups */
+    int32_t renorm;        /* 0 or 1 */
+    float scale;
+    int32_t reserved;      /* 0 */
+    const void *logits;
+    const void *bias;
+    void *ids;
+    void *weights;
+} ql_routing;
+
+int route_experts(const ql_routing *routing, void *stream);
+
+/* Every token through its experts' gated layers:
+ *   xq         = daq_quantize_f8(x[t])
+ *   [g | u]    = xq times the two matrices w_up[e], as qgemm_f8 does, in fp32
+ *   hq         = daq_quantize_f8 of silu(g) * u
+ *   o[t,j]     = fp16( hq times w_down[e] ), e = ids[t,j]   (fp32 where few rows are at hand)
+ *   y[t]       = fp16( residual[t] + sum_j weights[t,j] * o[t,j] ),  added up in the order of j, in fp32
+ *   x        (device) [T,K] fp16;  ids (device) [T,k] int32: an id outside [0,E) is no
+ *            expert, adds nothing and its weight is not read into any result
+ *            (padding, or the experts of another device);  weights (device) [T,k] fp32
+ *   w_up     (device) [E,2,I,K] e4m3, gate and up;  up_scale (device)
+ *            [E,2,ceil(I/128),ceil(K/128)] fp32
+ *   w_down   (device) [E,N,I] e4m3;  down_scale (device) [E,ceil(N/128),ceil(I/128)] fp32
+ *   residual (device) [T,N] fp16 or NULL;  y (device) [T,N] fp16, which may be residual
+ * A token without an expert gets its residual, or 0.  Its x is not read into any result.
+ * K and I: multiples of 16, N of 8.  E <= 512, k <= 64; T * k up to 2^24; T * K,
+ * T * k * I, T * k * N, I * K and N * I below 2^31 (offsets between experts are 64 bits wide).
+ * experts_f8_workspace_bytes: enough for every call of these experts with up to T
+ * tokens and k choices. */
+typedef struct ql_experts_f8 {
+    int64_t T;
+    int32_t k, E;
+    int64_t K, I, N;
+    const void *x, *ids, *weights;
+    const void *w_up, *up_scale;
+    const void *w_down, *down_scale;
+    const void *residual;
+    void *y;
+} ql_experts_f8;
+
+size_t experts_f8_workspace_bytes(int64_t T, int32_t k, int32_t E, int64_t K, int64_t I, int64_t N);
+int experts_f8(const ql_experts_f8 *experts, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
  * Offline side, host memory only (no device call): the stages that produce what
  * the calls above consume.
  *

@@ -30,7 +30,8 @@ EXPORTS = ("ql_status_string", "ql_last_device_error", "ql_version", "daq_worksp
            "ql_schedule_topk", "ql_plan_greedy", "ql_gptq_quantize_host", "daq_quantize_ln",
            "daq_cg_workspace_bytes", "daq_quantize_cg", "qlinear_grouped_workspace_bytes", "qlinear_grouped", "ql_pack_bits_host",
            "ql_unpack_bits_host", "ql_zero_point_fold_host",
-           "attention_f16_workspace_bytes", "attention_f16", "daq_kv_append", "attention_kv8_workspace_bytes", "attention_kv8")
+           "attention_f16_workspace_bytes", "attention_f16", "daq_kv_append", "attention_kv8_workspace_bytes", "attention_kv8",
+           "daq_quantize_f8", "qgemm_f8", "qlinear_f8_workspace_bytes", "qlinear_f8", "route_experts", "experts_f8_workspace_bytes", "experts_f8")
 
 
 class QlError(RuntimeError):
@@ -142,6 +143,20 @@ def lib():
     L.attention_kv8_workspace_bytes.argtypes = [_i64, i32, i32, i32, i32]
     L.attention_kv8.argtypes = [_vp, _vp, _vp, _sz, _vp]
     L.attention_kv8.restype = _int
+    L.daq_quantize_f8.argtypes = [_vp, _i64, _i64, i32, _vp, _vp, _vp]
+    L.daq_quantize_f8.restype = _int
+    L.qgemm_f8.argtypes = [_vp, _vp, _i64, _i64, _vp, _vp, _vp, _i64, ctypes.POINTER(ql_fusion), _vp, _vp]
+    L.qgemm_f8.restype = _int
+    L.qlinear_f8_workspace_bytes.restype = _sz
+    L.qlinear_f8_workspace_bytes.argtypes = [_i64, _i64, _i64]
+    L.qlinear_f8.argtypes = [_vp, _i64, _i64, i32, _vp, _vp, _vp, _i64, ctypes.POINTER(ql_fusion), _vp, _vp, _sz, _vp]
+    L.qlinear_f8.restype = _int
+    L.route_experts.argtypes = [_vp, _vp]
+    L.route_experts.restype = _int
+    L.experts_f8_workspace_bytes.restype = _sz
+    L.experts_f8_workspace_bytes.argtypes = [_i64, i32, i32, _i64, _i64, _i64]
+    L.experts_f8.argtypes = [_vp, _vp, _sz, _vp]
+    L.experts_f8.restype = _int
     _lib = L
     return L
 
@@ -746,6 +761,169 @@ def attention_kv8(q, cache, page_table, len_k, cu_q=None, mask=MASK_CAUSAL, pref
         _elsewhere(ws, "ws")
     _check(lib().attention_kv8(a, c, _ptr(ws), ws.numel(), _stream(stream)), "attention_kv8")
     return o
+
+
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+
+
+class ql_routing(ctypes.Structure):
+    _fields_ = [("T", _i64), ("E", ctypes.c_int32), ("k", ctypes.c_int32), ("score", ctypes.c_int32), ("logits_fp32", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("top_groups", ctypes.c_int32), ("group_top", ctypes.c_int32), ("renorm", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("reserved", ctypes.c_int32), ("logits", _vp), ("bias", _vp), ("ids", _vp), ("weights", _vp)]
+
+
+class ql_experts_f8(ctypes.Structure):
+    _fields_ = [("T", _i64), ("k", ctypes.c_int32), ("E", ctypes.c_int32), ("K", _i64), ("I", _i64), ("N", _i64), ("x", _vp), ("ids", _vp),
+                ("weights", _vp), ("w_up", _vp), ("up_scale", _vp), ("w_down", _vp), ("down_scale", _vp), ("residual", _vp), ("y", _vp)]
+
+
+_ROUTING = struct.Struct("=q8ifi4Q")
+_EXPERTS = struct.Struct("=q2i3q9Q")
+
+
+def _blocks(n):
+    return (n + 127) // 128
+
+
+def _two(t, dtype, name, dev):
+    """A dense [rows, columns] tensor on the current device: its address and sizes."""
+    p = _at(t, dtype, None, name, dev)
+    if t is None or t.dim() != 2:
+        raise TypeError("%s must be a [rows, columns] CUDA tensor of %s" % (name, dtype))
+    return p, t.shape[0], t.shape[1]
+
+
+def _width(columns, glu, name="x"):
+    if glu and columns % 2:
+        raise ValueError("%s has %d columns, with glu it is [g | u]" % (name, columns))
+    return columns // 2 if glu else columns
+
+
+def daq_quantize_f8(x, glu=False, q=None, scales=None, stream=None):
+    """x fp16 [M,K] -> (q float8_e4m3fn [M,K], scales fp32 [M, ceil(K/128)]); glu: x is [M,2K] = [g | u] and silu(g) * u is quantized."""
+    torch = _torch or _load_torch()
+    dev = _current()
+    _here(stream, dev)
+    xp, M, columns = _two(x, torch.float16, "x", dev)
+    K = _width(columns, glu)
+    if q is None:
+        q = _empty((M, K), torch.float8_e4m3fn, x.device, stream, True)
+    if scales is None:
+        scales = _empty((M, _blocks(K)), torch.float32, x.device, stream, True)
+    qp, sp = _at(q, torch.float8_e4m3fn, (M, K), "q", dev), _at(scales, torch.float32, (M, _blocks(K)), "scales", dev)
+    _check(lib().daq_quantize_f8(xp, M, K, 1 if glu else 0, qp, sp, _stream(stream)), "daq_quantize_f8")
+    return q, scales
+
+
+def _layer_f8(dev, M, K, w, w_scale, bias, act, residual, gate, gate_rows, y, device, stream):
+    """What qgemm_f8 and qlinear_f8 have in common: addresses of weights, scales, bias, the fusion and the output."""
+    torch = _torch or _load_torch()
+    wp, N, k = _two(w, torch.float8_e4m3fn, "w", dev)
+    if k != K:
+        raise ValueError("w has shape %s, expected [N, %d]" % (tuple(w.shape), K))
+    if w_scale is None:
+        raise TypeError("w_scale is missing")
+    sp, bp = _at(w_scale, torch.float32, (_blocks(N), _blocks(K)), "w_scale", dev), _at(bias, torch.float16, (N,), "bias", dev)
+    fusion = None
+    if act != ACT_NONE or residual is not None or gate is not None:
+        if gate is not None and (gate_rows < 1 or M % gate_rows):
+            raise ValueError("gate_rows is %s and x has %d rows" % (gate_rows, M))
+        fusion = ql_fusion(act, 0, _at(residual, torch.float16, (M, N), "residual", dev) or None,
+                           None if gate is None else _at(gate, torch.float16, (M // gate_rows, N), "gate", dev), gate_rows, None)
+    if y is None:
+        y = _empty((M, N), torch.float16, device, stream, True)
+    return wp, sp, bp or None, N, None if fusion is None else ctypes.byref(fusion), _at(y, torch.float16, (M, N), "y", dev), y
+
+
+def qgemm_f8(q, scales, w, w_scale, bias=None, act=ACT_NONE, residual=None, gate=None, gate_rows=1, y=None, stream=None):
+    """Codes and scales of daq_quantize_f8 times w float8_e4m3fn [N,K] with w_scale fp32 [ceil(N/128), ceil(K/128)] -> y fp16 [M,N]; bias fp16 [N];
+    act, residual, gate as in qlinear_fused."""
+    torch = _torch or _load_torch()
+    dev = _current()
+    _here(stream, dev)
+    qp, M, K = _two(q, torch.float8_e4m3fn, "q", dev)
+    if scales is None:
+        raise TypeError("scales is missing")
+    sp = _at(scales, torch.float32, (M, _blocks(K)), "scales", dev)
+    wp, ws_p, bp, N, fusion, yp, y = _layer_f8(dev, M, K, w, w_scale, bias, act, residual, gate, gate_rows, y, q.device, stream)
+    _check(lib().qgemm_f8(qp, sp, M, K, wp, ws_p, bp, N, fusion, yp, _stream(stream)), "qgemm_f8")
+    return y
+
+
+def qlinear_f8_workspace_bytes(M, K, N):
+    return int(lib().qlinear_f8_workspace_bytes(M, K, N))
+
+
+def qlinear_f8(x, w, w_scale, bias=None, glu=False, act=ACT_NONE, residual=None, gate=None, gate_rows=1, y=None, ws=None, stream=None):
+    """daq_quantize_f8 and qgemm_f8: x fp16 [M,K] ([M,2K] with glu), w float8_e4m3fn [N,K], w_scale fp32 [ceil(N/128), ceil(K/128)] -> y fp16 [M,N]."""
+    torch = _torch or _load_torch()
+    dev = _current()
+    _here(stream, dev)
+    xp, M, columns = _two(x, torch.float16, "x", dev)
+    K = _width(columns, glu)
+    wp, sp, bp, N, fusion, yp, y = _layer_f8(dev, M, K, w, w_scale, bias, act, residual, gate, gate_rows, y, x.device, stream)
+    if ws is None:
+        ws = workspace(qlinear_f8_workspace_bytes(M, K, N), x.device, stream)
+    elif ws.get_device() != dev:
+        _elsewhere(ws, "ws")
+    _check(lib().qlinear_f8(xp, M, K, 1 if glu else 0, wp, sp, bp, N, fusion, yp, _ptr(ws), ws.numel(), _stream(stream)), "qlinear_f8")
+    return y
+
+
+def route_experts(logits, k, bias=None, score=SCORE_SOFTMAX, groups=1, top_groups=1, group_top=2, renorm=True, scale=1.0, ids=None, weights=None,
+                  stream=None):
+    """logits fp16 or fp32 [T,E] -> (ids int32 [T,k], weights fp32 [T,k]): the k experts of every token by score (SCORE_SOFTMAX / SCORE_SIGMOID) plus bias
+    (fp32 [E]) and the weights that their scores give them.  groups: neighbouring experts cut into as many groups, of which the top_groups with the largest sum of
+    their group_top best stay in; renorm: the weights of a token add up to scale.  -inf hides an expert; ids is -1 where none is left."""
+    torch = _torch or _load_torch()
+    dev = _current()
+    _here(stream, dev)
+    wide = getattr(logits, "dtype", None) == torch.float32
+    lp, T, E = _two(logits, torch.float32 if wide else torch.float16, "logits", dev)
+    if ids is None:
+        ids = _empty((T, k), torch.int32, logits.device, stream, True)
+    if weights is None:
+        weights = _empty((T, k), torch.float32, logits.device, stream, True)
+    r = _ROUTING.pack(T, E, k, score, 1 if wide else 0, groups, top_groups, group_top, 1 if renorm else 0, scale, 0, lp, _at(bias, torch.float32, (E,), "bias", dev),
+                      _at(ids, torch.int32, (T, k), "ids", dev), _at(weights, torch.float32, (T, k), "weights", dev))
+    _check(lib().route_experts(r, _stream(stream)), "route_experts")
+    return ids, weights
+
+
+def experts_f8_workspace_bytes(T, k, E, K, I, N):
+    return int(lib().experts_f8_workspace_bytes(T, k, E, K, I, N))
+
+
+def experts_f8(x, ids, weights, w_up, up_scale, w_down, down_scale, residual=None, y=None, ws=None, stream=None):
+    """Every token through its experts: x fp16 [T,K], ids int32 and weights fp32 [T,k] as route_experts gives them, w_up float8_e4m3fn [E,2,I,K] (gate, up),
+    w_down [E,N,I], their scales fp32 [E,2,ceil(I/128),ceil(K/128)] and [E,ceil(N/128),ceil(I/128)], residual fp16 [T,N] -> y fp16 [T,N].
+    An id outside [0,E) is no expert."""
+    torch = _torch or _load_torch()
+    dev = _current()
+    _here(stream, dev)
+    xp, T, K = _two(x, torch.float16, "x", dev)
+    ip, rows, k = _two(ids, torch.int32, "ids", dev)
+    up, down = _at(w_up, torch.float8_e4m3fn, None, "w_up", dev), _at(w_down, torch.float8_e4m3fn, None, "w_down", dev)
+    if not up or not down or w_up.dim() != 4 or w_down.dim() != 3 or rows != T:
+        raise ValueError("x has %d rows and ids %d; w_up must be [E, 2, I, K] and w_down [E, N, I]" % (T, rows))
+    E, two, I, _ = w_up.shape
+    N = w_down.shape[1]
+    if two != 2 or w_up.shape[3] != K or tuple(w_down.shape) != (E, N, I):
+        raise ValueError("w_up has shape %s and w_down %s, x %d columns" % (tuple(w_up.shape), tuple(w_down.shape), K))
+    if y is None:
+        y = _empty((T, N), torch.float16, x.device, stream, True)
+    if weights is None or up_scale is None or down_scale is None:
+        raise TypeError("weights, up_scale or down_scale is missing")
+    a = _EXPERTS.pack(T, k, E, K, I, N, xp, ip, _at(weights, torch.float32, (T, k), "weights", dev), up,
+                      _at(up_scale, torch.float32, (E, 2, _blocks(I), _blocks(K)), "up_scale", dev), down,
+                      _at(down_scale, torch.float32, (E, _blocks(N), _blocks(I)), "down_scale", dev), _at(residual, torch.float16, (T, N), "residual", dev),
+                      _at(y, torch.float16, (T, N), "y", dev))
+    if ws is None:
+        ws = workspace(experts_f8_workspace_bytes(T, k, E, K, I, N), x.device, stream)
+    elif ws.get_device() != dev:
+        _elsewhere(ws, "ws")
+    _check(lib().experts_f8(a, _ptr(ws), ws.numel(), _stream(stream)), "experts_f8")
+    return y
 
 
 class Plan:

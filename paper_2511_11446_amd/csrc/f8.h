@@ -1,0 +1,155 @@
+// The layers in 8-bit floating point, routing to experts and the experts' layers: launch interface between the host side (f8_api.hip) and
+// the kernels, and device helpers that they share.  Not part of the public ABI.
+#pragma once
+#include "ql_internal.h"
+
+namespace ql {
+
+constexpr int F8_BLOCK = 128;   // channels that share an activation scale, and the side of a weight block
+constexpr float F8_MAX = 448.0f;
+
+inline int f8_blocks(int64_t n) { return (int)((n + F8_BLOCK - 1) / F8_BLOCK); }
+
+struct F8DaqArgs {
+    const void *x;       // fp16 [M,K]; [M,2K] with glu; fp32 [M,K] with wide
+    void *q;             // e4m3 [M,K]
+    float *scales;       // [M, KB]
+    int M, K, KB;
+    bool glu, wide;
+    const int *rows;     // device: rows that there are (at most M), or null: M
+};
+hipError_t launch_daq_f8(const F8DaqArgs &a, hipStream_t stream);
+
+// Where the rows of (token, choice) lie when they are sorted by expert.  All in device memory.
+struct ExpertRows {
+    int *first;          // [E+1] first row of each expert, and how many rows there are
+    int *order;          // [P] row -> token * k + choice
+    int *place;          // [P] token * k + choice -> row, -1 without an expert
+    int *tiles;          // [1 + 2 * most]: how many tiles of `tile` rows there are, then expert and first row of each
+    int *counts;         // [chunks][E] scratch
+    int P, E, tile;
+};
+constexpr int EXPERT_CHUNK = 2048;   // rows that a workgroup sorts
+inline int expert_chunks(int64_t P) { return (int)((P + EXPERT_CHUNK - 1) / EXPERT_CHUNK); }
+inline int64_t expert_tiles_most(int64_t P, int64_t E, int tile) { return P / tile + (P < E ? P : E); }
+hipError_t launch_expert_rows(const int *ids, const ExpertRows &r, hipStream_t stream);
+
+// y[t] = residual[t] + sum_j weights[t,j] * o[place[t,j]]
+struct ExpertSumArgs {
+    const void *o;       // fp16 or (wide) fp32 [rows, N]
+    const int *place;    // [T,k]
+    const float *weights;
+    const void *residual;
+    void *y;
+    int T, k, N;
+    bool wide;
+};
+hipError_t launch_expert_sum(const ExpertSumArgs &a, hipStream_t stream);
+
+struct RouteArgs {
+    const void *logits;
+    const float *bias;
+    int *ids;
+    float *weights;
+    int T, E, k, groups, top_groups, group_top;
+    bool wide, sigmoid, renorm;
+    float scale;
+};
+hipError_t launch_route(const RouteArgs &a, hipStream_t stream);
+
+struct F8Gemm {
+    const uint8_t *q;    // e4m3 [M,K]
+    const float *s;      // [M,KB]
+    const uint8_t *w;    // e4m3 [N,K]; of experts [E][N,K], with gated [E][2][N,K]
+    const float *s_w;    // [NB,KB] of each of these matrices
+    int M, N, K, KB, NB;
+    // a layer's epilogue
+    const void *bias;
+    int act;
+    const void *residual, *gate;
+    int gate_rows;
+    void *y;             // fp16 [M,N]; of experts the rows' outputs, fp32 with wide
+    // experts: rows as ExpertRows says, or null
+    const int *first, *tiles;
+    const int *order;    // row -> token * k + choice where the rows of q are tokens, or null
+    int k, tiles_most, tile;
+    bool gated;          // y = silu(g) * u in fp32 [M,N]
+    bool wide;
+};
+hipError_t launch_qgemm_f8(const F8Gemm &a, hipStream_t stream);
+// rows of an expert's tile, by the rows that an expert has on average
+int f8_expert_tile(int64_t P, int64_t E);
+
+// ---- device helpers -------------------------------------------------------------------------------------------------------------
+
+#ifdef __HIPCC__
+typedef int v8i __attribute__((ext_vector_type(8)));
+
+// silu(a) = a / (1 + 2^(-a log2 e)).  The exponent is taken in two parts (the product and what its rounding lost), so that the power is
+// off by about 2^-22 for every a, not by 2^-24 of the exponent's size; v_exp_f32 and v_rcp_f32 are off by an ulp each.  Below a = -87 the
+// result may be 0 where it is less than 2^-118.
+__device__ __forceinline__ float silu_dev(float a)
+{
+    constexpr float L = -1.44269502f, L_REST = -1.92596299e-8f;   // -log2(e) = L + L_REST
+    const float h = a * L;
+    const float rest = __builtin_fmaf(a, L, -h) + a * L_REST;
+    // 2^rest = 1 + rest ln 2, |rest| < 2^-6 even at the end of binary16's range, where the power is infinite or 0; an infinite power stays so
+    const float e = __builtin_amdgcn_exp2f(h) * __builtin_fmaf(rest, 0.693147182f, 1.0f);
+    return a * __builtin_amdgcn_rcpf(1.0f + e);
+}
+
+// The codes of one block: 448 v / amax to the nearest e4m3 value.  With r = fl(1 / amax), q0 = fl(t r) and the remainder t - q0 amax, which an fma gives without
+// error, q0 + remainder * r is the quotient with less than one rounding of error and exactly where it is representable.  t = 448 v is exact for binary16 v; a quotient of
+// such a t (14 bits) and a binary16 amax (11 bits) that is no tie of e4m3 (5 bits) is at least 2^-16 away from one, so the codes are those of the exact quotient.
+// An amax so small that 1 / amax would be infinite (gated values only) is brought up with the values.
+struct F8Scale {
+    float amax, r, up;
+    __device__ __forceinline__ explicit F8Scale(float a)
+    {
+        up = a < 0x1p-60f ? 0x1p64f * F8_MAX : F8_MAX;
+        amax = a == 0.0f ? 1.0f : a < 0x1p-60f ? a * 0x1p64f : a;
+        r = 1.0f / amax;
+    }
+    __device__ __forceinline__ float code(float v) const
+    {
+        const float t = v * up, q = t * r;
+        return __builtin_fmaf(__builtin_fmaf(-q, amax, t), r, q);
+    }
+    __device__ static __forceinline__ float scale(float a) { return a == 0.0f ? 1.0f : a / F8_MAX; }
+};
+
+// The products of a step of 128 channels, 16 x 16 of them, a lane's 32 bytes of either operand.
+//
+// The codes are taken to binary16, which holds every e4m3 value, and multiplied by v_mfma_f32_16x16x32_f16, whose sums keep 24 bits.
+typedef _Float16 f8_h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f8_h8 __attribute__((ext_vector_type(8)));
+typedef float f8_v4f __attribute__((ext_vector_type(4)));
+struct Wide {
+    f8_h8 h[4];
+    Wide() = default;
+    __device__ __forceinline__ explicit Wide(v8i c)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f8_h2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[2 * i], 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[2 * i], 1.0f, true);
+            const f8_h2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[2 * i + 1], 1.0f, false), e = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[2 * i + 1], 1.0f, true);
+            h[i] = f8_h8{a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
+        }
+    }
+};
+__device__ __forceinline__ f8_v4f step_product(const Wide &a, const Wide &b)
+{
+    f8_v4f d = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.h[i], b.h[i], d, 0, 0, 0);
+    return d;
+}
+// four values to e4m3, round to nearest even; lowest first
+__device__ __forceinline__ unsigned f8_pack4(float a, float b, float c, float d)
+{
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+#endif
+
+}  // namespace ql

@@ -1,0 +1,380 @@
+"""daq_quantize_f8, qgemm_f8, qlinear_f8, route_experts and experts_f8 against the 64-bit oracle, through the C ABI.  Codes of binary16 inputs, scales and
+chosen experts are compared exactly; every other tolerance is the oracle's own count of roundings (oracle/f8.py)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2511_11446_amd as ql
+from oracle import f8 as of
+
+pytestmark = pytest.mark.gpu
+
+F8 = torch.float8_e4m3fn
+
+
+def _rng(*key):
+    return np.random.default_rng([1511, 8, *[k if isinstance(k, int) else sum(map(ord, str(k))) for k in key]])
+
+
+def _dev(x):
+    return None if x is None else torch.from_numpy(np.ascontiguousarray(x)).cuda()
+
+
+def _codes(x):
+    """Values of a float8 tensor."""
+    return of.decode(x.view(torch.uint8).cpu().numpy())
+
+
+def _weights(g, *shape):
+    """Random e4m3 codes (none of them NaN) of every exponent, and scales of differing size: device tensors and the values."""
+    c = g.integers(0, 256, shape).astype(np.uint8)
+    c[(c & 0x7f) == 0x7f] ^= 1
+    s = g.uniform(0.5, 2.0, shape[:-2] + (of.blocks(shape[-2]), of.blocks(shape[-1]))).astype(np.float32) * np.float32(2.0 ** -9)
+    return _dev(c).view(F8), _dev(s), of.decode(c), s
+
+
+def _rows(g, M, K, size=1.0):
+    """Channels of differing size, an outlier, a block of zeros and one of subnormals."""
+    x = g.standard_normal((M, K)) * g.uniform(0.2, 2.0, K) * size
+    x[:, K // 2] *= 30.0
+    x[0, :128] = 0.0
+    x[-1, -16:] = np.float16(6e-8)
+    return x.astype(np.float16)
+
+
+def _close(out, ref, tol, name=""):
+    out = out.float().cpu().numpy().astype(np.float64) if isinstance(out, torch.Tensor) else out
+    bad = ~(np.abs(out - ref) <= tol)
+    assert not bad.any(), "%s: %d of %d off, worst %.3g times the tolerance at %s" % (
+        name, bad.sum(), bad.size, np.nanmax(np.abs(out - ref) / tol), np.argwhere(bad)[:3].tolist())
+
+
+# ---- the quantizer --------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("M, K", [(1, 16), (1, 128), (2, 144), (3, 1152), (17, 272), (64, 4096), (5, 16384), (333, 4608), (1021, 2224), (4097, 128)])
+def test_codes_and_scales_of_binary16(M, K):
+    x = _rows(_rng("q", M, K), M, K)
+    q, s = ql.daq_quantize_f8(_dev(x))
+    _, c, scales = of.quantize(x.astype(np.float64))
+    assert np.array_equal(s.cpu().numpy(), scales)
+    assert np.array_equal(_codes(q), c)
+
+
+def test_codes_at_ties_and_of_every_input():
+    """Every finite binary16 number under its own maximum, and rows whose quotients are exact ties: amax = 448 / 2^j."""
+    every = np.arange(0x7c00, dtype=np.uint16).view(np.float16)
+    rows = np.concatenate([every, -every, np.zeros(-2 * every.size % 127, np.float16)]).reshape(-1, 127)
+    x = np.concatenate([rows, np.abs(rows).max(1, keepdims=True)], axis=1)
+    t = np.zeros((9, 128))
+    for j in range(9):
+        n = np.arange(127)
+        t[j, :127] = (n % 16 + 16.5) * 2.0 ** (n // 16 - j) * (-1.0) ** n      # in the middle of two codes
+        t[j, 127] = 448.0 * 2.0 ** -j
+    x = np.concatenate([x, t.clip(-65504, 65504).astype(np.float16)])
+    assert np.array_equal(x[-9:].astype(np.float64), t)
+    q, s = ql.daq_quantize_f8(_dev(x))
+    _, c, scales = of.quantize(x.astype(np.float64))
+    assert np.array_equal(s.cpu().numpy(), scales) and np.array_equal(_codes(q), c)
+
+
+@pytest.mark.parametrize("M, K", [(1, 16), (3, 128), (33, 1040), (257, 4608), (1021, 2224)])
+def test_codes_and_scales_of_the_gated_product(M, K):
+    g = _rng("glu", M, K)
+    gu = np.concatenate([g.standard_normal((M, K)) * 3.0, _rows(g, M, K)], axis=1).astype(np.float16)
+    gu[0, :K // 2] = -100.0                                # silu of which is 0 or next to it
+    q, s = ql.daq_quantize_f8(_dev(gu), glu=True)
+    a, u = gu[:, :K].astype(np.float64), gu[:, K:].astype(np.float64)
+    v, off = of.gated(a, u, np.zeros_like(a), np.zeros_like(u))
+    amax, s = of.block_max(v), s.cpu().numpy().astype(np.float64)
+    live = amax > 2.0 ** -100
+    assert (np.abs(s * 448.0 - amax)[live] <= 2.0 ** -19 * amax[live]).all()
+    # the scale is the quantizer's own: the code is one of the nearest of the quotient, up to what silu is off
+    t = v / of.by_block(s, K)
+    c = _codes(q)
+    step = np.maximum(of._step(t), of._step(c))
+    assert (np.abs(c - t) <= 0.5 * step + 2.0 ** -19 * np.abs(t) + off / of.by_block(s, K))[of.by_block(live, K)].all()
+
+
+# ---- the product ----------------------------------------------------------------------------------------------------------------
+
+SHAPES = [(1, 16, 1), (1, 128, 16), (1, 4096, 1024), (2, 272, 130), (3, 1152, 384), (7, 128, 1001), (16, 8192, 256), (17, 1152, 1152), (31, 144, 33), (33, 2224, 257),
+          (64, 4096, 512), (65, 384, 2304), (96, 1040, 640), (127, 128, 129), (128, 1152, 1152), (129, 256, 4608), (200, 1024, 500), (255, 640, 255), (256, 384, 512),
+          (257, 272, 513), (300, 1152, 1296), (512, 4608, 1152), (513, 1168, 1000), (1000, 128, 384), (1021, 2224, 1001), (1024, 2048, 2048), (2048, 1152, 3456)]
+
+
+@pytest.mark.parametrize("M, K, N", SHAPES)
+def test_layer_against_the_formula(M, K, N):
+    g = _rng("layer", M, K, N)
+    x, (dw, ds, w, s) = _rows(g, M, K), _weights(g, N, K)
+    bias = g.standard_normal(N).astype(np.float16)
+    y = torch.full((M + 1, N), 7.0, dtype=torch.float16, device="cuda")
+    out = ql.qlinear_f8(_dev(x), dw, ds, bias=_dev(bias), y=y[:M])
+    torch.cuda.synchronize()
+    assert out.data_ptr() == y.data_ptr() and bool((y[M] == 7.0).all())
+    _, c, sx = of.quantize(x.astype(np.float64))
+    _close(out, *of.layer(c, sx, w, s, bias), name=str((M, K, N)))
+    q, scales = ql.daq_quantize_f8(_dev(x))
+    assert torch.equal(ql.qgemm_f8(q, scales, dw, ds, bias=_dev(bias)), out)
+
+
+@pytest.mark.parametrize("M, K, N", [(1, 128, 257), (12, 1152, 384), (48, 272, 1001), (256, 640, 512), (768, 384, 1000), (1024, 1152, 1152)])
+@pytest.mark.parametrize("what", ["gelu", "residual", "gate", "all"])
+def test_layer_with_glue(M, K, N, what):
+    g = _rng("glue", M, K, N, what)
+    x, (dw, ds, w, s) = _rows(g, M, K, 0.05), _weights(g, N, K)
+    res = (g.standard_normal((M, N)) * 2).astype(np.float16) if what in ("residual", "all") else None
+    rows = next(r for r in (4, 3, 1) if M % r == 0)
+    gate = g.standard_normal((M // rows, N)).astype(np.float16) if what in ("gate", "all") else None
+    bias = g.standard_normal(N).astype(np.float16) if what == "all" else None
+    act = ql.ACT_GELU_TANH if what in ("gelu", "all") else ql.ACT_NONE
+    out = ql.qlinear_f8(_dev(x), dw, ds, bias=_dev(bias), act=act, residual=_dev(res), gate=_dev(gate), gate_rows=rows)
+    _, c, sx = of.quantize(x.astype(np.float64))
+    _close(out, *of.layer(c, sx, w, s, bias, act, res, gate, rows), name=what)
+
+
+@pytest.mark.parametrize("M, K, N", [(1, 256, 128), (64, 1040, 384), (640, 1152, 512)])
+def test_gated_input_is_the_quantizer_then_the_product(M, K, N):
+    g = _rng("glu layer", M, K, N)
+    gu = np.concatenate([_rows(g, M, K, 0.5), _rows(g, M, K)], axis=1)
+    dw, ds, w, s = _weights(g, N, K)
+    q, scales = ql.daq_quantize_f8(_dev(gu), glu=True)
+    out = ql.qlinear_f8(_dev(gu), dw, ds, glu=True)
+    assert torch.equal(out, ql.qgemm_f8(q, scales, dw, ds))
+    _close(out, *of.layer(_codes(q), scales.cpu().numpy(), w, s))
+
+
+def test_residual_in_place():
+    """y may be the residual: every element is read before it is written."""
+    g = _rng("in place")
+    for M in (5, 300):
+        x, (dw, ds, w, s) = _rows(g, M, 384), _weights(g, 520, 384)
+        res = g.standard_normal((M, 520)).astype(np.float16)
+        y = _dev(res)
+        apart = ql.qlinear_f8(_dev(x), dw, ds, residual=_dev(res))
+        ql.qlinear_f8(_dev(x), dw, ds, residual=y, y=y)
+        assert torch.equal(apart, y)
+
+
+# ---- routing --------------------------------------------------------------------------------------------------------------------
+
+def _check_route(x, k, **kw):
+    bias = kw.pop("bias", None)
+    ids, w = ql.route_experts(_dev(x), k, bias=_dev(bias), score=ql.SCORE_SIGMOID if kw.get("sigmoid") else ql.SCORE_SOFTMAX,
+                              **{n: v for n, v in kw.items() if n != "sigmoid"})
+    ref_ids, ref_w = of.route(x, k, bias, **kw)
+    assert np.array_equal(ids.cpu().numpy(), ref_ids)
+    _close(w, ref_w, 2.0 ** -23 * np.abs(ref_w) + 2.0 ** -149)
+
+
+@pytest.mark.parametrize("T, E, k", [(1, 1, 1), (1, 8, 2), (3, 60, 4), (64, 64, 6), (65, 72, 1), (130, 128, 8), (257, 160, 8), (300, 256, 8), (33, 384, 6), (20, 512, 64), (7, 512, 9)])
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("half", [False, True])
+def test_routes(T, E, k, sigmoid, half):
+    g = _rng("route", T, E, k)
+    x = (g.standard_normal((T, E)) * 2).astype(np.float16 if half else np.float32)
+    bias = (g.standard_normal(E) * 0.1).astype(np.float32)
+    _check_route(x, k, sigmoid=sigmoid)
+    _check_route(x, k, sigmoid=sigmoid, bias=bias, renorm=False, scale=2.5)
+
+
+@pytest.mark.parametrize("E, groups, top_groups, group_top, k", [(8, 8, 3, 2, 3), (64, 8, 4, 2, 6), (64, 4, 1, 1, 8), (256, 8, 4, 2, 8), (60, 15, 4, 2, 4), (512, 128, 20, 2, 8), (128, 128, 7, 1, 8),
+                                                             (72, 2, 1, 2, 2), (256, 8, 8, 2, 8)])
+@pytest.mark.parametrize("bias", [False, True])
+def test_routes_by_groups(E, groups, top_groups, group_top, k, bias):
+    g = _rng("groups", E, groups, k)
+    x = g.standard_normal((77, E)).astype(np.float32)
+    x[5, :] = x[5, 0]                                       # all alike: the lowest numbers
+    x[6, g.random(E) < 0.7] = -np.inf
+    x[7, :] = -np.inf
+    x[7, E - 1] = 0.0
+    x[8, :] = -np.inf
+    b = (g.standard_normal(E) * 0.2).astype(np.float32) if bias else None
+    for sigmoid in (False, True):
+        _check_route(x, k, sigmoid=sigmoid, bias=b, groups=groups, top_groups=top_groups, group_top=group_top)
+
+
+def test_routes_of_masked_infinite_and_equal_logits():
+    g = _rng("masked")
+    for dtype in (np.float16, np.float32):
+        x = g.standard_normal((9, 100)).astype(dtype)
+        x[0] = -np.inf                                      # a row that its mask leaves empty
+        x[1, 3:] = -np.inf                                  # fewer experts than choices
+        x[2, ::2] = np.nan
+        x[3, 7] = np.inf
+        x[4, [2, 9, 50]] = np.inf
+        x[5] = np.finfo(dtype).min                          # a mask of the type's lowest value, everywhere
+        x[6, 1:] = np.finfo(dtype).min
+        x[7] = 0.0
+        x[8, :50] = -0.0
+        bias = np.zeros(100, np.float32)
+        bias[11], bias[12] = -np.inf, np.nan
+        for sigmoid in (False, True):
+            _check_route(x, 5, sigmoid=sigmoid)
+            _check_route(x, 5, sigmoid=sigmoid, bias=bias)
+            _check_route(x, 5, sigmoid=sigmoid, renorm=False)
+
+
+def test_routes_that_32_bits_cannot_tell_apart():
+    """Biases and logits that meet in the 40th bit."""
+    g = _rng("near")
+    T, E = 64, 64
+    x = g.standard_normal((T, E)).astype(np.float32)
+    s = 1.0 / (1.0 + np.exp(-x[0].astype(np.float64)))
+    x[:] = x[0]
+    bias = (0.7 - s).astype(np.float32)                    # choices within 2^-25 of each other
+    x[1:, :] += (g.integers(-2, 3, (T - 1, E)) * np.spacing(x[1:])).astype(np.float32)
+    _check_route(x, 8, sigmoid=True, bias=bias)
+    _check_route(np.round(x, 1).astype(np.float16), 8, sigmoid=True)
+
+
+# ---- the experts ----------------------------------------------------------------------------------------------------------------
+
+def _experts(g, T, E, k, K, I, N, residual=False, ids=None):
+    up, ups, w_up, s_up = _weights(g, E, 2, I, K)
+    down, downs, w_down, s_down = _weights(g, E, N, I)
+    x = _rows(g, T, K, 0.3)
+    if ids is None:
+        ids = np.stack([g.permutation(E)[:k] if k <= E else g.integers(0, E, k) for _ in range(T)]).astype(np.int32)
+    weights = g.uniform(-0.2, 1.0, (T, k)).astype(np.float32)
+    res = g.standard_normal((T, N)).astype(np.float16) if residual else None
+    ref = of.experts(x, ids, weights, w_up, s_up, w_down, s_down, res)
+    return (_dev(x), _dev(ids), _dev(weights), up, ups, down, downs), res, ref
+
+
+@pytest.mark.parametrize("T, E, k, K, I, N", [(1, 1, 1, 16, 16, 8), (1, 8, 2, 128, 128, 128), (1, 64, 6, 1152, 384, 256), (2, 4, 4, 272, 144, 136), (5, 60, 4, 256, 400, 264), (16, 3, 2, 384, 256, 384),
+                                              (33, 8, 8, 144, 272, 520), (64, 128, 8, 256, 128, 256), (100, 2, 1, 640, 128, 640), (300, 4, 3, 256, 336, 264), (700, 5, 2, 384, 256, 256),
+                                              (1500, 3, 2, 128, 400, 384), (600, 512, 1, 128, 128, 128), (2100, 2, 2, 144, 128, 136)])
+def test_experts_against_the_formula(T, E, k, K, I, N):
+    g = _rng("experts", T, E, k, K, I, N)
+    args, res, (ref, tol) = _experts(g, T, E, k, K, I, N, residual=T % 2 == 0)
+    y = torch.full((T + 1, N), 7.0, dtype=torch.float16, device="cuda")
+    ql.experts_f8(*args, residual=_dev(res), y=y[:T])
+    torch.cuda.synchronize()
+    assert bool((y[T] == 7.0).all())
+    _close(y[:T], ref, tol, str((T, E, k, K, I, N)))
+
+
+@pytest.mark.parametrize("T, E, k, I", [(40, 8, 2, 144), (400, 4, 3, 256), (3, 16, 5, 128)])
+def test_tokens_without_experts_and_experts_twice(T, E, k, I):
+    """Padding, experts of another device, the same expert twice, an expert that has all tokens and others that have none."""
+    g = _rng("ids", T, E, k)
+    ids = g.integers(0, E, (T, k)).astype(np.int32)
+    ids[0] = -1
+    ids[1, 0] = E
+    ids[2, 0], ids[2, k - 1] = 2 ** 31 - 1, -2 ** 31
+    ids[T // 2:, 0] = 1
+    ids[T // 3: T // 2] = 1                                 # every choice the same
+    ids[ids == 2] = 3
+    args, res, (ref, tol) = _experts(g, T, E, k, 256, I, 264, True, ids)
+    args[2][0] = float("nan")                               # weights of choices that are none
+    _close(ql.experts_f8(*args, residual=_dev(res)), ref, tol)
+    y = _dev(res)
+    ql.experts_f8(*args, residual=y, y=y)
+    _close(y, ref, tol, "in place")
+    args[1][:] = -1
+    assert bool((ql.experts_f8(*args) == 0).all()) and torch.equal(ql.experts_f8(*args, residual=_dev(res)), _dev(res))
+
+
+def test_rows_of_a_token_do_not_depend_on_the_batch():
+    """A token alone and the same token among others, in calls of the same size: bit for bit."""
+    g = _rng("batch")
+    args, _, _ = _experts(g, 96, 8, 2, 256, 256, 256)
+    y = ql.experts_f8(*args)
+    order = torch.randperm(96, generator=torch.Generator().manual_seed(3)).cuda()
+    again = ql.experts_f8(args[0][order].contiguous(), args[1][order].contiguous(), args[2][order].contiguous(), *args[3:])
+    assert torch.equal(again, y[order]) and torch.equal(ql.experts_f8(*args), y)
+
+
+# ---- together, as a program has them --------------------------------------------------------------------------------------------
+
+def _block(T, E, k, K, I, seed=0):
+    """A block of a mixture: router's logits from a layer in FP16, routing, a shared gated layer, the experts on top of it."""
+    g = _rng("block", T, E, seed)
+    w_router = _dev((g.standard_normal((E, K)) * K ** -0.5).astype(np.float16))
+    up, ups, w_up, s_up = _weights(g, E, 2, I, K)
+    down, downs, w_down, s_down = _weights(g, E, K, I)
+    su, sus, _, _ = _weights(g, 2 * I, K)
+    sd, sds, _, _ = _weights(g, K, I)
+    x = _dev(_rows(g, T, K, 0.3))
+    bias = _dev((g.standard_normal(E) * 0.05).astype(np.float32))
+    room = dict(ids=torch.empty((T, k), dtype=torch.int32, device="cuda"), weights=torch.empty((T, k), device="cuda"), logits=torch.empty((T, E), dtype=torch.float16, device="cuda"),
+                gu=torch.empty((T, 2 * I), dtype=torch.float16, device="cuda"), shared=torch.empty((T, K), dtype=torch.float16, device="cuda"),
+                y=torch.empty((T, K), dtype=torch.float16, device="cuda"), ws=ql.workspace(max(ql.experts_f8_workspace_bytes(T, k, E, K, I, K), ql.qlinear_f8_workspace_bytes(T, K, 2 * I),
+                                                                                        ql.qlinear_f8_workspace_bytes(T, I, K))))
+
+    def step():
+        ql.qlinear_f16(x, w_router, y=room["logits"])
+        ql.route_experts(room["logits"], k, bias=bias, score=ql.SCORE_SIGMOID, groups=4, top_groups=2, ids=room["ids"], weights=room["weights"])
+        ql.qlinear_f8(x, su, sus, y=room["gu"], ws=room["ws"])
+        ql.qlinear_f8(room["gu"], sd, sds, glu=True, residual=x, y=room["shared"], ws=room["ws"])
+        return ql.experts_f8(x, room["ids"], room["weights"], up, ups, down, downs, residual=room["shared"], y=room["y"], ws=room["ws"])
+
+    def check():
+        ids, w = room["ids"].cpu().numpy(), room["weights"].cpu().numpy()
+        ref_ids, ref_w = of.route(room["logits"].cpu().numpy(), k, bias.cpu().numpy(), True, 4, 2)
+        assert np.array_equal(ids, ref_ids)
+        _close(w, ref_w, 2.0 ** -23 * ref_w)
+        ref, tol = of.experts(x.cpu().numpy(), ids, w, w_up, s_up, w_down, s_down, room["shared"].cpu().numpy())
+        _close(room["y"], ref, tol)
+
+    return step, check, x, room
+
+
+@pytest.mark.parametrize("T, E, k, K, I", [(1, 16, 4, 256, 128), (50, 16, 4, 384, 256), (700, 8, 2, 256, 272)])
+def test_a_block_of_a_mixture(T, E, k, K, I):
+    step, check, _, _ = _block(T, E, k, K, I)
+    step()
+    check()
+
+
+@pytest.mark.parametrize("T", [1, 60, 600])
+def test_a_captured_block(T):
+    """Replayed with other tokens in the same buffers, eager work of another block in between: every replay is the eager result."""
+    step, check, x, room = _block(T, 8, 2, 256, 256)
+    other, other_check, _, _ = _block(T + 3, 8, 2, 256, 256, seed=1)
+    step()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        x.copy_(_dev(_rows(_rng("replay", T, i), T, 256, 0.3)))
+        other()
+        room["y"].fill_(9.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = room["y"].clone()
+        check()
+        room["y"].fill_(9.0)
+        step()
+        assert torch.equal(room["y"], replayed)
+    other_check()
+
+
+def test_two_streams_at_once():
+    """Two blocks with workspaces of their own, on two streams."""
+    (a, check_a, _, _), (b, check_b, _, _) = _block(200, 8, 2, 256, 256, seed=2), _block(3, 8, 2, 256, 256, seed=3)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for fn in (a, b):
+            s = torch.cuda.Stream()
+            with torch.cuda.stream(s):
+                fn()
+    torch.cuda.synchronize()
+    check_a()
+    check_b()
+
+
+def test_one_workspace_for_calls_of_fewer_tokens():
+    g = _rng("fewer")
+    E, k, K, I = 8, 2, 256, 144
+    ws = torch.full((ql.experts_f8_workspace_bytes(300, k, E, K, I, K),), 255, dtype=torch.uint8, device="cuda")
+    for T in (300, 299, 128, 17, 1):
+        args, res, (ref, tol) = _experts(g, T, E, k, K, I, K, True)
+        _close(ql.experts_f8(*args, residual=_dev(res), ws=ws), ref, tol, str(T))
+    dw, ds, w, s = _weights(g, 384, 1152)
+    ws = ql.workspace(ql.qlinear_f8_workspace_bytes(500, 1152, 384))
+    for M in (500, 64, 3, 1):
+        x = _rows(g, M, 1152)
+        _, c, sx = of.quantize(x.astype(np.float64))
+        _close(ql.qlinear_f8(_dev(x), dw, ds, ws=ws), *of.layer(c, sx, w, s))

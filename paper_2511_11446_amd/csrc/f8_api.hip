@@ -66,8 +66,9 @@ ql::F8Gemm gemm_args(const void *q, const void *scales, int64_t M, int64_t K, co
     return g;
 }
 
-int run_layer(ql::F8Gemm g, const void *bias, const ql_fusion *f, hipStream_t s)
+int run_layer(ql::F8Gemm g, const void *bias, const ql_fusion *f, bool glu, hipStream_t s)
 {
+    g.codes = !glu;
     g.bias = bias;
     if (f) {
         g.act = f->act;
@@ -95,7 +96,7 @@ struct ExpertRoom {
         P = T * k;
         tile = ql::f8_expert_tile(P, E);
         tiles_most = ql::expert_tiles_most(P, E, tile);
-        wide = true;
+        wide = tile < ql::F8_TILE_ROWS;
         size_t at = 0;
         auto take = [&](size_t bytes) {
             const size_t here = at;
@@ -145,7 +146,7 @@ int qgemm_f8(const void *q, const void *scales, int64_t M, int64_t K, const void
     int rc = check_layer(M, K, N, 0);
     if (rc || (rc = check_fusion(fusion, M))) return rc;
     if (off(q, 16) || off(w, 16) || off(y, 16) || off(scales, 4) || off(w_scale, 4) || off(bias, 2)) return QL_ERR_ALIGN;
-    return run_layer(gemm_args(q, scales, M, K, w, w_scale, N, y), bias, fusion, static_cast<hipStream_t>(stream));
+    return run_layer(gemm_args(q, scales, M, K, w, w_scale, N, y), bias, fusion, false, static_cast<hipStream_t>(stream));
 }
 
 size_t qlinear_f8_workspace_bytes(int64_t M, int64_t K, int64_t N)
@@ -165,7 +166,7 @@ int qlinear_f8(const void *x, int64_t M, int64_t K, int32_t glu, const void *w, 
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     hipStream_t s = static_cast<hipStream_t>(stream);
     if ((rc = ql::status_of(ql::launch_daq_f8(daq_args(x, M, K, glu, ws, ws + room.scales), s)))) return rc;
-    return run_layer(gemm_args(ws, ws + room.scales, M, K, w, w_scale, N, y), bias, fusion, s);
+    return run_layer(gemm_args(ws, ws + room.scales, M, K, w, w_scale, N, y), bias, fusion, glu != 0, s);
 }
 
 int route_experts(const ql_routing *r, void *stream)
@@ -234,11 +235,15 @@ int experts_f8(const ql_experts_f8 *x, void *workspace, size_t workspace_bytes, 
     up.tiles_most = (int)room.tiles_most;
     up.tile = room.tile;
     up.gated = true;
+    up.hq = ws + room.hq;
+    up.hs = reinterpret_cast<float *>(ws + room.hs);
     if ((rc = ql::status_of(ql::launch_qgemm_f8(up, s)))) return rc;
-    ql::F8DaqArgs d = daq_args(ws + room.h, room.P, x->I, 0, ws + room.hq, ws + room.hs);
-    d.wide = true;
-    d.rows = rows.first + x->E;
-    if ((rc = ql::status_of(ql::launch_daq_f8(d, s)))) return rc;
+    if (room.tile < ql::F8_TILE_ROWS) {
+        ql::F8DaqArgs d = daq_args(ws + room.h, room.P, x->I, 0, ws + room.hq, ws + room.hs);
+        d.wide = true;
+        d.rows = rows.first + x->E;
+        if ((rc = ql::status_of(ql::launch_daq_f8(d, s)))) return rc;
+    }
     ql::F8Gemm down = gemm_args(ws + room.hq, ws + room.hs, room.P, x->I, x->w_down, x->down_scale, x->N, ws + room.o);
     down.first = rows.first;
     down.tiles = rows.tiles;

@@ -4,8 +4,7 @@
 // A K step is one block of 128 channels: the matrix cores give its 16 x 16 sums from zero (f8.h), one fma a sum takes them into the
 // result with the product of the two scales.  The weights are the instruction's first operand: a lane's four sums are then four outputs of one row, and as
 // 16 outputs lie in one weight block, all its sums of a step have one scale: s[row] * s_w.
-#include "f8.h"
-#include "qgemm_common.h"
+#include "qgemm_f8.h"
 
 namespace ql {
 
@@ -42,24 +41,6 @@ __device__ __forceinline__ void store4(void *y, long long m, int N, int n, const
             for (int r = 0; r < 4; ++r)
                 if (n + r < N) at[r] = h[r];
         }
-    }
-}
-
-// a layer's epilogue: u, the fp32 value -> h = fp16(act(u)), then fma(gate, h, residual)
-__device__ __forceinline__ void finish4(const F8Gemm &a, int m, int n, float (&u)[4])
-{
-    const _Float16 *bias = static_cast<const _Float16 *>(a.bias), *res = static_cast<const _Float16 *>(a.residual), *gate = static_cast<const _Float16 *>(a.gate);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const int c = min(n + r, a.N - 1);
-        if (bias) u[r] += (float)bias[c];
-        if (a.act == 1) u[r] = gelu_tanh_dev(u[r]);
-        if (res || gate) {
-            asm volatile("" : "+v"(u[r]));
-            const float h = (float)(_Float16)u[r];
-            u[r] = __builtin_fmaf(gate ? (float)gate[(long long)(m / a.gate_rows) * a.N + c] : 1.0f, h, res ? (float)res[(long long)m * a.N + c] : 0.0f);
-        }
-        asm volatile("" : "+v"(u[r]));   // the fp32 value is rounded to fp16 in the store and nowhere earlier
     }
 }
 
@@ -150,10 +131,11 @@ __global__ __launch_bounds__(64 * WAVES) void qgemm_f8_few(F8Gemm a)
     }
 }
 
-int f8_expert_tile(int64_t, int64_t) { return 16; }
+int f8_expert_tile(int64_t P, int64_t E) { return P >= 64 * E ? F8_TILE_ROWS : 16; }
 
 hipError_t launch_qgemm_f8(const F8Gemm &a, hipStream_t stream)
 {
+    if (a.first ? a.tile >= F8_TILE_ROWS : a.M > 256) return launch_qgemm_f8_tiles(a, stream);
     if (a.first) {
         const dim3 grid((unsigned)((a.N + 31) / 32) * (unsigned)a.tiles_most);
         if (a.gated) hipLaunchKernelGGL((qgemm_f8_few<1, 2, 4, true, true>), grid, dim3(256), 0, stream, a);

@@ -42,6 +42,9 @@ def _rows(g, M, K, size=1.0):
     return x.astype(np.float16)
 
 
+MANY = 256      # rows from which on the matrix cores' own sums of codes are taken (the header's bound has a term for them)
+
+
 def _close(out, ref, tol, name=""):
     out = out.float().cpu().numpy().astype(np.float64) if isinstance(out, torch.Tensor) else out
     bad = ~(np.abs(out - ref) <= tol)
@@ -112,7 +115,7 @@ def test_layer_against_the_formula(M, K, N):
     torch.cuda.synchronize()
     assert out.data_ptr() == y.data_ptr() and bool((y[M] == 7.0).all())
     _, c, sx = of.quantize(x.astype(np.float64))
-    _close(out, *of.layer(c, sx, w, s, bias), name=str((M, K, N)))
+    _close(out, *of.layer(c, sx, w, s, bias, core=M > MANY), name=str((M, K, N)))
     q, scales = ql.daq_quantize_f8(_dev(x))
     assert torch.equal(ql.qgemm_f8(q, scales, dw, ds, bias=_dev(bias)), out)
 
@@ -129,7 +132,7 @@ def test_layer_with_glue(M, K, N, what):
     act = ql.ACT_GELU_TANH if what in ("gelu", "all") else ql.ACT_NONE
     out = ql.qlinear_f8(_dev(x), dw, ds, bias=_dev(bias), act=act, residual=_dev(res), gate=_dev(gate), gate_rows=rows)
     _, c, sx = of.quantize(x.astype(np.float64))
-    _close(out, *of.layer(c, sx, w, s, bias, act, res, gate, rows), name=what)
+    _close(out, *of.layer(c, sx, w, s, bias, act, res, gate, rows, M > MANY), name=what)
 
 
 @pytest.mark.parametrize("M, K, N", [(1, 256, 128), (64, 1040, 384), (640, 1152, 512)])
@@ -139,7 +142,10 @@ def test_gated_input_is_the_quantizer_then_the_product(M, K, N):
     dw, ds, w, s = _weights(g, N, K)
     q, scales = ql.daq_quantize_f8(_dev(gu), glu=True)
     out = ql.qlinear_f8(_dev(gu), dw, ds, glu=True)
-    assert torch.equal(out, ql.qgemm_f8(q, scales, dw, ds))
+    apart = ql.qgemm_f8(q, scales, dw, ds)
+    if M <= MANY:
+        assert torch.equal(out, apart)
+    _close(apart, *of.layer(_codes(q), scales.cpu().numpy(), w, s, core=M > MANY))
     _close(out, *of.layer(_codes(q), scales.cpu().numpy(), w, s))
 
 
@@ -377,4 +383,4 @@ def test_one_workspace_for_calls_of_fewer_tokens():
     for M in (500, 64, 3, 1):
         x = _rows(g, M, 1152)
         _, c, sx = of.quantize(x.astype(np.float64))
-        _close(ql.qlinear_f8(_dev(x), dw, ds, ws=ws), *of.layer(c, sx, w, s))
+        _close(ql.qlinear_f8(_dev(x), dw, ds, ws=ws), *of.layer(c, sx, w, s, core=M > MANY))

@@ -11,7 +11,7 @@ struct TileF8 {
     static constexpr bool WIDE = WIDE_;
     static constexpr int NW = WM * WN, NTHR = 64 * NW, BM = 16 * MT * WM, BN = 16 * NT * WN;
     static constexpr int NA = BM / 8 / NW, NB = BN / 8 / NW;             // DMA instructions of 8 rows for each wavefront and step
-    static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, S_AT = A_BYTES + B_BYTES, STAGE = S_AT + BM * 4;
+    static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, S_AT = A_BYTES + B_BYTES, STAGE = S_AT + BM * 4 + 256;
     static constexpr int ISSUED = NA + NB + 1;                           // and one for the rows' scales
     static constexpr int LDS_BYTES = STAGES * STAGE;
     static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && BM % 64 == 0 && NT % 2 == 0 && (16 * NT <= 128), "whole DMA instructions");
@@ -79,26 +79,36 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
     // rows of one DMA instruction begin at a multiple of 8: (r >> 1) & 3 is the lane's, bit 2 that of the instruction's number
 #pragma unroll
     for (int h = 0; h < 2; ++h) dead[h] = 16 * ((lane & 7) ^ ((lane >> 4 & 3) + 4 * h)) >= last;
-    offS = (unsigned)source_row(64 * (wave % (T::BM / 64)) + lane) * (unsigned)a.KB * 4u;
+    // One operation a wavefront brings scales: the first BM / 64 wavefronts those of 64 rows, the others (all of them the same, so that every wavefront has as
+    // many operations under way) those of the tile's two weight blocks: of neighbouring outputs, or of gate and up.
+    constexpr int SW = T::BM / 64;
+    const bool row_scales = wave < SW;
+    const float *scales = row_scales ? a.s : s_w;
+    if (row_scales) offS = (unsigned)source_row(64 * wave + lane) * (unsigned)a.KB * 4u;
+    else offS = (unsigned)(GATED ? n0 / F8_BLOCK + (lane & 1) * a.NB : min(n0 / F8_BLOCK + (lane & 1), a.NB - 1)) * (unsigned)a.KB * 4u;
+    const unsigned s_at = T::S_AT + (row_scales ? wave : SW) * 256;
 
     auto issue = [&](int kt, int stage) {
         unsigned char *st = smem + stage * T::STAGE;
-        const bool tail = kt == a.KB - 1 && last != F8_BLOCK;
+        if (kt == a.KB - 1 && last != F8_BLOCK) {
 #pragma unroll
-        for (int i = 0; i < T::NA; ++i) {
-            const int at = wave + i * T::NW;
-            if (tail) dma16_buf(a.q, bytesA, st + at * 1024, dead[at & 1] ? 0xfffffff0u : offA[i] + (unsigned)kt * 128u, 0);
-            else dma16_buf(a.q, bytesA, st + at * 1024, offA[i], kt * 128);
-        }
+            for (int i = 0; i < T::NA; ++i) {
+                const int at = wave + i * T::NW;
+                dma16_buf(a.q, bytesA, st + at * 1024, dead[at & 1] ? 0xfffffff0u : offA[i] + (unsigned)kt * 128u, 0);
+            }
 #pragma unroll
-        for (int i = 0; i < T::NB; ++i) {
-            const int at = wave + i * T::NW;
-            if (tail) dma16_buf(w, bytesB, st + T::A_BYTES + at * 1024, dead[at & 1] ? 0xfffffff0u : offB[i] + (unsigned)kt * 128u, 0);
-            else dma16_buf(w, bytesB, st + T::A_BYTES + at * 1024, offB[i], kt * 128);
+            for (int i = 0; i < T::NB; ++i) {
+                const int at = wave + i * T::NW;
+                dma16_buf(w, bytesB, st + T::A_BYTES + at * 1024, dead[at & 1] ? 0xfffffff0u : offB[i] + (unsigned)kt * 128u, 0);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < T::NA; ++i) dma16_buf(a.q, bytesA, st + (wave + i * T::NW) * 1024, offA[i], kt * 128);
+#pragma unroll
+            for (int i = 0; i < T::NB; ++i) dma16_buf(w, bytesB, st + T::A_BYTES + (wave + i * T::NW) * 1024, offB[i], kt * 128);
         }
-        // (several wavefronts bring the same scales, so that all have as many operations under way)
-        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(a.s), 0, 0xffffffff, 0x00020000);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(st + T::S_AT + wave % (T::BM / 64) * 256), 4, offS, kt * 4, 0, 0);
+        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(scales), 0, 0xffffffff, 0x00020000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(st + s_at), 4, offS, kt * 4, 0, 0);
     };
 
     // ---- fragments
@@ -116,7 +126,7 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
 
     // a wavefront's outputs lie in one weight block (of each matrix)
     const int col0 = n0 + wn * (GATED ? 8 * NT : 16 * NT);
-    const float *sw_row = s_w + (long long)(min(col0, a.N - 1) / F8_BLOCK) * a.KB, *sw_up = sw_row + (long long)a.NB * a.KB;
+    const int sw_at = T::S_AT + SW * 256 + (GATED ? 0 : (col0 - n0) / F8_BLOCK) * 4;
 
 #pragma unroll
     for (int s = 0; s < T::STAGES - 1; ++s)
@@ -130,7 +140,7 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
         asm volatile("" ::: "memory");
         if (kt + T::STAGES - 1 < a.KB) issue(kt + T::STAGES - 1, stage == 0 ? T::STAGES - 1 : stage - 1);
         const unsigned char *st = smem + stage * T::STAGE;
-        const float sw = sw_row[kt], su = GATED ? sw_up[kt] : 0.0f;
+        const float sw = *reinterpret_cast<const float *>(st + sw_at), su = *reinterpret_cast<const float *>(st + (GATED ? sw_at + 4 : sw_at));
         operand x[MT];
         float scale[MT], scale_up[MT];
 #pragma unroll
@@ -200,35 +210,86 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
             if (wn == 0 && g == 0) a.hs[(long long)m * a.NB + n0 / F8_BLOCK] = F8Scale::scale(amax);
         }
     } else {
-        const bool pieces = a.N % 8 == 0;
+        constexpr bool LAYER = OUT == F8Out::LAYER;
+        const _Float16 *bias = static_cast<const _Float16 *>(LAYER ? a.bias : nullptr), *res = static_cast<const _Float16 *>(LAYER ? a.residual : nullptr),
+                       *gate = static_cast<const _Float16 *>(LAYER ? a.gate : nullptr);
+        _Float16 *y = static_cast<_Float16 *>(a.y);
+        // u -> fp16(act(u + bias)), of 8 neighbouring outputs
+        auto value = [&](int i, int b, const float (&add)[8]) {
+            h8 out;
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const int m = m0 + (wm * MT + i) * 16 + p;
-            if (m >= m_end) continue;
+            for (int e = 0; e < 8; ++e) {
+                float u = acc[2 * b + e / 4][i][e % 4] + add[e];
+                if (LAYER && a.act == 1) u = gelu_tanh_dev(u);
+                asm volatile("" : "+v"(u));   // the fp32 value is rounded to fp16 here and nowhere earlier
+                out[e] = (_Float16)u;
+            }
+            return out;
+        };
+        auto bias8 = [&](int n, float (&add)[8]) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) add[e] = bias ? (float)bias[min(n + e, a.N - 1)] : -0.0f;   // x + -0.0 is x, signed zeros included
+        };
+        if (a.N % 8 == 0 && (uintptr_t)res % 16 == 0 && (uintptr_t)gate % 16 == 0) {
 #pragma unroll
             for (int b = 0; b < NT / 2; ++b) {
                 const int n = col0 + 32 * b + 8 * g;
                 if (n >= a.N) continue;
-                const long long at = (long long)m * a.N + n;
-                float u[8];
+                float add[8];
+                bias8(n, add);
+                h8 r[MT], gt[MT];
+                if (res || gate) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) u[e] = acc[2 * b + e / 4][i][e % 4];
-                if constexpr (OUT == F8Out::LAYER) {
-                    float v[4] = {u[0], u[1], u[2], u[3]}, x[4] = {u[4], u[5], u[6], u[7]};
-                    finish4(a, m, n, v);
-                    if (n + 4 < a.N) finish4(a, m, n + 4, x);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) u[e] = v[e], u[4 + e] = x[e];
+                    for (int i = 0; i < MT; ++i) {
+                        const int m = min(m0 + (wm * MT + i) * 16 + p, m_end - 1);
+                        if (res) r[i] = *reinterpret_cast<const h8a *>(res + (long long)m * a.N + n);
+                        if (gate) gt[i] = *reinterpret_cast<const h8a *>(gate + (long long)(m / a.gate_rows) * a.N + n);
+                    }
                 }
-                h8 out;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) out[e] = (_Float16)u[e];
-                _Float16 *y = static_cast<_Float16 *>(a.y) + at;
-                if (pieces) *reinterpret_cast<h8a *>(y) = out;
-                else {
+                for (int i = 0; i < MT; ++i) {
+                    const int m = m0 + (wm * MT + i) * 16 + p;
+                    h8 out = value(i, b, add);
+                    if (res || gate) out = __builtin_bit_cast(h8, glue_piece(gate != nullptr, res != nullptr, __builtin_bit_cast(v4i, out), gt[i], r[i]));
+                    if (m < m_end) *reinterpret_cast<h8a *>(y + (long long)m * a.N + n) = out;
+                }
+            }
+        } else {
+            // rows that do not begin at a multiple of 16 bytes: through LDS, so that 64 neighbouring outputs leave together (one by one from where they
+            // are summed, 128 stores of 64 rows each a wavefront, the epilogue took longer than the sums)
+            constexpr int PITCH = T::BN * 2 + 8;
+            static_assert(T::BM * PITCH <= T::LDS_BYTES, "the tile in binary16");
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();                // the last step has been read everywhere
+            asm volatile("" ::: "memory");
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (n + e < a.N) y[e] = out[e];
+            for (int b = 0; b < NT / 2; ++b) {
+                float add[8];
+                bias8(col0 + 32 * b + 8 * g, add);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    const uint4 out = __builtin_bit_cast(uint4, value(i, b, add));
+                    uint2 *to = reinterpret_cast<uint2 *>(smem + ((wm * MT + i) * 16 + p) * PITCH + (wn * 16 * NT + 32 * b + 8 * g) * 2);
+                    to[0] = make_uint2(out.x, out.y);
+                    to[1] = make_uint2(out.z, out.w);
+                }
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            const int rows = min(T::BM, m_end - m0), columns = min(T::BN, a.N - n0);
+            for (int r = wave; r < rows; r += T::NW) {
+                const long long at = (long long)(m0 + r) * a.N + n0, gate_at = gate ? (long long)((m0 + r) / a.gate_rows) * a.N + n0 : 0;
+#pragma unroll
+                for (int c = 0; c < T::BN; c += 64) {
+                    if (c + lane >= columns) continue;
+                    _Float16 h = *reinterpret_cast<const half_alias *>(smem + r * PITCH + (c + lane) * 2);
+                    if (res || gate) {
+                        float v = __builtin_fmaf(gate ? (float)gate[gate_at + c + lane] : 1.0f, (float)h, res ? (float)res[at + c + lane] : 0.0f);
+                        asm volatile("" : "+v"(v));
+                        h = (_Float16)v;
+                    }
+                    y[at + c + lane] = h;
                 }
             }
         }

@@ -14,7 +14,8 @@ struct TileF8 {
     static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, S_AT = A_BYTES + B_BYTES, STAGE = S_AT + BM * 4 + 256;
     static constexpr int ISSUED = NA + NB + 1;                           // and one for the rows' scales
     static constexpr int LDS_BYTES = STAGES * STAGE;
-    static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && BM % 64 == 0 && NT % 2 == 0 && (16 * NT <= 128), "whole DMA instructions");
+    static constexpr int BUFS = 2, DIST = BUFS - 1;            // weight fragments in registers, and how many groups ahead one is read
+    static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && BM % 64 == 0 && NT % 2 == 0 && NT % BUFS == 0 && 16 * NT <= 128, "whole DMA instructions");
     static_assert(LDS_BYTES <= 160 * 1024 && ISSUED * (STAGES - 2) < 64, "LDS, outstanding operations");
 };
 
@@ -128,43 +129,95 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
     const int col0 = n0 + wn * (GATED ? 8 * NT : 16 * NT);
     const int sw_at = T::S_AT + SW * 256 + (GATED ? 0 : (col0 - n0) / F8_BLOCK) * 4;
 
+    // One step a pass, its weight fragments in groups of MT products.  A fragment is read DIST groups ahead.  Before the last group all of the step's
+    // fragments are in registers: there the stages change hands (the next step has arrived, nobody reads this one any more), this stage is requested
+    // again, and the next step's first fragments are read under the last products.  A group's sums are taken into the result one group later, when they are there.
+    Wide x[T::WIDE ? MT : 1];
+    v8i rx[MT], rf[T::BUFS];
+    float rs[MT], rw, ru, scale[MT], scale_up[MT];
+    v4f d[2][MT];
+    auto read_scales = [&](const unsigned char *st) {
 #pragma unroll
-    for (int s = 0; s < T::STAGES - 1; ++s)
+        for (int i = 0; i < MT; ++i) rs[i] = *reinterpret_cast<const float *>(st + T::S_AT + (wm * MT + i) * 64 + p * 4);
+        rw = *reinterpret_cast<const float *>(st + sw_at);
+        if (GATED) ru = *reinterpret_cast<const float *>(st + sw_at + 4);
+    };
+    auto read_x = [&](const unsigned char *st, int i) { rx[i] = read(st + (wm * MT + i) * 2048); };
+    auto read_f = [&](const unsigned char *st, int j) { rf[j % T::BUFS] = read(st + T::A_BYTES + (wn * NT + j) * 2048); };
+    auto fold = [&](int j, int i) {
+        const float s = GATED && j >= NT / 2 ? scale_up[i] : scale[i];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[j][i][r] = __builtin_fmaf(d[j & 1][i][r], s, acc[j][i][r]);
+        asm volatile("" : "+v"(acc[j][i]));   // here: left to itself the compiler moves all of a step's behind its products, whose sums then have no room
+    };
+#pragma unroll
+    for (int s = 0; s < T::STAGES; ++s)
         if (s < a.KB) issue(s, s);
+    if (a.KB >= T::STAGES) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(T::ISSUED * (T::STAGES - 1)) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < MT; ++i) read_x(smem, i);
+#pragma unroll
+    for (int j = 0; j < T::DIST; ++j) read_f(smem, j);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        d[1][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        scale[i] = scale_up[i] = 0.0f;
+    }
     int stage = 0;
     for (int kt = 0; kt < a.KB; ++kt) {
-        // the step has arrived, and everybody is done with the stage in front of it
-        if (T::STAGES > 2 && kt + T::STAGES - 2 < a.KB) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(T::ISSUED * (T::STAGES - 2)) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        if (kt + T::STAGES - 1 < a.KB) issue(kt + T::STAGES - 1, stage == 0 ? T::STAGES - 1 : stage - 1);
         const unsigned char *st = smem + stage * T::STAGE;
-        const float sw = *reinterpret_cast<const float *>(st + sw_at), su = *reinterpret_cast<const float *>(st + (GATED ? sw_at + 4 : sw_at));
-        operand x[MT];
-        float scale[MT], scale_up[MT];
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            x[i] = operand(read(st + (wm * MT + i) * 2048));
-            const float s = *reinterpret_cast<const float *>(st + T::S_AT + (wm * MT + i) * 64 + p * 4);
-            scale[i] = s * sw;
-            scale_up[i] = s * su;
-        }
+        const int next = stage + 1 == T::STAGES ? 0 : stage + 1;
+        const unsigned char *st_next = smem + next * T::STAGE;
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            const operand f(read(st + T::A_BYTES + (wn * NT + j) * 2048));
-            v4f d[MT];
+            if (j == NT - 1) {
+                // (as many steps as there are stages are under way, fewer at the end; the oldest of them is the next)
+                if (T::STAGES > 2 && kt + T::STAGES - 1 < a.KB) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(T::ISSUED * (T::STAGES - 2)) : "memory");
+                else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+                if (kt + T::STAGES < a.KB) issue(kt + T::STAGES, stage);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (T::WIDE) {
+                if (j == 0) {
 #pragma unroll
-            for (int i = 0; i < MT; ++i) d[i] = step_product(f, x[i]);
+                    for (int i = 0; i < MT; ++i) x[i] = Wide(rx[i]);
+                }
+            }
+            const operand f(rf[j % T::BUFS]);
+            if (j + T::DIST < NT) read_f(st, j + T::DIST);
+            else if (j == NT - 1) {
+#pragma unroll
+                for (int k = 0; k < T::DIST; ++k) read_f(st_next, k);
+            }
+            if (j == 0) read_scales(st);
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
-                const float s = GATED && j >= NT / 2 ? scale_up[i] : scale[i];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) acc[j][i][r] = __builtin_fmaf(d[i][r], s, acc[j][i][r]);
+                if constexpr (T::WIDE) d[j & 1][i] = step_product(f, x[i]);
+                else d[j & 1][i] = step_product(f, rx[i]);
+                fold(j == 0 ? NT - 1 : j - 1, i);
             }
+            if (j == 0) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    scale[i] = rs[i] * rw;
+                    if (GATED) scale_up[i] = rs[i] * ru;
+                }
+            }
+            if (j == NT - 1) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i) read_x(st_next, i);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
-        if (++stage == T::STAGES) stage = 0;
+        stage = next;
     }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) fold(NT - 1, i);
 
     // ---- epilogue
     typedef _Float16 h8a __attribute__((ext_vector_type(8), may_alias));

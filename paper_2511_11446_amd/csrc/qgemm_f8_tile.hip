@@ -14,7 +14,7 @@ struct TileF8 {
     static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, S_AT = A_BYTES + B_BYTES, STAGE = S_AT + BM * 4 + 256;
     static constexpr int ISSUED = NA + NB + 1;                           // and one for the rows' scales
     static constexpr int LDS_BYTES = STAGES * STAGE;
-    static constexpr int BUFS = 2, DIST = BUFS - 1;            // weight fragments in registers, and how many groups ahead one is read
+    static constexpr int BUFS = WIDE ? 2 : 4, DIST = WIDE ? 1 : 2;            // weight fragments in registers, and how many groups ahead one is read
     static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && BM % 64 == 0 && NT % 2 == 0 && NT % BUFS == 0 && 16 * NT <= 128, "whole DMA instructions");
     static_assert(LDS_BYTES <= 160 * 1024 && ISSUED * (STAGES - 2) < 64, "LDS, outstanding operations");
 };
@@ -192,7 +192,7 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
             if (j + T::DIST < NT) read_f(st, j + T::DIST);
             else if (j == NT - 1) {
 #pragma unroll
-                for (int k = 0; k < T::DIST; ++k) read_f(st_next, k);
+                for (int k = 0; k < T::DIST; ++k) read_f(st_next, k);   // into the buffers of groups that are through
             }
             if (j == 0) read_scales(st);
 #pragma unroll
@@ -200,6 +200,8 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
                 if constexpr (T::WIDE) d[j & 1][i] = step_product(f, x[i]);
                 else d[j & 1][i] = step_product(f, rx[i]);
                 fold(j == 0 ? NT - 1 : j - 1, i);
+                if (j == NT - 1) read_x(st_next, i);
+                __builtin_amdgcn_sched_barrier(0);   // in this order: a sum is four products old when it is folded
             }
             if (j == 0) {
 #pragma unroll
@@ -207,10 +209,6 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
                     scale[i] = rs[i] * rw;
                     if (GATED) scale_up[i] = rs[i] * ru;
                 }
-            }
-            if (j == NT - 1) {
-#pragma unroll
-                for (int i = 0; i < MT; ++i) read_x(st_next, i);
             }
             __builtin_amdgcn_sched_barrier(0);
         }

@@ -8,15 +8,6 @@
 
 namespace ql {
 
-// chunk c of 16 bytes at a lane's row: lane group g has chunks g and 4 + g of a step (the order along K is free, if both operands have it)
-__device__ __forceinline__ v8i load_step(const uint8_t *row, int at, int K)
-{
-    v4i lo = {0, 0, 0, 0}, hi = lo;
-    if (at < K) lo = *reinterpret_cast<const v4i *>(row + at);
-    if (at + 64 < K) hi = *reinterpret_cast<const v4i *>(row + at + 64);
-    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-}
-
 // four neighbouring outputs of row m from column n on
 template <bool WIDE>
 __device__ __forceinline__ void store4(void *y, long long m, int N, int n, const float (&u)[4])
@@ -44,14 +35,16 @@ __device__ __forceinline__ void store4(void *y, long long m, int N, int n, const
     }
 }
 
-// 16 MB rows and 16 NB outputs a workgroup, whose wavefronts share the steps and add up through LDS.  The operands come straight from memory.
-// EXPERTS: the rows of expert tiles[2 t + 1]; GATED: NB blocks of the gate and the same NB of the up matrix, y = silu(g) * u.
-template <int MB, int NB, int WAVES, bool EXPERTS, bool GATED>
+// Few rows: 16 MB rows and 16 NB outputs a workgroup, whose wavefronts take every WAVES-th step and add up through LDS.  The weights are read once, by one
+// wavefront, straight into the operands' registers: bound by memory, so what counts is how much is under way: AHEAD steps a wavefront.
+// Lane group g reads chunks g and 4 + g (of 16 bytes) of a step's 8: the order along K is free, if both operands have it.
+// EXPERTS: the rows of a tile of ExpertRows; GATED: NB blocks of the gate and the same NB of the up matrix, y = silu(g) * u.
+template <int MB, int NB, int WAVES, int AHEAD, bool EXPERTS, bool GATED>
 __global__ __launch_bounds__(64 * WAVES) void qgemm_f8_few(F8Gemm a)
 {
-    constexpr int TOTAL = MB * NB * (GATED ? 2 : 1);
+    constexpr int COLS = NB * (GATED ? 2 : 1), TOTAL = MB * COLS;
     __shared__ v4f sums[WAVES][TOTAL][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, p = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), p = lane & 15, g = lane >> 4;
     const int across = (a.N + 16 * NB - 1) / (16 * NB), tile = blockIdx.x / across;
     int m0 = tile * 16 * MB, m_end = a.M;
     const uint8_t *w = a.w;
@@ -66,42 +59,84 @@ __global__ __launch_bounds__(64 * WAVES) void qgemm_f8_few(F8Gemm a)
         s_w += matrix * a.NB * a.KB;
     }
     const int n0 = ((int)blockIdx.x - tile * across) * 16 * NB;
-    const uint8_t *row[MB];
+    const auto rows_x = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.q), 0, 0xffffffe0u, 0x00020000);
+    const auto rows_w = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(w), 0, (unsigned)a.N * (unsigned)a.K * (GATED ? 2u : 1u), 0x00020000);
+    unsigned at_x[MB], at_w[COLS];
     const float *s[MB];
+    int sw_row[COLS];
 #pragma unroll
     for (int i = 0; i < MB; ++i) {
         int m = min(m0 + 16 * i + p, m_end - 1);
         if (EXPERTS && a.order) m = a.order[m] / a.k;
-        row[i] = a.q + (long long)m * a.K;
+        at_x[i] = (unsigned)m * (unsigned)a.K + 16 * g;
         s[i] = a.s + (long long)m * a.KB;
     }
+#pragma unroll
+    for (int j = 0; j < COLS; ++j) {
+        const int n = n0 + 16 * (j % NB);
+        at_w[j] = (unsigned)(min(n + p, a.N - 1) + (j < NB ? 0 : a.N)) * (unsigned)a.K + 16 * g;
+        sw_row[j] = ((j < NB ? 0 : a.NB) + min(n, a.N - 1) / F8_BLOCK) * a.KB;
+    }
+    // chunks behind the end of a row are zero: their offset lies behind the operand
+    const int last = a.K - (a.KB - 1) * F8_BLOCK;
+    const bool dead_lo = 16 * g >= last, dead_hi = 16 * g + 64 >= last;
+    auto load = [&](__amdgpu_buffer_rsrc_t rows, unsigned at, int kb) {
+        const unsigned off = at + (unsigned)kb * F8_BLOCK;
+        const bool end = kb == a.KB - 1;
+        typedef unsigned u4 __attribute__((ext_vector_type(4)));
+        const u4 lo = __builtin_amdgcn_raw_buffer_load_b128(rows, end && dead_lo ? 0xfffffff0u : off, 0, 0);
+        const u4 hi = __builtin_amdgcn_raw_buffer_load_b128(rows, end && dead_hi ? 0xfffffff0u : off + 64, 0, 0);
+        return __builtin_bit_cast(v8i, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    v8i x[AHEAD][MB], f[AHEAD][COLS];
+    float sa[AHEAD][MB], sw[AHEAD][COLS];
+    auto request = [&](int u, int kb) {
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) f[u][j] = load(rows_w, at_w[j], kb);
+#pragma unroll
+        for (int i = 0; i < MB; ++i) x[u][i] = load(rows_x, at_x[i], kb);
+#pragma unroll
+        for (int i = 0; i < MB; ++i) sa[u][i] = s[i][kb];
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) sw[u][j] = s_w[sw_row[j] + kb];
+    };
     v4f acc[TOTAL];
 #pragma unroll
     for (int t = 0; t < TOTAL; ++t) acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int kb = wave; kb < a.KB; kb += WAVES) {
-        const int at = kb * F8_BLOCK + 16 * g;
-        Wide x[MB];
-        float sa[MB];
+    // steps behind the last one are the last one again, with a scale of 0: no branch stands between requests and their use, where the compiler would wait for
+    // what is under way
+    auto step_of = [&](int n) { return wave + n * WAVES; };
+    auto consume = [&](int u, int kb) {
+        Wide xw[MB];
 #pragma unroll
-        for (int i = 0; i < MB; ++i) {
-            x[i] = Wide(load_step(row[i], at, a.K));
-            sa[i] = s[i][kb];
-        }
+        for (int i = 0; i < MB; ++i) xw[i] = Wide(x[u][i]);
 #pragma unroll
-        for (int j = 0; j < NB * (GATED ? 2 : 1); ++j) {
-            const int nb = n0 + 16 * (j % NB);
-            const uint8_t *wm = w + (j < NB ? 0ll : (long long)a.N * a.K);
-            const float sw = s_w[(j < NB ? 0 : a.NB * a.KB) + (min(nb, a.N - 1) / F8_BLOCK) * a.KB + kb];
-            const Wide f(load_step(wm + (long long)min(nb + p, a.N - 1) * a.K, at, a.K));
+        for (int j = 0; j < COLS; ++j) {
+            const Wide fw(f[u][j]);
+            const float sj = kb < a.KB ? sw[u][j] : 0.0f;
 #pragma unroll
             for (int i = 0; i < MB; ++i) {
-                const v4f d = step_product(f, x[i]);
-                const float scale = sa[i] * sw;
+                const v4f d = step_product(fw, xw[i]);
+                const float scale = sa[u][i] * sj;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) acc[j * MB + i][r] = __builtin_fmaf(d[r], scale, acc[j * MB + i][r]);
             }
         }
+    };
+    const int steps = (a.KB + WAVES - 1) / WAVES;
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) request(u, min(step_of(u), a.KB - 1));
+    int n = 0;
+    for (; n + AHEAD < steps; n += AHEAD) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            consume(u, step_of(n + u));
+            request(u, min(step_of(n + u + AHEAD), a.KB - 1));
+        }
     }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+        if (n + u < steps) consume(u, step_of(n + u));
 #pragma unroll
     for (int t = 0; t < TOTAL; ++t) sums[wave][t][lane] = acc[t];
     __syncthreads();
@@ -131,20 +166,43 @@ __global__ __launch_bounds__(64 * WAVES) void qgemm_f8_few(F8Gemm a)
     }
 }
 
+// Workgroups of 32 outputs from which on it is their number that keeps the memory busy
+constexpr int64_t FEW_GROUPS = 1024;
+
 int f8_expert_tile(int64_t P, int64_t E) { return P >= 64 * E ? F8_TILE_ROWS : 16; }
 
-hipError_t launch_qgemm_f8(const F8Gemm &a, hipStream_t stream)
+template <int MB, int NB, int WAVES, int AHEAD, bool EXPERTS, bool GATED>
+static hipError_t run_few(const F8Gemm &a, hipStream_t s)
 {
-    if (a.first ? a.tile >= F8_TILE_ROWS : a.M > 256) return launch_qgemm_f8_tiles(a, stream);
-    if (a.first) {
-        const dim3 grid((unsigned)((a.N + 31) / 32) * (unsigned)a.tiles_most);
-        if (a.gated) hipLaunchKernelGGL((qgemm_f8_few<1, 2, 4, true, true>), grid, dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((qgemm_f8_few<1, 2, 4, true, false>), grid, dim3(256), 0, stream, a);
-    } else {
-        const dim3 grid((unsigned)((a.N + 31) / 32) * (unsigned)((a.M + 31) / 32));
-        hipLaunchKernelGGL((qgemm_f8_few<2, 2, 4, false, false>), grid, dim3(256), 0, stream, a);
-    }
+    const unsigned across = (unsigned)((a.N + 16 * NB - 1) / (16 * NB)), down = EXPERTS ? (unsigned)a.tiles_most : (unsigned)((a.M + 16 * MB - 1) / (16 * MB));
+    hipLaunchKernelGGL((qgemm_f8_few<MB, NB, WAVES, AHEAD, EXPERTS, GATED>), dim3(across * down), dim3(64 * WAVES), 0, s, a);
     return hipGetLastError();
+}
+
+// A wavefront requests as many steps ahead as it has, up to MOST (steps that there are not would be requested for nothing)
+template <int MB, int NB, int WAVES, int MOST, bool EXPERTS, bool GATED>
+static hipError_t run_ahead(const F8Gemm &a, hipStream_t s)
+{
+    const int steps = (a.KB + WAVES - 1) / WAVES;
+    if constexpr (MOST >= 4) {
+        if (steps >= 4) return run_few<MB, NB, WAVES, 4, EXPERTS, GATED>(a, s);
+    }
+    if (steps >= 2) return run_few<MB, NB, WAVES, 2, EXPERTS, GATED>(a, s);
+    return run_few<MB, NB, WAVES, 1, EXPERTS, GATED>(a, s);
+}
+
+hipError_t launch_qgemm_f8(const F8Gemm &a, hipStream_t s)
+{
+    if (a.first) {
+        if (a.tile >= F8_TILE_ROWS) return launch_qgemm_f8_tiles(a, s);
+        const bool many = (int64_t)a.tiles_most * (a.N / 32) >= FEW_GROUPS;
+        if (a.gated) return many ? run_few<1, 2, 4, 1, true, true>(a, s) : run_ahead<1, 1, 8, 2, true, true>(a, s);
+        return many ? run_few<1, 2, 4, 1, true, false>(a, s) : run_ahead<1, 1, 4, 2, true, false>(a, s);
+    }
+    if (a.M > 64) return launch_qgemm_f8_tiles(a, s);
+    if (a.M <= 16) return a.N / 32 >= FEW_GROUPS ? run_few<1, 2, 4, 1, false, false>(a, s) : run_ahead<1, 1, 8, 4, false, false>(a, s);
+    if (a.M <= 32) return run_ahead<2, 1, 8, 2, false, false>(a, s);
+    return run_ahead<4, 1, 8, 2, false, false>(a, s);
 }
 
 }  // namespace ql

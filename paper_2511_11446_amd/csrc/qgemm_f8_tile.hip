@@ -366,6 +366,7 @@ static_assert(WideTile::BM == F8_TILE_ROWS, "what the rows of experts are cut in
 hipError_t launch_qgemm_f8_tiles(const F8Gemm &a, hipStream_t s)
 {
     if (a.first) return a.gated ? run_tile<WideTile, F8Out::GATED>(a, s) : run_tile<WideTile, F8Out::ROWS>(a, s);
+    if (a.M <= 256) return run_tile<TileF8<2, 4, 2, 2, 4, true>, F8Out::LAYER>(a, s);
     return a.codes ? run_tile<CoreTile, F8Out::LAYER>(a, s) : run_tile<WideTile, F8Out::LAYER>(a, s);
 }
 

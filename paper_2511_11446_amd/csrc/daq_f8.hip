@@ -8,18 +8,6 @@
 
 namespace ql {
 
-// the largest of 16 lanes' values, in all of them
-__device__ __forceinline__ float max16(float m)
-{
-#define QL_ROR(ctrl) m = fmaxf(m, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, m), ctrl, 0xF, 0xF, true)));
-    QL_ROR(0x128)
-    QL_ROR(0x124)
-    QL_ROR(0x122)
-    QL_ROR(0x121)
-#undef QL_ROR
-    return m;
-}
-
 template <bool GLU, bool WIDE>
 __global__ __launch_bounds__(256) void daq_f8(F8DaqArgs a)
 {

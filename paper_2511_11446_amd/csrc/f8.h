@@ -37,7 +37,9 @@ hipError_t launch_expert_rows(const int *ids, const ExpertRows &r, hipStream_t s
 // y[t] = residual[t] + sum_j weights[t,j] * o[place[t,j]]
 struct ExpertSumArgs {
     const void *o;       // fp16 or (wide) fp32 [rows, N]
-    const int *place;    // [T,k]
+    const int *place;    // [T,k] rows, or (ids) an expert where there is one: row token * k + choice
+    bool ids;
+    int E;
     const float *weights;
     const void *residual;
     void *y;
@@ -77,12 +79,19 @@ struct F8Gemm {
     uint8_t *hq;
     float *hs;
     bool wide;
+    // rows that the launch quantizes itself (qgemm_f8_takes_rows, experts_f8_takes_ids), in the place of q and s
+    const void *x;       // fp16 [M,K], [M,2K] with glu; of experts fp16 [M / k, K] gated, else fp32 [M,K]
+    bool glu;
+    const int *ids;      // of experts: [M] (M up to 64) in the place of first, tiles and order; outputs at row token * k + choice
+    int E;
     bool codes;          // the matrix cores' own sums of codes will do (a layer of many rows that is not behind a gated product)
 };
 hipError_t launch_qgemm_f8(const F8Gemm &a, hipStream_t stream);
 // rows of an expert's tile, by the rows that an expert has on average; F8_TILE_ROWS and more: tiles that quantize the gated product themselves
 constexpr int F8_TILE_ROWS = 128;
 int f8_expert_tile(int64_t P, int64_t E);
+bool qgemm_f8_takes_rows(int64_t M, int64_t K, int64_t N, bool glu);
+inline bool experts_f8_takes_ids(int64_t P, int64_t K, int64_t I) { return P <= 16 && K <= 4096 && I <= 4096; }
 hipError_t launch_qgemm_f8_tiles(const F8Gemm &a, hipStream_t stream);
 
 // ---- device helpers -------------------------------------------------------------------------------------------------------------
@@ -158,6 +167,18 @@ __device__ __forceinline__ f8_v4f step_product(const Wide &a, const Wide &b)
 __device__ __forceinline__ f8_v4f step_product(v8i a, v8i b)
 {
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f8_v4f{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0, 0, 0, 0);
+}
+
+// the largest of 16 lanes' values, in all of them
+__device__ __forceinline__ float max16(float m)
+{
+#define QL_ROR(ctrl) m = fmaxf(m, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, m), ctrl, 0xF, 0xF, true)));
+    QL_ROR(0x128)
+    QL_ROR(0x124)
+    QL_ROR(0x122)
+    QL_ROR(0x121)
+#undef QL_ROR
+    return m;
 }
 
 // four values to e4m3, round to nearest even; lowest first

@@ -96,7 +96,7 @@ struct ExpertRoom {
         P = T * k;
         tile = ql::f8_expert_tile(P, E);
         tiles_most = ql::expert_tiles_most(P, E, tile);
-        wide = tile < ql::F8_TILE_ROWS;
+        wide = tile < ql::F8_TILE_ROWS || ql::experts_f8_takes_ids(P, K, I);
         size_t at = 0;
         auto take = [&](size_t bytes) {
             const size_t here = at;
@@ -165,6 +165,12 @@ int qlinear_f8(const void *x, int64_t M, int64_t K, int32_t glu, const void *w, 
     if ((rc = check_workspace(workspace, workspace_bytes, room.total))) return rc;
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     hipStream_t s = static_cast<hipStream_t>(stream);
+    if (ql::qgemm_f8_takes_rows(M, K, N, glu != 0)) {
+        ql::F8Gemm g = gemm_args(nullptr, nullptr, M, K, w, w_scale, N, y);
+        g.x = x;
+        g.glu = glu != 0;
+        return run_layer(g, bias, fusion, g.glu, s);
+    }
     if ((rc = ql::status_of(ql::launch_daq_f8(daq_args(x, M, K, glu, ws, ws + room.scales), s)))) return rc;
     return run_layer(gemm_args(ws, ws + room.scales, M, K, w, w_scale, N, y), bias, fusion, glu != 0, s);
 }
@@ -215,47 +221,54 @@ int experts_f8(const ql_experts_f8 *x, void *workspace, size_t workspace_bytes, 
     hipStream_t s = static_cast<hipStream_t>(stream);
     auto ints = [&](size_t at) { return reinterpret_cast<int *>(ws + at); };
 
-    ql::ExpertRows rows{};
-    rows.first = ints(room.first);
-    rows.order = ints(room.order);
-    rows.place = ints(room.place);
-    rows.tiles = ints(room.tiles);
-    rows.counts = ints(room.counts);
-    rows.P = (int)room.P;
-    rows.E = x->E;
-    rows.tile = room.tile;
-    if ((rc = ql::status_of(ql::launch_expert_rows(static_cast<const int *>(x->ids), rows, s)))) return rc;
-    if ((rc = ql::status_of(ql::launch_daq_f8(daq_args(x->x, x->T, x->K, 0, ws + room.q, ws + room.s), s)))) return rc;
-
+    const int *ids = static_cast<const int *>(x->ids);
+    const bool few = ql::experts_f8_takes_ids(room.P, x->K, x->I);
     ql::F8Gemm up = gemm_args(ws + room.q, ws + room.s, room.P, x->K, x->w_up, x->up_scale, x->I, ws + room.h);
-    up.first = rows.first;
-    up.tiles = rows.tiles;
-    up.order = rows.order;
-    up.k = x->k;
-    up.tiles_most = (int)room.tiles_most;
-    up.tile = room.tile;
-    up.gated = true;
-    up.hq = ws + room.hq;
-    up.hs = reinterpret_cast<float *>(ws + room.hs);
-    if ((rc = ql::status_of(ql::launch_qgemm_f8(up, s)))) return rc;
-    if (room.tile < ql::F8_TILE_ROWS) {
-        ql::F8DaqArgs d = daq_args(ws + room.h, room.P, x->I, 0, ws + room.hq, ws + room.hs);
-        d.wide = true;
-        d.rows = rows.first + x->E;
-        if ((rc = ql::status_of(ql::launch_daq_f8(d, s)))) return rc;
-    }
     ql::F8Gemm down = gemm_args(ws + room.hq, ws + room.hs, room.P, x->I, x->w_down, x->down_scale, x->N, ws + room.o);
-    down.first = rows.first;
-    down.tiles = rows.tiles;
-    down.k = x->k;
-    down.tiles_most = (int)room.tiles_most;
-    down.tile = room.tile;
+    up.k = down.k = x->k;
+    up.E = down.E = x->E;
+    up.gated = true;
     down.wide = room.wide;
-    if ((rc = ql::status_of(ql::launch_qgemm_f8(down, s)))) return rc;
+    if (few) {
+        up.ids = down.ids = ids;
+        up.x = x->x;
+        down.x = ws + room.h;
+        if ((rc = ql::status_of(ql::launch_qgemm_f8(up, s)))) return rc;
+        if ((rc = ql::status_of(ql::launch_qgemm_f8(down, s)))) return rc;
+    } else {
+        ql::ExpertRows rows{};
+        rows.first = ints(room.first);
+        rows.order = ints(room.order);
+        rows.place = ints(room.place);
+        rows.tiles = ints(room.tiles);
+        rows.counts = ints(room.counts);
+        rows.P = (int)room.P;
+        rows.E = x->E;
+        rows.tile = room.tile;
+        if ((rc = ql::status_of(ql::launch_expert_rows(ids, rows, s)))) return rc;
+        if ((rc = ql::status_of(ql::launch_daq_f8(daq_args(x->x, x->T, x->K, 0, ws + room.q, ws + room.s), s)))) return rc;
+        up.first = down.first = rows.first;
+        up.tiles = down.tiles = rows.tiles;
+        up.tiles_most = down.tiles_most = (int)room.tiles_most;
+        up.tile = down.tile = room.tile;
+        up.order = rows.order;
+        up.hq = ws + room.hq;
+        up.hs = reinterpret_cast<float *>(ws + room.hs);
+        if ((rc = ql::status_of(ql::launch_qgemm_f8(up, s)))) return rc;
+        if (room.tile < ql::F8_TILE_ROWS) {
+            ql::F8DaqArgs d = daq_args(ws + room.h, room.P, x->I, 0, ws + room.hq, ws + room.hs);
+            d.wide = true;
+            d.rows = rows.first + x->E;
+            if ((rc = ql::status_of(ql::launch_daq_f8(d, s)))) return rc;
+        }
+        if ((rc = ql::status_of(ql::launch_qgemm_f8(down, s)))) return rc;
+    }
 
     ql::ExpertSumArgs sum{};
     sum.o = ws + room.o;
-    sum.place = rows.place;
+    sum.place = few ? ids : ints(room.place);
+    sum.ids = few;
+    sum.E = x->E;
     sum.weights = static_cast<const float *>(x->weights);
     sum.residual = x->residual;
     sum.y = x->y;

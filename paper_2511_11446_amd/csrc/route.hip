@@ -299,6 +299,7 @@ template <bool WIDE>
 __global__ __launch_bounds__(256) void expert_sum(ExpertSumArgs a)
 {
     typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+    constexpr int TOGETHER = 8;   // choices whose rows are under way together
     const long long pieces = a.N / 8, all = pieces * a.T;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
         const long long t = i / pieces, n = (i - t * pieces) * 8;
@@ -307,18 +308,37 @@ __global__ __launch_bounds__(256) void expert_sum(ExpertSumArgs a)
         if (a.residual) res = *reinterpret_cast<const h8 *>(static_cast<const _Float16 *>(a.residual) + t * a.N + n);
 #pragma unroll
         for (int c = 0; c < 8; ++c) y[c] = (float)res[c];
-        for (int j = 0; j < a.k; ++j) {
-            const int row = a.place[t * a.k + j];
-            if (row < 0) continue;
-            const float w = a.weights[t * a.k + j];
+        for (int first = 0; first < a.k; first += TOGETHER) {
+            int row[TOGETHER];
+            float w[TOGETHER];
+#pragma unroll
+            for (int j = 0; j < TOGETHER; ++j) {
+                const long long at = t * a.k + min(first + j, a.k - 1);
+                const int place = a.place[at];
+                w[j] = a.weights[at];
+                row[j] = first + j >= a.k ? -1 : !a.ids ? place : place >= 0 && place < a.E ? (int)at : -1;
+            }
             if constexpr (WIDE) {
-                const float *o = static_cast<const float *>(a.o) + (long long)row * a.N + n;
+                float4 o[TOGETHER][2];
 #pragma unroll
-                for (int c = 0; c < 8; ++c) y[c] = __builtin_fmaf(w, o[c], y[c]);
+                for (int j = 0; j < TOGETHER; ++j) {
+                    const float4 *from = reinterpret_cast<const float4 *>(static_cast<const float *>(a.o) + (long long)max(row[j], 0) * a.N + n);
+                    o[j][0] = from[0], o[j][1] = from[1];
+                }
+#pragma unroll
+                for (int j = 0; j < TOGETHER; ++j) {
+                    const float v[8] = {o[j][0].x, o[j][0].y, o[j][0].z, o[j][0].w, o[j][1].x, o[j][1].y, o[j][1].z, o[j][1].w};
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) y[c] = row[j] >= 0 ? __builtin_fmaf(w[j], v[c], y[c]) : y[c];
+                }
             } else {
-                const h8 o = *reinterpret_cast<const h8 *>(static_cast<const _Float16 *>(a.o) + (long long)row * a.N + n);
+                h8 o[TOGETHER];
 #pragma unroll
-                for (int c = 0; c < 8; ++c) y[c] = __builtin_fmaf(w, (float)o[c], y[c]);
+                for (int j = 0; j < TOGETHER; ++j) o[j] = *reinterpret_cast<const h8 *>(static_cast<const _Float16 *>(a.o) + (long long)max(row[j], 0) * a.N + n);
+#pragma unroll
+                for (int j = 0; j < TOGETHER; ++j)
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) y[c] = row[j] >= 0 ? __builtin_fmaf(w[j], (float)o[j][c], y[c]) : y[c];
             }
         }
         h8 out;

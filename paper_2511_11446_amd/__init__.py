@@ -785,12 +785,24 @@ def _blocks(n):
     return (n + 127) // 128
 
 
+def _dense(t, dtype, shape, name, dev):
+    """_at, where all is well in a third of its time (a call has up to nine tensors)."""
+    if t is None:
+        return 0
+    try:
+        if t.dtype is dtype and t.get_device() == dev >= 0 and t.is_contiguous() and t.shape == shape:
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    return _at(t, dtype, shape, name, dev)
+
+
 def _two(t, dtype, name, dev):
     """A dense [rows, columns] tensor on the current device: its address and sizes."""
-    p = _at(t, dtype, None, name, dev)
-    if t is None or t.dim() != 2:
+    if t is None or not hasattr(t, "shape") or len(t.shape) != 2:
         raise TypeError("%s must be a [rows, columns] CUDA tensor of %s" % (name, dtype))
-    return p, t.shape[0], t.shape[1]
+    rows, columns = t.shape
+    return _dense(t, dtype, (rows, columns), name, dev), rows, columns
 
 
 def _width(columns, glu, name="x"):
@@ -810,7 +822,7 @@ def daq_quantize_f8(x, glu=False, q=None, scales=None, stream=None):
         q = _empty((M, K), torch.float8_e4m3fn, x.device, stream, True)
     if scales is None:
         scales = _empty((M, _blocks(K)), torch.float32, x.device, stream, True)
-    qp, sp = _at(q, torch.float8_e4m3fn, (M, K), "q", dev), _at(scales, torch.float32, (M, _blocks(K)), "scales", dev)
+    qp, sp = _dense(q, torch.float8_e4m3fn, (M, K), "q", dev), _dense(scales, torch.float32, (M, _blocks(K)), "scales", dev)
     _check(lib().daq_quantize_f8(xp, M, K, 1 if glu else 0, qp, sp, _stream(stream)), "daq_quantize_f8")
     return q, scales
 
@@ -823,16 +835,16 @@ def _layer_f8(dev, M, K, w, w_scale, bias, act, residual, gate, gate_rows, y, de
         raise ValueError("w has shape %s, expected [N, %d]" % (tuple(w.shape), K))
     if w_scale is None:
         raise TypeError("w_scale is missing")
-    sp, bp = _at(w_scale, torch.float32, (_blocks(N), _blocks(K)), "w_scale", dev), _at(bias, torch.float16, (N,), "bias", dev)
+    sp, bp = _dense(w_scale, torch.float32, (_blocks(N), _blocks(K)), "w_scale", dev), _dense(bias, torch.float16, (N,), "bias", dev)
     fusion = None
     if act != ACT_NONE or residual is not None or gate is not None:
         if gate is not None and (gate_rows < 1 or M % gate_rows):
             raise ValueError("gate_rows is %s and x has %d rows" % (gate_rows, M))
-        fusion = ql_fusion(act, 0, _at(residual, torch.float16, (M, N), "residual", dev) or None,
-                           None if gate is None else _at(gate, torch.float16, (M // gate_rows, N), "gate", dev), gate_rows, None)
+        fusion = ql_fusion(act, 0, _dense(residual, torch.float16, (M, N), "residual", dev) or None,
+                           None if gate is None else _dense(gate, torch.float16, (M // gate_rows, N), "gate", dev), gate_rows, None)
     if y is None:
         y = _empty((M, N), torch.float16, device, stream, True)
-    return wp, sp, bp or None, N, None if fusion is None else ctypes.byref(fusion), _at(y, torch.float16, (M, N), "y", dev), y
+    return wp, sp, bp or None, N, None if fusion is None else ctypes.byref(fusion), _dense(y, torch.float16, (M, N), "y", dev), y
 
 
 def qgemm_f8(q, scales, w, w_scale, bias=None, act=ACT_NONE, residual=None, gate=None, gate_rows=1, y=None, stream=None):
@@ -844,7 +856,7 @@ def qgemm_f8(q, scales, w, w_scale, bias=None, act=ACT_NONE, residual=None, gate
     qp, M, K = _two(q, torch.float8_e4m3fn, "q", dev)
     if scales is None:
         raise TypeError("scales is missing")
-    sp = _at(scales, torch.float32, (M, _blocks(K)), "scales", dev)
+    sp = _dense(scales, torch.float32, (M, _blocks(K)), "scales", dev)
     wp, ws_p, bp, N, fusion, yp, y = _layer_f8(dev, M, K, w, w_scale, bias, act, residual, gate, gate_rows, y, q.device, stream)
     _check(lib().qgemm_f8(qp, sp, M, K, wp, ws_p, bp, N, fusion, yp, _stream(stream)), "qgemm_f8")
     return y
@@ -884,8 +896,8 @@ def route_experts(logits, k, bias=None, score=SCORE_SOFTMAX, groups=1, top_group
         ids = _empty((T, k), torch.int32, logits.device, stream, True)
     if weights is None:
         weights = _empty((T, k), torch.float32, logits.device, stream, True)
-    r = _ROUTING.pack(T, E, k, score, 1 if wide else 0, groups, top_groups, group_top, 1 if renorm else 0, scale, 0, lp, _at(bias, torch.float32, (E,), "bias", dev),
-                      _at(ids, torch.int32, (T, k), "ids", dev), _at(weights, torch.float32, (T, k), "weights", dev))
+    r = _ROUTING.pack(T, E, k, score, 1 if wide else 0, groups, top_groups, group_top, 1 if renorm else 0, scale, 0, lp, _dense(bias, torch.float32, (E,), "bias", dev),
+                      _dense(ids, torch.int32, (T, k), "ids", dev), _dense(weights, torch.float32, (T, k), "weights", dev))
     _check(lib().route_experts(r, _stream(stream)), "route_experts")
     return ids, weights
 
@@ -914,10 +926,10 @@ def experts_f8(x, ids, weights, w_up, up_scale, w_down, down_scale, residual=Non
         y = _empty((T, N), torch.float16, x.device, stream, True)
     if weights is None or up_scale is None or down_scale is None:
         raise TypeError("weights, up_scale or down_scale is missing")
-    a = _EXPERTS.pack(T, k, E, K, I, N, xp, ip, _at(weights, torch.float32, (T, k), "weights", dev), up,
-                      _at(up_scale, torch.float32, (E, 2, _blocks(I), _blocks(K)), "up_scale", dev), down,
-                      _at(down_scale, torch.float32, (E, _blocks(N), _blocks(I)), "down_scale", dev), _at(residual, torch.float16, (T, N), "residual", dev),
-                      _at(y, torch.float16, (T, N), "y", dev))
+    a = _EXPERTS.pack(T, k, E, K, I, N, xp, ip, _dense(weights, torch.float32, (T, k), "weights", dev), up,
+                      _dense(up_scale, torch.float32, (E, 2, _blocks(I), _blocks(K)), "up_scale", dev), down,
+                      _dense(down_scale, torch.float32, (E, _blocks(N), _blocks(I)), "down_scale", dev), _dense(residual, torch.float16, (T, N), "residual", dev),
+                      _dense(y, torch.float16, (T, N), "y", dev))
     if ws is None:
         ws = workspace(experts_f8_workspace_bytes(T, k, E, K, I, N), x.device, stream)
     elif ws.get_device() != dev:

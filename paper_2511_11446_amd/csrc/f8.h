@@ -3,10 +3,13 @@
 #pragma once
 #include "ql_internal.h"
 
+#include <atomic>
+
 namespace ql {
 
 constexpr int F8_BLOCK = 128;   // channels that share an activation scale, and the side of a weight block
 constexpr float F8_MAX = 448.0f;
+constexpr int F8_LDS = 160 * 1024;   // of a compute unit
 
 inline int f8_blocks(int64_t n) { return (int)((n + F8_BLOCK - 1) / F8_BLOCK); }
 
@@ -90,9 +93,33 @@ hipError_t launch_qgemm_f8(const F8Gemm &a, hipStream_t stream);
 // rows of an expert's tile, by the rows that an expert has on average; F8_TILE_ROWS and more: tiles that quantize the gated product themselves
 constexpr int F8_TILE_ROWS = 128;
 int f8_expert_tile(int64_t P, int64_t E);
+// rows from which on a layer takes the matrix cores' own sums of codes, if it may
+constexpr int F8_MANY = 256;
+float qgemm_f8_tiles_us(const F8Gemm &a);
 bool qgemm_f8_takes_rows(int64_t M, int64_t K, int64_t N, bool glu);
-inline bool experts_f8_takes_ids(int64_t P, int64_t K, int64_t I) { return P <= 16 && K <= 4096 && I <= 4096; }
+// steps of eight wavefronts that are requested at once, and the LDS that they and the rows take
+inline int f8_self_steps(int KB) { return KB <= 8 ? 1 : KB <= 16 ? 2 : 4; }
+inline int64_t f8_self_bytes(int64_t rows, int KB, bool gated) { return 8 * f8_self_steps(KB) * (gated ? 2 : 1) * 2048 + KB * rows * (F8_BLOCK + 4) + 2048 + 64; }
+inline bool experts_f8_takes_ids(int64_t P, int64_t K, int64_t I)
+{
+    return P <= 16 && K <= 4096 && I <= 4096 && f8_self_bytes(P, f8_blocks(K), true) <= F8_LDS && f8_self_bytes(P, f8_blocks(I), false) <= F8_LDS;
+}
 hipError_t launch_qgemm_f8_tiles(const F8Gemm &a, hipStream_t stream);
+
+// Once for a kernel and device: that it may use F8_LDS bytes of LDS (asked for at every launch it is 1 us of the host's time)
+template <auto KERNEL>
+hipError_t allow_lds()
+{
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (dev < 64 && (done.load(std::memory_order_relaxed) & bit)) return hipSuccess;
+    e = hipFuncSetAttribute(reinterpret_cast<const void *>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, F8_LDS);
+    if (e == hipSuccess && dev < 64) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
 
 // ---- device helpers -------------------------------------------------------------------------------------------------------------
 

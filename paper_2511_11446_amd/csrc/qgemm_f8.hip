@@ -456,7 +456,7 @@ static hipError_t run_dma(const F8Gemm &a, hipStream_t s)
 {
     constexpr int bytes = WAVES * STAGES * ((MB + NB * (GATED ? 2 : 1)) * 2048 + 512);
     static_assert(bytes <= 160 * 1024, "LDS");
-    const hipError_t opt_in = hipFuncSetAttribute(reinterpret_cast<const void *>(&qgemm_f8_few_dma<MB, NB, WAVES, STAGES, EXPERTS, GATED>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    const hipError_t opt_in = allow_lds<&qgemm_f8_few_dma<MB, NB, WAVES, STAGES, EXPERTS, GATED>>();
     if (opt_in != hipSuccess) return opt_in;
     const unsigned across = (unsigned)((a.N + 16 * NB - 1) / (16 * NB)), down = EXPERTS ? (unsigned)a.tiles_most : (unsigned)((a.M + 16 * MB - 1) / (16 * MB));
     hipLaunchKernelGGL((qgemm_f8_few_dma<MB, NB, WAVES, STAGES, EXPERTS, GATED>), dim3(across * down), dim3(64 * WAVES), bytes, s, a);
@@ -467,10 +467,10 @@ template <int STEPS, Self SELF>
 static hipError_t run_self_steps(const F8Gemm &a, hipStream_t s)
 {
     constexpr bool EXPERTS = SELF == Self::UP || SELF == Self::DOWN;
-    const int most = a.M < 16 ? a.M : 16, bytes = 8 * STEPS * (SELF == Self::UP ? 2 : 1) * 2048 + a.KB * most * (F8_BLOCK + 4) + 2048 + 64;
-    const hipError_t opt_in = hipFuncSetAttribute(reinterpret_cast<const void *>(&qgemm_f8_self<STEPS, SELF>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    const int most = a.M < 16 ? a.M : 16, bytes = (int)f8_self_bytes(most, a.KB, SELF == Self::UP);
+    const hipError_t opt_in = allow_lds<&qgemm_f8_self<STEPS, SELF>>();
     if (opt_in != hipSuccess) return opt_in;
-    if (bytes > 160 * 1024) return hipErrorInvalidValue;
+    if (bytes > F8_LDS || STEPS != f8_self_steps(a.KB)) return hipErrorInvalidValue;
     const unsigned tiles = EXPERTS ? (unsigned)a.M : 1u;   // a tile has a row at least
     hipLaunchKernelGGL((qgemm_f8_self<STEPS, SELF>), dim3((unsigned)((a.N + 15) / 16) * tiles), dim3(512), bytes, s, a, most);
     return hipGetLastError();
@@ -479,8 +479,8 @@ static hipError_t run_self_steps(const F8Gemm &a, hipStream_t s)
 template <Self SELF>
 static hipError_t run_self(const F8Gemm &a, hipStream_t s)
 {
-    if (a.KB <= 8) return run_self_steps<1, SELF>(a, s);
-    return a.KB <= 16 ? run_self_steps<2, SELF>(a, s) : run_self_steps<4, SELF>(a, s);
+    const int steps = f8_self_steps(a.KB);
+    return steps == 1 ? run_self_steps<1, SELF>(a, s) : steps == 2 ? run_self_steps<2, SELF>(a, s) : run_self_steps<4, SELF>(a, s);
 }
 
 // A wavefront requests as many steps ahead as it has, up to MOST (steps that there are not would be requested for nothing)
@@ -493,6 +493,15 @@ static hipError_t run_ahead(const F8Gemm &a, hipStream_t s)
     }
     if (steps >= 2) return run_few<MB, NB, WAVES, 2, EXPERTS, GATED>(a, s);
     return run_few<MB, NB, WAVES, 1, EXPERTS, GATED>(a, s);
+}
+
+// What few rows take on workgroups of 16 mb rows and 16 nb outputs: what such a workgroup brings to LDS at 55 bytes a nanosecond, and 2.5 us for the launch, the first bytes'
+// way and the sum over the wavefronts.  us, measured and so: 64 x 8192 x 4096 on 32 x 32 12.5 and 12.0, on 64 x 32 17.7 and 16.8; 128 x 4096 x 4096 on 64 x 32 11.3 and
+// 9.6, on 32 x 32 13.4 and 12.0, on 32 x 16 20.9 and 16.8; 128 x 12288 x 512 on 32 x 16 11.5 and 13.2, on 64 x 32 22.6 and 23.9.
+static float few_us(const F8Gemm &a, int mb, int nb)
+{
+    const int64_t groups = ((a.M + 16ll * mb - 1) / (16 * mb)) * ((a.N + 16ll * nb - 1) / (16 * nb));
+    return (float)((groups + 255) / 256) * (float)((mb + nb) * 16) * (float)(a.KB * F8_BLOCK) / 55e3f + 2.5f;
 }
 
 bool qgemm_f8_takes_rows(int64_t M, int64_t K, int64_t N, bool glu)
@@ -510,10 +519,14 @@ hipError_t launch_qgemm_f8(const F8Gemm &a, hipStream_t s)
         if (a.gated) return run_dma<1, 1, 4, 2, true, true>(a, s);
         return many ? run_dma<1, 2, 4, 2, true, false>(a, s) : run_ahead<1, 1, 4, 2, true, false>(a, s);
     }
-    if (a.M > 64) return launch_qgemm_f8_tiles(a, s);
-    if (a.M <= 16) return run_dma<1, 1, 8, 2, false, false>(a, s);
-    if (a.M <= 32) return run_dma<2, 1, 8, 3, false, false>(a, s);
-    return a.N >= 8192 ? run_dma<4, 2, 4, 3, false, false>(a, s) : run_dma<4, 1, 4, 2, false, false>(a, s);
+    // Sums in binary16 products (f8.h) up to F8_MANY rows and behind gated products
+    if (a.M > F8_MANY && a.codes) return launch_qgemm_f8_tiles(a, s);
+    const float tiles = qgemm_f8_tiles_us(a), by16 = few_us(a, 1, 1), by32 = few_us(a, 2, 1), by32w = few_us(a, 2, 2), by64w = few_us(a, 4, 2);
+    const float least = fminf(fminf(fminf(by32, by32w), by64w), a.M <= 16 ? by16 : 1e30f);
+    if (tiles < least) return launch_qgemm_f8_tiles(a, s);
+    if (a.M <= 16 && by16 <= least) return run_dma<1, 1, 8, 2, false, false>(a, s);
+    if (by32 <= least) return run_dma<2, 1, 8, 3, false, false>(a, s);
+    return by32w <= least ? run_dma<2, 2, 8, 2, false, false>(a, s) : run_dma<4, 2, 4, 3, false, false>(a, s);
 }
 
 }  // namespace ql

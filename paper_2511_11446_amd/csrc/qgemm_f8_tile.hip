@@ -14,7 +14,7 @@ struct TileF8 {
     static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, S_AT = A_BYTES + B_BYTES, STAGE = S_AT + BM * 4 + 256;
     static constexpr int ISSUED = NA + NB + 1;                           // and one for the rows' scales
     static constexpr int LDS_BYTES = STAGES * STAGE;
-    static constexpr int BUFS = WIDE ? 2 : 4, DIST = WIDE ? 1 : 2;            // weight fragments in registers, and how many groups ahead one is read
+    static constexpr int BUFS = WIDE || NT < 4 ? 2 : 4, DIST = BUFS == 2 ? 1 : 2;            // weight fragments in registers, and how many groups ahead one is read
     static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && BM % 64 == 0 && NT % 2 == 0 && NT % BUFS == 0 && 16 * NT <= 128, "whole DMA instructions");
     static_assert(LDS_BYTES <= 160 * 1024 && ISSUED * (STAGES - 2) < 64, "LDS, outstanding operations");
 };
@@ -350,7 +350,7 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
 template <class T, F8Out OUT>
 static hipError_t run_tile(const F8Gemm &a, hipStream_t s)
 {
-    const hipError_t opt_in = hipFuncSetAttribute(reinterpret_cast<const void *>(&qgemm_f8_tile<T, OUT>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES);
+    const hipError_t opt_in = allow_lds<&qgemm_f8_tile<T, OUT>>();
     if (opt_in != hipSuccess) return opt_in;
     const int cols = OUT == F8Out::GATED ? T::BN / 2 : T::BN;
     const int tiles_m = OUT == F8Out::LAYER ? (a.M + T::BM - 1) / T::BM : a.tiles_most, tiles_n = (a.N + cols - 1) / cols;
@@ -359,15 +359,37 @@ static hipError_t run_tile(const F8Gemm &a, hipStream_t s)
     return hipGetLastError();
 }
 
-using CoreTile = TileF8<4, 8, 4, 2, 2, false>;    // 256 x 256
-using WideTile = TileF8<4, 4, 2, 4, 3, true>;     // 128 x 256
-static_assert(WideTile::BM == F8_TILE_ROWS, "what the rows of experts are cut into");
+using Core256 = TileF8<4, 8, 4, 2, 2, false>;      // 256 x 256, one on a CU
+using Core128 = TileF8<4, 4, 2, 2, 2, false>;      // 128 x 128, two
+using Core64 = TileF8<2, 2, 2, 2, 2, false>;       // 64 x 64, four
+using Wide128 = TileF8<4, 4, 2, 2, 2, true>;
+using Wide64 = TileF8<2, 2, 2, 2, 2, true>;
+using ExpertTile = TileF8<4, 4, 2, 4, 3, true>;    // 128 x 256
+static_assert(ExpertTile::BM == F8_TILE_ROWS, "what the rows of experts are cut into");
+
+// What a layer takes on tiles of `side` of which `fit` are on a CU at a time: rounds of tiles, in each KB steps at step[l - 1] us where a CU has l of them, and `ends` us in
+// front of the first step and behind the last.  The steps are those of 4096 x 4096 and 8192 x 8192 weights; us, measured and so, with the matrix cores' own
+// sums: 1021 x 2224 x 1001 on 64 11.3 and 11.4, on 128 20.2 and 20.1, on 256 41 and 42; 2048 x 4096 x 4096 64, 42, 59 and 67, 42, 66; 16384 x 1152 x 4608 162, 124, 124 and 166, 127, 136.
+static float tiles_us(const F8Gemm &a, int side, int fit, const float *step, float ends)
+{
+    const int64_t tiles = ((a.M + side - 1ll) / side) * ((a.N + side - 1ll) / side), slots = 256ll * fit;
+    const int64_t left = tiles % slots;
+    float us = 2.0f + (float)(tiles / slots) * (step[fit - 1] * a.KB + ends);
+    if (left) us += step[(left + 255) / 256 - 1] * a.KB + ends;
+    return us;
+}
+constexpr float CORE64[] = {0.52f, 0.64f, 0.82f, 1.01f}, CORE128[] = {0.81f, 1.14f}, CORE256[] = {1.85f}, WIDE64[] = {0.60f, 0.80f, 1.04f, 1.27f}, WIDE128[] = {1.17f, 1.85f};
+
+float qgemm_f8_tiles_us(const F8Gemm &a) { return fminf(tiles_us(a, 64, 4, WIDE64, 0.2f), tiles_us(a, 128, 2, WIDE128, 3.5f)); }
 
 hipError_t launch_qgemm_f8_tiles(const F8Gemm &a, hipStream_t s)
 {
-    if (a.first) return a.gated ? run_tile<WideTile, F8Out::GATED>(a, s) : run_tile<WideTile, F8Out::ROWS>(a, s);
-    if (a.M <= 256) return run_tile<TileF8<2, 4, 2, 2, 4, true>, F8Out::LAYER>(a, s);
-    return a.codes ? run_tile<CoreTile, F8Out::LAYER>(a, s) : run_tile<WideTile, F8Out::LAYER>(a, s);
+    if (a.first) return a.gated ? run_tile<ExpertTile, F8Out::GATED>(a, s) : run_tile<ExpertTile, F8Out::ROWS>(a, s);
+    if (!a.codes || a.M <= F8_MANY)
+        return tiles_us(a, 64, 4, WIDE64, 0.2f) <= tiles_us(a, 128, 2, WIDE128, 3.5f) ? run_tile<Wide64, F8Out::LAYER>(a, s) : run_tile<Wide128, F8Out::LAYER>(a, s);
+    const float by64 = tiles_us(a, 64, 4, CORE64, 0.2f), by128 = tiles_us(a, 128, 2, CORE128, 3.5f), by256 = tiles_us(a, 256, 1, CORE256, 10.0f);
+    if (by64 <= by128 && by64 <= by256) return run_tile<Core64, F8Out::LAYER>(a, s);
+    return by128 <= by256 ? run_tile<Core128, F8Out::LAYER>(a, s) : run_tile<Core256, F8Out::LAYER>(a, s);
 }
 
 }  // namespace ql

@@ -28,7 +28,9 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
 {
     constexpr int MT = T::MT, NT = T::NT;
     constexpr bool EXPERTS = OUT != F8Out::LAYER, GATED = OUT == F8Out::GATED;
-    constexpr int COLS = GATED ? T::BN / 2 : T::BN;     // outputs of a tile
+    // of GATED a tile is one block of 128 channels, in one pass over the steps or, 64 channels each, in two
+    constexpr int PASSES = GATED ? F8_BLOCK / (T::BN / 2) : 1, COLS = GATED ? F8_BLOCK : T::BN;   // outputs of a tile
+    static_assert(PASSES == 1 || PASSES == 2, "passes");
     extern __shared__ __align__(1024) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / T::WN, wn = wave % T::WN, p = lane & 15, g = lane >> 4;
@@ -55,7 +57,7 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
     }
 
     // ---- DMA: lane l fills bytes [16 l, 16 l + 16) of 1024 = row l / 8, slot l % 8; chunk c of row r lies at slot c ^ ((r >> 1) & 7)
-    unsigned offA[T::NA], offB[T::NB], offS;
+    unsigned offA[T::NA], offB[PASSES][T::NB], offS;
     bool dead[2];   // the chunk lies behind the end of a row in the last step (of rows with (row >> 1) & 4 clear, set)
     const unsigned bytesA = EXPERTS && a.order ? 0xffffffe0u : (unsigned)a.M * (unsigned)a.K;
     const unsigned bytesB = (unsigned)a.N * (unsigned)a.K * (GATED ? 2u : 1u);
@@ -75,7 +77,8 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
         const int r = 8 * (wave + i * T::NW) + (lane >> 3), of = r / (16 * NT), b = r / 16 % NT, x = r % 16;
         const int half = GATED && b >= NT / 2, bb = GATED ? b % (NT / 2) : b;
         const int c = of * (GATED ? 8 * NT : 16 * NT) + 32 * (bb / 2) + 8 * (x / 4) + 4 * (bb % 2) + x % 4;
-        offB[i] = (unsigned)(min(n0 + c, a.N - 1) + half * a.N) * (unsigned)a.K + 16 * ((lane & 7) ^ ((r >> 1) & 7));
+#pragma unroll
+        for (int h = 0; h < PASSES; ++h) offB[h][i] = (unsigned)(min(n0 + 64 * h + c, a.N - 1) + half * a.N) * (unsigned)a.K + 16 * ((lane & 7) ^ ((r >> 1) & 7));
     }
     // rows of one DMA instruction begin at a multiple of 8: (r >> 1) & 3 is the lane's, bit 2 that of the instruction's number
 #pragma unroll
@@ -89,9 +92,13 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
     else offS = (unsigned)(GATED ? n0 / F8_BLOCK + (lane & 1) * a.NB : min(n0 / F8_BLOCK + (lane & 1), a.NB - 1)) * (unsigned)a.KB * 4u;
     const unsigned s_at = T::S_AT + (row_scales ? wave : SW) * 256;
 
-    auto issue = [&](int kt, int stage) {
+    const int steps = PASSES * a.KB;
+    auto issue = [&](int step, int stage) {
         unsigned char *st = smem + stage * T::STAGE;
-        if (kt == a.KB - 1 && last != F8_BLOCK) {
+        const bool second = PASSES == 2 && step >= a.KB;
+        const int kt = second ? step - a.KB : step;
+        const bool tail = kt == a.KB - 1 && last != F8_BLOCK;
+        if (tail) {
 #pragma unroll
             for (int i = 0; i < T::NA; ++i) {
                 const int at = wave + i * T::NW;
@@ -100,13 +107,19 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
 #pragma unroll
             for (int i = 0; i < T::NB; ++i) {
                 const int at = wave + i * T::NW;
-                dma16_buf(w, bytesB, st + T::A_BYTES + at * 1024, dead[at & 1] ? 0xfffffff0u : offB[i] + (unsigned)kt * 128u, 0);
+                const unsigned off = PASSES == 2 && second ? offB[PASSES - 1][i] : offB[0][i];
+                dma16_buf(w, bytesB, st + T::A_BYTES + at * 1024, dead[at & 1] ? 0xfffffff0u : off + (unsigned)kt * 128u, 0);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < T::NA; ++i) dma16_buf(a.q, bytesA, st + (wave + i * T::NW) * 1024, offA[i], kt * 128);
+            if (second) {
 #pragma unroll
-            for (int i = 0; i < T::NB; ++i) dma16_buf(w, bytesB, st + T::A_BYTES + (wave + i * T::NW) * 1024, offB[i], kt * 128);
+                for (int i = 0; i < T::NB; ++i) dma16_buf(w, bytesB, st + T::A_BYTES + (wave + i * T::NW) * 1024, offB[PASSES - 1][i], kt * 128);
+            } else {
+#pragma unroll
+                for (int i = 0; i < T::NB; ++i) dma16_buf(w, bytesB, st + T::A_BYTES + (wave + i * T::NW) * 1024, offB[0][i], kt * 128);
+            }
         }
         const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(scales), 0, 0xffffffff, 0x00020000);
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(st + s_at), 4, offS, kt * 4, 0, 0);
@@ -150,10 +163,15 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
         for (int r = 0; r < 4; ++r) acc[j][i][r] = __builtin_fmaf(d[j & 1][i][r], s, acc[j][i][r]);
         asm volatile("" : "+v"(acc[j][i]));   // here: left to itself the compiler moves all of a step's behind its products, whose sums then have no room
     };
+    float h[PASSES][GATED ? MT : 1][8];
+    auto gated_product = [&](int pass, int i) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[pass][GATED ? i : 0][e] = silu_dev(acc[e / 4][i][e % 4]) * acc[NT / 2 + e / 4][i][e % 4];
+    };
 #pragma unroll
     for (int s = 0; s < T::STAGES; ++s)
-        if (s < a.KB) issue(s, s);
-    if (a.KB >= T::STAGES) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(T::ISSUED * (T::STAGES - 1)) : "memory");
+        if (s < steps) issue(s, s);
+    if (steps >= T::STAGES) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(T::ISSUED * (T::STAGES - 1)) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
@@ -167,7 +185,7 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
         scale[i] = scale_up[i] = 0.0f;
     }
     int stage = 0;
-    for (int kt = 0; kt < a.KB; ++kt) {
+    for (int kt = 0; kt < steps; ++kt) {
         const unsigned char *st = smem + stage * T::STAGE;
         const int next = stage + 1 == T::STAGES ? 0 : stage + 1;
         const unsigned char *st_next = smem + next * T::STAGE;
@@ -175,11 +193,11 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
         for (int j = 0; j < NT; ++j) {
             if (j == NT - 1) {
                 // (as many steps as there are stages are under way, fewer at the end; the oldest of them is the next)
-                if (T::STAGES > 2 && kt + T::STAGES - 1 < a.KB) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(T::ISSUED * (T::STAGES - 2)) : "memory");
+                if (T::STAGES > 2 && kt + T::STAGES - 1 < steps) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(T::ISSUED * (T::STAGES - 2)) : "memory");
                 else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
                 __builtin_amdgcn_s_barrier();
                 asm volatile("" ::: "memory");
-                if (kt + T::STAGES < a.KB) issue(kt + T::STAGES, stage);
+                if (kt + T::STAGES < steps) issue(kt + T::STAGES, stage);
             }
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (T::WIDE) {
@@ -213,6 +231,17 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
             __builtin_amdgcn_sched_barrier(0);
         }
         stage = next;
+        if (PASSES == 2 && kt == a.KB - 1) {
+            // the first 64 channels are there: the last group is taken in, and what it leaves for the next step has a scale of 0
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                fold(NT - 1, i);
+                scale_up[i] = 0.0f;
+                gated_product(0, i);
+#pragma unroll
+                for (int k = 0; k < NT; ++k) acc[k][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            }
+        }
     }
 #pragma unroll
     for (int i = 0; i < MT; ++i) fold(NT - 1, i);
@@ -220,23 +249,19 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
     // ---- epilogue
     typedef _Float16 h8a __attribute__((ext_vector_type(8), may_alias));
     if constexpr (GATED) {
-        // h = silu(g) * u of 8 channels and MT rows a lane; the block's maximum over the lanes of a row and the WN wavefronts
-        static_assert(8 * NT * T::WN == F8_BLOCK, "a tile is one block of channels");
-        float h[MT][8];
+        // h = silu(g) * u of 8 channels (twice 8 in two passes) and MT rows a lane; the block's maximum over the lanes of a row and the WN wavefronts
         float *most = reinterpret_cast<float *>(smem);   // [BM][WN]
-        const int c = col0 + 8 * g;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();                    // the last step has been read everywhere
         asm volatile("" ::: "memory");
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
+            gated_product(PASSES - 1, i);
             float m = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                h[i][e] = silu_dev(acc[e / 4][i][e % 4]) * acc[NT / 2 + e / 4][i][e % 4];
-                m = fmaxf(m, fabsf(h[i][e]));
-            }
-            if (c >= a.N) m = 0.0f;
+            for (int k = 0; k < PASSES; ++k)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) m = fmaxf(m, col0 + 64 * k + 8 * g < a.N ? fabsf(h[k][i][e]) : 0.0f);
             m = fmaxf(m, __shfl_xor(m, 16));
             m = fmaxf(m, __shfl_xor(m, 32));
             if (g == 0) most[((wm * MT + i) * 16 + p) * T::WN + wn] = m;
@@ -252,10 +277,13 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
             for (int k = 1; k < T::WN; ++k) amax = fmaxf(amax, most[r * T::WN + k]);
             if (m >= m_end) continue;
             const F8Scale s(amax);
-            if (c < a.N) {
+#pragma unroll
+            for (int k = 0; k < PASSES; ++k) {
+                const int c = col0 + 64 * k + 8 * g;
+                if (c >= a.N) continue;
                 uint2 out;
-                out.x = f8_pack4(s.code(h[i][0]), s.code(h[i][1]), s.code(h[i][2]), s.code(h[i][3]));
-                out.y = f8_pack4(s.code(h[i][4]), s.code(h[i][5]), s.code(h[i][6]), s.code(h[i][7]));
+                out.x = f8_pack4(s.code(h[k][i][0]), s.code(h[k][i][1]), s.code(h[k][i][2]), s.code(h[k][i][3]));
+                out.y = f8_pack4(s.code(h[k][i][4]), s.code(h[k][i][5]), s.code(h[k][i][6]), s.code(h[k][i][7]));
                 *reinterpret_cast<uint2 *>(a.hq + (long long)m * a.N + c) = out;
             }
             if (wn == 0 && g == 0) a.hs[(long long)m * a.NB + n0 / F8_BLOCK] = F8Scale::scale(amax);
@@ -352,7 +380,7 @@ static hipError_t run_tile(const F8Gemm &a, hipStream_t s)
 {
     const hipError_t opt_in = allow_lds<&qgemm_f8_tile<T, OUT>>();
     if (opt_in != hipSuccess) return opt_in;
-    const int cols = OUT == F8Out::GATED ? T::BN / 2 : T::BN;
+    const int cols = OUT == F8Out::GATED ? F8_BLOCK : T::BN;
     const int tiles_m = OUT == F8Out::LAYER ? (a.M + T::BM - 1) / T::BM : a.tiles_most, tiles_n = (a.N + cols - 1) / cols;
     const unsigned grid = (unsigned)((tiles_m * tiles_n + XCDS - 1) / XCDS * XCDS);
     hipLaunchKernelGGL((qgemm_f8_tile<T, OUT>), dim3(grid), dim3(T::NTHR), T::LDS_BYTES, s, a, tiles_m, tiles_n, pick_group_m(T::BM));
@@ -364,8 +392,7 @@ using Core128 = TileF8<4, 4, 2, 2, 2, false>;      // 128 x 128, two
 using Core64 = TileF8<2, 2, 2, 2, 2, false>;       // 64 x 64, four
 using Wide128 = TileF8<4, 4, 2, 2, 2, true>;
 using Wide64 = TileF8<2, 2, 2, 2, 2, true>;
-using ExpertTile = TileF8<4, 4, 2, 4, 3, true>;    // 128 x 256
-static_assert(ExpertTile::BM == F8_TILE_ROWS, "what the rows of experts are cut into");
+static_assert(Wide128::BM == F8_TILE_ROWS, "what the rows of experts are cut into");
 
 // What a layer takes on tiles of `side` of which `fit` are on a CU at a time: rounds of tiles, in each KB steps at step[l - 1] us where a CU has l of them, and `ends` us in
 // front of the first step and behind the last.  The steps are those of 4096 x 4096 and 8192 x 8192 weights; us, measured and so, with the matrix cores' own
@@ -384,7 +411,7 @@ float qgemm_f8_tiles_us(const F8Gemm &a) { return fminf(tiles_us(a, 64, 4, WIDE6
 
 hipError_t launch_qgemm_f8_tiles(const F8Gemm &a, hipStream_t s)
 {
-    if (a.first) return a.gated ? run_tile<ExpertTile, F8Out::GATED>(a, s) : run_tile<ExpertTile, F8Out::ROWS>(a, s);
+    if (a.first) return a.gated ? run_tile<Wide128, F8Out::GATED>(a, s) : run_tile<Wide128, F8Out::ROWS>(a, s);
     if (!a.codes || a.M <= F8_MANY)
         return tiles_us(a, 64, 4, WIDE64, 0.2f) <= tiles_us(a, 128, 2, WIDE128, 3.5f) ? run_tile<Wide64, F8Out::LAYER>(a, s) : run_tile<Wide128, F8Out::LAYER>(a, s);
     const float by64 = tiles_us(a, 64, 4, CORE64, 0.2f), by128 = tiles_us(a, 128, 2, CORE128, 3.5f), by256 = tiles_us(a, 256, 1, CORE256, 10.0f);

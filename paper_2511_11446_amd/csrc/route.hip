@@ -4,7 +4,7 @@
 
 namespace ql {
 
-// ---- scores and choice: a wavefront per token, experts lane + 64 i in a lane's registers -----------------------------------------------
+// ---- scores and choice: a wavefront per token -------------------------------------------------------------------------------------------
 // In 64 bits throughout: two experts that 32 bits cannot tell apart would make the choice a matter of rounding.
 struct Best {
     double c;
@@ -18,13 +18,11 @@ __device__ __forceinline__ Best best_of_wave(Best b)
     return b;
 }
 
+// One token by the definition.  Experts lane + 64 i in a lane's registers; by: [E] in LDS where there are groups
 template <int PER, bool WIDE>
-__global__ __launch_bounds__(256) void route(RouteArgs a)
+__device__ __forceinline__ void route_exact(const RouteArgs &a, long long t, double *by)
 {
-    extern __shared__ double by_expert[];   // [4][E] where there are groups
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long t = (long long)blockIdx.x * 4 + wave;
-    if (t >= a.T) return;
+    const int lane = threadIdx.x & 63;
     const double none = -__builtin_inf();
     double s[PER], c[PER], key[PER];
     double top = none;
@@ -68,7 +66,6 @@ __global__ __launch_bounds__(256) void route(RouteArgs a)
         }
     }
     if (a.groups > 1 && a.top_groups < a.groups) {
-        double *by = by_expert + wave * a.E;
 #pragma unroll
         for (int i = 0; i < PER; ++i)
             if (lane + 64 * i < a.E) by[lane + 64 * i] = c[i];
@@ -131,6 +128,219 @@ __global__ __launch_bounds__(256) void route(RouteArgs a)
         if (a.renorm && sum > 0.0) mine /= sum;
         a.ids[t * a.k + lane] = id;
         a.weights[t * a.k + lane] = (float)(mine * (double)a.scale);
+    }
+}
+
+// ---- the same where 32 bits can tell the choices apart ---------------------------------------------------------------------------------
+// A lane's PER neighbouring experts as keys (32 bits whose order as whole numbers is that of the floats; 0: cannot be chosen), sorted by itself: a choice is
+// then the largest of 64 heads (6 instructions by DPP and a read), whose lane gives the next one of its own.  Without a bias the keys are the logits, which
+// decide exactly.  With one they are s + bias in 32 bits, off by at most ROUTE_NEAR / 2 (exponent, reciprocal, sum and their like, each 2^-22 of at most 1, and the
+// addition's 2^-24): where two that follow each other are nearer, or two groups at the border of those that are kept, the token is done again in 64 bits.
+// The weights are taken in 64 bits, of the chosen alone.
+// T = 16384, E = 256, k = 8, sigmoid, bias, 4 of 8 groups: 55 us in 64 bits throughout.
+constexpr float ROUTE_NEAR = 0x1p-17f;
+
+__device__ __forceinline__ unsigned key_of(float f)
+{
+    const unsigned u = __builtin_bit_cast(unsigned, f + 0.0f);   // -0 is 0
+    return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float float_of(unsigned k) { return __builtin_bit_cast(float, k >> 31 ? k ^ 0x80000000u : ~k); }
+
+// the largest over the wavefront
+__device__ __forceinline__ unsigned top_of_wave(unsigned m)
+{
+#define QL_TOP(ctrl, rows) m = max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, ctrl, rows, 0xF, false));
+    QL_TOP(0x111, 0xF)   // row_shr: 1, 2, 4, 8: lane 15 of a row has the row's
+    QL_TOP(0x112, 0xF)
+    QL_TOP(0x114, 0xF)
+    QL_TOP(0x118, 0xF)
+    QL_TOP(0x142, 0xA)   // row_bcast: 15 into rows 1 and 3, 31 into rows 2 and 3
+    QL_TOP(0x143, 0xC)
+#undef QL_TOP
+    return (unsigned)__builtin_amdgcn_readlane((int)m, 63);
+}
+
+template <int PER, bool WIDE>
+__global__ __launch_bounds__(256) void route(RouteArgs a)
+{
+    extern __shared__ double by_expert[];   // [4][E] where there are groups
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long t = (long long)blockIdx.x * 4 + wave;
+    if (t >= a.T) return;
+    const float inf = __builtin_inff();
+    const bool by_groups = a.groups > 1 && a.top_groups < a.groups, scores = a.bias || by_groups;
+    // ---- logits (as floats, -inf: dead), and keys
+    float x[PER];
+    unsigned key[PER];
+    int index[PER];
+    float top = -inf;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int e = lane * PER + i;
+        float f = -inf;
+        if (e < a.E) f = WIDE ? static_cast<const float *>(a.logits)[t * a.E + e] : (float)static_cast<const _Float16 *>(a.logits)[t * a.E + e];
+        const float most = WIDE ? 3.402823466e38f : 65504.0f;
+        f = f > most ? most : f;
+        x[i] = f > -inf ? f : -inf;   // NaN is not greater
+        top = fmaxf(top, x[i]);
+        index[i] = e;
+        key[i] = x[i] > -inf ? key_of(x[i]) : 0u;
+    }
+    if (!a.sigmoid) top = float_of(top_of_wave(key_of(top)));
+    bool near = false;
+    if (scores) {
+        constexpr float LOG2E = 1.44269504f;
+        float s[PER], sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const bool alive = x[i] > -inf;
+            // (the difference of two floats of one sign and size is exact or as good; its exponential matters while it is small)
+            s[i] = !alive ? 0.0f : a.sigmoid ? __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-x[i] * LOG2E)) : __builtin_amdgcn_exp2f((x[i] - top) * LOG2E);
+            sum += s[i];
+        }
+        if (!a.sigmoid) {
+#pragma unroll
+            for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+            const float r = sum > 0.0f ? __builtin_amdgcn_rcpf(sum) : 0.0f;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) s[i] *= r;
+        }
+        float c[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            c[i] = x[i] > -inf ? s[i] : -inf;
+            if (a.bias && x[i] > -inf) {
+                c[i] = s[i] + a.bias[lane * PER + i];
+                if (!(c[i] > -inf)) c[i] = -inf;   // NaN
+                // a choice of another size than the scores has lost more than the bound says
+                near |= fabsf(c[i]) > 4.0f && c[i] > -inf;
+                key[i] = c[i] > -inf ? key_of(c[i]) : 0u;
+            }
+        }
+        near = __any(near);
+        if (by_groups) {
+            float *by = reinterpret_cast<float *>(by_expert + wave * a.E);
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (lane * PER + i < a.E) by[lane * PER + i] = c[i];
+            __threadfence_block();
+            __builtin_amdgcn_wave_barrier();
+            const int size = a.E / a.groups;
+            // L lanes a group (a power of two), each with every L-th of its experts; groups beyond 64 in a second round
+            int L = 1;
+            while (2 * L * a.groups <= 64) L *= 2;
+            float worth[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int group = lane / L + 64 * h;
+                float one = -inf, two = -inf;
+                if (group < a.groups && (h == 0 || a.groups > 64)) {
+                    for (int j = lane % L; j < size; j += L) {
+                        const float v = by[group * size + j];
+                        two = fmaxf(two, fminf(one, v));
+                        one = fmaxf(one, v);
+                    }
+                }
+                for (int d = 1; d < L; d *= 2) {
+                    const float o1 = __shfl_xor(one, d), o2 = __shfl_xor(two, d);
+                    two = fmaxf(fmaxf(two, o2), fminf(one, o1));
+                    one = fmaxf(one, o1);
+                }
+                worth[h] = a.group_top == 2 && two > -inf ? one + two : one;
+            }
+            // a group's place among all: how many are worthier, or as worthy with a smaller number
+            unsigned long long keep[2] = {0, 0};
+            float least = inf, best = -inf;   // of those that are kept, of the others
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int group = lane / L + 64 * h;
+                int before = 0;
+                for (int o = 0; o < a.groups; ++o) {
+                    const float w = o < 64 ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, worth[0]), (o * L) & 63))
+                                           : __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, worth[1]), o - 64));
+                    before += w > worth[h] || (w == worth[h] && o < group);
+                }
+                const bool there = group < a.groups && worth[h] > -inf && (h == 0 || a.groups > 64), kept = there && before < a.top_groups;
+                keep[h] = __ballot(kept);
+                if (kept) least = fminf(least, worth[h]);
+                else if (there) best = fmaxf(best, worth[h]);
+            }
+#pragma unroll
+            for (int d = 32; d; d >>= 1) {
+                least = fminf(least, __shfl_xor(least, d));
+                best = fmaxf(best, __shfl_xor(best, d));
+            }
+            near |= least - best < 2.0f * ROUTE_NEAR;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int group = (lane * PER + i) / size, bit = group < 64 ? group * L : group - 64;
+                if (!((group < 64 ? keep[0] : keep[1]) >> (bit & 63) & 1)) key[i] = 0;
+            }
+        }
+    }
+    // ---- a lane's own in order, the lower number first among equals
+#pragma unroll
+    for (int i = 1; i < PER; ++i)
+#pragma unroll
+        for (int j = i; j > 0; --j) {
+            const bool swap = key[j] > key[j - 1];
+            const unsigned k0 = swap ? key[j] : key[j - 1], k1 = swap ? key[j - 1] : key[j];
+            const int i0 = swap ? index[j] : index[j - 1], i1 = swap ? index[j - 1] : index[j];
+            const float x0 = swap ? x[j] : x[j - 1], x1 = swap ? x[j - 1] : x[j];
+            key[j - 1] = k0, key[j] = k1, index[j - 1] = i0, index[j] = i1, x[j - 1] = x0, x[j] = x1;
+        }
+    // ---- choices: the j-th stays with lane j
+    int id = -1;
+    float logit = -inf;
+    unsigned last = 0xffffffffu;
+    // (one more than is asked for: whether the last one is far enough from the next)
+    for (int j = 0; j <= a.k; ++j) {
+        const unsigned best = top_of_wave(key[0]);
+        if (a.bias && j && best && float_of(last) - float_of(best) < ROUTE_NEAR) near = true;
+        if (!best || j == a.k || near) break;
+        last = best;
+        const int owner = __builtin_ctzll(__ballot(key[0] == best));   // the lowest lane has the lowest numbers
+        const int e = __builtin_amdgcn_readlane(index[0], owner);
+        const float l = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x[0]), owner));
+        if (lane == j) {
+            id = e;
+            logit = l;
+        }
+        if (lane == owner) {
+#pragma unroll
+            for (int i = 0; i + 1 < PER; ++i) key[i] = key[i + 1], index[i] = index[i + 1], x[i] = x[i + 1];
+            key[PER - 1] = 0;
+        }
+    }
+    if (near) {
+        route_exact<PER, WIDE>(a, t, by_expert + wave * a.E);
+        return;
+    }
+    // ---- weights
+    double total = 1.0;
+    if (!a.sigmoid && !a.renorm) {
+        total = 0.0;
+        for (int e = lane; e < a.E; e += 64) {
+            float f = WIDE ? static_cast<const float *>(a.logits)[t * a.E + e] : (float)static_cast<const _Float16 *>(a.logits)[t * a.E + e];
+            const float most = WIDE ? 3.402823466e38f : 65504.0f;
+            f = f > most ? most : f;
+            if (f > -inf) total += exp((double)f - (double)top);
+        }
+#pragma unroll
+        for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
+        if (!(total > 0.0)) total = 1.0;
+    }
+    double w = 0.0;
+    if (id >= 0) w = a.sigmoid ? 1.0 / (1.0 + exp(-(double)logit)) : exp((double)logit - (double)top);
+    if (a.renorm) {
+        total = lane < a.k ? w : 0.0;
+        for (int d = 1; d < a.k; d *= 2) total += __shfl_xor(total, d);
+        if (!(total > 0.0)) total = 1.0;
+    }
+    if (lane < a.k) {
+        a.ids[t * a.k + lane] = id;
+        a.weights[t * a.k + lane] = (float)(w / total * (double)a.scale);
     }
 }
 

@@ -2,6 +2,8 @@
 #include "daq_device.h"
 #include "f8.h"
 
+#include <type_traits>
+
 namespace ql {
 
 // ---- scores and choice: a wavefront per token -------------------------------------------------------------------------------------------
@@ -132,13 +134,15 @@ __device__ __forceinline__ void route_exact(const RouteArgs &a, long long t, dou
 }
 
 // ---- the same where 32 bits can tell the choices apart ---------------------------------------------------------------------------------
-// A lane's PER neighbouring experts as keys (32 bits whose order as whole numbers is that of the floats; 0: cannot be chosen), sorted by itself: a choice is
-// then the largest of 64 heads (6 instructions by DPP and a read), whose lane gives the next one of its own.  Without a bias the keys are the logits, which
-// decide exactly.  With one they are s + bias in 32 bits, off by at most ROUTE_NEAR / 2 (exponent, reciprocal, sum and their like, each 2^-22 of at most 1, and the
-// addition's 2^-24): where two that follow each other are nearer, or two groups at the border of those that are kept, the token is done again in 64 bits.
-// The weights are taken in 64 bits, of the chosen alone.
-// T = 16384, E = 256, k = 8, sigmoid, bias, 4 of 8 groups: 55 us in 64 bits throughout.
-constexpr float ROUTE_NEAR = 0x1p-17f;
+// A lane's PER neighbouring experts as keys: whole numbers in the order of the floats (0: cannot be chosen) whose lowest bits say which expert it is, the lower
+// number the larger.  The lane sorts its own; a choice is then the largest of 64 heads (six instructions by DPP and a read), whose lane brings up its next.
+//   binary16 logits without a bias: the float's lowest 13 bits are free, 9 of them hold the number: every key is another one, the order is exact.
+//   fp32 logits without a bias: 3 bits hold the place in the lane.  Two keys that are alike above them: the token is done again in 64 bits.
+//   with a bias: s + bias in 32 bits, off by at most ROUTE_NEAR / 2 (exponent, reciprocal and sum 2^-20 of at most 1, the addition 2^-24 of at most 4, the bits
+//   for the place 2^-19): two that follow each other and are nearer, or two groups at the border of those that are kept and nearer than GROUP_NEAR: in 64 bits, too.
+// The weights are taken in 64 bits, of the chosen alone.  Bound by vector instructions, about 1 us of them for 1024 tokens: T = 16384, E = 256, k = 8, sigmoid, bias,
+// 4 of 8 groups took 55 us in 64 bits throughout.
+constexpr float ROUTE_NEAR = 0x1p-17f, GROUP_NEAR = 0x1p-12f;
 
 __device__ __forceinline__ unsigned key_of(float f)
 {
@@ -161,186 +165,226 @@ __device__ __forceinline__ unsigned top_of_wave(unsigned m)
     return (unsigned)__builtin_amdgcn_readlane((int)m, 63);
 }
 
-template <int PER, bool WIDE>
-__global__ __launch_bounds__(256) void route(RouteArgs a)
+__device__ __forceinline__ float read_lane(float v, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); }
+
+// 1 / d of a finite d of ordinary size, to 2^-51 or so: two steps of Newton's iteration from the instruction's 2^-14
+__device__ __forceinline__ double inverse(double d)
+{
+    double r = __builtin_amdgcn_rcp(d);
+    r = __builtin_fma(__builtin_fma(-d, r, 1.0), r, r);
+    r = __builtin_fma(__builtin_fma(-d, r, 1.0), r, r);
+    return __builtin_fma(__builtin_fma(-d, r, 1.0), r, r);
+}
+
+template <bool WIDE>
+__device__ __forceinline__ float tame(float f)
+{
+    const float most = WIDE ? 3.402823466e38f : 65504.0f;
+    return f > most ? most : f > -__builtin_inff() ? f : -__builtin_inff();   // NaN is not greater
+}
+template <bool WIDE>
+__device__ __forceinline__ float logit_at(const RouteArgs &a, long long at)
+{
+    return tame<WIDE>(WIDE ? static_cast<const float *>(a.logits)[at] : (float)static_cast<const _Float16 *>(a.logits)[at]);
+}
+
+// whole: PER divides E and the logits and the bias begin at 16 bytes
+template <int PER, bool WIDE, bool BIAS, bool GROUPS>
+__global__ __launch_bounds__(256) void route(RouteArgs a, bool whole)
 {
     extern __shared__ double by_expert[];   // [4][E] where there are groups
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const long long t = (long long)blockIdx.x * 4 + wave;
     if (t >= a.T) return;
     const float inf = __builtin_inff();
-    const bool by_groups = a.groups > 1 && a.top_groups < a.groups, scores = a.bias || by_groups;
-    // ---- logits (as floats, -inf: dead), and keys
-    float x[PER];
-    unsigned key[PER];
-    int index[PER];
+    constexpr bool EXACT = !WIDE && !BIAS;
+    // ---- logits (-inf: dead)
+    float x[PER], c[PER];
     float top = -inf;
+    const int e0 = lane * PER;
+    if (whole) {
+        typedef typename std::conditional<WIDE, float, _Float16>::type type;
+        typedef type types __attribute__((ext_vector_type(PER)));
+        types v;
+        if (e0 < a.E) v = *reinterpret_cast<const types *>(static_cast<const type *>(a.logits) + t * a.E + e0);
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int e = lane * PER + i;
-        float f = -inf;
-        if (e < a.E) f = WIDE ? static_cast<const float *>(a.logits)[t * a.E + e] : (float)static_cast<const _Float16 *>(a.logits)[t * a.E + e];
-        const float most = WIDE ? 3.402823466e38f : 65504.0f;
-        f = f > most ? most : f;
-        x[i] = f > -inf ? f : -inf;   // NaN is not greater
-        top = fmaxf(top, x[i]);
-        index[i] = e;
-        key[i] = x[i] > -inf ? key_of(x[i]) : 0u;
+        for (int i = 0; i < PER; ++i) x[i] = e0 < a.E ? tame<WIDE>((float)v[i]) : -inf;
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            x[i] = -inf;
+            if (e0 + i < a.E) x[i] = logit_at<WIDE>(a, t * a.E + e0 + i);
+        }
+    }
+    if (!a.sigmoid) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) top = fmaxf(top, x[i]);
     }
     if (!a.sigmoid) top = float_of(top_of_wave(key_of(top)));
     bool near = false;
-    if (scores) {
+    if constexpr (BIAS || GROUPS) {
         constexpr float LOG2E = 1.44269504f;
-        float s[PER], sum = 0.0f;
+        if (a.sigmoid) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const bool alive = x[i] > -inf;
-            // (the difference of two floats of one sign and size is exact or as good; its exponential matters while it is small)
-            s[i] = !alive ? 0.0f : a.sigmoid ? __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-x[i] * LOG2E)) : __builtin_amdgcn_exp2f((x[i] - top) * LOG2E);
-            sum += s[i];
-        }
-        if (!a.sigmoid) {
+            for (int i = 0; i < PER; ++i) c[i] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-x[i] * LOG2E));   // (dead: 0)
+        } else {
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                c[i] = x[i] > -inf ? __builtin_amdgcn_exp2f((x[i] - top) * LOG2E) : 0.0f;
+                sum += c[i];
+            }
 #pragma unroll
             for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
             const float r = sum > 0.0f ? __builtin_amdgcn_rcpf(sum) : 0.0f;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) s[i] *= r;
+            for (int i = 0; i < PER; ++i) c[i] *= r;
         }
-        float c[PER];
+        if constexpr (BIAS) {
+            float bias[PER];
+            if (whole) {
+                typedef float floats __attribute__((ext_vector_type(PER)));
+                floats v;
+                if (e0 < a.E) v = *reinterpret_cast<const floats *>(a.bias + e0);
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            c[i] = x[i] > -inf ? s[i] : -inf;
-            if (a.bias && x[i] > -inf) {
-                c[i] = s[i] + a.bias[lane * PER + i];
-                if (!(c[i] > -inf)) c[i] = -inf;   // NaN
-                // a choice of another size than the scores has lost more than the bound says
-                near |= fabsf(c[i]) > 4.0f && c[i] > -inf;
-                key[i] = c[i] > -inf ? key_of(c[i]) : 0u;
+                for (int i = 0; i < PER; ++i) bias[i] = v[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < PER; ++i) bias[i] = a.bias[min(e0 + i, a.E - 1)];
             }
-        }
-        near = __any(near);
-        if (by_groups) {
-            float *by = reinterpret_cast<float *>(by_expert + wave * a.E);
-#pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if (lane * PER + i < a.E) by[lane * PER + i] = c[i];
-            __threadfence_block();
-            __builtin_amdgcn_wave_barrier();
-            const int size = a.E / a.groups;
-            // L lanes a group (a power of two), each with every L-th of its experts; groups beyond 64 in a second round
-            int L = 1;
-            while (2 * L * a.groups <= 64) L *= 2;
-            float worth[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int group = lane / L + 64 * h;
-                float one = -inf, two = -inf;
-                if (group < a.groups && (h == 0 || a.groups > 64)) {
-                    for (int j = lane % L; j < size; j += L) {
-                        const float v = by[group * size + j];
-                        two = fmaxf(two, fminf(one, v));
-                        one = fmaxf(one, v);
-                    }
-                }
-                for (int d = 1; d < L; d *= 2) {
-                    const float o1 = __shfl_xor(one, d), o2 = __shfl_xor(two, d);
-                    two = fmaxf(fmaxf(two, o2), fminf(one, o1));
-                    one = fmaxf(one, o1);
-                }
-                worth[h] = a.group_top == 2 && two > -inf ? one + two : one;
-            }
-            // a group's place among all: how many are worthier, or as worthy with a smaller number
-            unsigned long long keep[2] = {0, 0};
-            float least = inf, best = -inf;   // of those that are kept, of the others
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int group = lane / L + 64 * h;
-                int before = 0;
-                for (int o = 0; o < a.groups; ++o) {
-                    const float w = o < 64 ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, worth[0]), (o * L) & 63))
-                                           : __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, worth[1]), o - 64));
-                    before += w > worth[h] || (w == worth[h] && o < group);
-                }
-                const bool there = group < a.groups && worth[h] > -inf && (h == 0 || a.groups > 64), kept = there && before < a.top_groups;
-                keep[h] = __ballot(kept);
-                if (kept) least = fminf(least, worth[h]);
-                else if (there) best = fmaxf(best, worth[h]);
-            }
-#pragma unroll
-            for (int d = 32; d; d >>= 1) {
-                least = fminf(least, __shfl_xor(least, d));
-                best = fmaxf(best, __shfl_xor(best, d));
-            }
-            near |= least - best < 2.0f * ROUTE_NEAR;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int group = (lane * PER + i) / size, bit = group < 64 ? group * L : group - 64;
-                if (!((group < 64 ? keep[0] : keep[1]) >> (bit & 63) & 1)) key[i] = 0;
+                if (x[i] > -inf) c[i] += bias[i];
+                near |= fabsf(c[i]) > 4.0f && c[i] > -inf;   // of another size than the scores: more is lost than the bound says
             }
         }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) c[i] = x[i] > -inf && c[i] > -inf ? c[i] : -inf;   // (NaN is not greater)
+        if (BIAS) near = __any(near);
     }
-    // ---- a lane's own in order, the lower number first among equals
+    // ---- keys
+    unsigned key[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const float f = BIAS ? c[i] : x[i];
+        const unsigned k = key_of(f);
+        key[i] = f == -inf ? 0u : EXACT ? (k & ~511u) | (511 - (e0 + i)) : (k & ~7u) | (7 - i);
+    }
+    if (GROUPS && !near) {
+        float *by = reinterpret_cast<float *>(by_expert + wave * a.E);
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (e0 + i < a.E) by[e0 + i] = c[i];
+        __threadfence_block();
+        __builtin_amdgcn_wave_barrier();
+        const int size = a.E / a.groups;
+        // 2^l lanes a group, each with every 2^l-th of its experts; groups beyond 64 in a second round
+        int l = 0;
+        while (a.groups << (l + 1) <= 64) ++l;
+        const int rounds = a.groups > 64 ? 2 : 1;
+        float worth[2] = {-inf, -inf};
+        for (int h = 0; h < rounds; ++h) {
+            const int group = (lane >> l) + 64 * h;
+            float one = -inf, two = -inf;
+            if (group < a.groups) {
+                for (int j = lane & ((1 << l) - 1); j < size; j += 1 << l) {
+                    const float v = by[group * size + j];
+                    two = fmaxf(two, fminf(one, v));
+                    one = fmaxf(one, v);
+                }
+            }
+            for (int d = 1; d >> l == 0; d *= 2) {
+                const float o1 = __shfl_xor(one, d), o2 = __shfl_xor(two, d);
+                two = fmaxf(fmaxf(two, o2), fminf(one, o1));
+                one = fmaxf(one, o1);
+            }
+            worth[h] = a.group_top == 2 && two > -inf ? one + two : one;
+        }
+        // The worthiest groups, as keys with the number in 7 bits (2^-14 of a worth of up to 8): where the last that is kept and the first that is not are
+        // nearer than GROUP_NEAR, in 64 bits.  Every lane of a group has its key, and the group's bit in `keep` is its number.
+        unsigned group_key[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int group = (lane >> l) + 64 * h;
+            group_key[h] = h < rounds && group < a.groups && worth[h] > -inf ? (key_of(worth[h]) & ~127u) | (127 - group) : 0u;
+        }
+        unsigned long long keep[2] = {0, 0};
+        unsigned before = 0, best = 0;
+        for (int j = 0; j <= a.top_groups; ++j) {
+            before = best;
+            best = top_of_wave(max(group_key[0], group_key[1]));
+            const int group = 127 - (int)(best & 127);
+            const unsigned long long bit = best && j < a.top_groups ? 1ull << (group & 63) : 0;
+            if (group < 64) keep[0] |= bit;
+            else keep[1] |= bit;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) group_key[h] = group_key[h] == best ? 0u : group_key[h];
+        }
+        near = best && float_of(before) - float_of(best) < GROUP_NEAR;
+        const float per_group = __builtin_amdgcn_rcpf((float)size);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int group = (int)(((float)(e0 + i) + 0.5f) * per_group);   // ((e + 1/2) / size is 1/1024 from any whole number at least)
+            key[i] = (group < 64 ? keep[0] : keep[1]) >> (group & 63) & 1 ? key[i] : 0u;
+        }
+    }
+    // ---- a lane's own in order
 #pragma unroll
     for (int i = 1; i < PER; ++i)
 #pragma unroll
         for (int j = i; j > 0; --j) {
-            const bool swap = key[j] > key[j - 1];
-            const unsigned k0 = swap ? key[j] : key[j - 1], k1 = swap ? key[j - 1] : key[j];
-            const int i0 = swap ? index[j] : index[j - 1], i1 = swap ? index[j - 1] : index[j];
-            const float x0 = swap ? x[j] : x[j - 1], x1 = swap ? x[j - 1] : x[j];
-            key[j - 1] = k0, key[j] = k1, index[j - 1] = i0, index[j] = i1, x[j - 1] = x0, x[j] = x1;
+            const unsigned hi = max(key[j - 1], key[j]), lo = min(key[j - 1], key[j]);
+            key[j - 1] = hi, key[j] = lo;
         }
     // ---- choices: the j-th stays with lane j
     int id = -1;
-    float logit = -inf;
-    unsigned last = 0xffffffffu;
-    // (one more than is asked for: whether the last one is far enough from the next)
-    for (int j = 0; j <= a.k; ++j) {
+    unsigned last = 0;
+    // (where keys are not exact, one more than is asked for: whether the last one is far enough from the next)
+    const int looks = EXACT ? a.k : a.k + 1;
+    for (int j = 0; j < looks; ++j) {   // (without branches: a choice that there is not is key 0, whose number is not taken)
         const unsigned best = top_of_wave(key[0]);
-        if (a.bias && j && best && float_of(last) - float_of(best) < ROUTE_NEAR) near = true;
-        if (!best || j == a.k || near) break;
-        last = best;
-        const int owner = __builtin_ctzll(__ballot(key[0] == best));   // the lowest lane has the lowest numbers
-        const int e = __builtin_amdgcn_readlane(index[0], owner);
-        const float l = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x[0]), owner));
-        if (lane == j) {
-            id = e;
-            logit = l;
+        int e;
+        if (EXACT) e = 511 - (int)(best & 511);
+        else {
+            const unsigned long long owners = __ballot(key[0] == best);
+            const bool alike = (owners & (owners - 1)) || (j && (last ^ best) < 8u) || (BIAS && j && float_of(last) - float_of(best) < ROUTE_NEAR);
+            near |= best && alike;
+            e = __builtin_ctzll(owners) * PER + 7 - (int)(best & 7);
+            last = best;
         }
-        if (lane == owner) {
+        id = lane == j && best ? e : id;
+        const bool mine = key[0] == best;
 #pragma unroll
-            for (int i = 0; i + 1 < PER; ++i) key[i] = key[i + 1], index[i] = index[i + 1], x[i] = x[i + 1];
-            key[PER - 1] = 0;
-        }
+        for (int i = 0; i < PER; ++i) key[i] = mine ? (i + 1 < PER ? key[i + 1 < PER ? i + 1 : i] : 0u) : key[i];
     }
+    if (lane >= a.k) id = -1;
     if (near) {
         route_exact<PER, WIDE>(a, t, by_expert + wave * a.E);
         return;
     }
     // ---- weights
-    double total = 1.0;
-    if (!a.sigmoid && !a.renorm) {
+    double total = 1.0, w = 0.0;
+    if (id >= 0) {
+        const double l = (double)logit_at<WIDE>(a, t * a.E + id);
+        const double e = exp(a.sigmoid ? -l : l - (double)top);
+        w = !a.sigmoid ? e : e < __builtin_inf() ? inverse(1.0 + e) : 0.0;
+    }
+    if (a.renorm) {
+        total = w;
+        for (int d = 1; d < a.k; d *= 2) total += __shfl_xor(total, d);   // (lanes behind the last choice have 0)
+    } else if (!a.sigmoid) {
         total = 0.0;
         for (int e = lane; e < a.E; e += 64) {
-            float f = WIDE ? static_cast<const float *>(a.logits)[t * a.E + e] : (float)static_cast<const _Float16 *>(a.logits)[t * a.E + e];
-            const float most = WIDE ? 3.402823466e38f : 65504.0f;
-            f = f > most ? most : f;
+            const float f = logit_at<WIDE>(a, t * a.E + e);
             if (f > -inf) total += exp((double)f - (double)top);
         }
 #pragma unroll
         for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
-        if (!(total > 0.0)) total = 1.0;
-    }
-    double w = 0.0;
-    if (id >= 0) w = a.sigmoid ? 1.0 / (1.0 + exp(-(double)logit)) : exp((double)logit - (double)top);
-    if (a.renorm) {
-        total = lane < a.k ? w : 0.0;
-        for (int d = 1; d < a.k; d *= 2) total += __shfl_xor(total, d);
-        if (!(total > 0.0)) total = 1.0;
     }
     if (lane < a.k) {
+        if (total != 1.0) w = total > 0.0 ? w / total : 0.0;
         a.ids[t * a.k + lane] = id;
-        a.weights[t * a.k + lane] = (float)(w / total * (double)a.scale);
+        a.weights[t * a.k + lane] = (float)(w * (double)a.scale);
     }
 }
 
@@ -349,8 +393,15 @@ static void run_route(const RouteArgs &a, hipStream_t s)
 {
     const dim3 grid((unsigned)((a.T + 3ll) / 4));
     const size_t lds = a.groups > 1 ? (size_t)4 * a.E * sizeof(double) : 0;
-    if (a.wide) hipLaunchKernelGGL((route<PER, true>), grid, dim3(256), lds, s, a);
-    else hipLaunchKernelGGL((route<PER, false>), grid, dim3(256), lds, s, a);
+    const bool groups = a.groups > 1 && a.top_groups < a.groups, whole = a.E % PER == 0 && (uintptr_t)a.logits % 16 == 0 && (uintptr_t)a.bias % 16 == 0;
+    auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), lds, s, a, whole); };
+    if (a.wide) {
+        if (a.bias) groups ? run(route<PER, true, true, true>) : run(route<PER, true, true, false>);
+        else groups ? run(route<PER, true, false, true>) : run(route<PER, true, false, false>);
+    } else {
+        if (a.bias) groups ? run(route<PER, false, true, true>) : run(route<PER, false, true, false>);
+        else groups ? run(route<PER, false, false, true>) : run(route<PER, false, false, false>);
+    }
 }
 
 hipError_t launch_route(const RouteArgs &a, hipStream_t s)

@@ -310,27 +310,27 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
             for (int e = 0; e < 8; ++e) add[e] = bias ? (float)bias[min(n + e, a.N - 1)] : -0.0f;   // x + -0.0 is x, signed zeros included
         };
         if (a.N % 8 == 0 && (uintptr_t)res % 16 == 0 && (uintptr_t)gate % 16 == 0) {
+            float add[NT / 2][8];
 #pragma unroll
-            for (int b = 0; b < NT / 2; ++b) {
-                const int n = col0 + 32 * b + 8 * g;
-                if (n >= a.N) continue;
-                float add[8];
-                bias8(n, add);
-                h8 r[MT], gt[MT];
+            for (int b = 0; b < NT / 2; ++b) bias8(col0 + 32 * b + 8 * g, add[b]);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const int m = m0 + (wm * MT + i) * 16 + p;
+                h8 r[NT / 2], gt[NT / 2];
                 if (res || gate) {
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        const int m = min(m0 + (wm * MT + i) * 16 + p, m_end - 1);
-                        if (res) r[i] = *reinterpret_cast<const h8a *>(res + (long long)m * a.N + n);
-                        if (gate) gt[i] = *reinterpret_cast<const h8a *>(gate + (long long)(m / a.gate_rows) * a.N + n);
+                    for (int b = 0; b < NT / 2; ++b) {
+                        const int n = min(col0 + 32 * b + 8 * g, a.N - 8), from = min(m, m_end - 1);
+                        if (res) r[b] = *reinterpret_cast<const h8a *>(res + (long long)from * a.N + n);
+                        if (gate) gt[b] = *reinterpret_cast<const h8a *>(gate + (long long)(from / a.gate_rows) * a.N + n);
                     }
                 }
 #pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    const int m = m0 + (wm * MT + i) * 16 + p;
-                    h8 out = value(i, b, add);
-                    if (res || gate) out = __builtin_bit_cast(h8, glue_piece(gate != nullptr, res != nullptr, __builtin_bit_cast(v4i, out), gt[i], r[i]));
-                    if (m < m_end) *reinterpret_cast<h8a *>(y + (long long)m * a.N + n) = out;
+                for (int b = 0; b < NT / 2; ++b) {   // (the halves of a line one behind the other)
+                    const int n = col0 + 32 * b + 8 * g;
+                    h8 out = value(i, b, add[b]);
+                    if (res || gate) out = __builtin_bit_cast(h8, glue_piece(gate != nullptr, res != nullptr, __builtin_bit_cast(v4i, out), gt[b], r[b]));
+                    if (m < m_end && n < a.N) *reinterpret_cast<h8a *>(y + (long long)m * a.N + n) = out;
                 }
             }
         } else {

@@ -293,6 +293,8 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
         const _Float16 *bias = static_cast<const _Float16 *>(LAYER ? a.bias : nullptr), *res = static_cast<const _Float16 *>(LAYER ? a.residual : nullptr),
                        *gate = static_cast<const _Float16 *>(LAYER ? a.gate : nullptr);
         _Float16 *y = static_cast<_Float16 *>(a.y);
+        // outputs that the caches will not hold until they are read are streamed (16384 x 1152 x 4608 with its quantizer, inputs from memory: 152 -> 140 us)
+        const bool streamed = LAYER && (long long)a.M * a.N > (32ll << 20);
         // u -> fp16(act(u + bias)), of 8 neighbouring outputs
         auto value = [&](int i, int b, const float (&add)[8]) {
             h8 out;
@@ -313,6 +315,7 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
             float add[NT / 2][8];
 #pragma unroll
             for (int b = 0; b < NT / 2; ++b) bias8(col0 + 32 * b + 8 * g, add[b]);
+            auto store_rows = [&](auto stream) {
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
                 const int m = m0 + (wm * MT + i) * 16 + p;
@@ -330,9 +333,16 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
                     const int n = col0 + 32 * b + 8 * g;
                     h8 out = value(i, b, add[b]);
                     if (res || gate) out = __builtin_bit_cast(h8, glue_piece(gate != nullptr, res != nullptr, __builtin_bit_cast(v4i, out), gt[b], r[b]));
-                    if (m < m_end && n < a.N) *reinterpret_cast<h8a *>(y + (long long)m * a.N + n) = out;
+                    if (m >= m_end || n >= a.N) continue;
+                    h8a *to = reinterpret_cast<h8a *>(y + (long long)m * a.N + n);
+                    if constexpr (decltype(stream)::value) __builtin_nontemporal_store(out, to);
+                    else *to = out;
                 }
             }
+            };
+            if constexpr (!LAYER) store_rows(std::false_type{});
+            else if (streamed) store_rows(std::true_type{});   // (two copies: of one with both stores the compiler makes plain ones)
+            else store_rows(std::false_type{});
         } else {
             // rows that do not begin at a multiple of 16 bytes: through LDS, so that 64 neighbouring outputs leave together (one by one from where they
             // are summed, 128 stores of 64 rows each a wavefront, the epilogue took longer than the sums)

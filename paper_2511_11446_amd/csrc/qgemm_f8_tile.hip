@@ -148,6 +148,7 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
     Wide x[T::WIDE ? MT : 1];
     v8i rx[MT], rf[T::BUFS];
     float rs[MT], rw, ru, scale[MT], scale_up[MT];
+    static_assert(MT <= 4, "a fold behind each of a group's four rounds");
     v4f d[2][MT];
     auto read_scales = [&](const unsigned char *st) {
 #pragma unroll
@@ -213,13 +214,30 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
                 for (int k = 0; k < T::DIST; ++k) read_f(st_next, k);   // into the buffers of groups that are through
             }
             if (j == 0) read_scales(st);
+            if constexpr (T::WIDE) {
+                // a sum's four products in turn with those of the group's others: one behind the other they wait for each other (16384 tokens through 8 of 64 experts)
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                if constexpr (T::WIDE) d[j & 1][i] = step_product(f, x[i]);
-                else d[j & 1][i] = step_product(f, rx[i]);
-                fold(j == 0 ? NT - 1 : j - 1, i);
-                if (j == NT - 1) read_x(st_next, i);
-                __builtin_amdgcn_sched_barrier(0);   // in this order: a sum is four products old when it is folded
+                for (int q = 0; q < 4; ++q) {
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        if (q == 0) d[j & 1][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+                        d[j & 1][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.h[q], x[i].h[q], d[j & 1][i], 0, 0, 0);
+                    }
+                    if (q < MT) fold(j == 0 ? NT - 1 : j - 1, q);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (j == NT - 1) {
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) read_x(st_next, i);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    d[j & 1][i] = step_product(f, rx[i]);
+                    fold(j == 0 ? NT - 1 : j - 1, i);
+                    if (j == NT - 1) read_x(st_next, i);
+                    __builtin_amdgcn_sched_barrier(0);   // in this order: a sum is four products old when it is folded
+                }
             }
             if (j == 0) {
 #pragma unroll

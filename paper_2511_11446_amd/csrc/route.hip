@@ -495,10 +495,15 @@ __global__ __launch_bounds__(ROWS_THREADS) void expert_place(const int *ids, Exp
         if (gridDim.x == 1) {
             for (int w = 0; w < ROWS_WAVES; ++w) all += counts[w * r.E + e];
         } else {
-            for (int c = 0; c < (int)gridDim.x; ++c) {
-                const int n = r.counts[c * r.E + e];
-                all += n;
-                front += c < (int)blockIdx.x ? n : 0;
+            for (int first = 0; first < (int)gridDim.x; first += 16) {   // sixteen under way together: one after the other they were 18 us of 131072 rows' 23
+                int n[16];
+#pragma unroll
+                for (int c = 0; c < 16; ++c) n[c] = r.counts[min(first + c, (int)gridDim.x - 1) * r.E + e];
+#pragma unroll
+                for (int c = 0; c < 16; ++c) {
+                    all += first + c < (int)gridDim.x ? n[c] : 0;
+                    front += first + c < (int)blockIdx.x ? n[c] : 0;
+                }
             }
         }
     }

@@ -90,8 +90,8 @@ struct F8Gemm {
     bool codes;          // the matrix cores' own sums of codes will do (a layer of many rows that is not behind a gated product)
 };
 hipError_t launch_qgemm_f8(const F8Gemm &a, hipStream_t stream);
-// rows of an expert's tile, by the rows that an expert has on average; F8_TILE_ROWS and more: tiles that quantize the gated product themselves
-constexpr int F8_TILE_ROWS = 128;
+// rows of an expert's tile, by the rows that an expert has on average: 16, or F8_TILE_ROWS and more where the tiles quantize the gated product themselves
+constexpr int F8_TILE_ROWS = 64;
 int f8_expert_tile(int64_t P, int64_t E);
 // rows from which on a layer takes the matrix cores' own sums of codes, if it may
 constexpr int F8_MANY = 256;

@@ -68,118 +68,13 @@ __device__ __forceinline__ void finish_few(const F8Gemm &a, const v4f *sums, int
     }
 }
 
-// Few rows: 16 MB rows and 16 NB outputs a workgroup, whose wavefronts take every WAVES-th step and add up through LDS.  The weights are read once, by one
-// wavefront, straight into the operands' registers: bound by memory, so what counts is how much is under way: AHEAD steps a wavefront.
-// Lane group g reads chunks g and 4 + g (of 16 bytes) of a step's 8: the order along K is free, if both operands have it.
+// Few rows: 16 MB rows and 16 NB outputs a workgroup, whose wavefronts take every WAVES-th step and add up through LDS.  Every byte of the weights is read by one
+// wavefront alone: bound by memory.  A wavefront brings its own steps to its own STAGES places in LDS by DMA (no barrier): loads straight into the operands' order touch
+// 16 lines of memory each and pass 16 bytes a clock through a CU, by DMA, 8 rows of 128 bytes at a time, it is 45 (64 x 8192 x 4096 27 -> 13 us, 16 x 14336 x 4096
+// 20 -> 12, the rate of a copy).
 // EXPERTS: the rows of a tile of ExpertRows; GATED: NB blocks of the gate and the same NB of the up matrix, y = silu(g) * u.
-template <int MB, int NB, int WAVES, int AHEAD, bool EXPERTS, bool GATED>
-__global__ __launch_bounds__(64 * WAVES) void qgemm_f8_few(F8Gemm a)
-{
-    constexpr int COLS = NB * (GATED ? 2 : 1), TOTAL = MB * COLS;
-    __shared__ v4f sums[WAVES][TOTAL][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), p = lane & 15, g = lane >> 4;
-    const int across = (a.N + 16 * NB - 1) / (16 * NB), tile = blockIdx.x / across;
-    int m0 = tile * 16 * MB, m_end = a.M;
-    const uint8_t *w = a.w;
-    const float *s_w = a.s_w;
-    if constexpr (EXPERTS) {
-        if (tile >= a.tiles[0]) return;
-        const int e = a.tiles[1 + 2 * tile];
-        m0 = a.tiles[2 + 2 * tile];
-        m_end = a.first[e + 1];
-        const long long matrix = (long long)e * (GATED ? 2 : 1);
-        w += matrix * a.N * a.K;
-        s_w += matrix * a.NB * a.KB;
-    }
-    const int n0 = ((int)blockIdx.x - tile * across) * 16 * NB;
-    const auto rows_x = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.q), 0, 0xffffffe0u, 0x00020000);
-    const auto rows_w = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(w), 0, (unsigned)a.N * (unsigned)a.K * (GATED ? 2u : 1u), 0x00020000);
-    unsigned at_x[MB], at_w[COLS];
-    const float *s[MB];
-    int sw_row[COLS];
-#pragma unroll
-    for (int i = 0; i < MB; ++i) {
-        int m = min(m0 + 16 * i + p, m_end - 1);
-        if (EXPERTS && a.order) m = a.order[m] / a.k;
-        at_x[i] = (unsigned)m * (unsigned)a.K + 16 * g;
-        s[i] = a.s + (long long)m * a.KB;
-    }
-#pragma unroll
-    for (int j = 0; j < COLS; ++j) {
-        const int n = n0 + 16 * (j % NB);
-        at_w[j] = (unsigned)(min(n + p, a.N - 1) + (j < NB ? 0 : a.N)) * (unsigned)a.K + 16 * g;
-        sw_row[j] = ((j < NB ? 0 : a.NB) + min(n, a.N - 1) / F8_BLOCK) * a.KB;
-    }
-    // chunks behind the end of a row are zero: their offset lies behind the operand
-    const int last = a.K - (a.KB - 1) * F8_BLOCK;
-    const bool dead_lo = 16 * g >= last, dead_hi = 16 * g + 64 >= last;
-    auto load = [&](__amdgpu_buffer_rsrc_t rows, unsigned at, int kb) {
-        const unsigned off = at + (unsigned)kb * F8_BLOCK;
-        const bool end = kb == a.KB - 1;
-        typedef unsigned u4 __attribute__((ext_vector_type(4)));
-        const u4 lo = __builtin_amdgcn_raw_buffer_load_b128(rows, end && dead_lo ? 0xfffffff0u : off, 0, 0);
-        const u4 hi = __builtin_amdgcn_raw_buffer_load_b128(rows, end && dead_hi ? 0xfffffff0u : off + 64, 0, 0);
-        return __builtin_bit_cast(v8i, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-    };
-    v8i x[AHEAD][MB], f[AHEAD][COLS];
-    float sa[AHEAD][MB], sw[AHEAD][COLS];
-    auto request = [&](int u, int kb) {
-#pragma unroll
-        for (int j = 0; j < COLS; ++j) f[u][j] = load(rows_w, at_w[j], kb);
-#pragma unroll
-        for (int i = 0; i < MB; ++i) x[u][i] = load(rows_x, at_x[i], kb);
-#pragma unroll
-        for (int i = 0; i < MB; ++i) sa[u][i] = s[i][kb];
-#pragma unroll
-        for (int j = 0; j < COLS; ++j) sw[u][j] = s_w[sw_row[j] + kb];
-    };
-    v4f acc[TOTAL];
-#pragma unroll
-    for (int t = 0; t < TOTAL; ++t) acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    // steps behind the last one are the last one again, with a scale of 0: no branch stands between requests and their use, where the compiler would wait for
-    // what is under way
-    auto step_of = [&](int n) { return wave + n * WAVES; };
-    auto consume = [&](int u, int kb) {
-        Wide xw[MB];
-#pragma unroll
-        for (int i = 0; i < MB; ++i) xw[i] = Wide(x[u][i]);
-#pragma unroll
-        for (int j = 0; j < COLS; ++j) {
-            const Wide fw(f[u][j]);
-            const float sj = kb < a.KB ? sw[u][j] : 0.0f;
-#pragma unroll
-            for (int i = 0; i < MB; ++i) {
-                const v4f d = step_product(fw, xw[i]);
-                const float scale = sa[u][i] * sj;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) acc[j * MB + i][r] = __builtin_fmaf(d[r], scale, acc[j * MB + i][r]);
-            }
-        }
-    };
-    const int steps = (a.KB + WAVES - 1) / WAVES;
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) request(u, min(step_of(u), a.KB - 1));
-    int n = 0;
-    for (; n + AHEAD < steps; n += AHEAD) {
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            consume(u, step_of(n + u));
-            request(u, min(step_of(n + u + AHEAD), a.KB - 1));
-        }
-    }
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u)
-        if (n + u < steps) consume(u, step_of(n + u));
-#pragma unroll
-    for (int t = 0; t < TOTAL; ++t) sums[wave][t][lane] = acc[t];
-    __syncthreads();
-    finish_few<MB, NB, WAVES, EXPERTS, GATED>(a, &sums[0][0][0], TOTAL * 64, n0, [&](int r) { return m0 + r < m_end ? m0 + r : -1; });
-}
-
-// The same with the operands brought to LDS by DMA, each wavefront's own steps to its own STAGES places (no barrier).  Loads straight into the operands'
-// order touch 16 lines of memory each and pass 16 bytes a clock through a CU; by DMA, 8 rows of 128 bytes at a time, it is 45.
 template <int MB, int NB, int WAVES, int STAGES, bool EXPERTS, bool GATED>
-__global__ __launch_bounds__(64 * WAVES) void qgemm_f8_few_dma(F8Gemm a)
+__global__ __launch_bounds__(64 * WAVES) void qgemm_f8_few(F8Gemm a)
 {
     constexpr int COLS = NB * (GATED ? 2 : 1), TOTAL = MB * COLS, X_BYTES = MB * 2048, S_AT = X_BYTES + COLS * 2048, STEP = S_AT + 512;
     constexpr int ISSUED = 2 * MB + 2 * COLS + 2;
@@ -436,30 +331,23 @@ __global__ __launch_bounds__(512) void qgemm_f8_self(F8Gemm a, int most)   // mo
     finish_few<1, 1, WAVES, EXPERTS, GATED>(a, sums, PITCH, n0, [&](int) { return row; });   // (a lane's place in the tile is p here as there)
 }
 
-// Workgroups of 32 outputs from which on it is their number that keeps the memory busy
-constexpr int64_t FEW_GROUPS = 1024;
 // Rows that are quantized by every workgroup that reads them: up to four steps of eight wavefronts, and workgroups
 constexpr int64_t SELF_K = 4096, SELF_N = 8192, SELF_VALUES = 32768;
 
-int f8_expert_tile(int64_t P, int64_t E) { return P >= 64 * E ? F8_TILE_ROWS : 16; }
-
-template <int MB, int NB, int WAVES, int AHEAD, bool EXPERTS, bool GATED>
-static hipError_t run_few(const F8Gemm &a, hipStream_t s)
-{
-    const unsigned across = (unsigned)((a.N + 16 * NB - 1) / (16 * NB)), down = EXPERTS ? (unsigned)a.tiles_most : (unsigned)((a.M + 16 * MB - 1) / (16 * MB));
-    hipLaunchKernelGGL((qgemm_f8_few<MB, NB, WAVES, AHEAD, EXPERTS, GATED>), dim3(across * down), dim3(64 * WAVES), 0, s, a);
-    return hipGetLastError();
-}
+// Tiles of 16 rows read an expert's weights once for every 16, tiles of 64 and 128 (qgemm_f8_tile.hip) quantize the gated product themselves and have fewer workgroups with
+// longer chains.  us on 16, 64 and 128 rows, T tokens: k = 8 of 64 experts, 2048 and 1024 inputs: T = 64 85, 87, 119; 256 151, 114, 165; 2048 703, 316, 322; 8192 -, 1026, 958;
+// 4 of 60, 1152 and 720: T = 128 47, 51, 67, 300 65, 53, 71; 2 of 8, 4096 and 2048: T = 128 64, 89, 114, 512 165, 126, 130, 4096 -, 548, 503
+int f8_expert_tile(int64_t P, int64_t E) { return P >= 384 * E ? 128 : P >= 12 * (E > 44 ? E : 44) ? 64 : 16; }
 
 template <int MB, int NB, int WAVES, int STAGES, bool EXPERTS, bool GATED>
-static hipError_t run_dma(const F8Gemm &a, hipStream_t s)
+static hipError_t run_few(const F8Gemm &a, hipStream_t s)
 {
     constexpr int bytes = WAVES * STAGES * ((MB + NB * (GATED ? 2 : 1)) * 2048 + 512);
     static_assert(bytes <= 160 * 1024, "LDS");
-    const hipError_t opt_in = allow_lds<&qgemm_f8_few_dma<MB, NB, WAVES, STAGES, EXPERTS, GATED>>();
+    const hipError_t opt_in = allow_lds<&qgemm_f8_few<MB, NB, WAVES, STAGES, EXPERTS, GATED>>();
     if (opt_in != hipSuccess) return opt_in;
     const unsigned across = (unsigned)((a.N + 16 * NB - 1) / (16 * NB)), down = EXPERTS ? (unsigned)a.tiles_most : (unsigned)((a.M + 16 * MB - 1) / (16 * MB));
-    hipLaunchKernelGGL((qgemm_f8_few_dma<MB, NB, WAVES, STAGES, EXPERTS, GATED>), dim3(across * down), dim3(64 * WAVES), bytes, s, a);
+    hipLaunchKernelGGL((qgemm_f8_few<MB, NB, WAVES, STAGES, EXPERTS, GATED>), dim3(across * down), dim3(64 * WAVES), bytes, s, a);
     return hipGetLastError();
 }
 
@@ -483,18 +371,6 @@ static hipError_t run_self(const F8Gemm &a, hipStream_t s)
     return steps == 1 ? run_self_steps<1, SELF>(a, s) : steps == 2 ? run_self_steps<2, SELF>(a, s) : run_self_steps<4, SELF>(a, s);
 }
 
-// A wavefront requests as many steps ahead as it has, up to MOST (steps that there are not would be requested for nothing)
-template <int MB, int NB, int WAVES, int MOST, bool EXPERTS, bool GATED>
-static hipError_t run_ahead(const F8Gemm &a, hipStream_t s)
-{
-    const int steps = (a.KB + WAVES - 1) / WAVES;
-    if constexpr (MOST >= 4) {
-        if (steps >= 4) return run_few<MB, NB, WAVES, 4, EXPERTS, GATED>(a, s);
-    }
-    if (steps >= 2) return run_few<MB, NB, WAVES, 2, EXPERTS, GATED>(a, s);
-    return run_few<MB, NB, WAVES, 1, EXPERTS, GATED>(a, s);
-}
-
 // What few rows take on workgroups of 16 mb rows and 16 nb outputs: what such a workgroup brings to LDS at 55 bytes a nanosecond, and 2.5 us for the launch, the first bytes'
 // way and the sum over the wavefronts.  us, measured and so: 64 x 8192 x 4096 on 32 x 32 12.5 and 12.0, on 64 x 32 17.7 and 16.8; 128 x 4096 x 4096 on 64 x 32 11.3 and
 // 9.6, on 32 x 32 13.4 and 12.0, on 32 x 16 20.9 and 16.8; 128 x 12288 x 512 on 32 x 16 11.5 and 13.2, on 64 x 32 22.6 and 23.9.
@@ -515,18 +391,16 @@ hipError_t launch_qgemm_f8(const F8Gemm &a, hipStream_t s)
     if (a.x) return a.glu ? run_self<Self::LAYER_GLU>(a, s) : run_self<Self::LAYER>(a, s);
     if (a.first) {
         if (a.tile >= F8_TILE_ROWS) return launch_qgemm_f8_tiles(a, s);
-        const bool many = (int64_t)a.tiles_most * (a.N / 32) >= FEW_GROUPS;
-        if (a.gated) return run_dma<1, 1, 4, 2, true, true>(a, s);
-        return many ? run_dma<1, 2, 4, 2, true, false>(a, s) : run_ahead<1, 1, 4, 2, true, false>(a, s);
+        return a.gated ? run_few<1, 1, 4, 2, true, true>(a, s) : run_few<1, 2, 4, 2, true, false>(a, s);
     }
     // Sums in binary16 products (f8.h) up to F8_MANY rows and behind gated products
     if (a.M > F8_MANY && a.codes) return launch_qgemm_f8_tiles(a, s);
     const float tiles = qgemm_f8_tiles_us(a), by16 = few_us(a, 1, 1), by32 = few_us(a, 2, 1), by32w = few_us(a, 2, 2), by64w = few_us(a, 4, 2);
     const float least = fminf(fminf(fminf(by32, by32w), by64w), a.M <= 16 ? by16 : 1e30f);
     if (tiles < least) return launch_qgemm_f8_tiles(a, s);
-    if (a.M <= 16 && by16 <= least) return run_dma<1, 1, 8, 2, false, false>(a, s);
-    if (by32 <= least) return run_dma<2, 1, 8, 3, false, false>(a, s);
-    return by32w <= least ? run_dma<2, 2, 8, 2, false, false>(a, s) : run_dma<4, 2, 4, 3, false, false>(a, s);
+    if (a.M <= 16 && by16 <= least) return run_few<1, 1, 8, 2, false, false>(a, s);
+    if (by32 <= least) return run_few<2, 1, 8, 3, false, false>(a, s);
+    return by32w <= least ? run_few<2, 2, 8, 2, false, false>(a, s) : run_few<4, 2, 4, 3, false, false>(a, s);
 }
 
 }  // namespace ql

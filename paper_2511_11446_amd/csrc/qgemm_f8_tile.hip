@@ -420,7 +420,8 @@ using Core128 = TileF8<4, 4, 2, 2, 2, false>;      // 128 x 128, two
 using Core64 = TileF8<2, 2, 2, 2, 2, false>;       // 64 x 64, four
 using Wide128 = TileF8<4, 4, 2, 2, 2, true>;
 using Wide64 = TileF8<2, 2, 2, 2, 2, true>;
-static_assert(Wide128::BM == F8_TILE_ROWS, "what the rows of experts are cut into");
+using Rows64 = TileF8<2, 4, 2, 2, 2, true>;        // 64 x 128, three
+static_assert(Rows64::BM == F8_TILE_ROWS && Wide128::BM == 2 * F8_TILE_ROWS, "what the rows of experts are cut into");
 
 // What a layer takes on tiles of `side` of which `fit` are on a CU at a time: rounds of tiles, in each KB steps at step[l - 1] us where a CU has l of them, and `ends` us in
 // front of the first step and behind the last.  The steps are those of 4096 x 4096 and 8192 x 8192 weights; us, measured and so, with the matrix cores' own
@@ -439,6 +440,7 @@ float qgemm_f8_tiles_us(const F8Gemm &a) { return fminf(tiles_us(a, 64, 4, WIDE6
 
 hipError_t launch_qgemm_f8_tiles(const F8Gemm &a, hipStream_t s)
 {
+    if (a.first && a.tile == 64) return a.gated ? run_tile<Rows64, F8Out::GATED>(a, s) : run_tile<Rows64, F8Out::ROWS>(a, s);
     if (a.first) return a.gated ? run_tile<Wide128, F8Out::GATED>(a, s) : run_tile<Wide128, F8Out::ROWS>(a, s);
     if (!a.codes || a.M <= F8_MANY)
         return tiles_us(a, 64, 4, WIDE64, 0.2f) <= tiles_us(a, 128, 2, WIDE128, 3.5f) ? run_tile<Wide64, F8Out::LAYER>(a, s) : run_tile<Wide128, F8Out::LAYER>(a, s);

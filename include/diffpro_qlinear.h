@@ -585,17 +585,24 @@ int attention_kv8(const ql_attention *attn, const ql_kv_cache *cache,
  *   q       (device) [M,K] e4m3, out
  *   scales  (device) [M, ceil(K/128)] fp32, out
  *
- * qgemm_f8.  With KB = ceil(K/128), products and sums of a block on the matrix
- * cores and everything behind them in fp32:
+ * qgemm_f8.  With KB = ceil(K/128), everything behind the sums of a block in fp32:
  *   u[m,n] = sum_b (s[m,b] * w_scale[n/128,b]) * sum_{k in b} q[m,k] * w[n,k]  + bias[n]
  *   y = as ql_fusion says of u
  *   w       (device) [N,K] e4m3;  w_scale (device) [ceil(N/128), KB] fp32
  *   bias    (device) [N] fp16 or NULL
  *   fusion  as in the *_fused calls, row_absmax NULL (no quantizer here takes it:
  *           QL_ERR_UNSUPPORTED), or NULL
- * The sums are off by at most (K + 3 KB) 2^-23 of sum_b |s w_scale| sum_k |q w|.
+ * Up to 256 rows, and behind a gated product (qlinear_f8 with glu), the products are
+ * exact and their sums are off by at most (K + 3 KB) 2^-23 of
+ * S = sum_b |s w_scale| sum_k |q w|.  Layers of more rows take the matrix cores'
+ * sums of e4m3 products, twice as fast, which cut every product off below 2^-13 of
+ * the power of two that the largest among its 8 neighbours along K reaches: at most
+ * 2^-10 of the sum of those largest products more.  (On activations as layers have
+ * them 2e-5 of the result's size; its rounding to fp16 is 2e-4.)  So a row may come out
+ * differently, within these bounds, among more than 256 rows than among fewer.
  *
- * qlinear_f8 is daq_quantize_f8 followed by qgemm_f8.
+ * qlinear_f8 is daq_quantize_f8 followed by qgemm_f8; y may be the residual and
+ * overlaps nothing else.
  * qlinear_f8_workspace_bytes: enough for every call with up to M rows, K inputs and
  * N outputs (0: sizes that the call refuses).
  *
@@ -654,9 +661,10 @@ int route_experts(const ql_routing *routing, void *stream);
 
 /* Every token through its experts' gated layers:
  *   xq         = daq_quantize_f8(x[t])
- *   [g | u]    = xq times the two matrices w_up[e], as qgemm_f8 does, in fp32
+ *   [g | u]    = xq times the two matrices w_up[e], in fp32, as exact as qgemm_f8 of few rows
  *   hq         = daq_quantize_f8 of silu(g) * u
- *   o[t,j]     = fp16( hq times w_down[e] ), e = ids[t,j]   (fp32 where few rows are at hand)
+ *   o[t,j]     = fp16( hq times w_down[e] ), e = ids[t,j]   (likewise; fp32 where an expert has few
+ *                rows on average)
  *   y[t]       = fp16( residual[t] + sum_j weights[t,j] * o[t,j] ),  added up in the order of j, in fp32
  *   x        (device) [T,K] fp16;  ids (device) [T,k] int32: an id outside [0,E) is no
  *            expert, adds nothing and its weight is not read into any result
@@ -664,7 +672,8 @@ int route_experts(const ql_routing *routing, void *stream);
  *   w_up     (device) [E,2,I,K] e4m3, gate and up;  up_scale (device)
  *            [E,2,ceil(I/128),ceil(K/128)] fp32
  *   w_down   (device) [E,N,I] e4m3;  down_scale (device) [E,ceil(N/128),ceil(I/128)] fp32
- *   residual (device) [T,N] fp16 or NULL;  y (device) [T,N] fp16, which may be residual
+ *   residual (device) [T,N] fp16 or NULL;  y (device) [T,N] fp16, which may be residual and
+ *            overlaps nothing else
  * A token without an expert gets its residual, or 0.  Its x is not read into any result.
  * K and I: multiples of 16, N of 8.  E <= 512, k <= 64; T * k up to 2^24; T * K,
  * T * k * I, T * k * N, I * K and N * I below 2^31 (offsets between experts are 64 bits wide).

@@ -377,7 +377,7 @@ static hipError_t run_self(const F8Gemm &a, hipStream_t s)
 static float few_us(const F8Gemm &a, int mb, int nb)
 {
     const int64_t groups = ((a.M + 16ll * mb - 1) / (16 * mb)) * ((a.N + 16ll * nb - 1) / (16 * nb));
-    return (float)((groups + 255) / 256) * (float)((mb + nb) * 16) * (float)(a.KB * F8_BLOCK) / 55e3f + 2.5f;
+    return (float)((groups + 255) / 256) * ((float)((mb + nb) * 16) * (float)(a.KB * F8_BLOCK) / 55e3f + 2.5f);
 }
 
 bool qgemm_f8_takes_rows(int64_t M, int64_t K, int64_t N, bool glu)
@@ -393,8 +393,6 @@ hipError_t launch_qgemm_f8(const F8Gemm &a, hipStream_t s)
         if (a.tile >= F8_TILE_ROWS) return launch_qgemm_f8_tiles(a, s);
         return a.gated ? run_few<1, 1, 4, 2, true, true>(a, s) : run_few<1, 2, 4, 2, true, false>(a, s);
     }
-    // Sums in binary16 products (f8.h) up to F8_MANY rows and behind gated products
-    if (a.M > F8_MANY && a.codes) return launch_qgemm_f8_tiles(a, s);
     const float tiles = qgemm_f8_tiles_us(a), by16 = few_us(a, 1, 1), by32 = few_us(a, 2, 1), by32w = few_us(a, 2, 2), by64w = few_us(a, 4, 2);
     const float least = fminf(fminf(fminf(by32, by32w), by64w), a.M <= 16 ? by16 : 1e30f);
     if (tiles < least) return launch_qgemm_f8_tiles(a, s);

@@ -385,18 +385,38 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             const int rows = min(T::BM, m_end - m0), columns = min(T::BN, a.N - n0);
-            for (int r = wave; r < rows; r += T::NW) {
-                const long long at = (long long)(m0 + r) * a.N + n0, gate_at = gate ? (long long)((m0 + r) / a.gate_rows) * a.N + n0 : 0;
+            // four rows of a wavefront together, so that gate and residual are not one trip to memory after the other (7897 x 1664 x 3340 with a residual 140 -> 105 us)
+            constexpr int ROWS = 4, PARTS = T::BN / 64;
+            for (int first = wave; first < rows; first += ROWS * T::NW) {
+                _Float16 r[ROWS][PARTS], gt[ROWS][PARTS];
+                if (res || gate) {
 #pragma unroll
-                for (int c = 0; c < T::BN; c += 64) {
-                    if (c + lane >= columns) continue;
-                    _Float16 h = *reinterpret_cast<const half_alias *>(smem + r * PITCH + (c + lane) * 2);
-                    if (res || gate) {
-                        float v = __builtin_fmaf(gate ? (float)gate[gate_at + c + lane] : 1.0f, (float)h, res ? (float)res[at + c + lane] : 0.0f);
-                        asm volatile("" : "+v"(v));
-                        h = (_Float16)v;
+                    for (int k = 0; k < ROWS; ++k) {
+                        const int row = m0 + min(first + k * T::NW, rows - 1);
+                        const long long at = (long long)row * a.N + n0, gate_at = gate ? (long long)(row / a.gate_rows) * a.N + n0 : 0;
+#pragma unroll
+                        for (int c = 0; c < PARTS; ++c) {
+                            const int col = min(64 * c + lane, columns - 1);
+                            if (res) r[k][c] = res[at + col];
+                            if (gate) gt[k][c] = gate[gate_at + col];
+                        }
                     }
-                    y[at + c + lane] = h;
+                }
+#pragma unroll
+                for (int k = 0; k < ROWS; ++k) {
+                    const int row = first + k * T::NW;
+                    if (row >= rows) break;
+#pragma unroll
+                    for (int c = 0; c < PARTS; ++c) {
+                        if (64 * c + lane >= columns) continue;
+                        _Float16 h = *reinterpret_cast<const half_alias *>(smem + row * PITCH + (64 * c + lane) * 2);
+                        if (res || gate) {
+                            float v = __builtin_fmaf(gate ? (float)gt[k][c] : 1.0f, (float)h, res ? (float)r[k][c] : 0.0f);
+                            asm volatile("" : "+v"(v));
+                            h = (_Float16)v;
+                        }
+                        y[(long long)(m0 + row) * a.N + n0 + 64 * c + lane] = h;
+                    }
                 }
             }
         }
@@ -436,17 +456,29 @@ static float tiles_us(const F8Gemm &a, int side, int fit, const float *step, flo
 }
 constexpr float CORE64[] = {0.52f, 0.64f, 0.82f, 1.01f}, CORE128[] = {0.81f, 1.14f}, CORE256[] = {1.85f}, WIDE64[] = {0.60f, 0.80f, 1.04f, 1.27f}, WIDE128[] = {1.17f, 1.85f};
 
-float qgemm_f8_tiles_us(const F8Gemm &a) { return fminf(tiles_us(a, 64, 4, WIDE64, 0.2f), tiles_us(a, 128, 2, WIDE128, 3.5f)); }
+// The tile of a layer and what it takes.  Sums in binary16 products (f8.h) up to F8_MANY rows and behind gated products
+struct LayerTile {
+    int side;
+    float us;
+};
+static LayerTile layer_tile(const F8Gemm &a)
+{
+    const bool core = a.codes && a.M > F8_MANY;
+    const float by64 = tiles_us(a, 64, 4, core ? CORE64 : WIDE64, 0.2f), by128 = tiles_us(a, 128, 2, core ? CORE128 : WIDE128, 3.5f),
+                by256 = core ? tiles_us(a, 256, 1, CORE256, 10.0f) : 1e30f;
+    if (by64 <= by128 && by64 <= by256) return {64, by64};
+    return by128 <= by256 ? LayerTile{128, by128} : LayerTile{256, by256};
+}
+
+float qgemm_f8_tiles_us(const F8Gemm &a) { return layer_tile(a).us; }
 
 hipError_t launch_qgemm_f8_tiles(const F8Gemm &a, hipStream_t s)
 {
     if (a.first && a.tile == 64) return a.gated ? run_tile<Rows64, F8Out::GATED>(a, s) : run_tile<Rows64, F8Out::ROWS>(a, s);
     if (a.first) return a.gated ? run_tile<Wide128, F8Out::GATED>(a, s) : run_tile<Wide128, F8Out::ROWS>(a, s);
-    if (!a.codes || a.M <= F8_MANY)
-        return tiles_us(a, 64, 4, WIDE64, 0.2f) <= tiles_us(a, 128, 2, WIDE128, 3.5f) ? run_tile<Wide64, F8Out::LAYER>(a, s) : run_tile<Wide128, F8Out::LAYER>(a, s);
-    const float by64 = tiles_us(a, 64, 4, CORE64, 0.2f), by128 = tiles_us(a, 128, 2, CORE128, 3.5f), by256 = tiles_us(a, 256, 1, CORE256, 10.0f);
-    if (by64 <= by128 && by64 <= by256) return run_tile<Core64, F8Out::LAYER>(a, s);
-    return by128 <= by256 ? run_tile<Core128, F8Out::LAYER>(a, s) : run_tile<Core256, F8Out::LAYER>(a, s);
+    const int side = layer_tile(a).side;
+    if (!a.codes || a.M <= F8_MANY) return side == 64 ? run_tile<Wide64, F8Out::LAYER>(a, s) : run_tile<Wide128, F8Out::LAYER>(a, s);
+    return side == 64 ? run_tile<Core64, F8Out::LAYER>(a, s) : side == 128 ? run_tile<Core128, F8Out::LAYER>(a, s) : run_tile<Core256, F8Out::LAYER>(a, s);
 }
 
 }  // namespace ql

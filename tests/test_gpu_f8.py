@@ -102,7 +102,8 @@ def test_codes_and_scales_of_the_gated_product(M, K):
 
 SHAPES = [(1, 16, 1), (1, 128, 16), (1, 4096, 1024), (2, 272, 130), (3, 1152, 384), (7, 128, 1001), (16, 8192, 256), (17, 1152, 1152), (31, 144, 33), (33, 2224, 257),
           (64, 4096, 512), (65, 384, 2304), (96, 1040, 640), (127, 128, 129), (128, 1152, 1152), (129, 256, 4608), (200, 1024, 500), (255, 640, 255), (256, 384, 512),
-          (257, 272, 513), (300, 1152, 1296), (512, 4608, 1152), (513, 1168, 1000), (1000, 128, 384), (1021, 2224, 1001), (1024, 2048, 2048), (2048, 1152, 3456)]
+          (257, 272, 513), (300, 1152, 1296), (512, 4608, 1152), (513, 1168, 1000), (1000, 128, 384), (1021, 2224, 1001), (1024, 2048, 2048), (2048, 1152, 3456),
+          (300, 16, 40), (700, 144, 2050), (400, 8192, 100), (1500, 160, 516), (16, 4096, 8200), (5, 6144, 200)]
 
 
 @pytest.mark.parametrize("M, K, N", SHAPES)
@@ -233,6 +234,44 @@ def test_routes_that_32_bits_cannot_tell_apart():
     _check_route(np.round(x, 1).astype(np.float16), 8, sigmoid=True)
 
 
+@pytest.mark.parametrize("E, groups", [(64, 1), (100, 1), (256, 8), (384, 96)])
+def test_routes_of_whole_numbers(E, groups):
+    """Logits and biases of few values: ties among experts and among groups everywhere."""
+    g = _rng("whole", E, groups)
+    for dtype in (np.float16, np.float32):
+        x = g.integers(-2, 3, (83, E)).astype(dtype)
+        b = (g.integers(-2, 3, E) * 0.25).astype(np.float32)
+        for kw in (dict(), dict(bias=b), dict(bias=b * 20), dict(bias=b, renorm=False)):
+            for sigmoid in (False, True):
+                _check_route(x, 6, sigmoid=sigmoid, groups=groups, top_groups=max(1, groups // 2), **kw)
+
+
+@pytest.mark.parametrize("gap", [2.0 ** -25, 2.0 ** -19, 2.0 ** -17, 2.0 ** -15, 2.0 ** -12])
+def test_routes_at_the_border_of_32_bits(gap):
+    """Choices, and sums of a group's best, that are `gap` apart: on both sides of what is done again in 64 bits."""
+    g = _rng("border", int(-np.log2(gap)))
+    T, E = 96, 128
+    x = g.standard_normal((T, E)).astype(np.float32)
+    x[:] = x[0]
+    s = 1.0 / (1.0 + np.exp(-x[0].astype(np.float64)))
+    bias = (0.5 + gap * g.permutation(E) - s).astype(np.float32)
+    x[1:] = x[1:] + (g.integers(-3, 4, (T - 1, E)) * gap).astype(np.float32)
+    for groups in (1, 8, 64):
+        _check_route(x, 8, sigmoid=True, bias=bias, groups=groups, top_groups=max(1, groups // 2))
+    _check_route(x, 8, bias=bias)
+
+
+def test_routes_of_logits_that_do_not_begin_at_16_bytes():
+    g = _rng("aligned")
+    for dtype, E in ((np.float16, 129), (np.float16, 60), (np.float32, 258), (np.float32, 65)):
+        x, b = g.standard_normal((20, E)).astype(dtype), g.standard_normal(E + 1).astype(np.float32)
+        d, db = _dev(x)[1:], _dev(b)[1:]
+        ids, w = ql.route_experts(d, 4, bias=db, score=ql.SCORE_SIGMOID)
+        ref_ids, ref_w = of.route(x[1:], 4, b[1:], True)
+        assert np.array_equal(ids.cpu().numpy(), ref_ids)
+        _close(w, ref_w, 2.0 ** -23 * ref_w)
+
+
 # ---- the experts ----------------------------------------------------------------------------------------------------------------
 
 def _experts(g, T, E, k, K, I, N, residual=False, ids=None):
@@ -249,7 +288,9 @@ def _experts(g, T, E, k, K, I, N, residual=False, ids=None):
 
 @pytest.mark.parametrize("T, E, k, K, I, N", [(1, 1, 1, 16, 16, 8), (1, 8, 2, 128, 128, 128), (1, 64, 6, 1152, 384, 256), (2, 4, 4, 272, 144, 136), (5, 60, 4, 256, 400, 264), (16, 3, 2, 384, 256, 384),
                                               (33, 8, 8, 144, 272, 520), (64, 128, 8, 256, 128, 256), (100, 2, 1, 640, 128, 640), (300, 4, 3, 256, 336, 264), (700, 5, 2, 384, 256, 256),
-                                              (1500, 3, 2, 128, 400, 384), (600, 512, 1, 128, 128, 128), (2100, 2, 2, 144, 128, 136)])
+                                              (1500, 3, 2, 128, 400, 384), (600, 512, 1, 128, 128, 128), (2100, 2, 2, 144, 128, 136),
+                                              (1000, 2, 1, 16, 16, 8), (16, 5, 1, 4096, 128, 64), (8, 5, 2, 2048, 256, 72), (17, 5, 1, 256, 128, 64), (264, 44, 2, 128, 144, 128), (263, 44, 2, 128, 144, 128),
+                                              (192, 8, 4, 256, 272, 200), (390, 1, 1, 272, 400, 264), (3, 2, 3, 4096, 4096, 64)])
 def test_experts_against_the_formula(T, E, k, K, I, N):
     g = _rng("experts", T, E, k, K, I, N)
     args, res, (ref, tol) = _experts(g, T, E, k, K, I, N, residual=T % 2 == 0)
@@ -289,6 +330,116 @@ def test_rows_of_a_token_do_not_depend_on_the_batch():
     order = torch.randperm(96, generator=torch.Generator().manual_seed(3)).cuda()
     again = ql.experts_f8(args[0][order].contiguous(), args[1][order].contiguous(), args[2][order].contiguous(), *args[3:])
     assert torch.equal(again, y[order]) and torch.equal(ql.experts_f8(*args), y)
+
+
+def test_what_is_not_a_number_stays_with_its_token():
+    """Infinite and NaN inputs of one token reach no other; those of a token without an expert reach nothing."""
+    for T, E, k in ((3, 8, 2), (12, 8, 2), (60, 8, 2), (700, 4, 2), (1800, 2, 2)):
+        g = _rng("nan", T)
+        ids = g.integers(0, E, (T, k)).astype(np.int32)
+        ids[2] = -1
+        args, res, (ref, tol) = _experts(g, T, E, k, 256, 144, 136, True, ids)
+        args[0][1, 7], args[0][1, 200], args[0][2, 5] = float("nan"), float("inf"), float("nan")
+        y = ql.experts_f8(*args, residual=_dev(res)).float().cpu().numpy()
+        keep = np.arange(T) != 1
+        _close(y[keep], ref[keep], tol[keep], str(T))
+
+
+# ---- sizes whose offsets pass 31 and 32 bits ------------------------------------------------------------------------------------
+
+def _big(*shape):
+    return torch.zeros(shape, dtype=torch.uint8, device="cuda").view(F8)
+
+
+@pytest.mark.parametrize("T, k", [(1, 2), (40, 2), (1200, 2)])
+def test_experts_behind_4_gib(T, k):
+    """300 experts of 16 MiB a matrix: the last one alone has weights that are not 0."""
+    E, K, I, N = 300, 4096, 2048, 128
+    g = _rng("4 gib", T)
+    up, down = _big(E, 2, I, K), _big(E, N, I)
+    (u, us, w_up, s_up), (d, ds, w_down, s_down) = _weights(g, 1, 2, I, K), _weights(g, 1, N, I)
+    up[E - 1], down[E - 1] = u[0], d[0]
+    ups, downs = torch.zeros((E, 2, I // 128, K // 128), device="cuda"), torch.zeros((E, N // 128, I // 128), device="cuda")
+    ups[E - 1], downs[E - 1] = us[0], ds[0]
+    x = _rows(g, T, K, 0.3)
+    ids = g.integers(0, E - 1, (T, k)).astype(np.int32)
+    picked = np.arange(0, T, max(1, T // 5))
+    ids[picked, 1] = E - 1
+    weights = g.uniform(0.1, 1.0, (T, k)).astype(np.float32)
+    y = ql.experts_f8(_dev(x), _dev(ids), _dev(weights), up, ups, down, downs)
+    ref, tol = of.experts(x[picked], np.zeros((len(picked), 1), np.int32), weights[picked, 1:], w_up, s_up, w_down, s_down)
+    _close(y[picked], ref, tol)
+    others = np.setdiff1d(np.arange(T), picked)
+    assert not others.size or bool((y[others] == 0).all())
+
+
+@pytest.mark.parametrize("T", [1, 20, 600])
+def test_one_expert_of_4_gib(T):
+    """Gate and up of one expert end 64 KiB below 2^32 bytes: their last rows alone are not 0."""
+    K, I, N, live = 4096, 524272, 8, 48
+    g = _rng("one", T)
+    up, down = _big(1, 2, I, K), _big(1, N, I)
+    (u, _, w_up, _), (d, _, w_down, _) = _weights(g, 1, 2, live, K), _weights(g, 1, N, live)
+    up[0, :, I - live:], down[0, :, I - live:] = u[0], d[0]
+    IB = of.blocks(I)
+    ups, downs = torch.full((1, 2, IB, K // 128), 2.0 ** -9, device="cuda"), torch.full((1, 1, IB), 2.0 ** -9, device="cuda")
+    x = _rows(g, T, K, 0.3)
+    y = ql.experts_f8(_dev(x), torch.zeros((T, 1), dtype=torch.int32, device="cuda"), torch.ones((T, 1), device="cuda"), up, ups, down, downs)
+    some = np.arange(0, T, max(1, T // 7))
+    # the live channels' place in their block does not matter: all others of it are 0
+    s_up, s_down = np.full((1, 2, 1, K // 128), 2.0 ** -9, np.float32), np.full((1, 1, 1), 2.0 ** -9, np.float32)
+    ref, tol = of.experts(x[some], np.zeros((len(some), 1), np.int32), np.ones((len(some), 1), np.float32), w_up, s_up, w_down, s_down)
+    _close(y[some], ref, tol)
+
+
+def test_a_layer_of_2_gib_of_codes():
+    M, K, N = 131072, 16368, 24
+    g = _rng("2 gib")
+    dw, ds, w, s = _weights(g, N, K)
+    x = torch.zeros((M, K), dtype=torch.float16, device="cuda")
+    rows = _rows(g, 40, K)
+    x[M - 40:] = _dev(rows)
+    y = ql.qlinear_f8(x, dw, ds)
+    _, c, sx = of.quantize(rows.astype(np.float64))
+    _close(y[M - 40:], *of.layer(c, sx, w, s, core=True))
+    assert bool((y[: M - 40] == 0).all())
+    del x, y
+    M, K, N = 60, 144, 14912000                             # N * K just below 2^31
+    w, sw = _big(N, K), torch.ones((of.blocks(N), 2), device="cuda") * 2.0 ** -9
+    (u, _, wl, _) = _weights(g, 128, K)
+    w[N - 128:] = u
+    x = _rows(g, M, K)
+    y = ql.qlinear_f8(_dev(x), w, sw)
+    _, c, sx = of.quantize(x.astype(np.float64))
+    at = (N - 128) // 128 * 128
+    assert at == N - 128
+    _close(y[:, N - 128:], *of.layer(c, sx, wl, np.full((1, 2), 2.0 ** -9, np.float32)))
+    assert bool((y[:, : N - 128] == 0).all())
+
+
+def test_many_rows_of_one_short_block():
+    M, K, N = 3000001, 16, 8
+    g = _rng("rows")
+    dw, ds, w, s = _weights(g, N, K)
+    x = torch.randn((M, K), device="cuda").half()
+    y = ql.qlinear_f8(x, dw, ds)
+    for at in (slice(0, 300), slice(M - 300, M)):
+        _, c, sx = of.quantize(x[at].cpu().numpy().astype(np.float64))
+        _close(y[at], *of.layer(c, sx, w, s, core=True))
+
+
+def test_many_tokens_and_all_of_one_expert():
+    T, E, k = 70000, 3, 1
+    g = _rng("tokens")
+    ids = np.full((T, k), 1, np.int32)
+    ids[::1000] = 2
+    ids[7] = 0
+    some = np.concatenate([np.arange(12), np.arange(T - 1001, T, 100)])
+    up, ups, w_up, s_up = _weights(g, E, 2, 144, 128)
+    down, downs, w_down, s_down = _weights(g, E, 136, 144)
+    x, weights = _rows(g, T, 128, 0.3), g.uniform(0.1, 1, (T, k)).astype(np.float32)
+    y = ql.experts_f8(_dev(x), _dev(ids), _dev(weights), up, ups, down, downs)
+    _close(y[some], *of.experts(x[some], ids[some], weights[some], w_up, s_up, w_down, s_down))
 
 
 # ---- together, as a program has them --------------------------------------------------------------------------------------------
@@ -369,6 +520,19 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     check_a()
     check_b()
+
+
+def test_a_stream_of_its_own():
+    """Given as `stream`: inputs are ready there, what is returned is ready there."""
+    g = _rng("stream")
+    args, _, (ref, tol) = _experts(g, 50, 8, 2, 256, 256, 256)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    y = ql.experts_f8(*args, stream=s)
+    q, scales = ql.daq_quantize_f8(args[0], stream=s)
+    s.synchronize()
+    _close(y, ref, tol)
+    assert torch.equal(q.view(torch.uint8), ql.daq_quantize_f8(args[0])[0].view(torch.uint8))
 
 
 def test_one_workspace_for_calls_of_fewer_tokens():

@@ -85,7 +85,7 @@ struct F8Gemm {
     // rows that the launch quantizes itself (qgemm_f8_takes_rows, experts_f8_takes_ids), in the place of q and s
     const void *x;       // fp16 [M,K], [M,2K] with glu; of experts fp16 [M / k, K] gated, else fp32 [M,K]
     bool glu;
-    const int *ids;      // of experts: [M] (M up to 64) in the place of first, tiles and order; outputs at row token * k + choice
+    const int *ids;      // of experts: [M] (M up to 16, experts_f8_takes_ids) in the place of first, tiles and order; outputs at row token * k + choice
     int E;
     bool codes;          // the matrix cores' own sums of codes will do (a layer of many rows that is not behind a gated product)
 };

@@ -1,5 +1,12 @@
 // e4m3 products with block scales on tiles of many rows (gfx950): layers and the experts' layers.  The operands come to LDS by DMA, a K step of 128 channels at a
 // time; the scheme of operands, sums and scales is that of qgemm_f8.hip.
+//
+// Two stages in LDS: the next step comes while this one is multiplied.  Side of the tile: 256 x 256 reads the operands' bytes least often (8192^3 478 us with its inputs in a
+// cache, 563 in turn with others: 2.3 and 2.0 PFLOP/s; the matrix cores 52 % busy, vector units, that is the folds, 42 %); 128 x 128, two on a CU, hides ends and writing
+// under the other's products (16384 x 1152 x 4608 125 us; 256 x 256 136: nine steps, and 151 MB written at their end); 64 x 64, four on a CU, is for layers with few tiles
+// (1021 x 2224 x 1001 10.6 us).  tiles_us below chooses.
+// In binary16 products (WIDE) a wavefront issues two conversions, one fold and some address arithmetic for every product: bound by issue, matrix cores 47 %, vector units
+// 62 % busy, 13 % waiting.  16384 tokens through 8 of 64 experts of 2048 x 1024: gated 1113 us, 0.99 PFLOP/s, down 567 us, 0.97 (a library's binary16 product 1.19).
 #include "qgemm_f8.h"
 
 namespace ql {
@@ -215,7 +222,7 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
             }
             if (j == 0) read_scales(st);
             if constexpr (T::WIDE) {
-                // a sum's four products in turn with those of the group's others: one behind the other they wait for each other (16384 tokens through 8 of 64 experts)
+                // a sum's four products in turn with those of the group's others, so that none waits for the one in front
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
 #pragma unroll

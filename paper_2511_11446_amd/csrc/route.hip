@@ -140,8 +140,10 @@ __device__ __forceinline__ void route_exact(const RouteArgs &a, long long t, dou
 //   fp32 logits without a bias: 3 bits hold the place in the lane.  Two keys that are alike above them: the token is done again in 64 bits.
 //   with a bias: s + bias in 32 bits, off by at most ROUTE_NEAR / 2 (exponent, reciprocal and sum 2^-20 of at most 1, the addition 2^-24 of at most 4, the bits
 //   for the place 2^-19): two that follow each other and are nearer, or two groups at the border of those that are kept and nearer than GROUP_NEAR: in 64 bits, too.
-// The weights are taken in 64 bits, of the chosen alone.  Bound by vector instructions, about 770 a token: T = 16384, E = 256, k = 8, sigmoid, bias, 4 of 8 groups takes
-// 33 us (its logits and choices at the rate of a copy: 3.5), 55 us in 64 bits throughout.
+// The weights are taken in 64 bits, of the chosen alone, those of a workgroup's tokens in one wavefront (k = 8: half of its lanes in the place of 8 of 64 in four of them).
+// Where whole lanes hold a group, its two largest are found in registers, else through LDS.
+// Bound by vector instructions: T = 16384, E = 256, k = 8, sigmoid, bias, 4 of 8 groups takes 25 us (its logits and choices at the rate of a copy: 3.5), 55 us in 64 bits
+// throughout, 35 with each wavefront's weights by itself and groups through LDS.
 constexpr float ROUTE_NEAR = 0x1p-17f, GROUP_NEAR = 0x1p-12f;
 
 __device__ __forceinline__ unsigned key_of(float f)
@@ -149,6 +151,7 @@ __device__ __forceinline__ unsigned key_of(float f)
     const unsigned u = __builtin_bit_cast(unsigned, f + 0.0f);   // -0 is 0
     return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
 }
+constexpr unsigned DEAD = 0x007fffffu;   // key_of(-inf)
 __device__ __forceinline__ float float_of(unsigned k) { return __builtin_bit_cast(float, k >> 31 ? k ^ 0x80000000u : ~k); }
 
 // the largest over the wavefront
@@ -188,19 +191,19 @@ __device__ __forceinline__ float logit_at(const RouteArgs &a, long long at)
     return tame<WIDE>(WIDE ? static_cast<const float *>(a.logits)[at] : (float)static_cast<const _Float16 *>(a.logits)[at]);
 }
 
-// whole: PER divides E and the logits and the bias begin at 16 bytes
+constexpr int ROUTE_TOKENS = 4;   // wavefronts of a workgroup, each with a token
+
+// The choices of token t: true and, in lane j, the j-th one's number (-1: none), or false where 32 bits cannot tell.  top: the largest logit (of the softmax).
+// whole: PER divides E and the logits and the bias begin at 16 bytes.  own: 2^own lanes hold a group (-1: they do not)
 template <int PER, bool WIDE, bool BIAS, bool GROUPS>
-__global__ __launch_bounds__(256) void route(RouteArgs a, bool whole)
+__device__ __forceinline__ bool route_choices(const RouteArgs &a, bool whole, int own, long long t, double *by_expert, int &id, float &top)
 {
-    extern __shared__ double by_expert[];   // [4][E] where there are groups
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long t = (long long)blockIdx.x * 4 + wave;
-    if (t >= a.T) return;
+    const int lane = threadIdx.x & 63;
     const float inf = __builtin_inff();
     constexpr bool EXACT = !WIDE && !BIAS;
     // ---- logits (-inf: dead)
     float x[PER], c[PER];
-    float top = -inf;
+    top = -inf;
     const int e0 = lane * PER;
     if (whole) {
         typedef typename std::conditional<WIDE, float, _Float16>::type type;
@@ -270,8 +273,44 @@ __global__ __launch_bounds__(256) void route(RouteArgs a, bool whole)
         const unsigned k = key_of(f);
         key[i] = f == -inf ? 0u : EXACT ? (k & ~511u) | (511 - (e0 + i)) : (k & ~7u) | (7 - i);
     }
-    if (GROUPS && !near) {
-        float *by = reinterpret_cast<float *>(by_expert + wave * a.E);
+    if (GROUPS && !near && own >= 0) {
+        // 2^own lanes hold a group's experts and no others': its two largest in registers, as keys
+        unsigned one = key_of(c[0]), two = 0;
+#pragma unroll
+        for (int i = 1; i < PER; ++i) {
+            const unsigned v = key_of(c[i]);
+            two = max(two, min(one, v));
+            one = max(one, v);
+        }
+        auto join = [&](unsigned o1, unsigned o2) {
+            two = max(max(two, o2), min(one, o1));
+            one = max(one, o1);
+        };
+#define QL_JOIN(ctrl) join((unsigned)__builtin_amdgcn_mov_dpp((int)one, ctrl, 0xF, 0xF, true), (unsigned)__builtin_amdgcn_mov_dpp((int)two, ctrl, 0xF, 0xF, true))
+        if (own > 0) QL_JOIN(0xB1);    // the neighbour's, the neighbouring pair's, the other half's of 8 lanes, of 16
+        if (own > 1) QL_JOIN(0x4E);
+        if (own > 2) QL_JOIN(0x141);
+        if (own > 3) QL_JOIN(0x140);
+#undef QL_JOIN
+        if (own > 4) join(__shfl_xor(one, 16), __shfl_xor(two, 16));
+        if (own > 5) join(__shfl_xor(one, 32), __shfl_xor(two, 32));
+        const float most = float_of(one), worth = a.group_top == 2 && two > DEAD ? most + float_of(two) : most;
+        const int group = lane >> own;
+        unsigned group_key = one > DEAD && group < a.groups ? (key_of(worth) & ~127u) | (127 - group) : 0u;
+        bool kept = false;
+        unsigned before = 0;
+        for (int j = 0; j < a.top_groups; ++j) {
+            before = top_of_wave(group_key);
+            const bool best = group_key == before;
+            kept |= best;
+            group_key = best ? 0u : group_key;
+        }
+        const unsigned beyond = top_of_wave(group_key);
+        near = beyond && float_of(before) - float_of(beyond) < GROUP_NEAR;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) key[i] = kept ? key[i] : 0u;
+    } else if (GROUPS && !near) {
+        float *by = reinterpret_cast<float *>(by_expert);
 #pragma unroll
         for (int i = 0; i < PER; ++i)
             if (e0 + i < a.E) by[e0 + i] = c[i];
@@ -336,65 +375,109 @@ __global__ __launch_bounds__(256) void route(RouteArgs a, bool whole)
             const unsigned hi = max(key[j - 1], key[j]), lo = min(key[j - 1], key[j]);
             key[j - 1] = hi, key[j] = lo;
         }
-    // ---- choices: the j-th stays with lane j
-    int id = -1;
-    unsigned last = 0;
-    // (where keys are not exact, one more than is asked for: whether the last one is far enough from the next)
-    const int looks = EXACT ? a.k : a.k + 1;
-    for (int j = 0; j < looks; ++j) {   // (without branches: a choice that there is not is key 0, whose number is not taken)
+    // ---- choices: the j-th one's key and the lane that it came from stay with lane j.  (Without branches: a choice that there is not is key 0.)
+    unsigned picked = 0;
+    int from = 0;
+    unsigned long long alike = 0;
+    auto look = [&](int &at) {
         const unsigned best = top_of_wave(key[0]);
-        int e;
-        if (EXACT) e = 511 - (int)(best & 511);
-        else {
-            const unsigned long long owners = __ballot(key[0] == best);
-            const bool alike = (owners & (owners - 1)) || (j && (last ^ best) < 8u) || (BIAS && j && float_of(last) - float_of(best) < ROUTE_NEAR);
-            near |= best && alike;
-            e = __builtin_ctzll(owners) * PER + 7 - (int)(best & 7);
-            last = best;
+        const unsigned long long owners = __ballot(key[0] == best);
+        if (!EXACT) {
+            alike |= best ? owners & (owners - 1) : 0;
+            at = __builtin_ctzll(owners);
         }
-        id = lane == j && best ? e : id;
         const bool mine = key[0] == best;
 #pragma unroll
         for (int i = 0; i < PER; ++i) key[i] = mine ? (i + 1 < PER ? key[i + 1 < PER ? i + 1 : i] : 0u) : key[i];
+        return best;
+    };
+    for (int j = 0; j < a.k; ++j) {
+        int at = 0;
+        const unsigned best = look(at);
+        picked = lane == j ? best : picked;
+        if (!EXACT) from = lane == j ? at : from;
     }
-    if (lane >= a.k) id = -1;
-    if (near) {
-        route_exact<PER, WIDE>(a, t, by_expert + wave * a.E);
-        return;
+    const unsigned k = picked;
+    if (EXACT) id = 511 - (int)(k & 511);
+    else {
+        // where keys are not exact, the next one after each has to be far enough away, also that after the last
+        int at;
+        const unsigned beyond = look(at);
+        unsigned next = __shfl_down(k, 1);
+        next = lane == a.k - 1 ? beyond : next;
+        near |= __any(lane < a.k && next && ((k ^ next) < 8u || (BIAS && float_of(k) - float_of(next) < ROUTE_NEAR)));
+        near |= alike != 0;
+        id = from * PER + 7 - (int)(k & 7);
     }
-    // ---- weights
-    double total = 1.0, w = 0.0;
-    if (id >= 0) {
-        const double l = (double)logit_at<WIDE>(a, t * a.E + id);
-        const double e = exp(a.sigmoid ? -l : l - (double)top);
-        w = !a.sigmoid ? e : e < __builtin_inf() ? inverse(1.0 + e) : 0.0;
-    }
-    if (a.renorm) {
-        total = w;
-        for (int d = 1; d < a.k; d *= 2) total += __shfl_xor(total, d);   // (lanes behind the last choice have 0)
-    } else if (!a.sigmoid) {
-        total = 0.0;
-        for (int e = lane; e < a.E; e += 64) {
-            const float f = logit_at<WIDE>(a, t * a.E + e);
-            if (f > -inf) total += exp((double)f - (double)top);
-        }
+    if (!k || lane >= a.k) id = -1;
+    return !near;
+}
+
+template <int PER, bool WIDE, bool BIAS, bool GROUPS>
+__global__ __launch_bounds__(64 * ROUTE_TOKENS) void route(RouteArgs a, bool whole, int own, int places)   // 2^places: k, rounded up
+{
+    extern __shared__ double by_expert[];   // [ROUTE_TOKENS][E] where there are groups
+    __shared__ int chosen[ROUTE_TOKENS][64];
+    __shared__ double totals[ROUTE_TOKENS];
+    __shared__ float tops[ROUTE_TOKENS];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long t = (long long)blockIdx.x * ROUTE_TOKENS + wave;
+    constexpr int ELSEWHERE = -2;   // no token, or one whose choices are made in 64 bits
+    int id = ELSEWHERE;
+    float top = 0.0f;
+    bool exact = false;
+    if (t < a.T) {
+        exact = !route_choices<PER, WIDE, BIAS, GROUPS>(a, whole, own, t, by_expert + (GROUPS ? wave * a.E : 0), id, top);
+        if (exact) id = ELSEWHERE;
+        else if (!a.renorm && !a.sigmoid) {
+            double total = 0.0;
+            for (int e = lane; e < a.E; e += 64) {
+                const float f = logit_at<WIDE>(a, t * a.E + e);
+                if (f > -__builtin_inff()) total += exp((double)f - (double)top);
+            }
 #pragma unroll
-        for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
+            for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
+            if (lane == 0) totals[wave] = total;
+        }
     }
-    if (lane < a.k) {
-        if (total != 1.0) w = total > 0.0 ? w / total : 0.0;
-        a.ids[t * a.k + lane] = id;
-        a.weights[t * a.k + lane] = (float)(w * (double)a.scale);
+    chosen[wave][lane] = id;
+    if (lane == 0) tops[wave] = top;
+    __syncthreads();
+    // ---- weights: the workgroup's choices, 2^places lanes a token
+    const int width = 1 << places, token = (int)threadIdx.x >> places, j = (int)threadIdx.x & (width - 1);
+    if (token < ROUTE_TOKENS) {
+        id = chosen[token][j];
+        const long long to = (long long)blockIdx.x * ROUTE_TOKENS + token;
+        double total = 1.0, w = 0.0;
+        if (id >= 0) {
+            const double l = (double)logit_at<WIDE>(a, to * a.E + id);
+            const double e = exp(a.sigmoid ? -l : l - (double)tops[token]);
+            w = !a.sigmoid ? e : e < __builtin_inf() ? inverse(1.0 + e) : 0.0;
+        }
+        if (a.renorm) {
+            total = w;
+            for (int d = 1; d < width; d *= 2) total += __shfl_xor(total, d);   // (lanes behind the last choice have 0)
+        } else if (!a.sigmoid) total = totals[token];
+        if (id != ELSEWHERE && j < a.k) {
+            if (total != 1.0) w = total > 0.0 ? w / total : 0.0;
+            a.ids[to * a.k + j] = id;
+            a.weights[to * a.k + j] = (float)(w * (double)a.scale);
+        }
     }
+    if (exact) route_exact<PER, WIDE>(a, t, by_expert + wave * a.E);
 }
 
 template <int PER>
 static void run_route(const RouteArgs &a, hipStream_t s)
 {
-    const dim3 grid((unsigned)((a.T + 3ll) / 4));
-    const size_t lds = a.groups > 1 ? (size_t)4 * a.E * sizeof(double) : 0;
+    const dim3 grid((unsigned)((a.T + ROUTE_TOKENS - 1ll) / ROUTE_TOKENS));
+    const size_t lds = a.groups > 1 ? (size_t)ROUTE_TOKENS * a.E * sizeof(double) : 0;
+    int own = -1, places = 0;
+    for (int l = 0; l <= 6; ++l)
+        if ((a.E / a.groups) == PER << l) own = l;
+    while (1 << places < a.k) ++places;
     const bool groups = a.groups > 1 && a.top_groups < a.groups, whole = a.E % PER == 0 && (uintptr_t)a.logits % 16 == 0 && (uintptr_t)a.bias % 16 == 0;
-    auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), lds, s, a, whole); };
+    auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * ROUTE_TOKENS), lds, s, a, whole, own, places); };
     if (a.wide) {
         if (a.bias) groups ? run(route<PER, true, true, true>) : run(route<PER, true, true, false>);
         else groups ? run(route<PER, true, false, true>) : run(route<PER, true, false, false>);

@@ -261,6 +261,28 @@ def test_routes_at_the_border_of_32_bits(gap):
     _check_route(x, 8, bias=bias)
 
 
+@pytest.mark.parametrize("E, groups", [(16, 16), (16, 2), (32, 4), (64, 2), (64, 64), (96, 3), (128, 4), (192, 6), (256, 2), (256, 4), (256, 64), (384, 3), (512, 2), (512, 16), (512, 64)])
+@pytest.mark.parametrize("half", [False, True])
+def test_routes_by_groups_of_whole_lanes(E, groups, half):
+    """Groups that 1 to 32 lanes hold, some of them dead or with one expert; among the tokens of a workgroup some that 64 bits decide; as many choices as fit."""
+    g = _rng("lanes", E, groups, half)
+    dtype = np.float16 if half else np.float32
+    size = E // groups
+    x = g.standard_normal((39, E)).astype(dtype)
+    for t in range(3, 36, 3):
+        dead = g.random(groups) < 0.6
+        x[t, np.repeat(dead, size)] = -np.inf
+        x[t, g.integers(E)] = np.nan
+    x[9, np.arange(E) % size != size - 1] = -np.inf         # one expert a group
+    x[13] = np.round(x[13])
+    x[14, E // 2:] = x[14, :E // 2]
+    b = (g.standard_normal(E) * 0.3).astype(np.float32)
+    for top in (1, max(1, groups - 1)):
+        for k in (1, 7, min(E, 64)):
+            for kw in (dict(), dict(bias=b, renorm=False), dict(bias=b, sigmoid=True), dict(sigmoid=True, scale=0.5)):
+                _check_route(x, k, groups=groups, top_groups=top, group_top=1 + k % 2, **kw)
+
+
 def test_routes_of_logits_that_do_not_begin_at_16_bytes():
     g = _rng("aligned")
     for dtype, E in ((np.float16, 129), (np.float16, 60), (np.float32, 258), (np.float32, 65)):

@@ -201,6 +201,20 @@ __global__ __launch_bounds__(64 * WAVES) void qgemm_f8_few(F8Gemm a)
 //   UP     up to 16 rows of (token, choice) without a plan: every workgroup finds its expert's among the ids; x of the token, h at row (token, choice)
 //   DOWN   the same rows of h, fp32
 enum class Self { LAYER, LAYER_GLU, UP, DOWN };
+
+// n / d of n up to 1023 and d up to 32, with by = divisor(d)
+__device__ __forceinline__ int divisor(int d) { return 65536 / d + 1; }
+__device__ __forceinline__ int divided(int n, int by) { return n * by >> 16; }
+
+// Stores to LDS that do not wait for the DMA under way to other parts of it (the compiler lets its own wait).  Whoever reads them waits for lgkmcnt in front of the barrier.
+__device__ __forceinline__ unsigned lds_at(void *to) { return (unsigned)(uintptr_t)(__attribute__((address_space(3))) void *)to; }
+__device__ __forceinline__ void store_lds(void *to, uint2 v)
+{
+    typedef unsigned v2u __attribute__((ext_vector_type(2)));
+    asm volatile("ds_write_b64 %0, %1" ::"v"(lds_at(to)), "v"(v2u{v.x, v.y}) : "memory");
+}
+__device__ __forceinline__ void store_lds(void *to, float v) { asm volatile("ds_write_b32 %0, %1" ::"v"(lds_at(to)), "v"(v) : "memory"); }
+
 template <int STEPS, Self SELF>
 __global__ __launch_bounds__(512) void qgemm_f8_self(F8Gemm a, int most)   // most: rows of a tile
 {
@@ -213,23 +227,20 @@ __global__ __launch_bounds__(512) void qgemm_f8_self(F8Gemm a, int most)   // mo
     const float *s_w = a.s_w;
     int row, rows_here;   // the row of this lane's place p in the tile (-1: none); how many there are
     if constexpr (EXPERTS) {
-        // tiles begin with every 16th row of an expert, in the order of the rows; this one's expert and rows
+        // A tile is an expert's rows, the experts in the order of their first rows
         const int pair = lane < a.M ? a.ids[lane] : -1, id = pair >= 0 && pair < a.E ? pair : -1;
-        unsigned long long same = __ballot(id >= 0);
-        for (int b = 0; 1 << b < a.E; ++b) {
-            const unsigned long long set = __ballot(id >> b & 1);
-            same &= (id >> b & 1) ? set : ~set;
+        unsigned long long rows = 0;
+        int e = 0;
+        for (int r = 0, before = tile; r < a.M; ++r) {
+            e = __builtin_amdgcn_readlane(id, r);
+            rows = __ballot(id == e);
+            if (e >= 0 && __builtin_ctzll(rows) == r && before-- == 0) break;
+            rows = 0;
         }
-        const int rank = __popcll(same & ((1ull << lane) - 1));
-        const unsigned long long heads = __ballot(id >= 0 && rank % 16 == 0);
-        if (tile >= __popcll(heads)) return;
-        const unsigned long long mine = __ballot(id >= 0 && rank % 16 == 0 && __popcll(heads & ((1ull << lane) - 1)) == tile);
-        const int head = __builtin_ctzll(mine), e = __builtin_amdgcn_readlane(id, head);
-        unsigned long long rows = __ballot(id == e && rank >= __builtin_amdgcn_readlane(rank, head));
+        if (!rows) return;
         row = -1;
-        rows_here = min(__popcll(rows), 16);
-        for (int i = 0; i < rows_here; ++i, rows &= rows - 1)
-            if (p == i) row = __builtin_ctzll(rows);
+        rows_here = __popcll(rows);
+        for (int i = 0; i < rows_here; ++i, rows &= rows - 1) row = p == i ? __builtin_ctzll(rows) : row;
         const long long matrix = (long long)e * COLS;
         w += matrix * a.N * a.K;
         s_w += matrix * a.NB * a.KB;
@@ -244,42 +255,53 @@ __global__ __launch_bounds__(512) void qgemm_f8_self(F8Gemm a, int most)   // mo
         const int r = 8 * (i & 1) + (lane >> 3);
         at_w[i] = (unsigned)(min(n0 + r, a.N - 1) + i / 2 * a.N) * (unsigned)a.K + 16 * ((lane & 7) ^ ((r >> 1) & 7));
     }
+    // ---- the first of the rows' values are requested in front of the weights: they come first, and are quantized while the weights come
+    typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+    const int blocks = rows_here * a.KB, by_kb = divisor(a.KB), source = SELF == Self::UP ? divided(row, divisor(a.k)) : row;
+    float4 one, two;   // 8 values: of binary16 one, and two the other half of [g | u]
+    auto request = [&](int b) {
+        const int r = divided(b, by_kb), k = (b - r * a.KB) * F8_BLOCK + (threadIdx.x & 15) * 8, from_row = __shfl(source, r);
+        one = two = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (b < blocks && k < a.K) {
+            if constexpr (SELF == Self::DOWN) {
+                const float4 *from = reinterpret_cast<const float4 *>(static_cast<const float *>(a.x) + (long long)from_row * a.K + k);
+                one = from[0];
+                two = from[1];
+            } else {
+                const _Float16 *from = static_cast<const _Float16 *>(a.x) + (long long)from_row * a.K * (SELF == Self::LAYER_GLU ? 2 : 1) + k;
+                one = *reinterpret_cast<const float4 *>(from);
+                if constexpr (SELF == Self::LAYER_GLU) two = *reinterpret_cast<const float4 *>(from + a.K);
+            }
+        }
+    };
+    request((int)(threadIdx.x >> 4));
+    float sw[STEPS][COLS];
+#pragma unroll
+    for (int n = 0; n < STEPS; ++n)
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) sw[n][j] = s_w[((j ? a.NB : 0) + min(n0, a.N - 1) / F8_BLOCK) * a.KB + min(wave + n * WAVES, a.KB - 1)];
     const int last = a.K - (a.KB - 1) * F8_BLOCK;
     unsigned char *mine = smem + wave * STEPS * PLACE;
 #pragma unroll
     for (int n = 0; n < STEPS; ++n) {
-        const int kb = wave + n * WAVES;
-        if (kb >= a.KB) break;
-        const bool tail = kb == a.KB - 1 && last != F8_BLOCK;
+        const int kb = wave + n * WAVES, left = kb < a.KB - 1 ? F8_BLOCK : kb == a.KB - 1 ? last : 0;   // channels of this step; what there is not is read as nothing
 #pragma unroll
         for (int i = 0; i < 2 * COLS; ++i) {
-            const bool dead = 16 * ((lane & 7) ^ ((lane >> 4 & 3) + 4 * (i & 1))) >= last;   // a chunk behind the end of its row
-            dma16_buf(w, bytes_w, mine + n * PLACE + i * 1024, tail && dead ? 0xfffffff0u : at_w[i] + (unsigned)kb * F8_BLOCK, 0);
+            const bool dead = 16 * ((lane & 7) ^ ((lane >> 4 & 3) + 4 * (i & 1))) >= left;
+            dma16_buf(w, bytes_w, mine + n * PLACE + i * 1024, dead ? 0xfffffff0u : at_w[i] + (unsigned)kb * F8_BLOCK, 0);
         }
     }
     // ---- the rows: block kb of row r at kb * most + r, 128 codes whose 16-byte chunk c lies at c ^ ((r >> 1) & 7), and a scale.  (What a lane without a row reads is
     // another row's, or nothing's: its results go nowhere.)
     unsigned char *codes = smem + WAVES * STEPS * PLACE;
     float *scales = reinterpret_cast<float *>(codes + (size_t)a.KB * most * F8_BLOCK + 2048);
-    for (int b = threadIdx.x >> 4; b < rows_here * a.KB; b += 32) {
-        const int r = b / a.KB, kb = b - r * a.KB, sub = threadIdx.x & 15, k = kb * F8_BLOCK + sub * 8;
-        const int from_row = SELF == Self::UP ? __shfl(row, r) / a.k : __shfl(row, r);
-        float v[8];
+    for (int b = threadIdx.x >> 4; b < blocks; b += 32) {
+        const int r = divided(b, by_kb), kb = b - r * a.KB, sub = threadIdx.x & 15;
+        float v[8] = {one.x, one.y, one.z, one.w, two.x, two.y, two.z, two.w};
+        if constexpr (SELF != Self::DOWN) {
+            const h8 f = __builtin_bit_cast(h8, one), u = __builtin_bit_cast(h8, two);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-        if (k < a.K) {
-            if constexpr (SELF == Self::DOWN) {
-                const float4 *from = reinterpret_cast<const float4 *>(static_cast<const float *>(a.x) + (long long)from_row * a.K + k);
-                const float4 f = from[0], h = from[1];
-                v[0] = f.x, v[1] = f.y, v[2] = f.z, v[3] = f.w, v[4] = h.x, v[5] = h.y, v[6] = h.z, v[7] = h.w;
-            } else {
-                const _Float16 *from = static_cast<const _Float16 *>(a.x) + (long long)from_row * a.K * (SELF == Self::LAYER_GLU ? 2 : 1) + k;
-                const h8 f = *reinterpret_cast<const h8 *>(from);
-                h8 u = f;
-                if constexpr (SELF == Self::LAYER_GLU) u = *reinterpret_cast<const h8 *>(from + a.K);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = SELF == Self::LAYER_GLU ? silu_dev((float)f[i]) * (float)u[i] : (float)f[i];
-            }
+            for (int i = 0; i < 8; ++i) v[i] = SELF == Self::LAYER_GLU ? silu_dev((float)f[i]) * (float)u[i] : (float)f[i];
         }
         float amax = 0.0f;
 #pragma unroll
@@ -289,15 +311,11 @@ __global__ __launch_bounds__(512) void qgemm_f8_self(F8Gemm a, int most)   // mo
         uint2 out;
         out.x = f8_pack4(s.code(v[0]), s.code(v[1]), s.code(v[2]), s.code(v[3]));
         out.y = f8_pack4(s.code(v[4]), s.code(v[5]), s.code(v[6]), s.code(v[7]));
-        *reinterpret_cast<uint2 *>(codes + ((size_t)kb * most + r) * F8_BLOCK + ((sub / 2) ^ ((r >> 1) & 7)) * 16 + (sub & 1) * 8) = out;
-        if (sub == 0) scales[kb * most + r] = F8Scale::scale(amax);
+        store_lds(codes + ((size_t)kb * most + r) * F8_BLOCK + ((sub / 2) ^ ((r >> 1) & 7)) * 16 + (sub & 1) * 8, out);
+        if (sub == 0) store_lds(scales + kb * most + r, F8Scale::scale(amax));
+        if (b + 32 < blocks) request(b + 32);
     }
-    float sw[STEPS][COLS];
-#pragma unroll
-    for (int n = 0; n < STEPS; ++n)
-#pragma unroll
-        for (int j = 0; j < COLS; ++j) sw[n][j] = s_w[((j ? a.NB : 0) + min(n0, a.N - 1) / F8_BLOCK) * a.KB + min(wave + n * WAVES, a.KB - 1)];
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __syncthreads();
     // ---- the products
     const int lo = p * 128 + (g ^ ((p >> 1) & 7)) * 16, hi = p * 128 + ((4 + g) ^ ((p >> 1) & 7)) * 16;

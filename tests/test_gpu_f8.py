@@ -344,6 +344,23 @@ def test_tokens_without_experts_and_experts_twice(T, E, k, I):
     assert bool((ql.experts_f8(*args) == 0).all()) and torch.equal(ql.experts_f8(*args, residual=_dev(res)), _dev(res))
 
 
+@pytest.mark.parametrize("T, E, k, K, I, N", [(1, 512, 16, 128, 4096, 40), (16, 64, 1, 4096, 2048, 24), (4, 16, 4, 512, 1536, 2056), (2, 8, 8, 256, 1040, 136), (1, 3, 3, 2048, 128, 8), (5, 40, 3, 1040, 1152, 264)])
+def test_few_rows_of_many_experts(T, E, k, K, I, N):
+    """Up to 16 rows: as many experts, and the same call with rows that have no expert or share one."""
+    g = _rng("few", T, E, k, I)
+    args, res, (ref, tol) = _experts(g, T, E, k, K, I, N, True)
+    _close(ql.experts_f8(*args, residual=_dev(res)), ref, tol)
+    ids = args[1].cpu().numpy()
+    ids.reshape(-1)[::3] = ids[0, 0]
+    ids.reshape(-1)[1::5] = -1
+    args, res, (ref, tol) = _experts(_rng("few", T, E, k, I), T, E, k, K, I, N, True, ids)
+    y = ql.experts_f8(*args, residual=_dev(res))
+    _close(y, ref, tol)
+    order = torch.arange(T - 1, -1, -1, device="cuda")      # a token's sums do not depend on which tokens are in front of it
+    again = ql.experts_f8(args[0][order].contiguous(), args[1][order].contiguous(), args[2][order].contiguous(), *args[3:], residual=_dev(res)[order].contiguous())
+    assert torch.equal(again, y[order])
+
+
 def test_rows_of_a_token_do_not_depend_on_the_batch():
     """A token alone and the same token among others, in calls of the same size: bit for bit."""
     g = _rng("batch")

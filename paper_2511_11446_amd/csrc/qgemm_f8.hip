@@ -196,7 +196,7 @@ __global__ __launch_bounds__(64 * WAVES) void qgemm_f8_few(F8Gemm a)
 
 // Up to 16 rows that every workgroup quantizes itself: one launch in the place of two (a small launch costs the GPU 2 to 3 us, the host 3.6).  All of a
 // wavefront's steps of weights, up to STEPS, are requested at once; while they come, the workgroup quantizes its rows into LDS as daq_f8.hip does.  Bound by the latencies of one
-// such chain: 1 x 4096 x 4096 4.8 us with its inputs in a cache, 6.8 from memory (16.8 MB: 3.3 at the rate of a copy).
+// such chain: 1 x 4096 x 4096 7.0 us (16.8 MB: 3.3 at the rate of a copy); with the rows requested behind the weights, which they then wait for, 7.2.
 //   LAYER  a layer's rows, binary16 (GLU: silu(g) * u of rows [g | u])
 //   UP     up to 16 rows of (token, choice) without a plan: every workgroup finds its expert's among the ids; x of the token, h at row (token, choice)
 //   DOWN   the same rows of h, fp32
@@ -259,7 +259,7 @@ __global__ __launch_bounds__(512) void qgemm_f8_self(F8Gemm a, int most)   // mo
     typedef _Float16 h8 __attribute__((ext_vector_type(8)));
     const int blocks = rows_here * a.KB, by_kb = divisor(a.KB), source = SELF == Self::UP ? divided(row, divisor(a.k)) : row;
     float4 one, two;   // 8 values: of binary16 one, and two the other half of [g | u]
-    auto request = [&](int b) {
+    auto request = [&](int b) {   // (the rows' numbers are in a wavefront's first 16 lanes, whose b is its least: they are there as long as any lane is)
         const int r = divided(b, by_kb), k = (b - r * a.KB) * F8_BLOCK + (threadIdx.x & 15) * 8, from_row = __shfl(source, r);
         one = two = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (b < blocks && k < a.K) {

@@ -142,7 +142,7 @@ __device__ __forceinline__ void route_exact(const RouteArgs &a, long long t, dou
 //   for the place 2^-19): two that follow each other and are nearer, or two groups at the border of those that are kept and nearer than GROUP_NEAR: in 64 bits, too.
 // The weights are taken in 64 bits, of the chosen alone, those of a workgroup's tokens in one wavefront (k = 8: half of its lanes in the place of 8 of 64 in four of them).
 // Where whole lanes hold a group, its two largest are found in registers, else through LDS.
-// Bound by vector instructions: T = 16384, E = 256, k = 8, sigmoid, bias, 4 of 8 groups takes 25 us (its logits and choices at the rate of a copy: 3.5), 55 us in 64 bits
+// Bound by vector instructions, 476 a token: T = 16384, E = 256, k = 8, sigmoid, bias, 4 of 8 groups takes 25 us (its logits and choices at the rate of a copy: 3.5), 55 us in 64 bits
 // throughout, 35 with each wavefront's weights by itself and groups through LDS.
 constexpr float ROUTE_NEAR = 0x1p-17f, GROUP_NEAR = 0x1p-12f;
 

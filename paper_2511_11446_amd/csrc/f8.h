@@ -35,7 +35,7 @@ struct ExpertRows {
 constexpr int EXPERT_CHUNK = 2048;   // rows that a workgroup sorts
 inline int expert_chunks(int64_t P) { return (int)((P + EXPERT_CHUNK - 1) / EXPERT_CHUNK); }
 inline int64_t expert_tiles_most(int64_t P, int64_t E, int tile) { return P / tile + (P < E ? P : E); }
-hipError_t launch_expert_rows(const int *ids, const ExpertRows &r, hipStream_t stream);
+hipError_t launch_expert_rows(const int *ids, const ExpertRows &r, const F8DaqArgs &x, hipStream_t stream);   // and quantizes x (fp16 rows, not gated)
 
 // y[t] = residual[t] + sum_j weights[t,j] * o[place[t,j]]
 struct ExpertSumArgs {

@@ -245,8 +245,7 @@ int experts_f8(const ql_experts_f8 *x, void *workspace, size_t workspace_bytes, 
         rows.P = (int)room.P;
         rows.E = x->E;
         rows.tile = room.tile;
-        if ((rc = ql::status_of(ql::launch_expert_rows(ids, rows, s)))) return rc;
-        if ((rc = ql::status_of(ql::launch_daq_f8(daq_args(x->x, x->T, x->K, 0, ws + room.q, ws + room.s), s)))) return rc;
+        if ((rc = ql::status_of(ql::launch_expert_rows(ids, rows, daq_args(x->x, x->T, x->K, 0, ws + room.q, ws + room.s), s)))) return rc;
         up.first = down.first = rows.first;
         up.tiles = down.tiles = rows.tiles;
         up.tiles_most = down.tiles_most = (int)room.tiles_most;

@@ -96,6 +96,8 @@ struct ExpertRoom {
         P = T * k;
         tile = ql::f8_expert_tile(P, E);
         tiles_most = ql::expert_tiles_most(P, E, tile);
+        // The rows' outputs: from tiles in binary16, which the sum over the choices reads again (in fp32 256 tokens through 8 of 64 experts of 2048 x 1024 took 117 us in the
+        // place of 113, 4096 through 2 of 8 201 in the place of 175).  The rounding is the one of every layer's output here; y is 3.0e-4 of its size off with it, 2.1e-4 without.
         wide = tile < ql::F8_TILE_ROWS || ql::experts_f8_takes_ids(P, K, I);
         size_t at = 0;
         auto take = [&](size_t bytes) {

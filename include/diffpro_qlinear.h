@@ -663,8 +663,9 @@ int route_experts(const ql_routing *routing, void *stream);
  *   xq         = daq_quantize_f8(x[t])
  *   [g | u]    = xq times the two matrices w_up[e], in fp32, as exact as qgemm_f8 of few rows
  *   hq         = daq_quantize_f8 of silu(g) * u
- *   o[t,j]     = fp16( hq times w_down[e] ), e = ids[t,j]   (likewise; fp32 where an expert has few
- *                rows on average)
+ *   o[t,j]     = hq times w_down[e], e = ids[t,j]   (likewise; fp32 where an expert has few rows on
+ *                average, else rounded to fp16, 64 neighbouring outputs that reach 2^15 times a power
+ *                of two that they share: off by at most 2^-11 of itself or 2^-39 of their largest)
  *   y[t]       = fp16( residual[t] + sum_j weights[t,j] * o[t,j] ),  added up in the order of j, in fp32
  *   x        (device) [T,K] fp16;  ids (device) [T,k] int32: an id outside [0,E) is no
  *            expert, adds nothing and its weight is not read into any result

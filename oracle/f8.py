@@ -79,6 +79,16 @@ def half_step(u):
     return np.maximum(np.abs(u) * 2.0 ** -11, 2.0 ** -25)
 
 
+def row_step(o):
+    """How far a row's output may be off by its rounding: binary16's half step, of 64 neighbours that reach 2^15 with the exponent that takes the largest of them
+    below 2^15 again: then the subnormals' half step, 2^-25, counts as many times as much."""
+    N = o.shape[-1]
+    pad = np.zeros(o.shape[:-1] + (-(-N // 64) * 64,))
+    pad[..., :N] = np.abs(o)
+    _, e = np.frexp(pad.reshape(o.shape[:-1] + (-1, 64)).max(-1))
+    return np.maximum(np.abs(o) * 2.0 ** -11, np.repeat(np.exp2(np.maximum(e - 15, 0) - 25.0), 64, axis=-1)[..., :N])
+
+
 def gelu(u):
     return u / (1.0 + np.exp(-2.0 * np.sqrt(2.0 / np.pi) * (u + 0.044715 * u ** 3)))
 
@@ -170,7 +180,7 @@ def experts(x, ids, weights, w_up, up_scale, w_down, down_scale, residual=None):
         o, do = product(hc, hs, w_down[e], down_scale[e])
         wide = np.abs(np.repeat(by_block(down_scale[e].astype(np.float64), I), BLOCK, axis=0)[:N] * w_down[e])
         do = do + dhq @ wide.T
-        do = do + half_step(np.abs(o) + do)
+        do = do + row_step(np.abs(o) + do)
         w = weights[t, j].astype(np.float64)[:, None]
         np.add.at(y, t, w * o)
         np.add.at(size, t, np.abs(w * o))

@@ -10,6 +10,7 @@ namespace ql {
 constexpr int F8_BLOCK = 128;   // channels that share an activation scale, and the side of a weight block
 constexpr float F8_MAX = 448.0f;
 constexpr int F8_LDS = 160 * 1024;   // of a compute unit
+constexpr int F8_UP = 64;       // outputs of an expert's row that share a power of two
 
 inline int f8_blocks(int64_t n) { return (int)((n + F8_BLOCK - 1) / F8_BLOCK); }
 
@@ -40,6 +41,7 @@ hipError_t launch_expert_rows(const int *ids, const ExpertRows &r, const F8DaqAr
 // y[t] = residual[t] + sum_j weights[t,j] * o[place[t,j]]
 struct ExpertSumArgs {
     const void *o;       // fp16 or (wide) fp32 [rows, N]
+    const uint8_t *up;   // of fp16 rows: F8Gemm::up
     const int *place;    // [T,k] rows, or (ids) an expert where there is one: row token * k + choice
     bool ids;
     int E;
@@ -82,6 +84,7 @@ struct F8Gemm {
     uint8_t *hq;
     float *hs;
     bool wide;
+    uint8_t *up;         // of experts' fp16 outputs: [M, ceil(N/64)] powers of two that 64 neighbours are times (0 below 2^15)
     // rows that the launch quantizes itself (qgemm_f8_takes_rows, experts_f8_takes_ids), in the place of q and s
     const void *x;       // fp16 [M,K], [M,2K] with glu; of experts fp16 [M / k, K] gated, else fp32 [M,K]
     bool glu;

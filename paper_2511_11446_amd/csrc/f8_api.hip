@@ -87,7 +87,7 @@ struct LayerRoom {
 
 // what the experts' layers keep between their launches: sizes grow with T and k
 struct ExpertRoom {
-    size_t first, order, place, tiles, counts, q, s, h, hq, hs, o, total;
+    size_t first, order, place, tiles, counts, q, s, h, hq, hs, o, up, total;
     int64_t P, tiles_most;
     int tile;
     bool wide;
@@ -98,6 +98,7 @@ struct ExpertRoom {
         tiles_most = ql::expert_tiles_most(P, E, tile);
         // The rows' outputs: from tiles in binary16, which the sum over the choices reads again (in fp32 256 tokens through 8 of 64 experts of 2048 x 1024 took 117 us in the
         // place of 113, 4096 through 2 of 8 201 in the place of 175).  The rounding is the one of every layer's output here; y is 3.0e-4 of its size off with it, 2.1e-4 without.
+        // Their range is fp32's all the same: 64 neighbours that reach 2^15 are kept with a power of two that they share (4096 tokens 168.5 -> 170.4 us).
         wide = tile < ql::F8_TILE_ROWS || ql::experts_f8_takes_ids(P, K, I);
         size_t at = 0;
         auto take = [&](size_t bytes) {
@@ -116,6 +117,7 @@ struct ExpertRoom {
         hq = take((size_t)(P * I));
         hs = take((size_t)P * ql::f8_blocks(I) * 4);
         o = take((size_t)(P * N) * 4);
+        up = take((size_t)P * ((N + ql::F8_UP - 1) / ql::F8_UP));
         total = at;
     }
 };
@@ -231,6 +233,7 @@ int experts_f8(const ql_experts_f8 *x, void *workspace, size_t workspace_bytes, 
     up.E = down.E = x->E;
     up.gated = true;
     down.wide = room.wide;
+    down.up = ws + room.up;
     if (few) {
         up.ids = down.ids = ids;
         up.x = x->x;
@@ -267,6 +270,7 @@ int experts_f8(const ql_experts_f8 *x, void *workspace, size_t workspace_bytes, 
 
     ql::ExpertSumArgs sum{};
     sum.o = ws + room.o;
+    sum.up = ws + room.up;
     sum.place = few ? ids : ints(room.place);
     sum.ids = few;
     sum.E = x->E;

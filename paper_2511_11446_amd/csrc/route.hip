@@ -689,8 +689,15 @@ __global__ __launch_bounds__(256) void expert_sum(ExpertSumArgs a)
                 }
             } else {
                 h8 o[TOGETHER];
+                int up[TOGETHER];
 #pragma unroll
-                for (int j = 0; j < TOGETHER; ++j) o[j] = *reinterpret_cast<const h8 *>(static_cast<const _Float16 *>(a.o) + (long long)max(row[j], 0) * a.N + n);
+                for (int j = 0; j < TOGETHER; ++j) {
+                    const long long from = max(row[j], 0);
+                    o[j] = *reinterpret_cast<const h8 *>(static_cast<const _Float16 *>(a.o) + from * a.N + n);
+                    up[j] = a.up[from * ((a.N + F8_UP - 1) / F8_UP) + n / F8_UP];
+                }
+#pragma unroll
+                for (int j = 0; j < TOGETHER; ++j) w[j] = __builtin_ldexpf(w[j], up[j]);
 #pragma unroll
                 for (int j = 0; j < TOGETHER; ++j)
 #pragma unroll

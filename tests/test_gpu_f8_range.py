@@ -1,0 +1,42 @@
+"""The e4m3 layers' and the experts' calls at the ends of their ranges: values beyond binary16 on the way."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2511_11446_amd as ql
+from oracle import f8 as of
+from test_gpu_f8 import _close, _codes, _dev, _experts, _rng
+
+pytestmark = pytest.mark.gpu
+
+# rows of (token, choice) that go without a plan, through tiles of 16, of 64 and of 128 rows
+PATHS = [(3, 8, 2, 256, 144, 136), (40, 8, 2, 256, 144, 136), (300, 8, 2, 256, 272, 200), (1800, 2, 2, 256, 144, 136)]
+
+
+@pytest.mark.parametrize("T, E, k, K, I, N", PATHS)
+@pytest.mark.parametrize("power", [17, 40])
+def test_outputs_of_experts_beyond_binary16(T, E, k, K, I, N, power):
+    """|o| up to 2^power, weights that bring it back: y is finite, also where a weight is 0 and where two outputs cancel."""
+    g = _rng("beyond", T, E, power)
+    args, res, _ = _experts(g, T, E, k, K, I, N, True)
+    x, ids, weights, up, ups, down, downs = args
+    w_up, w_down = _codes(up), _codes(down)
+    ids[2] = 0
+    xs, i, s_up = x.cpu().numpy(), ids.cpu().numpy(), ups.cpu().numpy()
+    # every expert's largest output, of all tokens that it has, is brought next to 2^power (of half of the experts: the others' stay)
+    _, c, s = of.quantize(xs.astype(np.float64))
+    for e in range(0, E, 2):
+        t = np.nonzero(i == e)[0]
+        if not t.size:
+            continue
+        h, _ = of.gated(*(of.product(c[t], s[t], w_up[e, j], s_up[e, j])[0] for j in (0, 1)), 0.0, 0.0)
+        _, hc, hs = of.quantize(h)
+        o, _ = of.product(hc, hs, w_down[e], downs[e].cpu().numpy())
+        downs[e] *= 2.0 ** (power - int(np.ceil(np.log2(np.abs(o).max()))))
+    weights.copy_(2.0 ** (4 - power) * _dev(g.uniform(-1, 1, (T, k)).astype(np.float32)))
+    weights[0, 0] = 0.0
+    weights[2, 0], weights[2, 1] = 1.0, -1.0
+    ref, tol = of.experts(xs, i, weights.cpu().numpy(), w_up, s_up, w_down, downs.cpu().numpy(), res)
+    y = ql.experts_f8(*args, residual=_dev(res))
+    assert np.isfinite(ref).all() and bool(torch.isfinite(y).all())
+    _close(y, ref, tol)

@@ -145,13 +145,15 @@ __device__ __forceinline__ float silu_dev(float a)
 // The codes of one block: 448 v / amax to the nearest e4m3 value.  With r = fl(1 / amax), q0 = fl(t r) and the remainder t - q0 amax, which an fma gives without
 // error, q0 + remainder * r is the quotient with less than one rounding of error and exactly where it is representable.  t = 448 v is exact for binary16 v; a quotient of
 // such a t (14 bits) and a binary16 amax (11 bits) that is no tie of e4m3 (5 bits) is at least 2^-16 away from one, so the codes are those of the exact quotient.
-// An amax so small that 1 / amax would be infinite (gated values only) is brought up with the values.
+// An amax so small that 1 / amax would be infinite, or so large that 448 of it would be (gated values only), is brought nearer to 1 with the values.  (What 2^-64 makes
+// subnormal of them is below 2^-120 of amax: its code is 0.)
 struct F8Scale {
     float amax, r, up;
     __device__ __forceinline__ explicit F8Scale(float a)
     {
-        up = a < 0x1p-60f ? 0x1p64f * F8_MAX : F8_MAX;
-        amax = a == 0.0f ? 1.0f : a < 0x1p-60f ? a * 0x1p64f : a;
+        const float by = a < 0x1p-60f ? 0x1p64f : a > 0x1p60f ? 0x1p-64f : 1.0f;
+        up = by * F8_MAX;
+        amax = a == 0.0f ? 1.0f : a * by;
         r = 1.0f / amax;
     }
     __device__ __forceinline__ float code(float v) const

@@ -1,4 +1,4 @@
-"""The e4m3 layers' and the experts' calls at the ends of their ranges: values beyond binary16 on the way."""
+"""The e4m3 layers' and the experts' calls at the ends of their ranges: values beyond binary16 and next to the end of fp32 on the way."""
 import numpy as np
 import pytest
 import torch
@@ -39,4 +39,27 @@ def test_outputs_of_experts_beyond_binary16(T, E, k, K, I, N, power):
     ref, tol = of.experts(xs, i, weights.cpu().numpy(), w_up, s_up, w_down, downs.cpu().numpy(), res)
     y = ql.experts_f8(*args, residual=_dev(res))
     assert np.isfinite(ref).all() and bool(torch.isfinite(y).all())
+    _close(y, ref, tol)
+
+
+@pytest.mark.parametrize("T, E, k, K, I, N", PATHS)
+def test_gated_products_next_to_the_end_of_fp32(T, E, k, K, I, N):
+    """silu(g) * u between 2^119 and 2^127, where 448 of them are no finite number in fp32, and outputs of ordinary size behind them."""
+    g = _rng("gated", T, E)
+    args, res, _ = _experts(g, T, E, k, K, I, N, True)
+    x, ids, weights, up, ups, down, downs = args
+    w_up, w_down = _codes(up), _codes(down)
+    xs, i = x.cpu().numpy(), ids.cpu().numpy()
+    _, c, s = of.quantize(xs.astype(np.float64))
+    most = 0.0
+    for e in range(E):
+        t = np.nonzero(i == e)[0]
+        if t.size:
+            most = max(most, *(np.abs(of.product(c[t], s[t], w_up[e, j], ups[e, j].cpu().numpy())[0]).max() for j in (0, 1)))
+    ups *= 2.0 ** (63 - int(np.ceil(np.log2(most))))        # |g| and |u| up to 2^63
+    downs *= 2.0 ** -118
+    with np.errstate(over="ignore"):                        # exp(-g) of large negative g
+        ref, tol = of.experts(xs, i, weights.cpu().numpy(), w_up, ups.cpu().numpy(), w_down, downs.cpu().numpy(), res)
+    y = ql.experts_f8(*args, residual=_dev(res))
+    assert np.isfinite(ref).all() and np.isfinite(tol).all()
     _close(y, ref, tol)

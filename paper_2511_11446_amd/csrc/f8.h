@@ -24,12 +24,13 @@ struct F8DaqArgs {
 };
 hipError_t launch_daq_f8(const F8DaqArgs &a, hipStream_t stream);
 
-// Where the rows of (token, choice) lie when they are sorted by expert.  All in device memory.
+// Where the rows of (token, choice) lie when they are sorted by expert.  All in device memory, in the call's workspace: whoever reads it holds what it says within the
+// arrays (within, below), so that a workspace which other work writes to meanwhile gives wrong numbers and no access elsewhere.
 struct ExpertRows {
     int *first;          // [E+1] first row of each expert, and how many rows there are
     int *order;          // [P] row -> token * k + choice
     int *place;          // [P] token * k + choice -> row, -1 without an expert
-    int *tiles;          // [1 + 2 * most]: how many tiles of `tile` rows there are, then expert and first row of each
+    int *tiles;          // [1 + 2 * most]: how many tiles of `tile` rows there are, then expert and first row of each; most = expert_tiles_most
     int *counts;         // [chunks][E] scratch
     int P, E, tile;
 };
@@ -128,6 +129,18 @@ hipError_t allow_lds()
 
 #ifdef __HIPCC__
 typedef int v8i __attribute__((ext_vector_type(8)));
+
+// v where it is one of 0..n-1, else one of them
+__device__ __forceinline__ int within(int v, int n) { return (int)min((unsigned)v, (unsigned)n - 1u); }
+
+// The expert's tile `tile` of a plan: its expert and rows [m0, m_end)
+struct ExpertTile {
+    int e, m0, m_end;
+    __device__ __forceinline__ ExpertTile(const int *tiles, const int *first, int tile, int E, int rows)
+        : e(within(tiles[1 + 2 * tile], E)), m0(within(tiles[2 + 2 * tile], rows)), m_end(max(m0, within(first[e + 1] - 1, rows)) + 1)
+    {
+    }
+};
 
 // silu(a) = a / (1 + 2^(-a log2 e)).  The exponent is taken in two parts (the product and what its rounding lost), so that the power is
 // off by about 2^-22 for every a, not by 2^-24 of the exponent's size; v_exp_f32 and v_rcp_f32 are off by an ulp each.  Below a = -87 the

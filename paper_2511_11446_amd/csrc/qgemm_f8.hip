@@ -86,11 +86,11 @@ __global__ __launch_bounds__(64 * WAVES) void qgemm_f8_few(F8Gemm a)
     const uint8_t *w = a.w;
     const float *s_w = a.s_w;
     if constexpr (EXPERTS) {
-        if (tile >= a.tiles[0]) return;
-        const int e = a.tiles[1 + 2 * tile];
-        m0 = a.tiles[2 + 2 * tile];
-        m_end = a.first[e + 1];
-        const long long matrix = (long long)e * (GATED ? 2 : 1);
+        if (tile >= a.tiles[0]) return;   // (the grid has tiles_most of them)
+        const ExpertTile t(a.tiles, a.first, tile, a.E, a.M);
+        m0 = t.m0;
+        m_end = t.m_end;
+        const long long matrix = (long long)t.e * (GATED ? 2 : 1);
         w += matrix * a.N * a.K;
         s_w += matrix * a.NB * a.KB;
     }
@@ -98,7 +98,7 @@ __global__ __launch_bounds__(64 * WAVES) void qgemm_f8_few(F8Gemm a)
     const unsigned bytes_w = (unsigned)a.N * (unsigned)a.K * (GATED ? 2u : 1u);
     auto source_row = [&](int r) {
         int m = min(m0 + r, m_end - 1);
-        if (EXPERTS && a.order) m = a.order[m] / a.k;
+        if (EXPERTS && a.order) m = within(a.order[m], a.M) / a.k;
         return m;
     };
     // lane l fills bytes [16 l, 16 l + 16) of 8 rows; chunk c of row r lies at slot c ^ ((r >> 1) & 7)

@@ -44,18 +44,19 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
     const int wm = wave / T::WN, wn = wave % T::WN, p = lane & 15, g = lane >> 4;
 
     // ---- the tile: neighbours in the launch's order share an XCD's L2
-    const int tiles = (EXPERTS ? a.tiles[0] : tiles_m) * tiles_n, per_xcd = (tiles + XCDS - 1) / XCDS;
+    const int tiles = (EXPERTS ? within(a.tiles[0], tiles_m + 1) : tiles_m) * tiles_n, per_xcd = (tiles + XCDS - 1) / XCDS;
     const int in_xcd = blockIdx.x / XCDS, logical = (blockIdx.x % XCDS) * per_xcd + in_xcd;
     if (in_xcd >= per_xcd || logical >= tiles) return;
     int m0, n0, m_end = a.M;
     const uint8_t *w = a.w;
     const float *s_w = a.s_w;
     if constexpr (EXPERTS) {
-        const int t = logical / tiles_n, e = a.tiles[1 + 2 * t];
-        m0 = a.tiles[2 + 2 * t];
-        n0 = (logical - t * tiles_n) * COLS;
-        m_end = a.first[e + 1];
-        const long long matrix = (long long)e * (GATED ? 2 : 1);
+        const int number = logical / tiles_n;
+        const ExpertTile t(a.tiles, a.first, number, a.E, a.M);
+        m0 = t.m0;
+        n0 = (logical - number * tiles_n) * COLS;
+        m_end = t.m_end;
+        const long long matrix = (long long)t.e * (GATED ? 2 : 1);
         w += matrix * a.N * a.K;
         s_w += matrix * a.NB * a.KB;
     } else {
@@ -71,7 +72,7 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
     const unsigned bytesB = (unsigned)a.N * (unsigned)a.K * (GATED ? 2u : 1u);
     auto source_row = [&](int r) {
         int m = min(m0 + r, m_end - 1);
-        if (EXPERTS && a.order) m = a.order[m] / a.k;
+        if (EXPERTS && a.order) m = within(a.order[m], a.M) / a.k;
         return m;
     };
     const int last = a.K - (a.KB - 1) * F8_BLOCK;

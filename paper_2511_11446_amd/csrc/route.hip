@@ -564,7 +564,7 @@ __device__ __forceinline__ int2 before_me(int2 v, int2 *of_wave)
 
 // The workgroups behind the chunks quantize the tokens meanwhile (64 tokens of 2048 channels, 8 of 128 experts: 7.7 us, apart 6.9 and
 // 4.8; 16384 tokens, 8 of 64: 29.5, apart 10.3 and 21.6)
-__global__ __launch_bounds__(ROWS_THREADS) void expert_place(const int *ids, ExpertRows r, int bits, int chunks, F8DaqArgs x)
+__global__ __launch_bounds__(ROWS_THREADS) void expert_place(const int *ids, ExpertRows r, int bits, int chunks, int most, F8DaqArgs x)
 {
     extern __shared__ int counts[];   // [waves][E]
     if ((int)blockIdx.x >= chunks) {
@@ -590,6 +590,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void expert_place(const int *ids, Exp
                 for (int c = 0; c < 16; ++c) n[c] = r.counts[min(first + c, chunks - 1) * r.E + e];
 #pragma unroll
                 for (int c = 0; c < 16; ++c) {
+                    n[c] = within(n[c], EXPERT_CHUNK + 1);
                     all += first + c < chunks ? n[c] : 0;
                     front += first + c < (int)blockIdx.x ? n[c] : 0;
                 }
@@ -607,7 +608,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void expert_place(const int *ids, Exp
         }
         if (blockIdx.x == 0) {
             r.first[e] = at.x;
-            for (int i = 0; i < tiles; ++i) {
+            for (int i = 0; i < tiles && (unsigned)(at.y + i) < (unsigned)most; ++i) {
                 r.tiles[1 + 2 * (at.y + i)] = e;
                 r.tiles[2 + 2 * (at.y + i)] = at.x + i * r.tile;
             }
@@ -624,7 +625,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void expert_place(const int *ids, Exp
         const int mine = expert_of(ids, p, r.P, r.E);
         const unsigned long long same = same_lanes(mine, bits);
         int row = -1;
-        if (mine >= 0) row = counts[wave * r.E + mine] + __popcll(same & ((1ull << lane) - 1));
+        if (mine >= 0) row = within(counts[wave * r.E + mine] + __popcll(same & ((1ull << lane) - 1)), r.P);
         __threadfence_block();
         if (mine >= 0 && (same & ((1ull << lane) - 1)) == 0) counts[wave * r.E + mine] += __popcll(same);
         __threadfence_block();
@@ -645,7 +646,8 @@ hipError_t launch_expert_rows(const int *ids, const ExpertRows &r, const F8DaqAr
         if (e != hipSuccess) return e;
     }
     const long long blocks = ((long long)x.M * x.KB * 16 + ROWS_THREADS - 1) / ROWS_THREADS;
-    hipLaunchKernelGGL(expert_place, dim3(chunks + (unsigned)(blocks < 1024 ? blocks : 1024)), dim3(ROWS_THREADS), lds, s, ids, r, bits, (int)chunks, x);
+    hipLaunchKernelGGL(expert_place, dim3(chunks + (unsigned)(blocks < 1024 ? blocks : 1024)), dim3(ROWS_THREADS), lds, s, ids, r, bits, (int)chunks,
+                       (int)expert_tiles_most(r.P, r.E, r.tile), x);
     return hipGetLastError();
 }
 
@@ -657,6 +659,7 @@ __global__ __launch_bounds__(256) void expert_sum(ExpertSumArgs a)
     typedef _Float16 h8 __attribute__((ext_vector_type(8)));
     constexpr int TOGETHER = 8;   // choices whose rows are under way together
     const long long pieces = a.N / 8, all = pieces * a.T;
+    const int rows = a.T * a.k;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
         const long long t = i / pieces, n = (i - t * pieces) * 8;
         float y[8];
@@ -678,7 +681,7 @@ __global__ __launch_bounds__(256) void expert_sum(ExpertSumArgs a)
                 float4 o[TOGETHER][2];
 #pragma unroll
                 for (int j = 0; j < TOGETHER; ++j) {
-                    const float4 *from = reinterpret_cast<const float4 *>(static_cast<const float *>(a.o) + (long long)max(row[j], 0) * a.N + n);
+                    const float4 *from = reinterpret_cast<const float4 *>(static_cast<const float *>(a.o) + (long long)within(row[j], rows) * a.N + n);
                     o[j][0] = from[0], o[j][1] = from[1];
                 }
 #pragma unroll
@@ -692,7 +695,7 @@ __global__ __launch_bounds__(256) void expert_sum(ExpertSumArgs a)
                 int up[TOGETHER];
 #pragma unroll
                 for (int j = 0; j < TOGETHER; ++j) {
-                    const long long from = max(row[j], 0);
+                    const long long from = within(row[j], rows);
                     o[j] = *reinterpret_cast<const h8 *>(static_cast<const _Float16 *>(a.o) + from * a.N + n);
                     up[j] = a.up[from * ((a.N + F8_UP - 1) / F8_UP) + n / F8_UP];
                 }

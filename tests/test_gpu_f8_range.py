@@ -1,11 +1,11 @@
-"""The e4m3 layers' and the experts' calls at the ends of their ranges: values beyond binary16 and next to the end of fp32 on the way."""
+"""The e4m3 layers' and the experts' calls at the ends of their ranges: values beyond binary16 and next to the end of fp32 on the way; two streams."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2511_11446_amd as ql
 from oracle import f8 as of
-from test_gpu_f8 import _close, _codes, _dev, _experts, _rng
+from test_gpu_f8 import _block, _close, _codes, _dev, _experts, _rng
 
 pytestmark = pytest.mark.gpu
 
@@ -63,3 +63,22 @@ def test_gated_products_next_to_the_end_of_fp32(T, E, k, K, I, N):
     y = ql.experts_f8(*args, residual=_dev(res))
     assert np.isfinite(ref).all() and np.isfinite(tol).all()
     _close(y, ref, tol)
+
+
+def test_two_blocks_each_on_its_stream():
+    """Two blocks of a mixture, each with its workspace and its stream, one behind the other there: only the two overlap.  What they give is poisoned before."""
+    blocks = [_block(200, 8, 2, 256, 256, seed=2), _block(3, 8, 2, 256, 256, seed=3)]
+    for _, _, _, room in blocks:
+        for name in ("logits", "gu", "shared", "y", "weights"):
+            room[name].fill_(float("nan"))
+        room["ids"].fill_(-1)
+        room["ws"].fill_(255)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        for s, (step, _, _, _) in zip(streams, blocks):
+            with torch.cuda.stream(s):
+                step()
+    torch.cuda.synchronize()
+    for _, check, _, _ in blocks:
+        check()

@@ -104,9 +104,9 @@ bool qgemm_f8_takes_rows(int64_t M, int64_t K, int64_t N, bool glu);
 // steps of eight wavefronts that are requested at once, and the LDS that they and the rows take
 inline int f8_self_steps(int KB) { return KB <= 8 ? 1 : KB <= 16 ? 2 : 4; }
 inline int64_t f8_self_bytes(int64_t rows, int KB, bool gated) { return 8 * f8_self_steps(KB) * (gated ? 2 : 1) * 2048 + KB * rows * (F8_BLOCK + 4) + 2048 + 64; }
-inline bool experts_f8_takes_ids(int64_t P, int64_t K, int64_t I)
+inline bool experts_f8_takes_ids(int64_t P, int64_t K, int64_t I, int64_t N)
 {
-    return P <= 16 && K <= 4096 && I <= 4096 && f8_self_bytes(P, f8_blocks(K), true) <= F8_LDS && f8_self_bytes(P, f8_blocks(I), false) <= F8_LDS;
+    return P <= 16 && N <= 1 << 26 /* 2^31 threads */ && K <= 4096 && I <= 4096 && f8_self_bytes(P, f8_blocks(K), true) <= F8_LDS && f8_self_bytes(P, f8_blocks(I), false) <= F8_LDS;
 }
 hipError_t launch_qgemm_f8_tiles(const F8Gemm &a, hipStream_t stream);
 

@@ -99,7 +99,7 @@ struct ExpertRoom {
         // The rows' outputs: from tiles in binary16, which the sum over the choices reads again (in fp32 256 tokens through 8 of 64 experts of 2048 x 1024 took 117 us in the
         // place of 113, 4096 through 2 of 8 201 in the place of 175).  The rounding is the one of every layer's output here; y is 3.0e-4 of its size off with it, 2.1e-4 without.
         // Their range is fp32's all the same: 64 neighbours that reach 2^15 are kept with a power of two that they share (4096 tokens 168.5 -> 170.4 us).
-        wide = tile < ql::F8_TILE_ROWS || ql::experts_f8_takes_ids(P, K, I);
+        wide = tile < ql::F8_TILE_ROWS || ql::experts_f8_takes_ids(P, K, I, N);
         size_t at = 0;
         auto take = [&](size_t bytes) {
             const size_t here = at;
@@ -226,7 +226,7 @@ int experts_f8(const ql_experts_f8 *x, void *workspace, size_t workspace_bytes, 
     auto ints = [&](size_t at) { return reinterpret_cast<int *>(ws + at); };
 
     const int *ids = static_cast<const int *>(x->ids);
-    const bool few = ql::experts_f8_takes_ids(room.P, x->K, x->I);
+    const bool few = ql::experts_f8_takes_ids(room.P, x->K, x->I, x->N);
     ql::F8Gemm up = gemm_args(ws + room.q, ws + room.s, room.P, x->K, x->w_up, x->up_scale, x->I, ws + room.h);
     ql::F8Gemm down = gemm_args(ws + room.hq, ws + room.hs, room.P, x->I, x->w_down, x->down_scale, x->N, ws + room.o);
     up.k = down.k = x->k;

@@ -72,7 +72,8 @@ __device__ __forceinline__ void finish_few(const F8Gemm &a, const v4f *sums, int
 // wavefront alone: bound by memory.  A wavefront brings its own steps to its own STAGES places in LDS by DMA (no barrier): loads straight into the operands' order touch
 // 16 lines of memory each and pass 16 bytes a clock through a CU, by DMA, 8 rows of 128 bytes at a time, it is 45 (64 x 8192 x 4096 27 -> 13 us, 16 x 14336 x 4096
 // 20 -> 12, the rate of a copy).
-// EXPERTS: the rows of a tile of ExpertRows; GATED: NB blocks of the gate and the same NB of the up matrix, y = silu(g) * u.
+// EXPERTS: the rows of a tile of ExpertRows, whose number is blockIdx.y (as one number workgroups would pass 2^32 threads); GATED: NB blocks of the gate and the same
+// NB of the up matrix, y = silu(g) * u.
 template <int MB, int NB, int WAVES, int STAGES, bool EXPERTS, bool GATED>
 __global__ __launch_bounds__(64 * WAVES) void qgemm_f8_few(F8Gemm a)
 {
@@ -81,7 +82,7 @@ __global__ __launch_bounds__(64 * WAVES) void qgemm_f8_few(F8Gemm a)
     static_assert(WAVES * STAGES * STEP >= WAVES * TOTAL * 1024 && ISSUED * (STAGES - 1) < 64 && MB <= 4, "the sums fit where the steps were");
     extern __shared__ __align__(1024) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), p = lane & 15, g = lane >> 4;
-    const int across = (a.N + 16 * NB - 1) / (16 * NB), tile = blockIdx.x / across;
+    const int across = (a.N + 16 * NB - 1) / (16 * NB), tile = EXPERTS ? blockIdx.y : blockIdx.x / across;
     int m0 = tile * 16 * MB, m_end = a.M;
     const uint8_t *w = a.w;
     const float *s_w = a.s_w;
@@ -94,7 +95,7 @@ __global__ __launch_bounds__(64 * WAVES) void qgemm_f8_few(F8Gemm a)
         w += matrix * a.N * a.K;
         s_w += matrix * a.NB * a.KB;
     }
-    const int n0 = ((int)blockIdx.x - tile * across) * 16 * NB;
+    const int n0 = ((int)blockIdx.x - (EXPERTS ? 0 : tile * across)) * 16 * NB;
     const unsigned bytes_w = (unsigned)a.N * (unsigned)a.K * (GATED ? 2u : 1u);
     auto source_row = [&](int r) {
         int m = min(m0 + r, m_end - 1);
@@ -222,7 +223,7 @@ __global__ __launch_bounds__(512) void qgemm_f8_self(F8Gemm a, int most)   // mo
     constexpr bool EXPERTS = SELF == Self::UP || SELF == Self::DOWN, GATED = SELF == Self::UP;
     extern __shared__ __align__(1024) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), p = lane & 15, g = lane >> 4;
-    const int across = (a.N + 15) / 16, tile = blockIdx.x / across, n0 = ((int)blockIdx.x - tile * across) * 16;
+    const int tile = blockIdx.y, n0 = (int)blockIdx.x * 16;
     const uint8_t *w = a.w;
     const float *s_w = a.s_w;
     int row, rows_here;   // the row of this lane's place p in the tile (-1: none); how many there are
@@ -366,7 +367,7 @@ static hipError_t run_few(const F8Gemm &a, hipStream_t s)
     const hipError_t opt_in = allow_lds<&qgemm_f8_few<MB, NB, WAVES, STAGES, EXPERTS, GATED>>();
     if (opt_in != hipSuccess) return opt_in;
     const unsigned across = (unsigned)((a.N + 16 * NB - 1) / (16 * NB)), down = EXPERTS ? (unsigned)a.tiles_most : (unsigned)((a.M + 16 * MB - 1) / (16 * MB));
-    hipLaunchKernelGGL((qgemm_f8_few<MB, NB, WAVES, STAGES, EXPERTS, GATED>), dim3(across * down), dim3(64 * WAVES), bytes, s, a);
+    hipLaunchKernelGGL((qgemm_f8_few<MB, NB, WAVES, STAGES, EXPERTS, GATED>), EXPERTS ? dim3(across, down) : dim3(across * down), dim3(64 * WAVES), bytes, s, a);
     return hipGetLastError();
 }
 
@@ -379,7 +380,7 @@ static hipError_t run_self_steps(const F8Gemm &a, hipStream_t s)
     if (opt_in != hipSuccess) return opt_in;
     if (bytes > F8_LDS || STEPS != f8_self_steps(a.KB)) return hipErrorInvalidValue;
     const unsigned tiles = EXPERTS ? (unsigned)a.M : 1u;   // a tile has a row at least
-    hipLaunchKernelGGL((qgemm_f8_self<STEPS, SELF>), dim3((unsigned)((a.N + 15) / 16) * tiles), dim3(512), bytes, s, a, most);
+    hipLaunchKernelGGL((qgemm_f8_self<STEPS, SELF>), dim3((unsigned)((a.N + 15) / 16), tiles), dim3(512), bytes, s, a, most);
     return hipGetLastError();
 }
 

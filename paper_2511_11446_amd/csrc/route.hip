@@ -191,6 +191,7 @@ __device__ __forceinline__ float logit_at(const RouteArgs &a, long long at)
 }
 
 constexpr int ROUTE_TOKENS = 4;   // wavefronts of a workgroup, each with a token
+constexpr long long ROUTE_ACROSS = 1 << 23;   // workgroups of a row of the grid, which has less than 2^32 threads
 
 // The choices of token t: true and, in lane j, the j-th one's number (-1: none), or false where 32 bits cannot tell.  top: the largest logit (of the softmax).
 // whole: PER divides E and the logits and the bias begin at 16 bytes.  own: 2^own lanes hold a group (-1: they do not)
@@ -420,7 +421,7 @@ __global__ __launch_bounds__(64 * ROUTE_TOKENS) void route(RouteArgs a, bool who
     __shared__ double totals[ROUTE_TOKENS];
     __shared__ float tops[ROUTE_TOKENS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long t = (long long)blockIdx.x * ROUTE_TOKENS + wave;
+    const long long t0 = ((long long)blockIdx.y * ROUTE_ACROSS + blockIdx.x) * ROUTE_TOKENS, t = t0 + wave;
     constexpr int ELSEWHERE = -2;   // no token, or one whose choices are made in 64 bits
     int id = ELSEWHERE;
     float top = 0.0f;
@@ -446,7 +447,7 @@ __global__ __launch_bounds__(64 * ROUTE_TOKENS) void route(RouteArgs a, bool who
     const int width = 1 << places, token = (int)threadIdx.x >> places, j = (int)threadIdx.x & (width - 1);
     if (token < ROUTE_TOKENS) {
         id = chosen[token][j];
-        const long long to = (long long)blockIdx.x * ROUTE_TOKENS + token;
+        const long long to = t0 + token;
         double total = 1.0, w = 0.0;
         if (id >= 0) {
             const double l = (double)logit_at<WIDE>(a, to * a.E + id);
@@ -469,7 +470,8 @@ __global__ __launch_bounds__(64 * ROUTE_TOKENS) void route(RouteArgs a, bool who
 template <int PER>
 static void run_route(const RouteArgs &a, hipStream_t s)
 {
-    const dim3 grid((unsigned)((a.T + ROUTE_TOKENS - 1ll) / ROUTE_TOKENS));
+    const long long groups_of_tokens = (a.T + ROUTE_TOKENS - 1ll) / ROUTE_TOKENS;
+    const dim3 grid((unsigned)(groups_of_tokens < ROUTE_ACROSS ? groups_of_tokens : ROUTE_ACROSS), (unsigned)((groups_of_tokens + ROUTE_ACROSS - 1) / ROUTE_ACROSS));
     const size_t lds = a.groups > 1 ? (size_t)ROUTE_TOKENS * a.E * sizeof(double) : 0;
     int own = -1, places = 0;
     for (int l = 0; l <= 6; ++l)

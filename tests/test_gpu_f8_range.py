@@ -1,11 +1,12 @@
-"""The e4m3 layers' and the experts' calls at the ends of their ranges: values beyond binary16 and next to the end of fp32 on the way; two streams."""
+"""The e4m3 layers' and the experts' calls at the ends of their ranges: values beyond binary16 and next to the end of fp32 on the way; two streams; very many
+tokens, outputs and channels."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2511_11446_amd as ql
 from oracle import f8 as of
-from test_gpu_f8 import _block, _close, _codes, _dev, _experts, _rng
+from test_gpu_f8 import _block, _close, _codes, _dev, _experts, _rng, _weights
 
 pytestmark = pytest.mark.gpu
 
@@ -82,3 +83,38 @@ def test_two_blocks_each_on_its_stream():
     torch.cuda.synchronize()
     for _, check, _, _ in blocks:
         check()
+
+
+# ---- sizes whose launches have more than 2^32 threads -------------------------------------------------------------------------------
+
+def test_routes_of_more_than_2_26_tokens():
+    T = 2 ** 26 + 5
+    x = torch.randint(-3, 4, (T, 2), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").half()
+    ids, w = ql.route_experts(x, 1, ids=torch.full((T, 1), 7, dtype=torch.int32, device="cuda"), weights=torch.full((T, 1), 7.0, device="cuda"))
+    assert torch.equal(ids[:, 0], (x[:, 1] > x[:, 0]).int()) and bool((w == 1.0).all())
+
+
+def _last(shape, rows, axis):
+    """e4m3 codes that are all 0 but those of the last expert's last rows."""
+    codes = torch.zeros(shape, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+    at = codes[-1].narrow(axis, codes.shape[axis + 1] - rows.shape[axis], rows.shape[axis])
+    at.view(torch.uint8).copy_(rows.view(torch.uint8))
+    return codes
+
+
+@pytest.mark.parametrize("T, E, K, I, N", [(16, 1, 16, 16, 8650752), (17, 17, 16, 16, 30000128), (17, 17, 16, 15000064, 8), (1, 1, 16, 16, 2 ** 27 - 8)])
+def test_experts_of_very_many_outputs_and_channels(T, E, K, I, N):
+    """Rows without a plan and tiles of 16 rows; every token goes to the last expert, whose last 64 channels or outputs alone are not 0."""
+    g = _rng("very many", T, I, N)
+    live_i, live_n = min(I, 64), min(N, 64)
+    (u, _, w_up, _), (d, _, w_down, _) = _weights(g, 2, live_i, K), _weights(g, live_n, live_i)
+    up, down = _last((E, 2, I, K), u, 1), torch.zeros((E, N, I), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+    down[-1].view(torch.uint8)[N - live_n:, I - live_i:] = d.view(torch.uint8)
+    ups, downs = torch.full((E, 2, of.blocks(I), of.blocks(K)), 2.0 ** -9, device="cuda"), torch.full((E, of.blocks(N), of.blocks(I)), 2.0 ** -9, device="cuda")
+    x = (g.standard_normal((T, K)) * 0.3).astype(np.float16)
+    y = ql.experts_f8(_dev(x), torch.full((T, 1), E - 1, dtype=torch.int32, device="cuda"), torch.ones((T, 1), device="cuda"), up, ups, down, downs)
+    # the live channels' place in their block does not matter: all others of it are 0
+    s_up, s_down = np.full((1, 2, 1, 1), 2.0 ** -9, np.float32), np.full((1, 1, 1), 2.0 ** -9, np.float32)
+    ref, tol = of.experts(x, np.zeros((T, 1), np.int32), np.ones((T, 1), np.float32), w_up[None], s_up, w_down[None], s_down)
+    _close(y[:, N - live_n:], ref, tol)
+    assert not N > live_n or bool((y[:, : N - live_n] == 0).all())

@@ -76,7 +76,7 @@ struct F8Gemm {
     int act;
     const void *residual, *gate;
     int gate_rows;
-    void *y;             // fp16 [M,N]; of experts the rows' outputs, fp32 with wide
+    void *y;             // fp16 [M,N]; of experts the rows' outputs, fp32 of few rows
     // experts: rows as ExpertRows says, or null
     const int *first, *tiles;
     const int *order;    // row -> token * k + choice where the rows of q are tokens, or null
@@ -84,7 +84,6 @@ struct F8Gemm {
     bool gated;          // the two matrices of an expert's gated layer: h = silu(g) * u, in fp32 [M,N] at y, or quantized at hq and hs
     uint8_t *hq;
     float *hs;
-    bool wide;
     uint8_t *up;         // of experts' fp16 outputs: [M, ceil(N/64)] powers of two that 64 neighbours are times (0 below 2^15)
     // rows that the launch quantizes itself (qgemm_f8_takes_rows, experts_f8_takes_ids), in the place of q and s
     const void *x;       // fp16 [M,K], [M,2K] with glu; of experts fp16 [M / k, K] gated, else fp32 [M,K]
@@ -97,6 +96,8 @@ hipError_t launch_qgemm_f8(const F8Gemm &a, hipStream_t stream);
 // rows of an expert's tile, by the rows that an expert has on average: 16, or F8_TILE_ROWS and more where the tiles quantize the gated product themselves
 constexpr int F8_TILE_ROWS = 64;
 int f8_expert_tile(int64_t P, int64_t E);
+// rows from which on tiles are not of 16: h and o of fewer are fp32
+inline int64_t f8_expert_few(int64_t E) { return E < 2 ? 384 * E : 12 * (E > 44 ? E : 44); }
 // rows from which on a layer takes the matrix cores' own sums of codes, if it may
 constexpr int F8_MANY = 256;
 float qgemm_f8_tiles_us(const F8Gemm &a);

@@ -2,6 +2,7 @@
 #include "../../include/diffpro_qlinear.h"
 #include "f8.h"
 
+#include <algorithm>
 #include <cmath>
 
 namespace {
@@ -90,7 +91,7 @@ struct ExpertRoom {
     size_t first, order, place, tiles, counts, q, s, h, hq, hs, o, up, total;
     int64_t P, tiles_most;
     int tile;
-    bool wide;
+    bool wide;   // h and o are fp32
     ExpertRoom(int64_t T, int64_t k, int64_t E, int64_t K, int64_t I, int64_t N)
     {
         P = T * k;
@@ -99,7 +100,8 @@ struct ExpertRoom {
         // The rows' outputs: from tiles in binary16, which the sum over the choices reads again (in fp32 256 tokens through 8 of 64 experts of 2048 x 1024 took 117 us in the
         // place of 113, 4096 through 2 of 8 201 in the place of 175).  The rounding is the one of every layer's output here; y is 3.0e-4 of its size off with it, 2.1e-4 without.
         // Their range is fp32's all the same: 64 neighbours that reach 2^15 are kept with a power of two that they share (4096 tokens 168.5 -> 170.4 us).
-        wide = tile < ql::F8_TILE_ROWS || ql::experts_f8_takes_ids(P, K, I, N);
+        wide = tile < ql::F8_TILE_ROWS;
+        const int64_t few = std::min(P, ql::f8_expert_few(E) - 1);   // (a call with fewer rows than this one's may be of few)
         size_t at = 0;
         auto take = [&](size_t bytes) {
             const size_t here = at;
@@ -113,10 +115,10 @@ struct ExpertRoom {
         counts = take((size_t)ql::expert_chunks(P) * E * 4);
         q = take((size_t)(T * K));
         s = take((size_t)T * ql::f8_blocks(K) * 4);
-        h = take((size_t)(P * I) * 4);
+        h = take((size_t)(few * I) * 4);
         hq = take((size_t)(P * I));
         hs = take((size_t)P * ql::f8_blocks(I) * 4);
-        o = take((size_t)(P * N) * 4);
+        o = take((size_t)std::max(P * N * 2, few * N * 4));
         up = take((size_t)P * ((N + ql::F8_UP - 1) / ql::F8_UP));
         total = at;
     }
@@ -232,7 +234,6 @@ int experts_f8(const ql_experts_f8 *x, void *workspace, size_t workspace_bytes, 
     up.k = down.k = x->k;
     up.E = down.E = x->E;
     up.gated = true;
-    down.wide = room.wide;
     down.up = ws + room.up;
     if (few) {
         up.ids = down.ids = ids;
@@ -259,7 +260,7 @@ int experts_f8(const ql_experts_f8 *x, void *workspace, size_t workspace_bytes, 
         up.hq = ws + room.hq;
         up.hs = reinterpret_cast<float *>(ws + room.hs);
         if ((rc = ql::status_of(ql::launch_qgemm_f8(up, s)))) return rc;
-        if (room.tile < ql::F8_TILE_ROWS) {
+        if (room.wide) {
             ql::F8DaqArgs d = daq_args(ws + room.h, room.P, x->I, 0, ws + room.hq, ws + room.hs);
             d.wide = true;
             d.rows = rows.first + x->E;

@@ -59,8 +59,7 @@ __device__ __forceinline__ void finish_few(const F8Gemm &a, const v4f *sums, int
             for (int r = 0; r < 4; ++r) u[r] = silu_dev(u[r]) * up[r];
             store4<true>(a.y, m, a.N, n, u);
         } else if constexpr (EXPERTS) {
-            if (a.wide) store4<true>(a.y, m, a.N, n, u);
-            else store4<false>(a.y, m, a.N, n, u);
+            store4<true>(a.y, m, a.N, n, u);
         } else {
             finish4(a, m, n, u);
             store4<false>(a.y, m, a.N, n, u);
@@ -357,7 +356,7 @@ constexpr int64_t SELF_K = 4096, SELF_N = 8192, SELF_VALUES = 32768;
 // Tiles of 16 rows read an expert's weights once for every 16, tiles of 64 and 128 (qgemm_f8_tile.hip) quantize the gated product themselves and have fewer workgroups with
 // longer chains.  us on 16, 64 and 128 rows, T tokens: k = 8 of 64 experts, 2048 and 1024 inputs: T = 64 85, 87, 119; 256 151, 114, 165; 2048 703, 316, 322; 8192 -, 1026, 958;
 // 4 of 60, 1152 and 720: T = 128 47, 51, 67, 300 65, 53, 71; 2 of 8, 4096 and 2048: T = 128 64, 89, 114, 512 165, 126, 130, 4096 -, 548, 503
-int f8_expert_tile(int64_t P, int64_t E) { return P >= 384 * E ? 128 : P >= 12 * (E > 44 ? E : 44) ? 64 : 16; }
+int f8_expert_tile(int64_t P, int64_t E) { return P < f8_expert_few(E) ? 16 : P >= 384 * E ? 128 : 64; }
 
 template <int MB, int NB, int WAVES, int STAGES, bool EXPERTS, bool GATED>
 static hipError_t run_few(const F8Gemm &a, hipStream_t s)

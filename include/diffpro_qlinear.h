@@ -570,7 +570,7 @@ int attention_kv8(const ql_attention *attn, const ql_kv_cache *cache,
  * carry DAQ (Step 3: scales taken at run time from the values at hand) and the
  * layer of Step 5 over to e4m3 weights with a scale for every block of 128 x 128,
  * for weights that are stored so.  Codes are e4m3 (4 exponent and 3 mantissa bits,
- * largest 448, no infinities; +-0x7f is NaN and is never written).
+ * largest 448, no infinities; 0x7f and 0xff are NaN).
  *
  * daq_quantize_f8.  For row m and the channels k of block b = k / 128 (the last
  * block of a row may be shorter):
@@ -580,6 +580,9 @@ int attention_kv8(const ql_attention *attn, const ql_kv_cache *cache,
  *            quotient decides where v is an input of x; silu below is off by about 2^-22)
  *   v = x[m,k]                                      glu = 0
  *   v = silu(x[m,k]) * x[m,K+k] in fp32, silu(a) = a / (1 + exp(-a))    glu = 1
+ * Finite v never get a NaN code unless their block has an infinite one: its scale is then
+ * infinite and all its codes are NaN.  A v that is NaN is left out of amax and its own code is
+ * NaN (a block of nothing else has the scale 1).  Every product of a row with a NaN code is NaN.
  *   x       (device) [M,K] fp16, in; [M,2K] with glu: the output [g | u] of the layer
  *           in front
  *   q       (device) [M,K] e4m3, out
@@ -601,8 +604,10 @@ int attention_kv8(const ql_attention *attn, const ql_kv_cache *cache,
  * them 2e-5 of the result's size; its rounding to fp16 is 2e-4.)  So a row may come out
  * differently, within these bounds, among more than 256 rows than among fewer.
  *
- * qlinear_f8 is daq_quantize_f8 followed by qgemm_f8; y may be the residual and
- * overlaps nothing else.
+ * qlinear_f8 is daq_quantize_f8 followed by qgemm_f8, up to the order of the sums in fp32 and to
+ * this: more than 256 rows of a gated product take the exact products there, while qgemm_f8, which
+ * does not know where its codes come from, takes the matrix cores' sums (2.6e-4 of the result's
+ * size off on gated products).  y may be the residual and overlaps nothing else.
  * qlinear_f8_workspace_bytes: enough for every call with up to M rows, K inputs and
  * N outputs (0: sizes that the call refuses).
  *

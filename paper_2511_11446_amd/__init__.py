@@ -867,7 +867,8 @@ def qlinear_f8_workspace_bytes(M, K, N):
 
 
 def qlinear_f8(x, w, w_scale, bias=None, glu=False, act=ACT_NONE, residual=None, gate=None, gate_rows=1, y=None, ws=None, stream=None):
-    """daq_quantize_f8 and qgemm_f8: x fp16 [M,K] ([M,2K] with glu), w float8_e4m3fn [N,K], w_scale fp32 [ceil(N/128), ceil(K/128)] -> y fp16 [M,N]."""
+    """daq_quantize_f8 and qgemm_f8: x fp16 [M,K] ([M,2K] with glu), w float8_e4m3fn [N,K], w_scale fp32 [ceil(N/128), ceil(K/128)] -> y fp16 [M,N].
+    (More than 256 rows behind a gated product: with the exact products that qgemm_f8 takes for fewer.)"""
     torch = _torch or _load_torch()
     dev = _current()
     _here(stream, dev)

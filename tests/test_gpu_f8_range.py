@@ -6,7 +6,7 @@ import torch
 
 import paper_2511_11446_amd as ql
 from oracle import f8 as of
-from test_gpu_f8 import _block, _close, _codes, _dev, _experts, _rng, _weights
+from test_gpu_f8 import _block, _close, _codes, _dev, _experts, _rng, _rows, _weights
 
 pytestmark = pytest.mark.gpu
 
@@ -118,3 +118,49 @@ def test_experts_of_very_many_outputs_and_channels(T, E, K, I, N):
     ref, tol = of.experts(x, np.zeros((T, 1), np.int32), np.ones((T, 1), np.float32), w_up[None], s_up, w_down[None], s_down)
     _close(y[:, N - live_n:], ref, tol)
     assert not N > live_n or bool((y[:, : N - live_n] == 0).all())
+
+
+# ---- what is no finite number ------------------------------------------------------------------------------------------------------
+
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.mark.parametrize("glu", [False, True])
+def test_codes_of_what_is_no_finite_number(glu):
+    """NaN is left out of a block's scale and its code alone is NaN; an infinite value makes its block's scale infinite and all its codes NaN; other blocks and rows are as without."""
+    g = _rng("nan codes")
+    K = 272
+    x = _rows(g, 40, K)
+    x[:, K // 2] = 1.0
+    gate = np.concatenate([_rows(g, 40, K), x], axis=1) if glu else x       # (of [g | u] the second half is changed)
+    bad = gate.copy()
+    v = bad[:, -K:]
+    v[1, 5], v[2, 130], v[3, 128:256], v[4, 270], v[5, 3], v[5, 4] = NAN, INF, NAN, -INF, INF, NAN
+    without = gate.copy()
+    w = without[:, -K:]
+    w[1, 5] = 0.0                                                           # the same block without the NaN
+    q, s = (t.view(torch.uint8).cpu().numpy() if t.dtype != torch.float32 else t.cpu().numpy() for t in ql.daq_quantize_f8(_dev(bad), glu=glu))
+    q0, s0 = (t.view(torch.uint8).cpu().numpy() if t.dtype != torch.float32 else t.cpu().numpy() for t in ql.daq_quantize_f8(_dev(without), glu=glu))
+    none = np.zeros((40, K), bool)
+    none[1, 5] = none[2, 128:256] = none[3, 128:256] = none[4, 256:] = none[5, :128] = True
+    assert np.array_equal((q & 0x7f) == 0x7f, none)
+    assert np.array_equal(q[~none], q0[~none])
+    scales = s0.copy()
+    scales[2, 1] = scales[4, 2] = scales[5, 0] = INF
+    scales[3, 1] = 1.0
+    assert np.array_equal(s, scales)
+
+
+@pytest.mark.parametrize("M, K, N", [(8, 272, 40), (30, 272, 72), (64, 4096, 4096), (200, 272, 1000), (300, 272, 500), (1100, 272, 520), (2100, 272, 2056)])
+@pytest.mark.parametrize("glu", [False, True])
+def test_a_row_with_a_nan_code_is_nan_and_no_other(M, K, N, glu):
+    g = _rng("nan rows", M, N)
+    dw, ds, _, _ = _weights(g, N, K)
+    dw.view(torch.uint8)[: N // 2] = 0                                      # (0 times NaN, too)
+    x = np.concatenate([_rows(g, M, K), _rows(g, M, K)], axis=1) if glu else _rows(g, M, K)
+    bad = x.copy()
+    bad[1, -2], bad[M - 2, -K + 7] = NAN, INF
+    y, y0 = ql.qlinear_f8(_dev(bad), dw, ds, glu=glu), ql.qlinear_f8(_dev(x), dw, ds, glu=glu)
+    there = torch.ones(M, dtype=torch.bool, device="cuda")
+    there[1] = there[M - 2] = False
+    assert bool(torch.isnan(y[~there]).all()) and torch.equal(y[there], y0[there]) and bool(torch.isfinite(y0).all())

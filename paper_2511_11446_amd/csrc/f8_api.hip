@@ -99,7 +99,7 @@ struct ExpertRoom {
         tiles_most = ql::expert_tiles_most(P, E, tile);
         // The rows' outputs: from tiles in binary16, which the sum over the choices reads again (in fp32 256 tokens through 8 of 64 experts of 2048 x 1024 took 117 us in the
         // place of 113, 4096 through 2 of 8 201 in the place of 175).  The rounding is the one of every layer's output here; y is 3.0e-4 of its size off with it, 2.1e-4 without.
-        // Their range is fp32's all the same: 64 neighbours that reach 2^15 are kept with a power of two that they share (4096 tokens 168.5 -> 170.4 us).
+        // Their range is fp32's all the same: 64 neighbours that reach 2^15 are kept with a power of two that they share (2048 tokens through 8 of 64 316 -> 319 us).
         wide = tile < ql::F8_TILE_ROWS;
         const int64_t few = std::min(P, ql::f8_expert_few(E) - 1);   // (a call with fewer rows than this one's may be of few)
         size_t at = 0;

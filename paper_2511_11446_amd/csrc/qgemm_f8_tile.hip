@@ -342,29 +342,46 @@ __global__ __launch_bounds__(T::NTHR, 2) void qgemm_f8_tile(F8Gemm a, int tiles_
             float add[NT / 2][8];
 #pragma unroll
             for (int b = 0; b < NT / 2; ++b) bias8(col0 + 32 * b + 8 * g, add[b]);
+            if constexpr (OUT == F8Out::ROWS) {
+                // A row's 64 outputs of this wavefront, where they reach 2^15: with the power of two that takes them below it, which the sum over the choices gives back.
+                // (Weights follow there, so that an output beyond binary16 need be none of y; infinite ones stay so.)
+                static_assert(16 * NT == F8_UP, "outputs that share a power");
+                float most[MT];
+                int up[MT];
+                bool far = false;
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    most[i] = 0.0f;
+                    up[i] = 0;
+#pragma unroll
+                    for (int j = 0; j < NT; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) most[i] = fmaxf(most[i], fabsf(acc[j][i][e]));
+                    far |= most[i] >= 0x1p15f;
+                }
+                if (__any(far)) {
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        most[i] = fmaxf(most[i], __shfl_xor(most[i], 16));
+                        most[i] = fmaxf(most[i], __shfl_xor(most[i], 32));
+                        up[i] = most[i] >= 0x1p15f && most[i] < __builtin_inff() ? __builtin_amdgcn_frexp_expf(most[i]) - 15 : 0;
+                        const float down = __builtin_bit_cast(float, (127 - up[i]) << 23);
+#pragma unroll
+                        for (int j = 0; j < NT; ++j)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[j][i][e] *= down;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    const int m = m0 + (wm * MT + i) * 16 + p;
+                    if (g == 0 && m < m_end && col0 < a.N) a.up[(long long)m * ((a.N + F8_UP - 1) / F8_UP) + col0 / F8_UP] = (uint8_t)up[i];
+                }
+            }
             auto store_rows = [&](auto stream) {
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
                 const int m = m0 + (wm * MT + i) * 16 + p;
-                if constexpr (OUT == F8Out::ROWS) {
-                    // A row's 64 outputs of this wavefront, where they reach 2^15: with the power of two that takes them below it, which the sum over the choices gives back.
-                    // (Weights follow there, so that an output beyond binary16 need be none of y; infinite ones stay so.)
-                    static_assert(16 * NT == F8_UP, "outputs that share a power");
-                    float most = 0.0f;
-#pragma unroll
-                    for (int j = 0; j < NT; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) most = fmaxf(most, fabsf(acc[j][i][e]));
-                    most = fmaxf(most, __shfl_xor(most, 16));
-                    most = fmaxf(most, __shfl_xor(most, 32));
-                    const int up = most >= 0x1p15f && most < __builtin_inff() ? __builtin_amdgcn_frexp_expf(most) - 15 : 0;
-                    const float down = __builtin_bit_cast(float, (127 - up) << 23);
-#pragma unroll
-                    for (int j = 0; j < NT; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[j][i][e] *= down;
-                    if (g == 0 && m < m_end && col0 < a.N) a.up[(long long)m * ((a.N + F8_UP - 1) / F8_UP) + col0 / F8_UP] = (uint8_t)up;
-                }
                 h8 r[NT / 2], gt[NT / 2];
                 if (res || gate) {
 #pragma unroll

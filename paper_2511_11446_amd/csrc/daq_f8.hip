@@ -3,7 +3,7 @@
 //
 // scale = amax / 448 of a block's values v, code = e4m3 nearest to 448 v / amax (f8.h).  Bound by memory: 3 bytes a value (5 gated) and about 12 vector instructions (31
 // gated, whose busy cycles the vector units fill, too).  16 lanes own a block, 8 values each: a 16-byte load, the maximum over 16 lanes by rotations inside the row of lanes,
-// an 8-byte store, nothing is read twice.  A copy moves 5.0 TB/s; 16384 x 4608 takes 38 us (6.0 TB/s, part of it from the caches), gated 77 us (4.9 TB/s); 16 x 4096 2.8 us.
+// an 8-byte store, nothing is read twice.  A copy moves 5.0 TB/s; 16384 x 4608 takes 38 us (6.0 TB/s, part of it from the caches), gated 77 us (4.9 TB/s), from memory 82; 16 x 4096 2.7 us.
 #include "daq_f8.h"
 
 namespace ql {

@@ -70,7 +70,7 @@ __device__ __forceinline__ void finish_few(const F8Gemm &a, const v4f *sums, int
 // Few rows: 16 MB rows and 16 NB outputs a workgroup, whose wavefronts take every WAVES-th step and add up through LDS.  Every byte of the weights is read by one
 // wavefront alone: bound by memory.  A wavefront brings its own steps to its own STAGES places in LDS by DMA (no barrier): loads straight into the operands' order touch
 // 16 lines of memory each and pass 16 bytes a clock through a CU, by DMA, 8 rows of 128 bytes at a time, it is 45 (64 x 8192 x 4096 27 -> 13 us, 16 x 14336 x 4096
-// 20 -> 12, the rate of a copy).
+// 20 -> 12, the rate of a copy; with inputs from memory the first takes 15 to 17).
 // EXPERTS: the rows of a tile of ExpertRows, whose number is blockIdx.y (as one number workgroups would pass 2^32 threads); GATED: NB blocks of the gate and the same
 // NB of the up matrix, y = silu(g) * u.
 template <int MB, int NB, int WAVES, int STAGES, bool EXPERTS, bool GATED>
@@ -196,7 +196,7 @@ __global__ __launch_bounds__(64 * WAVES) void qgemm_f8_few(F8Gemm a)
 
 // Up to 16 rows that every workgroup quantizes itself: one launch in the place of two (a small launch costs the GPU 2 to 3 us, the host 3.6).  All of a
 // wavefront's steps of weights, up to STEPS, are requested at once; while they come, the workgroup quantizes its rows into LDS as daq_f8.hip does.  Bound by the latencies of one
-// such chain: 1 x 4096 x 4096 7.0 us (16.8 MB: 3.3 at the rate of a copy); with the rows requested behind the weights, which they then wait for, 7.2.
+// such chain: 1 x 4096 x 4096 7.0 us, with inputs from memory 5.1 to 7.2 in the trace (16.8 MB: 3.3 at the rate of a copy); with the rows requested behind the weights, which they then wait for, 7.2.
 //   LAYER  a layer's rows, binary16 (GLU: silu(g) * u of rows [g | u])
 //   UP     up to 16 rows of (token, choice) without a plan: every workgroup finds its expert's among the ids; x of the token, h at row (token, choice)
 //   DOWN   the same rows of h, fp32
@@ -391,7 +391,7 @@ static hipError_t run_self(const F8Gemm &a, hipStream_t s)
 }
 
 // What few rows take on workgroups of 16 mb rows and 16 nb outputs: what such a workgroup brings to LDS at 55 bytes a nanosecond, and 2.5 us for the launch, the first bytes'
-// way and the sum over the wavefronts.  us, measured and so: 64 x 8192 x 4096 on 32 x 32 12.5 and 12.0, on 64 x 32 17.7 and 16.8; 128 x 4096 x 4096 on 64 x 32 11.3 and
+// way and the sum over the wavefronts.  us with inputs in the caches, measured and so: 64 x 8192 x 4096 on 32 x 32 12.5 and 12.0, on 64 x 32 17.7 and 16.8; 128 x 4096 x 4096 on 64 x 32 11.3 and
 // 9.6, on 32 x 32 13.4 and 12.0, on 32 x 16 20.9 and 16.8; 128 x 12288 x 512 on 32 x 16 11.5 and 13.2, on 64 x 32 22.6 and 23.9.
 static float few_us(const F8Gemm &a, int mb, int nb)
 {

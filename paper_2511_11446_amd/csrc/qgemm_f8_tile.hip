@@ -3,11 +3,11 @@
 //
 // Two stages in LDS: the next step comes while this one is multiplied.  Side of the tile: 256 x 256 reads the operands' bytes least often (8192^3 478 us with its inputs in a
 // cache, 563 in turn with others: 2.3 and 2.0 PFLOP/s; the matrix cores 52 % busy, vector units, that is the folds, 42 %); 128 x 128, two on a CU, hides ends and writing
-// under the other's products (16384 x 1152 x 4608 125 us; 256 x 256 136: nine steps, and 151 MB written at their end); 64 x 64, four on a CU, is for layers with few tiles
-// (1021 x 2224 x 1001 10.6 us).  tiles_us below chooses.
+// under the other's products (16384 x 1152 x 4608 125 us, 134 to 141 with inputs from memory; 256 x 256 136: nine steps, and 151 MB written at their end); 64 x 64, four on a CU, is for layers with few tiles
+// (1021 x 2224 x 1001 10.6 us, 14 to 15 with inputs from memory).  tiles_us below chooses.
 // In binary16 products (WIDE) a wavefront issues two conversions and one fold for every product: matrix cores 47 %, vector units 62 % busy, 13 % waiting, 2.0 GHz.  Half as many
 // products of 32 x 32, with the conversions between them, took as long.  16384 tokens through 8 of 64 experts of 2048 x 1024: gated 1113 us, 0.99 PFLOP/s, down 567 us, 0.97
-// (a library's binary16 product 1.19).
+// (a library's binary16 product 1.19); three inputs in turn, on another machine, 1131 and 604.
 #include "qgemm_f8.h"
 
 namespace ql {
